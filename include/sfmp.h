@@ -85,6 +85,15 @@ extern "C" {
 #define SFMP_LUT_TABLE_FP32 0  /* sfmp_lut_gemv: table entries held as fp32 */
 #define SFMP_LUT_TABLE_FP16 1  /* ... as fp16, the 2-byte entries of Appendix F (fp32 sum of the 8 activations, rounded once) */
 
+#define SFMP_KV_PAGE 64        /* tokens of a cache page */
+#define SFMP_KV_INT8 0         /* cache codes: whole numbers -127..127, stored plus 128 */
+#define SFMP_KV_FP8 1          /* ... 8-bit floating point, 4 exponent and 3 mantissa bits, no infinities (OCP E4M3) */
+#define SFMP_KV_MAX_BATCH 1024 /* sequences of one sfmp_kv_reserve call */
+
+#define SFMP_TYPE_FP16 0
+#define SFMP_TYPE_BF16 1
+#define SFMP_TYPE_FP32 2
+
 #define SFMP_STATIC_SCRATCH_BYTES (16 * 1024 * 1024)  /* scratch of sfmp_gemm_static, per GPU */
 
 /* Sizes of a packed matrix.  Filled by sfmp_pack_query / sfmp_pack; passed by the caller,
@@ -305,6 +314,151 @@ int sfmp_lut_gemv(const void* X_dev, const int32_t* col_perm_dev, int32_t N, int
                   const uint32_t* tile_off_dev, const void* scales_dev, const void* zeros_dev,
                   const int32_t* row_perm_dev, void* Y_dev, int32_t table_format, void* workspace_dev,
                   int64_t workspace_bytes, void* hip_stream);
+
+/* ---- 8-bit paged key/value cache, its attention, its pages --------------------------------------------------------
+ * What a decoder needs between its q|k|v projections and its o projection.  Keys and values of all sequences of a GPU
+ * live in one pool of pages of SFMP_KV_PAGE = 64 tokens, in 8 bits, with one fp32 scale for each page, head and of K and
+ * V; a table gives the pages of every sequence.
+ *
+ * Pool (device, owned by the caller):
+ *   codes   uint8 [layers][pages][kv_heads][2][64 * head_dim].  The first of the two blocks holds the keys as
+ *           [token][dim], the second the values TRANSPOSED, as [dim][token]: read 16 bytes per lane, both are operands of
+ *           the matrix instructions as they lie, without a transposition.
+ *   scales  fp32 [layers][pages][kv_heads][2]
+ *   An element is code * scale.  SFMP_KV_INT8: code = byte - 128, scale = m / 127 where m is the largest magnitude of the
+ *   block (one page, head, K or V).  SFMP_KV_FP8: scale = 2^e with the smallest e such that m <= 448 * 2^e.  Rounding to
+ *   nearest even.  A block whose largest magnitude is below 2^-100 is held as zeros with scale 0.  A block that is given
+ *   an infinity or a NaN gets the scale NaN: every element of it reads as NaN until its page is given to other tokens.
+ * Tables (device, owned by the caller):
+ *   page_table int32 [sequences][table_pages]; lengths int32 [sequences], tokens of each; refs int32 [pages], sequences
+ *   that hold a page (0 = free).  Sequence i holds exactly the first ceil(lengths[i] / 64) pages of its row.  An empty
+ *   pool has lengths and refs of 0; the page table need not be initialised.
+ * The order of a step: sfmp_kv_reserve (once for all layers: room for the new tokens, lengths grow), then for each layer
+ * sfmp_kv_append and sfmp_kv_attention on the new rows, which are THE LAST rows of their sequences.
+ * The kernels bound every index that they read from tables: an entry outside its range is read as page 0 or as an empty
+ * sequence, never out of bounds; what they then compute is unspecified.
+ * All calls are asynchronous on hip_stream, allocate nothing and keep nothing. */
+typedef struct sfmp_kv_layout {
+  int32_t pages, kv_heads;
+  int32_t head_dim;                /* 64, 128 or 256 */
+  int32_t format;                  /* SFMP_KV_INT8 or SFMP_KV_FP8 */
+  int32_t layers;                  /* layers that share the page table */
+  int32_t reserved;                /* 0 */
+  int64_t page_bytes;              /* codes of one page of one layer */
+  int64_t codes_bytes, scales_bytes;
+} sfmp_kv_layout_t;
+
+typedef struct sfmp_kv_tables {
+  int32_t* page_table_dev;
+  int32_t* lengths_dev;
+  int32_t* refs_dev;
+  int32_t sequences, table_pages;
+} sfmp_kv_tables_t;
+
+/* Rows of a call: batch entry b is sequence slots[b] (slots NULL: sequence b) and owns rows row_start[b] ..
+ * row_start[b+1]-1 of the row-major arguments (row_start NULL: row b).  Both are device arrays. */
+typedef struct sfmp_kv_batch {
+  const int32_t* slots_dev;
+  const int32_t* row_start_dev;    /* [batch + 1], ascending from 0 */
+  int32_t batch;
+  int32_t rows;                    /* rows of the arguments, row_start[batch] */
+  int32_t max_rows;                /* at least the most rows of one entry; 1 if row_start is NULL */
+  int32_t reserved;                /* 0 */
+} sfmp_kv_batch_t;
+
+/* Host only.  Fills a layout; SFMP_ERR_SHAPE (pages, kv_heads, layers < 1, kv_heads > 1024, head_dim not 64, 128 or
+ * 256), SFMP_ERR_LAYOUT (format). */
+int sfmp_kv_query(int32_t pages, int32_t kv_heads, int32_t head_dim, int32_t format, int32_t layers,
+                  sfmp_kv_layout_t* out);
+
+/* Device.  Quantises keys and values of new tokens into layer `layer`.  K, V: 16-bit (dtype SFMP_TYPE_FP16 or
+ * SFMP_TYPE_BF16), row r at K + r * k_stride elements, [kv_heads][head_dim] inside a row; 16-byte aligned, strides
+ * multiples of 8 (a slice of a fused q|k|v result can be passed as it is).  The n rows of an entry are the last n tokens
+ * of its sequence (rows that would lie before the first token are left out), and the pages that they go to have to be held by that sequence alone
+ * (sfmp_kv_reserve sees to it).  Where a page already holds earlier tokens of the sequence, its scale grows if the new
+ * ones need it, and the earlier codes are requantised: code * old / new scale, rounded to nearest even (exact for SFMP_KV_FP8 but for
+ * subnormal results).  The scale of a page whose first token is among the new rows is made from the new rows alone; its
+ * slots past the last token are zeroed. */
+int sfmp_kv_append(const sfmp_kv_layout_t* layout, int32_t layer, void* codes_dev, float* scales_dev,
+                   const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch, const void* K_dev, const void* V_dev,
+                   int32_t dtype, int64_t k_stride, int64_t v_stride, void* hip_stream);
+
+/* Device.  Reads cached tokens back: rows of entry b are the tokens first_dev[b], first_dev[b] + 1, ... of its sequence.
+ * K, V: [rows][kv_heads][head_dim], row strides in elements, dtype SFMP_TYPE_FP16, _BF16 or _FP32; code * scale rounded once.  Tokens past
+ * the end of a sequence read as 0. */
+int sfmp_kv_gather(const sfmp_kv_layout_t* layout, int32_t layer, const void* codes_dev, const float* scales_dev,
+                   const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch, const int32_t* first_dev, void* K_dev,
+                   void* V_dev, int32_t dtype, int64_t k_stride, int64_t v_stride, void* hip_stream);
+
+/* Device.  Attention of new rows over their sequences' cached tokens (theirs among them):
+ *   row i of the n rows of an entry of length t stands at position p = t - n + i and sees the tokens j <= p, with
+ *   window > 0 those with j > p - window;
+ *   O[row, head] = sum_j w_j V_j / sum_j w_j,  w_j = exp(scale * <Q[row, head], K_j>),  K and V of head / (q_heads/kv_heads).
+ * Q: 16-bit (dtype), row r at Q + r * q_stride, [q_heads][head_dim] inside a row, q_heads a multiple of kv_heads; O
+ * likewise with o_stride; both 16-byte aligned, strides multiples of 8.  lse: NULL, or fp32 [rows][q_heads], the natural
+ * logarithm of the sum of w.  A row that sees no token (p < 0, an empty sequence) gets O = 0, lse = -infinity.  Scores,
+ * softmax statistics and sums are held in fp32; products are taken on the matrix cores from exact fp16 values of the
+ * codes and of Q (bf16: each row scaled by a power of two); the softmax weights are rounded to fp16 before the product
+ * with V, which adds to a result about as much error as its own rounding to fp16.  max_tokens: at least the longest
+ * sequence of the batch; tokens past it are not read.  The same call on the same inputs gives the same bits; a sequence's
+ * result may differ in its last bits with the batch it is in (the work is cut by the whole batch).
+ * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads, strides, max_tokens < 1, window < 0, scale not finite or not positive, or
+ * batch * kv_heads * ceil(max_tokens / 64) * ceil(max_rows * q_heads / kv_heads / 16) >= 2^31.  SFMP_ERR_WORKSPACE as for sfmp_gemm; the
+ * workspace's contents are irrelevant on entry. */
+int sfmp_kv_attention_workspace(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t q_heads,
+                                int32_t max_rows, int32_t max_tokens, int64_t* bytes);
+int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, const void* codes_dev, const float* scales_dev,
+                      const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch, const void* Q_dev, int32_t q_heads,
+                      int32_t dtype, int64_t q_stride, int32_t max_tokens, int32_t window, float scale, void* O_dev,
+                      int64_t o_stride, float* lse_dev, void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
+
+/* Device.  Page management without the host: no call reads anything back, so a decode loop with all of them can be
+ * captured in a graph.  n sequences per call, each at most once; the arrays are int32 [n] on the device.
+ *
+ * sfmp_kv_reserve: makes room for counts[i] more tokens (counts NULL: one) of sequence slots[i] and adds them to its
+ * length.  In the order of i, each sequence gets first a copy of its last page in all layers, if that page is partly
+ * filled and still held by another sequence too (copy on write: the last of its holders keeps it), then the pages that
+ * the new tokens need; new pages are the free ones of lowest number.  status_dev[0] = 0, or, with nothing changed at
+ * all, the number of pages that were missing, or -1 if a slot is out of range, a count negative or a row of the page
+ * table too short.  n <= SFMP_KV_MAX_BATCH.
+ * sfmp_kv_fork: children[i] becomes a copy of parents[i] that holds the same pages (several may share a parent).  A
+ * child must be empty (length 0) and no sequence may be both a parent and a child.
+ * sfmp_kv_free: sequence slots[i] keeps its first keep[i] tokens (keep NULL: none) and gives back the other pages.
+ * sfmp_kv_compact: moves the live pages with numbers >= n_live, n_live being the number of live pages, in ascending order into the free pages
+ * below it, in all layers, and renumbers page table and refs: afterwards the pages n_live .. pages-1 are free.
+ * status_dev[0] = n_live.
+ * sfmp_kv_pages_workspace: bytes of workspace for sfmp_kv_reserve and sfmp_kv_compact (256-byte aligned, contents
+ * irrelevant on entry). */
+int sfmp_kv_pages_workspace(const sfmp_kv_layout_t* layout, int64_t* bytes);
+int sfmp_kv_reserve(const sfmp_kv_layout_t* layout, void* codes_dev, float* scales_dev, const sfmp_kv_tables_t* tables,
+                    const int32_t* slots_dev, const int32_t* counts_dev, int32_t n, int32_t* status_dev,
+                    void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
+int sfmp_kv_fork(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const int32_t* parents_dev,
+                 const int32_t* children_dev, int32_t n, void* hip_stream);
+int sfmp_kv_free(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const int32_t* slots_dev,
+                 const int32_t* keep_dev, int32_t n, void* hip_stream);
+int sfmp_kv_compact(const sfmp_kv_layout_t* layout, void* codes_dev, float* scales_dev, const sfmp_kv_tables_t* tables,
+                    int32_t* status_dev, void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
+
+/* ---- Choice of the next token --------------------------------------------------------------------------------------
+ * Device.  One token for every row of logits (dtype SFMP_TYPE_FP16, _BF16 or _FP32; row r at logits + r * stride
+ * elements, vocab of them), from the caller's random number uniform[r] in [0, 1).  With m the row's largest logit and T
+ * its temperature, token i weighs w_i = exp((l_i - m) / T), held as a whole number of 2^-31 (a token below 2^-32 of the
+ * most probable one is never chosen).  Tokens are ordered by falling logit, equal ones by rising number, and kept as long as they are among
+ *   the first top_k (top_k <= 0: all), of these
+ *   the shortest prefix that holds at least top_p of their weight (top_p >= 1: all), and
+ *   those with (l_i - m) / T >= ln min_p (min_p <= 0: all; the most probable token always stays).
+ * The token is the first of the order whose running sum of weights exceeds uniform * (sum of the kept ones).  T <= 0
+ * takes the first token of the order.  NaN logits count as -infinity; a row without a logit above -infinity gives -1
+ * and the log-probability -infinity.  Sums of weights are whole numbers: the result does not depend on how the row was cut.
+ * temperature, top_k, top_p, min_p: fp32 / int32 / fp32 / fp32 [rows], each may be NULL (1, all, all, all).  tokens: int32
+ * [rows].  logprobs: NULL, or fp32 [rows], ln of w_token over the sum of all w of the row.
+ * SFMP_ERR_SHAPE: rows < 0, vocab < 1 or above 2^24, stride < vocab.  Alignment: logits to their element size. */
+int sfmp_sample_workspace(int32_t rows, int32_t vocab, int64_t* bytes);
+int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32_t vocab, int64_t stride,
+                const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,
+                const float* uniform_dev, int32_t* tokens_dev, float* logprobs_dev, void* workspace_dev,
+                int64_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -39,10 +39,31 @@ class SfmpGemvProblem(C.Structure):
                                           "bitmap", "row_perm", "Y")]
 
 
+class SfmpKvLayout(C.Structure):
+    _fields_ = [
+        ("pages", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("format", C.c_int32),
+        ("layers", C.c_int32), ("reserved", C.c_int32),
+        ("page_bytes", C.c_int64), ("codes_bytes", C.c_int64), ("scales_bytes", C.c_int64),
+    ]
+
+
+class SfmpKvTables(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("lengths", C.c_void_p), ("refs", C.c_void_p),
+                ("sequences", C.c_int32), ("table_pages", C.c_int32)]
+
+
+class SfmpKvBatch(C.Structure):
+    _fields_ = [("slots", C.c_void_p), ("row_start", C.c_void_p),
+                ("batch", C.c_int32), ("rows", C.c_int32), ("max_rows", C.c_int32), ("reserved", C.c_int32)]
+
+
 EXPORTS = ("sfmp_strerror", "sfmp_pack_query", "sfmp_layout_set_quant", "sfmp_pack", "sfmp_unpack", "sfmp_gemm_workspace",
            "sfmp_workspace_init", "sfmp_gemm", "sfmp_gemm_static", "sfmp_gemv_batched", "sfmp_gemm_batched_workspace",
            "sfmp_gemm_batched", "sfmp_check_perm", "sfmp_fold_perms", "sfmp_lut_pack_query",
-           "sfmp_lut_pack", "sfmp_lut_gemv_workspace", "sfmp_lut_gemv")
+           "sfmp_lut_pack", "sfmp_lut_gemv_workspace", "sfmp_lut_gemv",
+           "sfmp_kv_query", "sfmp_kv_append", "sfmp_kv_gather", "sfmp_kv_attention_workspace", "sfmp_kv_attention",
+           "sfmp_kv_pages_workspace", "sfmp_kv_reserve", "sfmp_kv_fork", "sfmp_kv_free", "sfmp_kv_compact",
+           "sfmp_sample_workspace", "sfmp_sample")
 
 
 def lib_path() -> str:
@@ -77,6 +98,19 @@ def load_library():
     lib.sfmp_lut_gemv_workspace.argtypes = [i32, i32, C.POINTER(i64)]
     lib.sfmp_lut_gemv.argtypes = [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp, i64, vp]
     lib.sfmp_fold_perms.argtypes = [vp, vp, i32, vp]
+    f32, KP, TP, BP, NP = C.c_float, C.POINTER(SfmpKvLayout), C.POINTER(SfmpKvTables), C.POINTER(SfmpKvBatch), C.POINTER(i64)
+    lib.sfmp_kv_query.argtypes = [i32, i32, i32, i32, i32, KP]
+    lib.sfmp_kv_append.argtypes = [KP, i32, vp, vp, TP, BP, vp, vp, i32, i64, i64, vp]
+    lib.sfmp_kv_gather.argtypes = [KP, i32, vp, vp, TP, BP, vp, vp, vp, i32, i64, i64, vp]
+    lib.sfmp_kv_attention_workspace.argtypes = [KP, i32, i32, i32, i32, i32, NP]
+    lib.sfmp_kv_attention.argtypes = [KP, i32, vp, vp, TP, BP, vp, i32, i32, i64, i32, i32, f32, vp, i64, vp, vp, i64, vp]
+    lib.sfmp_kv_pages_workspace.argtypes = [KP, NP]
+    lib.sfmp_kv_reserve.argtypes = [KP, vp, vp, TP, vp, vp, i32, vp, vp, i64, vp]
+    lib.sfmp_kv_fork.argtypes = [KP, TP, vp, vp, i32, vp]
+    lib.sfmp_kv_free.argtypes = [KP, TP, vp, vp, i32, vp]
+    lib.sfmp_kv_compact.argtypes = [KP, vp, vp, TP, vp, vp, i64, vp]
+    lib.sfmp_sample_workspace.argtypes = [i32, i32, NP]
+    lib.sfmp_sample.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
     for name in EXPORTS:
         if name != "sfmp_strerror":
             getattr(lib, name).restype = C.c_int
@@ -87,6 +121,7 @@ def load_library():
 class _NoExtension:
     """Stands in for the extension where there is none to use: leaves every call to the ctypes path."""
     gemm = gemm_static = gemv_batched = gemm_batched = staticmethod(lambda *args: None)
+    kv_append = kv_gather = kv_attention = kv_reserve = kv_fork = kv_free = kv_compact = sample = gemm
 
 
 _LAUNCHER = None  # (library, extension module bound to it)
@@ -130,6 +165,9 @@ def _launcher():
         module.bind(SfmpLayout, torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream,
                     *(C.cast(f, C.c_void_p).value for f in (lib.sfmp_gemm, lib.sfmp_gemm_static, lib.sfmp_gemv_batched,
                                                             lib.sfmp_gemm_batched)))
+        module.bind_kv(SfmpKvLayout, *(C.cast(f, C.c_void_p).value for f in (
+            lib.sfmp_kv_append, lib.sfmp_kv_gather, lib.sfmp_kv_attention, lib.sfmp_kv_reserve, lib.sfmp_kv_fork, lib.sfmp_kv_free,
+            lib.sfmp_kv_compact, lib.sfmp_sample)))
     except ImportError as e:
         warnings.warn(f"launches are marshalled by ctypes, some 8 us of host time more per call: {e}; build it with "
                       "`python -m paper_2602_01027_amd.build` (or __graft_entry__.build())", RuntimeWarning, stacklevel=3)

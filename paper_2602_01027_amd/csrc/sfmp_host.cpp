@@ -87,7 +87,7 @@ const char* sfmp_strerror(int code) {
   switch (code) {
     case SFMP_OK: return "ok";
     case SFMP_ERR_NULL: return "a required pointer is NULL";
-    case SFMP_ERR_SHAPE: return "bad shape: N and K must be positive multiples of 128 and M >= 1";
+    case SFMP_ERR_SHAPE: return "bad shape: N and K must be positive multiples of 128 and M >= 1 (cache and sampling calls: a size or parameter outside the range that the header states)";
     case SFMP_ERR_BITWIDTH: return "bitmap entry is not 2, 3 or 4";
     case SFMP_ERR_CODE_RANGE: return "code out of range for its tile's bit-width";
     case SFMP_ERR_WORKSPACE: return "workspace missing, not 256-byte aligned, or too small";

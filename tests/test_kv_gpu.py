@@ -1,0 +1,539 @@
+"""The 8-bit paged cache on the GPU against the CPU oracle: writes and read-back, attention, pages."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import sfmp_kv_oracle as O
+from kv_util import (PAGE, U16, UB16, attention_bound, lse_bound, make_pool, make_tables, pages_of, random_codes, stale_slots, upload)
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _torch():
+    import torch
+    assert torch.cuda.is_available()
+    import paper_2602_01027_amd as S
+    return torch, S
+
+
+def _dev(torch, a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def _rows(torch, rng, rows, heads, dim, dtype, apart, std=1.0):
+    """(tensor whose rows lie `apart` elements further from each other than they are long, its exact values)."""
+    t = torch.from_numpy(rng.normal(0.0, std, size=(rows, heads * dim + apart)).astype(np.float32)).to(getattr(torch, dtype)).to(DEV)
+    t = t[:, :heads * dim].view(rows, heads, dim)
+    return t, t.float().cpu().numpy()
+
+
+def _starts(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+
+
+# ---- writes and read-back ---------------------------------------------------------------------------------------------
+
+# (tokens before, new tokens) of the entries of a call: none, one token into an empty, partly filled, full page; runs that
+# end before, at and behind page borders; more rows than the sequence has tokens
+RAGGED = [(0, 1), (40, 1), (63, 1), (64, 1), (5, 0), (0, 63), (1, 63), (0, 64), (30, 65), (64, 130), (100, 200)]
+SINGLE = [(0, 1), (1, 1), (40, 1), (63, 1), (64, 1), (200, 1)]
+
+
+def _append_both(fmt, dim, heads, dtype, entries, seed, ragged=True, layers=2, change=None):
+    torch, S = _torch()
+    rng = np.random.default_rng(seed)
+    counts = [n for _, n in entries]
+    lengths = [a + n for a, n in entries]
+    pages = sum(pages_of(n) for n in lengths) + 5
+    pool = make_pool(rng, layers, pages, heads, dim, fmt)
+    order = rng.permutation(len(entries))  # entry b is sequence order[b]
+    by_slot = np.zeros(len(entries), dtype=int)
+    by_slot[order] = lengths
+    tables = make_tables(rng, by_slot, max(pages_of(n) for n in lengths) + 1, pages)
+    cache, dt = upload(S, pool, tables, fmt)
+    start = _starts(counts)
+    K, k = _rows(torch, rng, start[-1], heads, dim, dtype, 16)
+    V, v = _rows(torch, rng, start[-1], heads, dim, dtype, 0)
+    if change:
+        change(K, V)
+        k, v = K.float().cpu().numpy(), V.float().cpu().numpy()
+    S.sfmp_kv_append(cache, 1, dt, _dev(torch, order.astype(np.int32)), _dev(torch, start) if ragged else None, K, V, max(counts))
+    torch.cuda.synchronize()
+    want = dict(codes=pool["codes"].copy(), scales=pool["scales"].copy())
+    O.append(want, 1, tables, order, start, k, v, fmt)
+    return S, torch, pool, want, tables, cache, dt, order, start
+
+
+def _same_codes(fmt, dim, pool, want, got):
+    """Codes of the oracle's rounding, except where its quotient lies at a tie: x / scale is computed in fp32 as x * (1 / scale),
+    off by 3 U32 of at most 127, so that only quotients within 2^-15 of a tie may go to the other side."""
+    if fmt == "fp8":  # scales are powers of two: no rounding before the one to 8 bits
+        assert np.array_equal(O.decode(got, fmt), O.decode(want, fmt), equal_nan=True)
+        return
+    off = np.abs(got.astype(int) - want.astype(int))
+    assert off.max() <= 1 and (off > 0).mean() < 2e-4, (off.max(), (off > 0).mean())
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("dim,heads,dtype,entries,ragged", [(128, 2, "float16", RAGGED, True), (64, 3, "bfloat16", RAGGED, True),
+                                                            (256, 1, "float16", RAGGED, True), (128, 8, "bfloat16", SINGLE, False),
+                                                            (64, 1, "float16", SINGLE, False), (256, 2, "bfloat16", SINGLE, False),
+                                                            (128, 2, "float16", [(0, 3), (20, 5)], True)])
+def test_append(fmt, dim, heads, dtype, entries, ragged):
+    S, torch, pool, want, tables, cache, dt, order, start = _append_both(fmt, dim, heads, dtype, entries, 100 + dim + heads, ragged)
+    got, scales = cache.codes.cpu().numpy(), cache.scales.cpu().numpy()
+    assert np.array_equal(got[0], pool["codes"][0]) and np.array_equal(scales[0], pool["scales"][0])  # the other layer
+    assert np.allclose(scales[1], want["scales"][1], rtol=2.0 ** -22, atol=0.0)
+    _same_codes(fmt, dim, pool, want["codes"][1], got[1])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_append_leaves_out_rows_before_the_first_token(fmt):
+    torch, S = _torch()
+    rng = np.random.default_rng(3)
+    pool = make_pool(rng, 1, 4, 2, 64, fmt)
+    tables = make_tables(rng, [70, 0, 2], 2, 4)
+    cache, dt = upload(S, pool, tables, fmt)
+    start = np.array([0, 75, 76, 79], dtype=np.int32)  # 75 rows for 70 tokens, one for none, 3 for 2
+    K, k = _rows(torch, rng, 79, 2, 64, "float16", 0)
+    V, v = _rows(torch, rng, 79, 2, 64, "float16", 0)
+    S.sfmp_kv_append(cache, 0, dt, None, _dev(torch, start), K, V, 75)
+    O.append(pool, 0, tables, [0, 1, 2], start, k, v, fmt)
+    assert np.allclose(cache.scales.cpu().numpy(), pool["scales"], rtol=2.0 ** -22, atol=0.0)
+    _same_codes(fmt, 64, None, pool["codes"], cache.codes.cpu().numpy())
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_append_of_zeros_tiny_huge_and_no_numbers(fmt):
+    def change(K, V):
+        K[0:1] = 0.0
+        V[0:1] = 1e-38
+        K[1:2, 0] = 3e38
+        V[1, 1, 7] = math.inf
+        K[2, 1, 100] = math.nan
+        V[3:4] *= 1e30
+    entries = [(0, 1), (0, 1), (10, 1), (12, 1), (64, 1), (3, 1)]
+    S, torch, pool, want, tables, cache, dt, order, start = _append_both(fmt, 128, 2, "bfloat16", entries, 11, change=change)
+    got, scales = cache.codes.cpu().numpy(), cache.scales.cpu().numpy()
+    assert np.allclose(scales[1], want["scales"][1], rtol=2.0 ** -22, atol=0.0, equal_nan=True)
+    assert np.isnan(scales[1]).sum() == 2 and (scales[1] == 0).sum() == 4
+    fine = ~np.isnan(want["scales"][1])
+    _same_codes(fmt, 128, None, want["codes"][1][fine], got[1][fine])
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("dim,dtype", [(64, "float32"), (128, "float16"), (256, "bfloat16"), (128, "float32")])
+def test_gather(fmt, dim, dtype):
+    torch, S = _torch()
+    rng = np.random.default_rng(21)
+    lengths = [0, 1, 63, 64, 65, 300]
+    first, counts = [0, 0, 5, 63, 64, 70], [2, 1, 58, 3, 1, 229]  # (some past the end of their sequences)
+    pool = make_pool(rng, 2, 14, 3, dim, fmt)
+    tables = make_tables(rng, lengths, 6, 14)
+    stale_slots(pool, tables, fmt, dim)
+    cache, dt = upload(S, pool, tables, fmt)
+    start = _starts(counts)
+    out = [torch.full((int(start[-1]), 3 * dim + 8), math.nan, dtype=getattr(torch, dtype), device=DEV) for _ in range(2)]
+    K, V = (t[:, :3 * dim].view(-1, 3, dim) for t in out)
+    S.sfmp_kv_gather(cache, 1, dt, None, _dev(torch, np.array(first, dtype=np.int32)), _dev(torch, start), K, V, max(counts))
+    for which, got in ((0, K), (1, V)):
+        for s in range(len(lengths)):
+            all_ = O.dense(pool, 1, tables, s, fmt, dim)[which]
+            want = np.zeros((counts[s], 3, dim))
+            part = all_[first[s]:first[s] + counts[s]]
+            want[:len(part)] = part
+            # one product in fp32, rounded once: to fp32 as it is, to 16 bits the oracle's value rounded to fp32 first
+            ref = torch.from_numpy(want.astype(np.float32)).to(getattr(torch, dtype))
+            assert torch.equal(got[start[s]:start[s + 1]].cpu(), ref), (which, s)
+    assert all(torch.isnan(t[:, 3 * dim:]).all() for t in out)  # nothing beside the rows
+
+
+# ---- attention --------------------------------------------------------------------------------------------------------
+
+def _attend(fmt, dim, heads, group, dtype, entries, window=0, seed=0, slots=True, apart=8, q_std=1.5, max_tokens=None, change=None,
+            scale=None):
+    """entries: (rows, tokens).  Runs the call, compares it with the oracle, returns what a test may look at."""
+    torch, S = _torch()
+    rng = np.random.default_rng(1000 + seed)
+    counts, lengths = [n for n, _ in entries], [t for _, t in entries]
+    pages = sum(pages_of(t) for t in lengths) + 3
+    pool = make_pool(rng, 2, pages, heads, dim, fmt)
+    order = rng.permutation(len(entries)) if slots else np.arange(len(entries))
+    by_slot = np.zeros(len(entries), dtype=int)
+    by_slot[order] = lengths
+    tables = make_tables(rng, by_slot, max(1, max(pages_of(t) for t in lengths)), pages)
+    stale_slots(pool, tables, fmt, dim)
+    if change:
+        change(pool, tables, order)
+    cache, dt = upload(S, pool, tables, fmt)
+    start = _starts(counts)
+    ragged = any(n != 1 for n in counts)
+    rows = int(start[-1])
+    Q, q = _rows(torch, rng, rows, heads * group, dim, dtype, apart, q_std)
+    out = torch.full((rows, heads * group * dim + apart), math.nan, dtype=getattr(torch, dtype), device=DEV)
+    got = out[:, :heads * group * dim].view(rows, heads * group, dim)
+    lse = torch.full((rows, heads * group), math.nan, dtype=torch.float32, device=DEV)
+    most, tokens = max(counts), max_tokens or max(1, max(lengths))
+    ws = torch.full((S.sfmp_kv_attention_workspace(cache.layout, len(entries), rows, heads * group, most, tokens),), 0xFF, dtype=torch.uint8,
+                    device=DEV)
+    scale = scale or 1.0 / math.sqrt(dim)
+    args = (cache, 1, dt, _dev(torch, order.astype(np.int32)) if slots else None, _dev(torch, start) if ragged or not slots else None, Q, got,
+            most, tokens, scale, ws)
+    S.sfmp_kv_attention(*args, window=window, lse=lse)
+    torch.cuda.synchronize()
+    a, z = got.float().cpu().numpy().astype(np.float64), lse.cpu().numpy().astype(np.float64)
+    assert torch.isnan(out[:, heads * group * dim:]).all() or apart == 0
+    for b in range(len(entries)):
+        k, v = O.dense(pool, 1, tables, order[b], fmt, dim)
+        r = slice(int(start[b]), int(start[b + 1]))
+        want, wlse, spread, products = O.attention(q[r], k, v, scale, window)
+        none = np.isneginf(wlse)
+        assert np.array_equal(none, np.isneginf(z[r])) and (a[r][none] == 0).all(), (b, entries[b])
+        nan = np.isnan(wlse)
+        assert np.isnan(z[r][nan]).all() and np.isnan(a[r][nan]).all() and np.isnan(want[nan]).all()
+        fine = ~(none | nan)
+        bound = attention_bound(U16 if dtype == "float16" else UB16, want, spread, products)[fine]
+        err = np.abs(a[r] - want)[fine]
+        bad = ~((err <= bound) | (np.isnan(a[r][fine]) & np.isnan(want[fine])))
+        assert not bad.any(), (b, entries[b], err[bad].max(), bound[bad].min())
+        assert (np.abs(z[r][fine] - wlse[fine]) <= lse_bound(wlse, products)[fine]).all(), (b, entries[b])
+    return args, dict(window=window, lse=lse), got, lse
+
+
+TOKENS = [(1, 1), (1, 63), (1, 64), (1, 65), (1, 500), (1, 1000), (1, 2)]
+DRAFTS = [(3, 3), (4, 64), (1, 200), (0, 70), (5, 66), (4, 700), (2, 1), (3, 0)]
+CHUNKS = [(40, 40), (17, 130), (1, 300), (33, 97), (0, 5), (64, 64), (9, 4), (65, 600)]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("dim,heads,group,dtype", [(128, 2, 4, "float16"), (128, 1, 8, "bfloat16"), (64, 3, 1, "bfloat16"), (64, 1, 5, "float16"),
+                                                   (256, 2, 2, "float16"), (128, 1, 16, "float16"), (128, 1, 20, "bfloat16"),
+                                                   (256, 1, 17, "bfloat16"), (64, 1, 40, "float16")])
+def test_attention_of_single_tokens(fmt, dim, heads, group, dtype):
+    _attend(fmt, dim, heads, group, dtype, TOKENS, seed=dim + group)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("window", [0, 1, 70])
+@pytest.mark.parametrize("dim,heads,group,dtype", [(128, 2, 4, "bfloat16"), (64, 2, 3, "float16"), (256, 1, 2, "float16"), (128, 1, 7, "float16")])
+def test_attention_of_a_few_rows(fmt, window, dim, heads, group, dtype):
+    _attend(fmt, dim, heads, group, dtype, DRAFTS, window=window, seed=dim + group + window)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("window", [0, 50])
+@pytest.mark.parametrize("dim,heads,group,dtype", [(128, 2, 4, "float16"), (64, 3, 1, "bfloat16"), (256, 1, 2, "bfloat16"), (128, 1, 3, "bfloat16"),
+                                                   (64, 1, 6, "float16")])
+def test_attention_of_chunks(fmt, window, dim, heads, group, dtype):
+    _attend(fmt, dim, heads, group, dtype, CHUNKS, window=window, seed=dim + group + window)
+
+
+@pytest.mark.parametrize("rows,tokens,heads,group,window", [(1, 20000, 1, 8, 0), (2, 9000, 2, 4, 5000), (1, 6000, 4, 2, 0), (130, 3000, 1, 4, 0),
+                                                            (300, 300, 2, 4, 0), (257, 700, 1, 8, 300)])
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+def test_attention_of_one_sequence(fmt, rows, tokens, heads, group, window):
+    _attend(fmt, 128, heads, group, "float16", [(rows, tokens)], window=window, seed=tokens)
+
+
+@pytest.mark.parametrize("batch", [1, 2, 65, 130, 300])
+def test_attention_of_batches(batch):
+    rng = np.random.default_rng(batch)
+    lengths = np.exp(rng.uniform(0, math.log(600), batch)).astype(int)
+    lengths[::7] = 0
+    lengths[-1] = 1500
+    _attend("int8", 64, 1, 4, "float16", [(1, int(t)) for t in lengths], seed=batch)
+
+
+def test_attention_without_slots_and_with_room_in_max_tokens():
+    _attend("int8", 128, 2, 4, "float16", TOKENS, slots=False, max_tokens=70000, apart=0)
+    _attend("fp8", 64, 2, 2, "bfloat16", CHUNKS, slots=False, max_tokens=9000, apart=0)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("entries", [TOKENS, CHUNKS])
+def test_attention_with_scales_far_apart(fmt, entries):
+    # scales of V that grow, fall and vanish from page to page: the sums are kept relative to the largest so far
+    def change(pool, tables, order):
+        rng = np.random.default_rng(5)
+        power = rng.choice([-90, -40, -12, 0, 12, 60], size=pool["scales"].shape[:3])
+        pool["scales"][..., 1] = 2.0 ** power
+        pool["scales"][:, ::5, :, 1] = 0.0
+        pool["scales"][:, 1::6, :, 0] = 0.0
+    torch, S = _torch()
+    _attend(fmt, 128, 2, 2, "bfloat16", entries, change=change, seed=77)
+
+
+@pytest.mark.parametrize("entries", [[(1, 200), (1, 64)], [(40, 200), (100, 100), (70, 64)]])
+def test_a_page_that_reads_as_nan_reaches_the_rows_that_see_it_and_no_others(entries):
+    # the last page of every sequence: rows that stand before it must not meet its scales
+    def change(pool, tables, order):
+        for s, n in enumerate(tables["lengths"]):
+            pool["scales"][:, tables["table"][s, (n - 1) // PAGE]] = math.nan
+    _attend("int8", 128, 1, 2, "float16", entries, change=change, seed=9)
+
+
+def test_attention_of_peaked_and_flat_rows():
+    _attend("int8", 128, 1, 4, "float16", TOKENS + DRAFTS, q_std=60.0, seed=1)
+    _attend("fp8", 128, 1, 4, "bfloat16", CHUNKS, q_std=1e-3, seed=2)
+    _attend("int8", 64, 1, 4, "bfloat16", CHUNKS, q_std=1e5, scale=1e-6, seed=3)
+
+
+@pytest.mark.parametrize("entries", [[(1, 5000)] * 3, DRAFTS, CHUNKS, [(200, 900)]])
+def test_attention_gives_the_same_bits_every_time_and_on_any_stream(entries):
+    torch, S = _torch()
+    args, more, got, lse = _attend("int8", 128, 2, 4, "float16", entries, seed=4)
+    first, flse = got.clone(), lse.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for stream in (None, side):
+        got.fill_(math.nan)
+        args[-1].fill_(0x7F)
+        if stream:
+            stream.wait_stream(torch.cuda.current_stream())
+        S.sfmp_kv_attention(*args, **more, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, first) and torch.equal(lse, flse)
+
+
+@pytest.mark.parametrize("path", ["attention", "append", "gather"])
+def test_cache_beyond_4_gib(path):
+    # page numbers whose byte offsets need more than 32 bits
+    torch, S = _torch()
+    heads, dim, pages = 8, 128, 40000  # 5.2 GB
+    layout = S.sfmp_kv_query(pages, heads, dim, "int8")
+    cache = S.make_kv_cache(layout)
+    tables = S.make_kv_tables(layout, 1, 4)
+    ids = [pages - 1, 33000, pages - 2]
+    tables.page_table[0, :3] = torch.tensor(ids, dtype=torch.int32)
+    tables.lengths[0] = 150
+    rng = np.random.default_rng(8)
+    small = make_pool(rng, 1, 3, heads, dim, "int8")
+    cache.codes[0, ids] = _dev(torch, small["codes"][0])
+    cache.scales[0, ids] = _dev(torch, small["scales"][0].astype(np.float32))
+    st = dict(table=np.array([[0, 1, 2, -1]]), lengths=np.array([150]), refs=np.ones(3))
+    k, v = O.dense(small, 0, st, 0, "int8", dim)
+    if path == "attention":
+        for n in (1, 30):
+            Q, q = _rows(torch, rng, n, heads, dim, "float16", 0)
+            got = torch.empty_like(Q)
+            ws = torch.empty(S.sfmp_kv_attention_workspace(layout, 1, n, heads, n, 150), dtype=torch.uint8, device=DEV)
+            S.sfmp_kv_attention(cache, 0, tables, None, _dev(torch, _starts([n])), Q, got, n, 150, 0.09, ws)
+            want, _, spread, products = O.attention(q, k, v, 0.09)
+            assert (np.abs(got.float().cpu().numpy() - want) <= attention_bound(U16, want, spread, products)).all()
+    elif path == "append":
+        X, x = _rows(torch, rng, 30, heads, dim, "float16", 0)
+        S.sfmp_kv_append(cache, 0, tables, None, _dev(torch, _starts([30])), X, X, 30)
+        O.append(small, 0, st, [0], [0, 30], x, x, "int8")
+        _same_codes("int8", dim, None, small["codes"][0], cache.codes[0, ids].cpu().numpy())
+    else:
+        out = torch.empty((150, heads, dim), dtype=torch.float32, device=DEV)
+        out2 = torch.empty_like(out)
+        S.sfmp_kv_gather(cache, 0, tables, None, torch.zeros(1, dtype=torch.int32, device=DEV), _dev(torch, _starts([150])), out, out2, 150)
+        assert np.array_equal(out.cpu().numpy(), k.astype(np.float32)) and np.array_equal(out2.cpu().numpy(), v.astype(np.float32))
+
+
+def test_tables_with_entries_out_of_range_are_never_followed():
+    # slots, lengths and page numbers outside their ranges: the calls return, the entries read as empty or as page 0
+    torch, S = _torch()
+    layout = S.sfmp_kv_query(4, 2, 64, "fp8")
+    cache = S.make_kv_cache(layout)
+    cache.codes.zero_(), cache.scales.fill_(1.0)
+    tables = S.make_kv_tables(layout, 3, 2)
+    tables.page_table.copy_(torch.tensor([[0, 99], [-7, 2 ** 31 - 1], [1, 2]], dtype=torch.int32))
+    tables.lengths.copy_(torch.tensor([10 ** 6, 100, -5], dtype=torch.int32))
+    slots = torch.tensor([0, 1, 2, -1, 3, 2 ** 31 - 1], dtype=torch.int32, device=DEV)
+    for n in (1, 40):
+        x = torch.ones((6 * n, 2, 64), dtype=torch.float16, device=DEV)
+        start = _dev(torch, _starts([n] * 6))
+        got = torch.full_like(x, math.nan)
+        ws = torch.empty(S.sfmp_kv_attention_workspace(layout, 6, 6 * n, 2, n, 128), dtype=torch.uint8, device=DEV)
+        S.sfmp_kv_attention(cache, 0, tables, slots, start, x, got, n, 128, 1.0, ws)
+        assert (got[2 * n:] == 0).all()
+        S.sfmp_kv_append(cache, 0, tables, slots, start, x, x, n)
+        S.sfmp_kv_gather(cache, 0, tables, slots, torch.zeros(6, dtype=torch.int32, device=DEV), start, x, x, n)
+    S.sfmp_kv_fork(cache, tables, slots[3:4], slots[4:5])
+    S.sfmp_kv_free(cache, tables, slots[3:])
+    torch.cuda.synchronize()
+
+
+# ---- pages ------------------------------------------------------------------------------------------------------------
+
+def _pages_equal(cache, dt, pool, tables):
+    assert np.array_equal(dt.lengths.cpu().numpy(), tables["lengths"])
+    assert np.array_equal(dt.refs.cpu().numpy(), tables["refs"])
+    table = dt.page_table.cpu().numpy()
+    for s, n in enumerate(tables["lengths"]):
+        assert np.array_equal(table[s, :pages_of(n)], tables["table"][s, :pages_of(n)]), s
+    live = tables["refs"] > 0
+    assert np.array_equal(cache.codes.cpu().numpy()[:, live], pool["codes"][:, live])
+    assert np.array_equal(cache.scales.cpu().numpy()[:, live], pool["scales"][:, live])
+
+
+@pytest.mark.parametrize("pages,sequences,dim,layers,seed", [(40, 8, 64, 1, 0), (300, 40, 64, 2, 1), (9000, 30, 64, 1, 2), (50, 12, 128, 3, 3)])
+def test_pages_through_a_random_history(pages, sequences, dim, layers, seed):
+    torch, S = _torch()
+    rng = np.random.default_rng(seed)
+    pool = make_pool(rng, layers, pages, 1, dim, "int8")
+    pool["scales"] = pool["scales"].astype(np.float32)
+    tables = dict(table=np.full((sequences, 30), -1, dtype=np.int32), lengths=np.zeros(sequences, dtype=np.int32),
+                  refs=np.zeros(pages, dtype=np.int32))
+    if pages > 4096:  # most of a large pool is in use by others
+        tables["refs"][:pages - 200] = 1
+    cache, dt = upload(S, pool, tables, "int8")
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = torch.full((S.sfmp_kv_pages_workspace(cache.layout),), 0xFF, dtype=torch.uint8, device=DEV)
+    seen = set()
+    for step in range(60):
+        what = rng.choice(["reserve", "one", "fork", "free", "trim", "compact"] if pages <= 4096 else ["reserve", "one", "fork", "free", "trim"])
+        some = rng.permutation(sequences)[:rng.integers(1, sequences + 1)].astype(np.int32)
+        if what in ("reserve", "one"):
+            counts = None if what == "one" else np.minimum(rng.geometric(0.005, len(some)) - 1, 2500).astype(np.int32)
+            S.sfmp_kv_reserve(cache, dt, _dev(torch, some), None if counts is None else _dev(torch, counts), status, ws)
+            want = O.reserve(pool, tables, some, [1] * len(some) if counts is None else counts)
+            assert int(status) == want
+            seen.add(np.sign(want))
+        elif what == "fork":
+            empty = [s for s in range(sequences) if tables["lengths"][s] == 0]
+            full = [s for s in range(sequences) if tables["lengths"][s] > 0]
+            if not empty or not full:
+                continue
+            children = np.array(empty[:rng.integers(1, len(empty) + 1)], dtype=np.int32)
+            parents = rng.choice(full[:3], len(children)).astype(np.int32)
+            S.sfmp_kv_fork(cache, dt, _dev(torch, parents), _dev(torch, children))
+            O.fork(tables, parents, children)
+        elif what in ("free", "trim"):
+            some = some[:max(1, len(some) // 3)]
+            keep = None if what == "free" else rng.integers(0, 300, len(some)).astype(np.int32)
+            S.sfmp_kv_free(cache, dt, _dev(torch, some), None if keep is None else _dev(torch, keep))
+            O.free(tables, some, keep)
+        else:
+            S.sfmp_kv_compact(cache, dt, status, ws)
+            assert int(status) == O.compact(pool, tables)
+        _pages_equal(cache, dt, pool, tables)
+    assert 0 in seen and (1 in seen or pages > 50)
+
+
+def test_reserve_changes_nothing_where_it_refuses():
+    torch, S = _torch()
+    rng = np.random.default_rng(0)
+    pool = make_pool(rng, 1, 6, 1, 64, "int8")
+    pool["scales"] = pool["scales"].astype(np.float32)
+    tables = make_tables(rng, [70, 64, 3], 3, 6, spare=1)
+    O.fork(tables, [0], [3])
+    cache, dt = upload(S, pool, tables, "int8")
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(S.sfmp_kv_pages_workspace(cache.layout), dtype=torch.uint8, device=DEV)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    # (two free pages; a copy of the shared page, two and one new ones are wanted)
+    for slots, counts, want in (((0, 1, 2), (1, 100, 62), 2), ((1, 0), (0, 123), -1), ((0, 4), (1, 1), -1), ((-1,), (1,), -1), ((2,), (-1,), -1),
+                                ((2,), (2 ** 31 - 1,), -1)):
+        S.sfmp_kv_reserve(cache, dt, i32(*slots), i32(*counts), status, ws)
+        assert int(status) == want, (slots, counts)
+        _pages_equal(cache, dt, pool, tables)
+    S.sfmp_kv_reserve(cache, dt, i32(), None, status, ws)
+    assert int(status) == 0
+
+
+def test_reserve_of_the_most_sequences_of_a_call():
+    torch, S = _torch()
+    rng = np.random.default_rng(1)
+    n, pages = 1024, 5000
+    pool = make_pool(rng, 1, pages, 1, 64, "int8")
+    pool["scales"] = pool["scales"].astype(np.float32)
+    tables = dict(table=np.full((n, 4), -1, dtype=np.int32), lengths=np.zeros(n, dtype=np.int32), refs=np.zeros(pages, dtype=np.int32))
+    cache, dt = upload(S, pool, tables, "int8")
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = torch.empty(S.sfmp_kv_pages_workspace(cache.layout), dtype=torch.uint8, device=DEV)
+    order = rng.permutation(n).astype(np.int32)
+    first, rest = order[:3], order[3:]
+    steps = [(first, np.array([70, 130, 1])), (order, rng.integers(0, 130, n)), (order, np.ones(n, dtype=int))]
+    for i, (slots, counts) in enumerate(steps):
+        if i == 1:  # many holders of three partly filled pages
+            parents = rng.choice(first, len(rest)).astype(np.int32)
+            S.sfmp_kv_fork(cache, dt, _dev(torch, parents), _dev(torch, rest))
+            O.fork(tables, parents, rest)
+        S.sfmp_kv_reserve(cache, dt, _dev(torch, slots), _dev(torch, counts.astype(np.int32)), status, ws)
+        assert int(status) == O.reserve(pool, tables, slots, counts)
+        _pages_equal(cache, dt, pool, tables)
+
+
+def test_a_decode_loop_in_a_graph():
+    # reserve, append and attention of one token per sequence, captured once and replayed: nothing in it asks the host
+    torch, S = _torch()
+    rng = np.random.default_rng(4)
+    heads, group, dim, n, fmt = 2, 4, 128, 5, "int8"
+    lengths = [1, 60, 63, 64, 300]
+    pool = make_pool(rng, 1, 40, heads, dim, fmt)
+    tables = make_tables(rng, lengths, 12, 40)
+    caches = [upload(S, pool, tables, fmt) for _ in range(2)]
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    slots = torch.arange(n, dtype=torch.int32, device=DEV)
+    layout = caches[0][0].layout
+    ws = torch.empty(S.sfmp_kv_pages_workspace(layout), dtype=torch.uint8, device=DEV)
+    aws = torch.empty(S.sfmp_kv_attention_workspace(layout, n, n, heads * group, 1, 12 * PAGE), dtype=torch.uint8, device=DEV)
+    x = [torch.zeros((n, h, dim), dtype=torch.float16, device=DEV) for h in (heads, heads, heads * group)]
+    out = torch.empty_like(x[2])
+
+    def step(cache, dt):
+        S.sfmp_kv_reserve(cache, dt, slots, None, status, ws)
+        S.sfmp_kv_append(cache, 0, dt, slots, None, x[0], x[1], 1)
+        S.sfmp_kv_attention(cache, 0, dt, slots, None, x[2], out, 1, 12 * PAGE, 0.1, aws)
+
+    scratch = upload(S, pool, tables, fmt)
+    step(*scratch)  # (first calls of the kernels outside the capture)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*caches[0])
+    for _ in range(6):
+        for t in x:
+            t.copy_(torch.randn(t.shape, generator=torch.Generator().manual_seed(int(rng.integers(1 << 30)))).half())
+        graph.replay()
+        torch.cuda.synchronize()
+        first = out.clone()
+        step(*caches[1])
+        assert torch.equal(first, out) and int(status) == 0
+        assert torch.equal(caches[0][1].lengths, caches[1][1].lengths) and torch.equal(caches[0][0].scales, caches[1][0].scales)
+    assert caches[0][1].lengths.tolist() == [t + 6 for t in lengths]
+
+
+# ---- marshalling ------------------------------------------------------------------------------------------------------
+
+def test_both_ways_of_marshalling_give_the_same(monkeypatch):
+    torch, S = _torch()
+    B = S.binding
+    results = []
+    for ctypes_only in (False, True):
+        if ctypes_only:
+            monkeypatch.setattr(B, "_LAUNCHER", (S.load_library(), B._NoExtension))
+        args, more, got, lse = _attend("fp8", 64, 2, 2, "bfloat16", DRAFTS, seed=6)
+        _, _, _, _, _, cache, _, _, _ = _append_both("int8", 64, 2, "float16", RAGGED, 5)
+        results.append((got.clone(), lse.clone(), cache.codes.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_binding_refuses_wrong_tensors():
+    torch, S = _torch()
+    layout = S.sfmp_kv_query(4, 2, 64)
+    cache, tables = S.make_kv_cache(layout), S.make_kv_tables(layout, 2, 3)
+    x = torch.zeros((2, 2, 64), dtype=torch.float16, device=DEV)
+    i = torch.zeros(2, dtype=torch.int32, device=DEV)
+    w = torch.zeros(1 << 16, dtype=torch.uint8, device=DEV)
+    attend = lambda **k: S.sfmp_kv_attention(*[k.get(n, d) for n, d in (  # noqa: E731
+        ("cache", cache), ("layer", 0), ("tables", tables), ("slots", i), ("row_start", None), ("Q", x), ("O", x.clone()), ("max_rows", 1),
+        ("max_tokens", 64), ("scale", 1.0), ("workspace", w))], lse=k.get("lse"))
+    attend()
+    for bad in (dict(Q=x.float()), dict(Q=x[:, :, :32]), dict(Q=x.transpose(0, 1)), dict(O=x.bfloat16()), dict(O=x[:1]), dict(slots=i.long()),
+                dict(slots=i[None]), dict(lse=x), dict(row_start=i), dict(Q=torch.zeros((2, 2, 128), dtype=torch.float16, device=DEV)[:, :, ::2]),
+                dict(cache=S.DeviceKvCache(layout, cache.codes[:, :2], cache.scales)), dict(cache=S.DeviceKvCache(layout, cache.codes, cache.scales.half())),
+                dict(tables=S.DeviceKvTables(tables.page_table.t(), tables.lengths, tables.refs)),
+                dict(tables=S.DeviceKvTables(tables.page_table, tables.lengths[:1], tables.refs)),
+                dict(tables=S.DeviceKvTables(tables.page_table, tables.lengths, tables.refs[:3]))):
+        with pytest.raises((ValueError, AttributeError)):
+            attend(**bad)
+    for bad, code in ((dict(layer=1), -2), (dict(workspace=w[:0]), -5), (dict(max_rows=2), -2), (dict(scale=-1.0), -2), (dict(workspace=None), -5)):
+        with pytest.raises(S.SfmpError) as e:
+            attend(**bad)
+        assert e.value.code == code
