@@ -4,7 +4,9 @@
 namespace sfmp {
 namespace {
 
-constexpr int kWaves = 8;  // wavefronts of a workgroup
+// Wavefronts of a workgroup: two per SIMD, or, where sums and operands take more than half of its registers, one.
+template <int D, int NT>
+constexpr int kWaves = D * NT >= 256 ? 4 : 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 // Weights are rounded to fp16 after multiplication by 2^14: a product with V then keeps its 11 bits down to 2^-28 of the largest.
 constexpr float kWeightUnit = 16384.0f;
@@ -162,25 +164,31 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) p.o[nt][dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
+  if (begin >= end) return;
   float reference = kLeastReference;  // largest scale of V so far: weights are multiplied by scale / reference
+  // Numbers and scales of 64 pages at a time, one per lane
   int held_page = 0;
   float held_k = 0.0f, held_v = 0.0f;
+  auto hold = [&](int page) {
+    held_page = max(kv_page(a.v, e.slot, min(page + lane, end - 1)), 0);
+    const float* const s = kv_scale(a.v, held_page, head, 0);
+    held_k = s[0];
+    held_v = s[1];
+  };
+  hold(begin);
+  const uint8_t* block = kv_block<D>(a.v, __builtin_amdgcn_readlane(held_page, 0), head, 0);
+  PageCodes<D> c;
+  load_keys<D>(block, c);
+  load_values<D>(block, c);
   for (int page = begin; page < end; ++page) {
-    if ((page - begin) % 64 == 0) {  // the next 64 pages' numbers and scales, one per lane
-      const int mine = min(page + lane, end - 1);
-      held_page = max(kv_page(a.v, e.slot, mine), 0);
-      const float* const s = kv_scale(a.v, held_page, head, 0);
-      held_k = s[0];
-      held_v = s[1];
-    }
     const int at = (page - begin) % 64;
-    const int id = __builtin_amdgcn_readlane(held_page, at);
     const float scale_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_k), at));
     const float scale_v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_v), at));
-    const uint8_t* const block = kv_block<D>(a.v, id, head, 0);
-    PageCodes<D> c;
-    load_keys<D>(block, c);
-    load_values<D>(block, c);
+    const bool more = page + 1 < end;
+    if (more) {
+      if (at == 63) hold(page + 1);
+      block = kv_block<D>(a.v, __builtin_amdgcn_readlane(held_page, (at + 1) % 64), head, 0);
+    }
 
     floatx4 s[NT][4];
 #pragma unroll
@@ -198,6 +206,7 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
           for (int nt = 0; nt < NT; ++nt)
             s[nt][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, r.q[nt][2 * x + h], s[nt][t], 0, 0, 0);
         }
+    if (more) load_keys<D>(block, c);  // (of the next page, while this one's values are used)
 
     const int token = page * kPage + 16 * g;  // of s[.][0][0]
     const bool masked = page * kPage + kPage - 1 > r.first || (a.window > 0 && page * kPage <= r.last - a.window);
@@ -222,15 +231,21 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          float z = s[nt][t][x] * factor[nt];
-          if (masked) {
+        for (int x = 0; x < 4; ++x) s[nt][t][x] *= factor[nt];
+      if (masked) {
+        const int from = a.window > 0 ? r.at[nt] - a.window : -1;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
             const int j = token + 4 * t + x;
-            if (j > r.at[nt] || (a.window > 0 && j <= r.at[nt] - a.window)) z = -INFINITY;
+            if (j > r.at[nt] || j <= from) s[nt][t][x] = -INFINITY;
           }
-          s[nt][t][x] = z;
-          m = fmaxf(m, z);
-        }
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) m = fmaxf(m, s[nt][t][x]);
       m = fmaxf(m, __shfl_xor(m, 16));
       m = fmaxf(m, __shfl_xor(m, 32));
       now[nt] = fmaxf(p.m[nt], m);
@@ -264,9 +279,16 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
         for (int x = 0; x < 4; ++x) {
           const float y = __builtin_amdgcn_exp2f(s[nt][t][x] - m);
           sum += y;
-          // (a scale that is NaN reaches the rows that see the page, and no others)
-          w[nt][t / 2][4 * (t % 2) + x] = (_Float16)(masked && y == 0.0f ? 0.0f : y * unit);
+          w[nt][t / 2][4 * (t % 2) + x] = (_Float16)(y * unit);
+          s[nt][t][x] = y;
         }
+      if (masked && unit != unit) {  // a scale that is NaN reaches the rows that see the page, and no others
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (s[nt][t][x] == 0.0f) w[nt][t / 2][4 * (t % 2) + x] = (_Float16)0.0f;
+      }
       p.l[nt] += sum;
     }
 #pragma unroll
@@ -278,6 +300,7 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
         for (int nt = 0; nt < NT; ++nt)
           p.o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[nt][u], p.o[nt][dt], 0, 0, 0);
       }
+    if (more) load_values<D>(block, c);
   }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
@@ -288,12 +311,34 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
   }
 }
 
+// Partial results in memory: as a wavefront holds them, a floatx4 per lane for every 16 rows and 16 dims, then m and l.
 template <int D, int NT>
-__device__ __forceinline__ void merge(Partial<D, NT>& p, const floatx4* o, const float* m, const float* l) {
+constexpr int kPartialVectors = NT * (D / 16) * 64;
+template <int D, int NT>
+constexpr int kPartialBytes = kPartialVectors<D, NT> * 16 + 2 * NT * 64 * 4;
+
+template <int D, int NT>
+__device__ __forceinline__ void store_partial(uint8_t* at, const Partial<D, NT>& p) {
   const int lane = threadIdx.x & 63;
+  floatx4* const o = reinterpret_cast<floatx4*>(at);
+  float* const ml = reinterpret_cast<float*>(at + kPartialVectors<D, NT> * 16);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const float m2 = m[nt * 64 + lane], l2 = l[nt * 64 + lane];
+    ml[nt * 64 + lane] = p.m[nt];
+    ml[(NT + nt) * 64 + lane] = p.l[nt];
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) o[(nt * (D / 16) + dt) * 64 + lane] = p.o[nt][dt];
+  }
+}
+
+template <int D, int NT>
+__device__ __forceinline__ void merge_partial(const uint8_t* at, Partial<D, NT>& p) {
+  const int lane = threadIdx.x & 63;
+  const floatx4* const o = reinterpret_cast<const floatx4*>(at);
+  const float* const ml = reinterpret_cast<const float*>(at + kPartialVectors<D, NT> * 16);
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const float m2 = ml[nt * 64 + lane], l2 = ml[(NT + nt) * 64 + lane];
     const float top = fmaxf(p.m[nt], m2), base = top == -INFINITY ? 0.0f : top;
     const float f1 = __builtin_amdgcn_exp2f(p.m[nt] - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
     p.m[nt] = top;
@@ -303,82 +348,307 @@ __device__ __forceinline__ void merge(Partial<D, NT>& p, const floatx4* o, const
   }
 }
 
-// Results of the rows of a unit.
+// Results of 16 rows, the dims 16 dt + 4 g + 0..3 of the lanes.
+struct RowResult {
+  bool there;
+  uint16_t* dst;  // of the row's dims 4 g ...
+  float inverse;
+};
+__device__ __forceinline__ RowResult row_result(const AttentionArgs& a, const KvEntry& e, int head, int row, int D, float m, float l,
+                                                bool with_lse) {
+  const int g = (threadIdx.x & 63) >> 4;
+  RowResult r{row < e.n * a.group, nullptr, 0.0f};
+  if (!r.there) return r;
+  const int token = row / a.group, h = head * a.group + row - token * a.group;
+  const bool empty = m == -INFINITY && l == 0.0f;  // (not where every score is a NaN)
+  r.inverse = empty ? 0.0f : 1.0f / l;
+  r.dst = a.O + (int64_t)(e.row0 + token) * a.o_stride + (int64_t)h * D + 4 * g;
+  if (a.lse && with_lse && g == 0)
+    a.lse[(int64_t)(e.row0 + token) * a.q_heads + h] = empty ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  return r;
+}
+__device__ __forceinline__ void store_dims(const AttentionArgs& a, const RowResult& r, int dt, const floatx4& o) {
+  u32x2 w;
+#pragma unroll
+  for (int x = 0; x < 2; ++x)
+    w[x] = bits_of(o[2 * x] * r.inverse, a.bf16) | (uint32_t)bits_of(o[2 * x + 1] * r.inverse, a.bf16) << 16;
+  *reinterpret_cast<u32x2*>(r.dst + 16 * dt) = w;
+}
 template <int D, int NT>
 __device__ __forceinline__ void store_rows(const AttentionArgs& a, const KvEntry& e, int head, int tile, const Partial<D, NT>& p) {
-  const int i16 = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    const int row = (tile * NT + nt) * 16 + i16;
-    if (row >= e.n * a.group) continue;
-    const int token = row / a.group, h = head * a.group + row - token * a.group;
-    const bool empty = p.m[nt] == -INFINITY && p.l[nt] == 0.0f;  // (not where every score is a NaN)
-    const float inverse = empty ? 0.0f : 1.0f / p.l[nt];
-    uint16_t* const dst = a.O + (int64_t)(e.row0 + token) * a.o_stride + (int64_t)h * D + 4 * g;
+    const RowResult r = row_result(a, e, head, (tile * NT + nt) * 16 + (threadIdx.x & 15), D, p.m[nt], p.l[nt], true);
+    if (!r.there) continue;
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) {
-      u32x2 w;
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        w[x] = bits_of(p.o[nt][dt][2 * x] * inverse, a.bf16) | (uint32_t)bits_of(p.o[nt][dt][2 * x + 1] * inverse, a.bf16) << 16;
-      *reinterpret_cast<u32x2*>(dst + 16 * dt) = w;
-    }
-    if (a.lse && g == 0)
-      a.lse[(int64_t)(e.row0 + token) * a.q_heads + h] = empty ? -INFINITY : (p.m[nt] + __builtin_amdgcn_logf(p.l[nt])) * kLn2;
+    for (int dt = 0; dt < D / 16; ++dt) store_dims(a, r, dt, p.o[nt][dt]);
   }
 }
 
 // One workgroup per unit: its wavefronts take ranges of the pages and are joined in LDS.
 template <int D, int FMT, int NT>
-__global__ __launch_bounds__(64 * kWaves) void attend_unit_kernel(AttentionArgs a) {
+__global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_unit_kernel(AttentionArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
-  constexpr int VALUES = NT * D / 16 * 64;  // floatx4 of a partial result
-  floatx4* const o = reinterpret_cast<floatx4*>(lds);
-  float* const ml = reinterpret_cast<float*>(lds + (kWaves - 1) * VALUES * 16);
-  const int tile = blockIdx.x, head = blockIdx.y, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  constexpr int WAVES = kWaves<D, NT>, BYTES = kPartialBytes<D, NT>;
+  const int tile = blockIdx.x, head = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const KvEntry e = kv_entry(a.v, blockIdx.z);
   if (tile * NT * 16 >= e.n * a.group) return;
   Rows<D, NT> r;
   load_rows<D, NT>(a, e, head, tile, r);
   const PageRange all = e.slot < 0 ? PageRange{0, 0} : pages_seen(a, r.first, r.last);
-  const int each = (all.end - all.begin + kWaves - 1) / kWaves;
+  const int each = (all.end - all.begin + WAVES - 1) / WAVES;
   const int begin = min(all.begin + wave * each, all.end), end = min(begin + each, all.end);
   Partial<D, NT> p;
   accumulate<D, FMT, NT>(a, e, head, begin, end, r, p);
-  if (wave > 0) {
-    const int at = wave - 1;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      ml[(at * 2 * NT + nt) * 64 + lane] = p.m[nt];
-      ml[(at * 2 * NT + NT + nt) * 64 + lane] = p.l[nt];
-#pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) o[at * VALUES + (nt * (D / 16) + dt) * 64 + lane] = p.o[nt][dt];
-    }
-  }
+  if (wave > 0) store_partial<D, NT>(lds + (wave - 1) * BYTES, p);
   __syncthreads();
   if (wave > 0) return;
-  for (int at = 0; at < kWaves - 1; ++at)
-    merge<D, NT>(p, o + at * VALUES, ml + at * 2 * NT * 64, ml + (at * 2 * NT + NT) * 64);
+#pragma unroll 1
+  for (int at = 0; at < WAVES - 1; ++at) merge_partial<D, NT>(lds + at * BYTES, p);
   store_rows<D, NT>(a, e, head, tile, p);
 }
 
+// ---- the work cut into equal parts ---------------------------------------------------------------------------------
+//
+// All pages of all units in a row, by (batch entry, head, tile of rows, page): every workgroup takes `share` of them, every
+// wavefront an equal part of that.  Each workgroup finds its part from the lengths of the batch (a prefix sum in LDS), so
+// that neither the host nor another launch has to know them, and sequences of any lengths load every compute unit alike.
+// A unit that lies inside one workgroup is finished there; one that is cut leaves a partial result per workgroup, which
+// join_kernel adds up in order.
+
+constexpr int kMostPlanned = 1024;  // batch entries
+
+struct Plan {
+  int before[kMostPlanned + 1];  // pages of all units of the entries before
+  int sums[16];
+  int left[8];  // of a wavefront whose part starts inside a unit: 1 if the unit ends in it, 2 if not
+  KvEntry entry[kMostPlanned];
+};
+
+struct CutArgs {
+  uint8_t* partials;  // [workgroup][2]: of a unit that began before the workgroup's part, of one that ends behind it
+  int32_t workgroups, waves;
+};
+
+// Pages that the units of an entry read: all of them the same ones.
+__device__ __forceinline__ PageRange pages_of_entry(const AttentionArgs& a, const KvEntry& e) {
+  if (e.slot < 0 || e.n < 1) return PageRange{0, 0};
+  return pages_seen(a, e.length - e.n, e.length - 1);
+}
+__device__ __forceinline__ int tiles_of_entry(const AttentionArgs& a, const KvEntry& e, int rows) {
+  return (e.n * a.group + rows - 1) / rows;
+}
+
+// Fills the plan; all threads of the workgroup.  Returns the pages of all units.
+template <int THREADS>
+__device__ int make_plan(const AttentionArgs& a, int rows, Plan* plan) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int carry = 0;
+  for (int base = 0; base < a.v.batch; base += THREADS) {
+    const int b = base + threadIdx.x;
+    int pages = 0;
+    if (b < a.v.batch) {
+      const KvEntry e = kv_entry(a.v, b);
+      plan->entry[b] = e;
+      const PageRange p = pages_of_entry(a, e);
+      pages = (p.end - p.begin) * a.v.heads * tiles_of_entry(a, e, rows);
+    }
+    int up = pages;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const int y = __shfl_up(up, s);
+      if (lane >= s) up += y;
+    }
+    if (lane == 63) plan->sums[wave] = up;
+    __syncthreads();
+    int all = 0, ahead = carry;
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) ahead += plan->sums[w];
+      all += plan->sums[w];
+    }
+    if (b < a.v.batch) plan->before[b] = ahead + up - pages;
+    carry += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) plan->before[a.v.batch] = carry;
+  __syncthreads();
+  return carry;
+}
+
+// Pages of every workgroup and wavefront.
+struct Share {
+  int of_wave, of_workgroup;
+};
+__device__ __forceinline__ Share share_of(const CutArgs& c, int total) {
+  Share s;
+  s.of_wave = max((total + c.workgroups * c.waves - 1) / (c.workgroups * c.waves), 1);
+  s.of_workgroup = s.of_wave * c.waves;
+  return s;
+}
+
+template <int D, int FMT, int NT>
+__global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_cut_kernel(AttentionArgs a, CutArgs c) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  constexpr int WAVES = kWaves<D, NT>, BYTES = kPartialBytes<D, NT>;
+  Plan& plan = *reinterpret_cast<Plan*>(lds + (WAVES - 1) * BYTES);
+  int* const left = plan.left;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int total = make_plan<64 * WAVES>(a, 16 * NT, &plan);
+  const Share share = share_of(c, total);
+  const int from = (int)min((int64_t)blockIdx.x * share.of_workgroup, (int64_t)total);
+  int at = min(from + wave * share.of_wave, total);
+  const int to = min(at + share.of_wave, total);
+  uint8_t* const partials = c.partials + (int64_t)blockIdx.x * 2 * BYTES;
+  int kind = 0;
+  enum { kNone, kFromBefore, kFromHere };  // (of a unit that this wavefront has to complete)
+  int open = kNone;
+  Partial<D, NT> p;
+  KvEntry e;
+  int head = 0, tile = 0;
+  while (at < to) {
+    int lo = 0, hi = a.v.batch;  // the last entry that starts at or before `at`
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      (plan.before[mid] <= at ? lo : hi) = mid;
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    e = plan.entry[lo];
+    const PageRange pages = pages_of_entry(a, e);
+    const int each = pages.end - pages.begin, tiles = tiles_of_entry(a, e, 16 * NT);
+    const int unit = (at - plan.before[lo]) / each, first = (at - plan.before[lo]) - unit * each;
+    const int count = min(each - first, to - at);
+    head = unit / tiles, tile = unit - head * tiles;
+    Rows<D, NT> r;
+    load_rows<D, NT>(a, e, head, tile, r);
+    accumulate<D, FMT, NT>(a, e, head, pages.begin + first, pages.begin + first + count, r, p);
+    at += count;
+    const bool begins = first == 0, ends = first + count == each;
+    if (begins && ends) {
+      store_rows<D, NT>(a, e, head, tile, p);
+    } else if (begins) {
+      open = kFromHere;
+    } else if (wave > 0) {
+      store_partial<D, NT>(lds + (wave - 1) * BYTES, p);
+      kind = ends ? 1 : 2;
+    } else if (ends) {
+      store_partial<D, NT>(partials, p);
+    } else {
+      open = kFromBefore;
+    }
+  }
+  if ((threadIdx.x & 63) == 0) left[wave] = kind;
+  __syncthreads();
+  if (open == kNone) return;
+  bool ended = false;
+#pragma unroll 1
+  for (int w = wave + 1; w < WAVES && !ended && left[w]; ++w) {
+    merge_partial<D, NT>(lds + (w - 1) * BYTES, p);
+    ended = left[w] == 1;
+  }
+  if (open == kFromBefore)
+    store_partial<D, NT>(partials, p);
+  else if (ended)
+    store_rows<D, NT>(a, e, head, tile, p);
+  else
+    store_partial<D, NT>(partials + BYTES, p);
+}
+
+// One workgroup per head and batch entry: adds up the partial results of its units that were cut, and stores zeros for an
+// entry without pages.  Wavefront w takes the dims 16 w + 0..15.
 template <int D, int NT>
-constexpr int unit_lds_bytes() { return (kWaves - 1) * (NT * D / 16 * 64 * 16 + 2 * NT * 64 * 4); }
+__global__ __launch_bounds__(4 * D) void join_kernel(AttentionArgs a, CutArgs c) {
+  constexpr int BYTES = kPartialBytes<D, NT>;
+  __shared__ Plan plan;
+  const int total = make_plan<4 * D>(a, 16 * NT, &plan);
+  const Share share = share_of(c, total);
+  const int b = blockIdx.x, head = blockIdx.y, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const KvEntry e = plan.entry[b];
+  const PageRange pages = pages_of_entry(a, e);
+  const int each = pages.end - pages.begin, tiles = tiles_of_entry(a, e, 16 * NT);
+  for (int tile = 0; tile < tiles; ++tile) {
+    const int start = plan.before[b] + (head * tiles + tile) * each;
+    const int w0 = start / share.of_workgroup, w1 = (start + each - 1) / share.of_workgroup;
+    if (each > 0 && w0 == w1) continue;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float m = -INFINITY, l = 0.0f;
+      floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (each > 0) {
+        auto ml_of = [&](int w) {
+          return reinterpret_cast<const float*>(c.partials + ((int64_t)w * 2 + (w == w0)) * BYTES + kPartialVectors<D, NT> * 16) + nt * 64 + lane;
+        };
+        auto o_of = [&](int w) {
+          return reinterpret_cast<const floatx4*>(c.partials + ((int64_t)w * 2 + (w == w0)) * BYTES) + (nt * (D / 16) + dt) * 64 + lane;
+        };
+#pragma unroll 8
+        for (int w = w0; w <= w1; ++w) m = fmaxf(m, *ml_of(w));
+        const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll 8
+        for (int w = w0; w <= w1; ++w) {
+          const float f = __builtin_amdgcn_exp2f(*ml_of(w) - base);
+          l += ml_of(w)[NT * 64] * f;
+          o += *o_of(w) * f;
+        }
+      }
+      const RowResult r = row_result(a, e, head, (tile * NT + nt) * 16 + (lane & 15), D, m, l, dt == 0);
+      if (r.there) store_dims(a, r, dt, o);
+    }
+  }
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
 
 template <int D, int FMT, int NT>
 int launch_units(const AttentionArgs& a, int max_rows, hipStream_t stream) {
   const void* const fn = (const void*)attend_unit_kernel<D, FMT, NT>;
   if (int e = allow_full_lds(fn, "attend_unit_kernel")) return e;
   const int64_t tiles = ((int64_t)max_rows * a.group + 16 * NT - 1) / (16 * NT);
-  attend_unit_kernel<D, FMT, NT><<<dim3((uint32_t)tiles, a.v.heads, a.v.batch), 64 * kWaves, unit_lds_bytes<D, NT>(), stream>>>(a);
+  constexpr int threads = 64 * kWaves<D, NT>, lds = (kWaves<D, NT> - 1) * kPartialBytes<D, NT>;
+  attend_unit_kernel<D, FMT, NT><<<dim3((uint32_t)tiles, a.v.heads, a.v.batch), threads, lds, stream>>>(a);
   return kv_launched("attend_unit_kernel");
 }
 
+template <int D, int FMT, int NT>
+int launch_cut(const AttentionArgs& a, const CutArgs& c, hipStream_t stream) {
+  const void* const fn = (const void*)attend_cut_kernel<D, FMT, NT>;
+  if (int e = allow_full_lds(fn, "attend_cut_kernel")) return e;
+  constexpr int threads = 64 * kWaves<D, NT>, lds = (kWaves<D, NT> - 1) * kPartialBytes<D, NT> + sizeof(Plan);
+  attend_cut_kernel<D, FMT, NT><<<c.workgroups, threads, lds, stream>>>(a, c);
+  join_kernel<D, NT><<<dim3(a.v.batch, a.v.heads), 4 * D, 0, stream>>>(a, c);
+  return kv_launched("attend_cut_kernel");
+}
+
+// How a call runs.
+struct AttentionForm {
+  int nt;          // tiles of 16 rows that a unit holds
+  int workgroups;  // 0: one per unit
+  int waves;       // of one
+  int64_t partial_bytes;
+};
+
+int waves_of(int dim, int nt) { return dim * nt >= 256 ? 4 : 8; }
+
+AttentionForm choose_form(int dim, int heads, int group, int batch, int max_rows, int max_tokens) {
+  AttentionForm f{};
+  const int64_t rows = (int64_t)max_rows * group;
+  f.nt = dim < 256 && rows > 16 ? 2 : 1;
+  f.waves = waves_of(dim, f.nt);
+  const int64_t tiles = (rows + 16 * f.nt - 1) / (16 * f.nt), units = tiles * heads * batch, pages = (max_tokens + kPage - 1) / kPage;
+  const int64_t alone = (units + 255) / 256 * ((pages + f.waves - 1) / f.waves);
+  const int64_t cut = (units * pages + 256 * f.waves - 1) / (256 * f.waves);
+  if (batch <= kMostPlanned && tiles <= 4 && alone > cut + 8) {
+    f.workgroups = 256;
+    f.partial_bytes = (int64_t)f.workgroups * 2 * (f.nt * (dim / 16) * 64 * 16 + 2 * f.nt * 64 * 4);
+  }
+  return f;
+}
+
 template <int D, int FMT>
-int launch_attention(const AttentionArgs& a, int max_rows, hipStream_t stream) {
+int launch_attention(const AttentionArgs& a, const AttentionForm& f, int max_rows, void* workspace, hipStream_t stream) {
+  const CutArgs c{(uint8_t*)workspace, f.workgroups, f.waves};
   if constexpr (D < 256)
-    if ((int64_t)max_rows * a.group > 16) return launch_units<D, FMT, 2>(a, max_rows, stream);
-  return launch_units<D, FMT, 1>(a, max_rows, stream);
+    if (f.nt == 2) return f.workgroups ? launch_cut<D, FMT, 2>(a, c, stream) : launch_units<D, FMT, 2>(a, max_rows, stream);
+  return f.workgroups ? launch_cut<D, FMT, 1>(a, c, stream) : launch_units<D, FMT, 1>(a, max_rows, stream);
 }
 
 }  // namespace
@@ -397,6 +667,10 @@ extern "C" int sfmp_kv_attention_workspace(const sfmp_kv_layout_t* layout, int32
   const int64_t tiles = ((int64_t)max_rows * (q_heads / layout->kv_heads) + 15) / 16;
   if ((tiles && pages > INT32_MAX / tiles) || (int64_t)batch * layout->kv_heads * pages * tiles > INT32_MAX) return SFMP_ERR_SHAPE;
   *bytes = 256;
+  if (batch && max_rows) {
+    const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch, max_rows, max_tokens);
+    *bytes = round_up_256(f.partial_bytes + 1);
+  }
   return SFMP_OK;
 }
 
@@ -430,10 +704,12 @@ extern "C" int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, 
   a.scale = scale;
   a.bf16 = dtype == SFMP_TYPE_BF16;
   const hipStream_t stream = (hipStream_t)hip_stream;
+  if (batch->max_rows == 0) return SFMP_OK;
+  const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, a.group, batch->batch, batch->max_rows, max_tokens);
   auto with_dim = [&](auto fmt) {
-    if (layout->head_dim == 64) return launch_attention<64, fmt()>(a, batch->max_rows, stream);
-    if (layout->head_dim == 128) return launch_attention<128, fmt()>(a, batch->max_rows, stream);
-    return launch_attention<256, fmt()>(a, batch->max_rows, stream);
+    if (layout->head_dim == 64) return launch_attention<64, fmt()>(a, f, batch->max_rows, workspace_dev, stream);
+    if (layout->head_dim == 128) return launch_attention<128, fmt()>(a, f, batch->max_rows, workspace_dev, stream);
+    return launch_attention<256, fmt()>(a, f, batch->max_rows, workspace_dev, stream);
   };
   if (layout->format == SFMP_KV_INT8) return with_dim(std::integral_constant<int, SFMP_KV_INT8>{});
   return with_dim(std::integral_constant<int, SFMP_KV_FP8>{});

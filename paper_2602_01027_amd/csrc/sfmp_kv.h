@@ -21,7 +21,7 @@ struct KvView {
   const int32_t* lengths;
   const int32_t* slots;
   const int32_t* row_start;
-  int32_t pages, heads, sequences, table_pages, batch, rows;
+  int32_t pages, heads, sequences, table_pages, batch, rows, max_rows;
 };
 
 inline bool kv_aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -60,7 +60,7 @@ inline int make_kv_view(const sfmp_kv_layout_t* L, int32_t layer, const void* co
   if (!kv_aligned(b->slots_dev, 4) || !kv_aligned(b->row_start_dev, 4)) return SFMP_ERR_ALIGN;
   *view = KvView{(uint8_t*)codes + (int64_t)layer * L->pages * L->page_bytes,
                  (float*)scales + (int64_t)layer * L->pages * L->kv_heads * 2, t->page_table_dev, t->lengths_dev,
-                 b->slots_dev, b->row_start_dev, L->pages, L->kv_heads, t->sequences, t->table_pages, b->batch, b->rows};
+                 b->slots_dev, b->row_start_dev, L->pages, L->kv_heads, t->sequences, t->table_pages, b->batch, b->rows, b->max_rows};
   return SFMP_OK;
 }
 
@@ -87,7 +87,7 @@ __device__ __forceinline__ KvEntry kv_entry(const KvView& v, int b) {
   e.length = min(max(e.length, 0), v.table_pages * kPage);
   if (v.row_start) {
     e.row0 = min(max(v.row_start[b], 0), v.rows);
-    e.n = min(max(v.row_start[b + 1], e.row0), v.rows) - e.row0;
+    e.n = min(min(max(v.row_start[b + 1], e.row0), v.rows) - e.row0, v.max_rows);
   } else {
     e.row0 = b;
     e.n = 1;
