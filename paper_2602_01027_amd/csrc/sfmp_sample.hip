@@ -1,10 +1,14 @@
 // Choice of the next token: temperature, top-k, top-p, min-p and one random number per row.
 //
 // Every filter keeps a prefix of the tokens ordered by (falling logit, rising number), and the token is where the running
-// sum of weights passes a threshold.  So no sort is needed, only positions in that order: a histogram of counts and
-// weights over 2048 bins of (l - m) / T finds the bin of a position, and the tokens of that one bin, a few hundred of a
-// hundred thousand, are ranked against each other in LDS.  Weights are whole numbers (2^31 for the most probable token), so
-// that their sums do not depend on the order in which workgroups and atomics add them.
+// sum of weights passes a threshold.  So no sort of the row is needed, only a few positions in that order: a histogram of
+// counts and weights over 4096 bins of (l - m) / T tells which bins the positions lie in, and the tokens of those bins, a few
+// hundred of a hundred thousand, are collected and sorted in LDS, the gaps between the bins being known from the histogram.
+// Weights are whole numbers (2^31 for the most probable token), so that their sums do not depend on the order in which
+// workgroups and atomics add them.
+//
+// Few rows are cut into slices over many workgroups, which takes three launches (largest logit; histogram; collection) and
+// a fourth for the choice.  Many rows have one workgroup each, which does all of it.
 #include <math.h>
 
 #include "sfmp_device.h"
@@ -13,11 +17,19 @@
 namespace sfmp {
 namespace {
 
-constexpr int kBins = 2048;
-constexpr float kBinsPerUnit = 92.0f;  // weights are 0 below (l - m) / T = -32 ln 2 = -22.2
+constexpr int kBins = 4096;
+constexpr float kBinsPerUnit = 184.0f;  // weights are 0 below (l - m) / T = -32 ln 2 = -22.2
+constexpr float kLeast = -23.0f;
 constexpr int kSliceThreads = 256;
 constexpr int kPickThreads = 1024;
-constexpr int kListed = 2048;          // tokens that are ranked in LDS
+constexpr int kListed = 2048;           // most tokens that are sorted
+
+struct Wanted;
+struct Listed {
+  uint64_t entry;                  // (key, token)
+  unsigned long long mass_before;  // sums before its bin
+  uint32_t count_before, none;
+};
 
 struct SampleArgs {
   const void* logits;
@@ -31,6 +43,9 @@ struct SampleArgs {
   int32_t* tokens;
   float* logprobs;
   float* slice_max;         // [rows][slices]
+  Listed* list;             // [rows][kListed]
+  Wanted* wanted;           // [rows]
+  uint32_t* listed;         // [rows]
   unsigned long long* mass; // [rows][kBins]
   uint32_t* count;          // [rows][kBins]
 };
@@ -44,7 +59,7 @@ __device__ __forceinline__ float logit_of(uint32_t bits) {
     x = __uint_as_float(bits << 16);
   else
     x = (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
-  return x != x ? -INFINITY : x;
+  return x;
 }
 
 // Calls f(number, logit) for the tokens [from, to) of a row; the threads take runs of 16 aligned bytes in turn.
@@ -53,18 +68,18 @@ __device__ __forceinline__ void for_each_logit(const void* row, int from, int to
   constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
   const int lead = (int)((reinterpret_cast<uintptr_t>(row) & 15) / SIZE);  // elements between the aligned address and the row
   const uint8_t* const base = (const uint8_t*)row - lead * SIZE;
-#pragma unroll 2
-  for (int v = (from + lead) / RUN + threadIdx.x; v * RUN < to + lead; v += THREADS) {
-    const int first = v * RUN - lead;
-    if (first >= from && first + RUN <= to) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(base + (int64_t)v * 16);
+  const int first = (from + lead + RUN - 1) / RUN, last = max((to + lead) / RUN, first);  // whole runs
+#pragma unroll 4
+  for (int v = first + threadIdx.x; v < last; v += THREADS) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(base + (int64_t)v * 16);
 #pragma unroll
-      for (int j = 0; j < RUN; ++j)
-        f(first + j, logit_of<T>(SIZE == 4 ? w[j] : (j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu));
-    } else {
-      for (int i = max(first, from); i < min(first + RUN, to); ++i)
-        f(i, logit_of<T>(SIZE == 4 ? ((const uint32_t*)row)[i] : ((const uint16_t*)row)[i]));
-    }
+    for (int j = 0; j < RUN; ++j) f(v * RUN - lead + j, logit_of<T>(SIZE == 4 ? w[j] : (j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu));
+  }
+  // before the first and behind the last
+  const int head = min(first * RUN - lead, to), tail = max(last * RUN - lead, head);
+  for (int side = 0; side < 2; ++side) {
+    const int i = (side ? tail : from) + threadIdx.x;
+    if (i < (side ? to : head)) f(i, logit_of<T>(SIZE == 4 ? ((const uint32_t*)row)[i] : ((const uint16_t*)row)[i]));
   }
 }
 
@@ -78,10 +93,15 @@ __device__ __forceinline__ float max_of_wave(float x) {
 struct Row {
   const void* logits;
   float m, inverse;
+  bool plain;  // m and 1 / T are finite
+  __device__ __forceinline__ Row(const void* p, float largest, float t) : logits(p), m(largest), inverse(1.0f / fmaxf(t, 0.0f)) {
+    plain = inverse < INFINITY && fabsf(m) < INFINITY;
+  }
+  // (l - m) / T; not above kLeast for a NaN
   __device__ __forceinline__ float y(float l) const {
+    if (plain) return (l - m) * inverse;
     return l == m ? 0.0f : l == -INFINITY ? -INFINITY : (l - m) * inverse;
   }
-  // (expf of a value far below is 0: the bins past the weights are not reached)
   static __device__ __forceinline__ uint32_t weight(float y) { return (uint32_t)rintf(expf(y) * 2147483648.0f); }
   static __device__ __forceinline__ int bin(float y) { return min((int)(-y * kBinsPerUnit), kBins - 1); }
 };
@@ -92,7 +112,13 @@ __device__ __forceinline__ Row make_row(const SampleArgs& a, int r) {
   float m = -INFINITY;
   for (int s = lane; s < a.slices; s += 64) m = fmaxf(m, a.slice_max[(int64_t)r * a.slices + s]);
   const float t = a.temperature ? a.temperature[r] : 1.0f;
-  return Row{(const uint8_t*)a.logits + r * a.stride * (T == SFMP_TYPE_FP32 ? 4 : 2), max_of_wave(m), 1.0f / fmaxf(t, 0.0f)};
+  return Row((const uint8_t*)a.logits + r * a.stride * (T == SFMP_TYPE_FP32 ? 4 : 2), max_of_wave(m), t);
+}
+
+// (Numbers in the order that logits have, falling: a smaller key is a more probable token.)
+__device__ __forceinline__ uint32_t falling_key(float l) {
+  const uint32_t u = __float_as_uint(l == 0.0f ? 0.0f : l);
+  return u & 0x80000000u ? u : ~u & 0x7FFFFFFFu;
 }
 
 __device__ __forceinline__ int slice_from(const SampleArgs& a, int s) { return (int)((int64_t)a.vocab * s / a.slices); }
@@ -109,6 +135,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_max_kernel(SampleArgs a)
     a.mass[(int64_t)r * kBins + i] = 0;
     a.count[(int64_t)r * kBins + i] = 0;
   }
+  if (s == 0 && threadIdx.x == 0) a.listed[r] = 0;
   m = max_of_wave(m);
   if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = m;
   __syncthreads();
@@ -133,7 +160,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_bins_kernel(SampleArgs a
   if (row.m == -INFINITY) return;
   for_each_logit<T, kSliceThreads>(row.logits, slice_from(a, s), slice_from(a, s + 1), [&](int, float l) {
     const float y = row.y(l);
-    if (y > -23.0f) {
+    if (y > kLeast) {
       const uint32_t w = Row::weight(y);
       if (w) atomicAdd(&bins[Row::bin(y)], (1ull << kCountBit) + w);
     }
@@ -146,52 +173,307 @@ __global__ __launch_bounds__(kSliceThreads) void sample_bins_kernel(SampleArgs a
     }
 }
 
-// (Numbers in the order that logits have, falling: a smaller key is a more probable token.)
-__device__ __forceinline__ uint32_t falling_key(float l) {
-  const uint32_t u = __float_as_uint(l == 0.0f ? 0.0f : l);
-  return u & 0x80000000u ? u : ~u & 0x7FFFFFFFu;
-}
-
-// A token found by position.
-struct Place {
-  unsigned long long before, through;  // running sum of weights up to it, and with it
-  int token;
-  float y;
+// What a workgroup that chooses, or collects for the choice, shares.
+struct Mark {
+  unsigned long long before, through;  // sums before a bin, and with it
+  int bin;
 };
-
-// Everything that one workgroup shares while it places positions in a row.
 struct PickShared {
-  unsigned long long mass[kBins];  // prefix sums up to and with each bin
+  unsigned long long mass[kBins];      // of a row kernel: the histogram; then, for the wanted bins, what `base` says
   uint32_t count[kBins];
-  unsigned long long list_mass[kListed];
-  uint64_t list_key[kListed];
+  uint64_t list[kListed];              // entries (key, token)
   unsigned long long wave_mass[kPickThreads / 64];
   uint32_t wave_count[kPickThreads / 64];
-  unsigned long long digit_mass[kBins];
-  uint32_t digit_count[kBins];
-  Place found;
-  int listed, bin, digit;
-  unsigned long long min_mass;
+  Mark mark[6];
+  unsigned long long through, min_mass, total;
+  uint64_t found;
+  float wave_max[kPickThreads / 64];
+  uint32_t listed, counted;
+  int last_bin, digit;
 };
 
-// Inclusive sums over kBins entries in place.
-__device__ void prefix_sums(unsigned long long* mass, uint32_t* count, PickShared* sh) {
-  const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
-  unsigned long long m1 = mass[2 * i], m2 = m1 + mass[2 * i + 1], m = m2;
-  uint32_t c1 = count[2 * i], c2 = c1 + count[2 * i + 1], c = c2;
+// Sum over the threads before this one, and over all.
+template <int THREADS>
+__device__ __forceinline__ unsigned long long sum_before(unsigned long long x, PickShared* sh, unsigned long long* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned long long up = x;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
-    const unsigned long long y = __shfl_up(m, s);
-    const uint32_t z = __shfl_up(c, s);
-    if (lane >= s) m += y, c += z;
+    const unsigned long long y = __shfl_up(up, s);
+    if (lane >= s) up += y;
   }
-  if (lane == 63) sh->wave_mass[wave] = m, sh->wave_count[wave] = c;
+  if (lane == 63) sh->wave_mass[wave] = up;
   __syncthreads();
-  unsigned long long mb = m - m2;
-  uint32_t cb = c - c2;
-  for (int w = 0; w < wave; ++w) mb += sh->wave_mass[w], cb += sh->wave_count[w];
-  mass[2 * i] = mb + m1, mass[2 * i + 1] = mb + m2;
-  count[2 * i] = cb + c1, count[2 * i + 1] = cb + c2;
+  unsigned long long ahead = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) {
+    const unsigned long long y = sh->wave_mass[w];
+    if (w < wave) ahead += y;
+    sum += y;
+  }
+  __syncthreads();
+  *all = sum;
+  return ahead + up - x;
+}
+
+// The filters of a row, and the bins that the end of each and the chosen token can lie in.
+struct Wanted {
+  int top_k;  // 0: all
+  float top_p, floor;
+  bool by_top_p, by_min_p;
+  unsigned long long total, min_before;  // (before the bin of min-p's floor)
+  int from[4], to[4];  // ranges of bins (from > to: none)
+  uint32_t tokens;     // in them
+  __device__ __forceinline__ bool has(int bin) const {
+    bool y = false;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) y |= bin >= from[x] && bin <= to[x];
+    return y;
+  }
+};
+__device__ __forceinline__ Wanted filters_of(const SampleArgs& a, int r, uint32_t counted, unsigned long long total) {
+  Wanted w;
+  w.total = total;
+  w.min_before = 0;
+  const bool greedy = a.temperature && a.temperature[r] <= 0.0f;
+  w.top_k = greedy ? 1 : a.top_k ? a.top_k[r] : 0;
+  if (w.top_k <= 0 || (uint32_t)w.top_k >= counted) w.top_k = 0;  // (counted: tokens whose weight is not 0)
+  w.top_p = a.top_p ? a.top_p[r] : 1.0f;
+  w.by_top_p = w.top_p < 1.0f;
+  const float min_p = a.min_p ? a.min_p[r] : 0.0f;
+  w.by_min_p = min_p > 0.0f;
+  w.floor = w.by_min_p ? logf(fminf(min_p, 1.0f)) : -INFINITY;
+  return w;
+}
+
+// The histogram in registers: every thread holds the bins EACH t .. EACH t + EACH - 1.
+template <int THREADS>
+struct Bins {
+  static constexpr int EACH = kBins / THREADS;
+  unsigned long long mass_before, mass[EACH];  // sums before the thread's bins, and with each
+  uint32_t count_before, count[EACH];
+
+  // mass and count hold the bins' own on entry
+  __device__ __forceinline__ void add_up(PickShared* sh) {
+    // (counts and weights of the threads in one go: a count below 2^24 under weights below 2^55 would not fit 64 bits)
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    unsigned long long m = 0;
+    uint32_t c = 0;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) mass[j] = m += mass[j], count[j] = c += count[j];
+    unsigned long long um = m;
+    uint32_t uc = c;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const unsigned long long y = __shfl_up(um, s);
+      const uint32_t z = __shfl_up(uc, s);
+      if (lane >= s) um += y, uc += z;
+    }
+    if (lane == 63) sh->wave_mass[wave] = um, sh->wave_count[wave] = uc;
+    __syncthreads();
+    mass_before = um - m, count_before = uc - c;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w)
+      if (w < wave) mass_before += sh->wave_mass[w], count_before += sh->wave_count[w];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) mass[j] += mass_before, count[j] += count_before;
+    if (threadIdx.x == THREADS - 1) sh->total = mass[EACH - 1], sh->counted = count[EACH - 1];
+    __syncthreads();
+  }
+  // Marks the first bin whose running sums satisfy `reached`
+  template <typename F>
+  __device__ __forceinline__ void mark_first(F reached, Mark* mark) const {
+    if (!reached(count[EACH - 1], mass[EACH - 1]) || (threadIdx.x > 0 && reached(count_before, mass_before))) return;
+    bool done = false;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j)
+      if (!done && reached(count[j], mass[j])) {
+        *mark = Mark{j ? mass[j - 1] : mass_before, mass[j], EACH * (int)threadIdx.x + j};
+        done = true;
+      }
+  }
+  __device__ __forceinline__ void mark_bin(int bin, Mark* mark) const {
+#pragma unroll
+    for (int j = 0; j < EACH; ++j)
+      if (EACH * (int)threadIdx.x + j == bin) *mark = Mark{j ? mass[j - 1] : mass_before, mass[j], bin};
+  }
+};
+
+// Which bins are wanted.  A position inside a bin leaves the weight kept by top-k uncertain by that bin, which may make two
+// bins of one for the filters after it.  Leaves the sums before the wanted bins in sh->mass and sh->count.
+template <int THREADS>
+__device__ __forceinline__ Wanted find_wanted(const SampleArgs& a, int r, const Bins<THREADS>& bins, PickShared* sh) {
+  Wanted w = filters_of(a, r, sh->counted, sh->total);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) w.from[x] = 1, w.to[x] = 0;
+  const float u = a.uniform[r];
+  unsigned long long least = w.total, most = w.total;  // both ends of the kept weight
+  if (threadIdx.x == 0) sh->listed = 0, sh->last_bin = 0;
+  const int min_bin = w.floor > kLeast ? Row::bin(w.floor) : kBins - 1;
+  if (w.by_min_p) bins.mark_bin(min_bin, &sh->mark[5]);
+  if (w.top_k) {
+    const uint32_t k = (uint32_t)w.top_k;
+    bins.mark_first([&](uint32_t c, unsigned long long) { return c >= k; }, &sh->mark[0]);
+    __syncthreads();
+    const Mark x = sh->mark[0];
+    w.from[0] = w.to[0] = x.bin;
+    least = x.before + 1, most = x.through;
+  }
+  if (w.by_top_p) {
+    const double low = (double)w.top_p * (double)least, high = (double)w.top_p * (double)most;
+    bins.mark_first([&](uint32_t, unsigned long long m) { return (double)m >= low; }, &sh->mark[1]);
+    bins.mark_first([&](uint32_t, unsigned long long m) { return (double)m >= high; }, &sh->mark[2]);
+    __syncthreads();
+    const Mark x = sh->mark[1], y = sh->mark[2];
+    w.from[1] = x.bin, w.to[1] = y.bin;
+    least = min(least, x.before + 1), most = min(most, y.through);
+  }
+  if (w.by_min_p) {
+    __syncthreads();
+    const Mark x = sh->mark[5];
+    w.from[2] = w.to[2] = min_bin;
+    w.min_before = x.before;
+    least = min(least, max(x.before, 1ull)), most = min(most, x.through);
+  }
+  const unsigned long long low = min((unsigned long long)((double)u * (double)least), least - 1);
+  const unsigned long long high = min((unsigned long long)((double)u * (double)most), most - 1);
+  bins.mark_first([&](uint32_t, unsigned long long m) { return m > low; }, &sh->mark[3]);
+  bins.mark_first([&](uint32_t, unsigned long long m) { return m > high; }, &sh->mark[4]);
+  __syncthreads();
+  w.from[3] = sh->mark[3].bin, w.to[3] = sh->mark[4].bin;
+  uint32_t tokens = 0;
+  int last = 0;
+#pragma unroll
+  for (int j = 0; j < Bins<THREADS>::EACH; ++j) {
+    const int bin = Bins<THREADS>::EACH * threadIdx.x + j;
+    if (w.has(bin)) {
+      const uint32_t before = j ? bins.count[j - 1] : bins.count_before;
+      tokens += bins.count[j] - before;
+      last = bin;
+      sh->mass[bin] = j ? bins.mass[j - 1] : bins.mass_before;
+      sh->count[bin] = before;
+    }
+  }
+  if (tokens) atomicAdd(&sh->listed, tokens);
+  if (last) atomicMax(&sh->last_bin, last);
+  __syncthreads();
+  w.tokens = sh->listed;
+  return w;
+}
+
+// The logit below which no token is in the wanted bins (with a margin for rounding).
+__device__ __forceinline__ float reach_of(const Row& row, int last_bin) {
+  const float reach = row.m - (float)(last_bin + 2) / kBinsPerUnit / row.inverse * 1.0001f - fabsf(row.m) * 1e-6f;
+  return reach == reach && row.m < INFINITY ? reach : -INFINITY;
+}
+__device__ __forceinline__ bool is_wanted(const Row& row, float l, float reach, const Wanted& w) {
+  if (l < reach) return false;
+  const float y = row.y(l);
+  return y > kLeast && w.has(Row::bin(y)) && Row::weight(y);
+}
+__device__ __forceinline__ uint64_t entry_of(int token, float l) { return (uint64_t)falling_key(l) << 32 | (uint32_t)token; }
+__device__ __forceinline__ float logit_of_entry(uint64_t e) {
+  const uint32_t f = (uint32_t)(e >> 32);
+  return __uint_as_float(f & 0x80000000u ? f : ~f & 0x7FFFFFFFu);
+}
+
+// Sorts list[0, n) upwards, n a power of two (at least 128).  With strides up to 64 the elements of a wavefront's threads lie
+// within 128 of its own: no barrier of the workgroup is needed between those steps.
+template <int THREADS>
+__device__ __forceinline__ void sort_list(uint64_t* list, int n) {
+  for (int size = 2; size <= n; size *= 2)
+    for (int stride = size / 2; stride > 0; stride /= 2) {
+      for (int t = threadIdx.x; t < n / 2; t += THREADS) {
+        const int i = 2 * stride * (t / stride) + t % stride, j = i + stride;
+        const uint64_t x = list[i], y = list[j];
+        if ((x > y) == ((i & size) == 0)) list[i] = y, list[j] = x;
+      }
+      if (stride > 64 || (stride == 1 && size >= 128))
+        __syncthreads();
+      else
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+}
+
+// The choice, from the list of the tokens in the wanted bins (w.tokens of them in sh->list), the sums before these bins
+// being in sh->mass and sh->count.
+template <int THREADS>
+__device__ __forceinline__ void choose_from_list(const SampleArgs& a, int r, const Row& row, const Wanted& w, PickShared* sh) {
+  constexpr int EACH = kListed / THREADS;
+  const int i = threadIdx.x, n = (int)w.tokens;
+  int size = 128;
+  while (size < n) size *= 2;
+  for (int j = n + i; j < size; j += THREADS) sh->list[j] = ~0ull;
+  const int min_bin = w.from[2];
+  if (i == 0) sh->min_mass = w.min_before, sh->found = 0;
+  __syncthreads();
+  sort_list<THREADS>(sh->list, size);
+  // Thread i holds the entries EACH i ...: running sums over the list first
+  float y[EACH];
+  unsigned long long through[EACH];
+  uint32_t weight[EACH];
+  int bin[EACH];
+  unsigned long long sum = 0;
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    const int j = EACH * i + x;
+    weight[x] = 0, bin[x] = 0, y[x] = 0.0f;
+    if (j < n) {
+      y[x] = row.y(logit_of_entry(sh->list[j]));
+      bin[x] = Row::bin(y[x]);
+      weight[x] = Row::weight(y[x]);
+    }
+    sum += weight[x];
+    through[x] = sum;
+  }
+  unsigned long long all;
+  const unsigned long long before = sum_before<THREADS>(sum, sh, &all);
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) through[x] += before;
+  // ... then the first entry of each bin sets off its running sums against those of the row
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    const int j = EACH * i + x;
+    if (j < n && (j == 0 || Row::bin(row.y(logit_of_entry(sh->list[j - 1]))) != bin[x])) {
+      sh->mass[bin[x]] -= through[x] - weight[x];
+      sh->count[bin[x]] -= (uint32_t)j;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < EACH; ++x)
+    if (weight[x]) through[x] += sh->mass[bin[x]];
+  unsigned long long kept = w.total;
+  if (w.top_k) {
+#pragma unroll
+    for (int x = 0; x < EACH; ++x)
+      if (weight[x] && sh->count[bin[x]] + (uint32_t)(EACH * i + x + 1) == (uint32_t)w.top_k) sh->through = through[x];
+    __syncthreads();
+    kept = sh->through;
+    __syncthreads();
+  }
+  if (w.by_top_p) {
+    const double aim = (double)w.top_p * (double)kept;
+#pragma unroll
+    for (int x = 0; x < EACH; ++x) {
+      const unsigned long long less = through[x] - weight[x];
+      if (weight[x] && (double)through[x] >= aim && (less == 0 || (double)less < aim)) sh->through = through[x];
+    }
+    __syncthreads();
+    kept = min(kept, sh->through);
+    __syncthreads();
+  }
+  if (w.by_min_p) {
+#pragma unroll
+    for (int x = 0; x < EACH; ++x)
+      if (weight[x] && bin[x] == min_bin && y[x] >= w.floor) atomicMax(&sh->min_mass, through[x]);
+    __syncthreads();
+    kept = min(kept, sh->min_mass);
+  }
+  const unsigned long long passed = min((unsigned long long)((double)a.uniform[r] * (double)kept), kept - 1);
+#pragma unroll
+  for (int x = 0; x < EACH; ++x)
+    if (weight[x] && through[x] > passed && through[x] - weight[x] <= passed) sh->found = sh->list[EACH * i + x];
   __syncthreads();
 }
 
@@ -207,141 +489,207 @@ struct Sought {
   }
 };
 
-// Finds the token at a position; the histogram's prefix sums are in sh->mass and sh->count and reach it.
+// Finds the token at a position where the wanted bins are too crowded to be sorted (rows of nearly equal logits): its bin is
+// narrowed by the digits of (logit, token), 12 bits at a time, until one token is left, each time over the whole row.
+// Leaves the token's entry in sh->found, returns the running sum with it.  kPickThreads threads; sh->mass and sh->count
+// are used for the digits.
 template <int T>
-__device__ Place place_of(const SampleArgs& a, const Row& row, const Sought& sought, PickShared* sh) {
+__device__ __noinline__ unsigned long long place_of(const SampleArgs& a, const Row& row, const Sought& sought, PickShared* sh) {
+  constexpr int kDigitBits = 12;
+  static_assert(kBins == 1 << kDigitBits, "digits are counted like bins");
   const int i = threadIdx.x;
-#pragma unroll
-  for (int j = 2 * i; j <= 2 * i + 1; ++j)
-    if (sought.reached(sh->count[j], sh->mass[j]) && (j == 0 || !sought.reached(sh->count[j - 1], sh->mass[j - 1])))
-      sh->bin = j;
-  __syncthreads();
-  const int bin = sh->bin;
-  unsigned long long mass_before = bin ? sh->mass[bin - 1] : 0;
-  uint32_t count_before = bin ? sh->count[bin - 1] : 0;
-  uint32_t members = sh->count[bin] - count_before;
-  // Among the tokens of a crowded bin the position is narrowed by the digits of (logit, number), 11 bits at a time
+  unsigned long long mass_before = 0;
+  uint32_t count_before = 0;
   uint64_t prefix = 0;
-  int shift = 64;
-  auto member = [&](int token, float l, float y) {
-    const uint64_t key = (uint64_t)falling_key(l) << 32 | (uint32_t)token;
-    return y > -23.0f && Row::bin(y) == bin && (shift == 64 || (key >> shift) == prefix);
-  };
-  while (members > kListed) {
-    for (int j = i; j < kBins; j += kPickThreads) sh->digit_mass[j] = 0, sh->digit_count[j] = 0;
+  int bin = -1;
+  for (int shift = 64 + kDigitBits; shift > 0;) {  // first the bins themselves, then the digits of one
+    for (int j = i; j < kBins; j += kPickThreads) sh->mass[j] = 0, sh->count[j] = 0;
     __syncthreads();
-    const int next = max(shift - 11, 0);
+    const int next = max(shift - kDigitBits, 0);
     for_each_logit<T, kPickThreads>(row.logits, 0, a.vocab, [&](int token, float l) {
       const float y = row.y(l);
-      if (!member(token, l, y)) return;
+      if (!(y > kLeast)) return;
       const uint32_t w = Row::weight(y);
       if (!w) return;
-      const uint64_t key = (uint64_t)falling_key(l) << 32 | (uint32_t)token;
-      const int digit = (int)((key >> next) & ((1ull << (shift - next)) - 1));
-      atomicAdd(&sh->digit_mass[digit], (unsigned long long)w);
-      atomicAdd(&sh->digit_count[digit], 1u);
+      int digit = Row::bin(y);
+      if (shift <= 64) {
+        const uint64_t key = entry_of(token, l);
+        if (digit != bin || (shift < 64 && (key >> shift) != prefix)) return;
+        digit = (int)((key >> next) & ((1ull << (shift - next)) - 1));
+      }
+      atomicAdd(&sh->mass[digit], (unsigned long long)w);
+      atomicAdd(&sh->count[digit], 1u);
     });
     __syncthreads();
-    prefix_sums(sh->digit_mass, sh->digit_count, sh);
+    Bins<kPickThreads> sums;
 #pragma unroll
-    for (int j = 2 * i; j <= 2 * i + 1; ++j)
-      if (sought.reached(count_before + sh->digit_count[j], mass_before + sh->digit_mass[j]) &&
-          (j == 0 || !sought.reached(count_before + sh->digit_count[j - 1], mass_before + sh->digit_mass[j - 1])))
-        sh->digit = j;
+    for (int j = 0; j < Bins<kPickThreads>::EACH; ++j) {
+      sums.mass[j] = sh->mass[Bins<kPickThreads>::EACH * i + j];
+      sums.count[j] = sh->count[Bins<kPickThreads>::EACH * i + j];
+    }
+    sums.add_up(sh);
+    sums.mark_first([&](uint32_t c, unsigned long long m) { return sought.reached(count_before + c, mass_before + m); }, &sh->mark[0]);
     __syncthreads();
-    const int digit = sh->digit;
-    members = sh->digit_count[digit] - (digit ? sh->digit_count[digit - 1] : 0);
-    mass_before += digit ? sh->digit_mass[digit - 1] : 0;
-    count_before += digit ? sh->digit_count[digit - 1] : 0;
-    prefix = (shift == 64 ? 0 : prefix << (shift - next)) | (uint32_t)digit;
+    const Mark x = sh->mark[0];
+    if (x.bin / Bins<kPickThreads>::EACH == i) {
+      uint32_t c = 0;
+#pragma unroll
+      for (int j = 0; j < Bins<kPickThreads>::EACH; ++j)
+        if (x.bin % Bins<kPickThreads>::EACH == j) c = j ? sums.count[j - 1] : sums.count_before;
+      sh->listed = c;
+    }
+    __syncthreads();
+    mass_before += x.before;
+    count_before += sh->listed;
+    if (shift > 64)
+      bin = x.bin;
+    else
+      prefix = (shift == 64 ? 0 : prefix << (shift - next)) | (uint32_t)x.bin;
     shift = next;
     __syncthreads();
   }
-  if (i == 0) sh->listed = 0;
+  if (i == 0) sh->found = prefix;
   __syncthreads();
-  for_each_logit<T, kPickThreads>(row.logits, 0, a.vocab, [&](int token, float l) {
-    const float y = row.y(l);
-    if (!member(token, l, y)) return;
-    const uint32_t w = Row::weight(y);
-    if (!w) return;
-    const int at = atomicAdd(&sh->listed, 1);
-    if (at < kListed) {
-      sh->list_key[at] = (uint64_t)falling_key(l) << 32 | (uint32_t)token;
-      sh->list_mass[at] = w;
-    }
-  });
-  __syncthreads();
-  const int listed = min(sh->listed, kListed);
-  for (int j = i; j < listed; j += kPickThreads) {
-    const uint64_t key = sh->list_key[j];
-    unsigned long long before = mass_before;
-    uint32_t rank = count_before;
-    for (int x = 0; x < listed; ++x)
-      if (sh->list_key[x] < key) before += sh->list_mass[x], ++rank;
-    const unsigned long long through = before + sh->list_mass[j];
-    if (sought.reached(rank + 1, through) && !((rank > 0) && sought.reached(rank, before))) {
-      const uint32_t f = (uint32_t)(key >> 32), u = f & 0x80000000u ? f : ~f & 0x7FFFFFFFu;
-      sh->found = Place{before, through, (int)(uint32_t)key, row.y(__uint_as_float(u))};
-    }
-  }
-  __syncthreads();
-  const Place p = sh->found;
-  __syncthreads();
-  return p;
+  return mass_before + Row::weight(row.y(logit_of_entry(prefix)));
 }
 
-// One workgroup per row: the kept weight, then the token.
+template <int T>
+__device__ void choose_crowded(const SampleArgs& a, int r, const Row& row, const Wanted& w, PickShared* sh) {
+  unsigned long long kept = w.total;
+  if (w.top_k) kept = place_of<T>(a, row, Sought{Sought::kCount, (uint32_t)w.top_k, 0.0, 0}, sh);
+  if (w.by_top_p) kept = min(kept, place_of<T>(a, row, Sought{Sought::kAtLeast, 0, (double)w.top_p * (double)kept, 0}, sh));
+  if (w.by_min_p) {
+    if (threadIdx.x == 0) sh->min_mass = 0;
+    __syncthreads();
+    unsigned long long mine = 0;
+    for_each_logit<T, kPickThreads>(row.logits, 0, a.vocab, [&](int, float l) {
+      const float y = row.y(l);
+      if (y >= w.floor && y > kLeast) mine += Row::weight(y);
+    });
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) mine += __shfl_xor(mine, s);
+    if ((threadIdx.x & 63) == 0) atomicAdd(&sh->min_mass, mine);
+    __syncthreads();
+    kept = min(kept, sh->min_mass);
+  }
+  const unsigned long long passed = min((unsigned long long)((double)a.uniform[r] * (double)kept), kept - 1);
+  place_of<T>(a, row, Sought{Sought::kAbove, 0, 0.0, passed}, sh);
+}
+
+__device__ __forceinline__ void store_choice(const SampleArgs& a, int r, const Row& row, const Wanted& w, const PickShared* sh) {
+  if (threadIdx.x) return;
+  const uint64_t found = sh->found;
+  a.tokens[r] = (int32_t)(uint32_t)found;
+  // (the most probable token weighs 2^31)
+  if (a.logprobs)
+    a.logprobs[r] = row.y(logit_of_entry(found)) - log1pf((float)(w.total - (1ull << 31)) * 4.65661287307739e-10f);
+}
+__device__ __forceinline__ void store_none(const SampleArgs& a, int r) {
+  if (threadIdx.x) return;
+  a.tokens[r] = -1;
+  if (a.logprobs) a.logprobs[r] = -INFINITY;
+}
+
+// Slices: the tokens of the wanted bins into the row's list, with the sums before their bins; the workgroup of the first
+// slice leaves what the choice needs to know beside.
+template <int T>
+__global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  PickShared* const sh = reinterpret_cast<PickShared*>(lds);
+  const int s = blockIdx.x, r = blockIdx.y;
+  Bins<kSliceThreads> bins;
+  {
+    const int64_t at = (int64_t)r * kBins + Bins<kSliceThreads>::EACH * threadIdx.x;
+#pragma unroll
+    for (int j = 0; j < Bins<kSliceThreads>::EACH; ++j) bins.mass[j] = a.mass[at + j], bins.count[j] = a.count[at + j];
+  }
+  const Row row = make_row<T>(a, r);
+  if (row.m == -INFINITY) return;
+  bins.add_up(sh);
+  const Wanted w = find_wanted<kSliceThreads>(a, r, bins, sh);
+  if (s == 0 && threadIdx.x == 0) a.wanted[r] = w;
+  if (w.tokens > kListed) return;
+  const float reach = reach_of(row, sh->last_bin);
+  for_each_logit<T, kSliceThreads>(row.logits, slice_from(a, s), slice_from(a, s + 1), [&](int token, float l) {
+    if (is_wanted(row, l, reach, w)) {
+      const int bin = Row::bin(row.y(l));
+      a.list[(int64_t)r * kListed + atomicAdd(&a.listed[r], 1u)] = Listed{entry_of(token, l), sh->mass[bin], sh->count[bin], 0};
+    }
+  });
+}
+
+// One workgroup per row: the choice.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
   PickShared* const sh = reinterpret_cast<PickShared*>(lds);
-  const int r = blockIdx.x, i = threadIdx.x;
+  const int r = blockIdx.x;
   const Row row = make_row<T>(a, r);
-  if (row.m == -INFINITY) {
-    if (i == 0) {
-      a.tokens[r] = -1;
-      if (a.logprobs) a.logprobs[r] = -INFINITY;
+  if (row.m == -INFINITY) return store_none(a, r);
+  const Wanted w = a.wanted[r];
+  if (w.tokens > kListed) {
+    choose_crowded<T>(a, r, row, w, sh);
+  } else {
+    for (int j = threadIdx.x; j < (int)w.tokens; j += kPickThreads) {
+      const Listed x = a.list[(int64_t)r * kListed + j];
+      sh->list[j] = x.entry;
+      const int bin = Row::bin(row.y(logit_of_entry(x.entry)));
+      sh->mass[bin] = x.mass_before;
+      sh->count[bin] = x.count_before;
     }
-    return;
+    choose_from_list<kPickThreads>(a, r, row, w, sh);
   }
-  for (int j = i; j < kBins; j += kPickThreads) {
-    sh->mass[j] = a.mass[(int64_t)r * kBins + j];
-    sh->count[j] = a.count[(int64_t)r * kBins + j];
-  }
-  if (i == 0) sh->min_mass = 0, sh->bin = sh->digit = 0, sh->found = Place{0, 0, 0, 0.0f};
+  store_choice(a, r, row, w, sh);
+}
+
+// One workgroup per row: everything.
+template <int T>
+__global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  PickShared* const sh = reinterpret_cast<PickShared*>(lds);
+  const int r = blockIdx.x, i = threadIdx.x;
+  const void* const logits = (const uint8_t*)a.logits + r * a.stride * (T == SFMP_TYPE_FP32 ? 4 : 2);
+  for (int j = i; j < kBins; j += kPickThreads) sh->mass[j] = 0, sh->count[j] = 0;
+  float m = -INFINITY;
+  for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) { m = fmaxf(m, l); });
+  m = max_of_wave(m);
+  if ((i & 63) == 0) sh->wave_max[i >> 6] = m;
   __syncthreads();
-  prefix_sums(sh->mass, sh->count, sh);
-  const unsigned long long total = sh->mass[kBins - 1];
-  const uint32_t counted = sh->count[kBins - 1];  // tokens whose weight is not 0
-  const bool greedy = a.temperature && a.temperature[r] <= 0.0f;
-  const int top_k = greedy ? 1 : a.top_k ? a.top_k[r] : 0;
-  const float top_p = a.top_p ? a.top_p[r] : 1.0f, min_p = a.min_p ? a.min_p[r] : 0.0f;
-  unsigned long long kept = total;
-  if (top_k > 0 && (uint32_t)top_k < counted)
-    kept = place_of<T>(a, row, Sought{Sought::kCount, (uint32_t)top_k, 0.0, 0}, sh).through;
-  const unsigned long long of_top_k = kept;
-  if (top_p < 1.0f)
-    kept = min(kept, place_of<T>(a, row, Sought{Sought::kAtLeast, 0, (double)top_p * (double)of_top_k, 0}, sh).through);
-  if (min_p > 0.0f) {
-    const float floor = logf(fminf(min_p, 1.0f));
-    unsigned long long mine = 0;
-    for_each_logit<T, kPickThreads>(row.logits, 0, a.vocab, [&](int, float l) {
-      const float y = row.y(l);
-      if (y >= floor && y > -23.0f) mine += Row::weight(y);
-    });
 #pragma unroll
-    for (int s = 1; s < 64; s *= 2) mine += __shfl_xor(mine, s);
-    if ((i & 63) == 0) atomicAdd(&sh->min_mass, mine);
+  for (int w = 0; w < kPickThreads / 64; ++w) m = fmaxf(m, sh->wave_max[w]);
+  const Row row(logits, m, a.temperature ? a.temperature[r] : 1.0f);
+  if (row.m == -INFINITY) return store_none(a, r);
+  for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) {
+    const float y = row.y(l);
+    if (!(y > kLeast)) return;
+    const uint32_t w = Row::weight(y);
+    if (!w) return;
+    atomicAdd(&sh->mass[Row::bin(y)], (unsigned long long)w);
+    atomicAdd(&sh->count[Row::bin(y)], 1u);
+  });
+  __syncthreads();
+  Bins<kPickThreads> bins;
+#pragma unroll
+  for (int j = 0; j < Bins<kPickThreads>::EACH; ++j) {
+    bins.mass[j] = sh->mass[Bins<kPickThreads>::EACH * i + j];
+    bins.count[j] = sh->count[Bins<kPickThreads>::EACH * i + j];
+  }
+  bins.add_up(sh);
+  const Wanted w = find_wanted<kPickThreads>(a, r, bins, sh);
+  if (w.tokens > kListed) {
+    choose_crowded<T>(a, r, row, w, sh);
+  } else {
+    const float reach = reach_of(row, sh->last_bin);
     __syncthreads();
-    kept = min(kept, sh->min_mass);
+    if (i == 0) sh->listed = 0;
+    __syncthreads();
+    for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int token, float l) {
+      if (is_wanted(row, l, reach, w)) sh->list[atomicAdd(&sh->listed, 1u)] = entry_of(token, l);
+    });
+    __syncthreads();
+    choose_from_list<kPickThreads>(a, r, row, w, sh);
   }
-  const unsigned long long passed = (unsigned long long)((double)a.uniform[r] * (double)kept);
-  const Place p = place_of<T>(a, row, Sought{Sought::kAbove, 0, 0.0, min(passed, kept - 1)}, sh);
-  if (i == 0) {
-    a.tokens[r] = p.token;
-    // (the most probable token weighs 2^31)
-    if (a.logprobs) a.logprobs[r] = p.y - log1pf((float)(total - (1ull << 31)) * 4.65661287307739e-10f);
-  }
+  store_choice(a, r, row, w, sh);
 }
 
 int slices_of(int32_t rows, int32_t vocab) {
@@ -353,27 +701,39 @@ int slices_of(int32_t rows, int32_t vocab) {
   return (int)s;
 }
 
+// From this many rows on, one workgroup per row.
+constexpr int kWholeRows = 96;
+
 struct SampleWorkspace {
-  int64_t max_at, mass_at, count_at, bytes;
+  int64_t max_at, mass_at, count_at, list_at, wanted_at, listed_at, bytes;
 };
 SampleWorkspace sample_workspace(int32_t rows, int32_t vocab) {
-  SampleWorkspace w;
-  w.mass_at = 0;
+  SampleWorkspace w{};
+  w.bytes = 256;
+  if (rows == 0 || rows >= kWholeRows) return w;
   w.count_at = round_up_256((int64_t)rows * kBins * 8);
-  w.max_at = w.count_at + round_up_256((int64_t)rows * kBins * 4);
-  w.bytes = w.max_at + round_up_256((int64_t)rows * slices_of(rows ? rows : 1, vocab) * 4);
-  if (w.bytes < 256) w.bytes = 256;
+  w.list_at = w.count_at + round_up_256((int64_t)rows * kBins * 4);
+  w.wanted_at = w.list_at + round_up_256((int64_t)rows * kListed * sizeof(Listed));
+  w.listed_at = w.wanted_at + round_up_256((int64_t)rows * sizeof(Wanted));
+  w.max_at = w.listed_at + round_up_256((int64_t)rows * 4);
+  w.bytes = w.max_at + round_up_256((int64_t)rows * slices_of(rows, vocab) * 4);
   return w;
 }
 
 template <int T>
 int launch_sample(const SampleArgs& a, hipStream_t stream) {
-  const dim3 grid(a.slices, a.rows);
-  sample_max_kernel<T><<<grid, kSliceThreads, 0, stream>>>(a);
-  sample_bins_kernel<T><<<grid, kSliceThreads, 0, stream>>>(a);
-  const void* const pick = (const void*)sample_pick_kernel<T>;
-  if (int e = allow_full_lds(pick, "sample_pick_kernel")) return e;
-  sample_pick_kernel<T><<<a.rows, kPickThreads, sizeof(PickShared), stream>>>(a);
+  if (a.rows >= kWholeRows) {
+    if (int e = allow_full_lds((const void*)sample_row_kernel<T>, "sample_row_kernel")) return e;
+    sample_row_kernel<T><<<a.rows, kPickThreads, sizeof(PickShared), stream>>>(a);
+  } else {
+    if (int e = allow_full_lds((const void*)sample_collect_kernel<T>, "sample_collect_kernel")) return e;
+    if (int e = allow_full_lds((const void*)sample_pick_kernel<T>, "sample_pick_kernel")) return e;
+    const dim3 grid(a.slices, a.rows);
+    sample_max_kernel<T><<<grid, kSliceThreads, 0, stream>>>(a);
+    sample_bins_kernel<T><<<grid, kSliceThreads, 0, stream>>>(a);
+    sample_collect_kernel<T><<<grid, kSliceThreads, sizeof(PickShared), stream>>>(a);
+    sample_pick_kernel<T><<<a.rows, kPickThreads, sizeof(PickShared), stream>>>(a);
+  }
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return SFMP_OK;
   note_hip_error("sfmp_sample", hipGetErrorString(e));
@@ -410,8 +770,8 @@ extern "C" int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, 
   const SampleWorkspace w = sample_workspace(rows, vocab);
   uint8_t* const at = (uint8_t*)workspace_dev;
   const SampleArgs a{logits_dev, rows, vocab, slices_of(rows, vocab), stride, temperature_dev, top_k_dev, top_p_dev, min_p_dev,
-                     uniform_dev, tokens_dev, logprobs_dev, (float*)(at + w.max_at),
-                     (unsigned long long*)(at + w.mass_at), (uint32_t*)(at + w.count_at)};
+                     uniform_dev, tokens_dev, logprobs_dev, (float*)(at + w.max_at), (Listed*)(at + w.list_at), (Wanted*)(at + w.wanted_at),
+                     (uint32_t*)(at + w.listed_at), (unsigned long long*)(at + w.mass_at), (uint32_t*)(at + w.count_at)};
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (dtype == SFMP_TYPE_FP16) return launch_sample<SFMP_TYPE_FP16>(a, stream);
   if (dtype == SFMP_TYPE_BF16) return launch_sample<SFMP_TYPE_BF16>(a, stream);

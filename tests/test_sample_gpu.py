@@ -82,6 +82,31 @@ def test_every_filter(dtype, rows, vocab, apart, offset):
     assert sure > 0.5 * all_
 
 
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+@pytest.mark.parametrize("rows,vocab,apart,offset", [(96, 3, 0, 0), (130, 5000, 1, 3), (100, 70001, 0, 0), (97, 140007, 2, 1)])
+def test_many_rows(dtype, rows, vocab, apart, offset):
+    # one workgroup per row, which keeps a part of it in registers: the same as the first rows alone, sliced, and as the oracle
+    rng = np.random.default_rng(rows + vocab)
+    x = _logits(rng, rows, vocab)
+    t, k = rng.choice([0.0, 0.6, 1.0, 2.0], rows), rng.choice([0, 1, 50, 2000], rows)
+    p, m, u = rng.choice([0.2, 0.95, 1.0], rows), rng.choice([0.0, 0.03], rows), rng.random(rows)
+    all_, logprobs, _ = _run(x, t, k, p, m, u, dtype=dtype, apart=apart, offset=offset)
+    some = slice(0, 40)
+    few, few_logprobs, _ = _run(x[some], t[some], k[some], p[some], m[some], u[some], dtype=dtype)
+    assert np.array_equal(all_[some], few) and np.array_equal(logprobs[some], few_logprobs)
+    sure, tokens = _check(x[:96], t[:96], k[:96], p[:96], m[:96], u[:96], dtype=dtype, apart=apart, offset=offset)
+    assert sure > 40 and np.array_equal(tokens, all_[:96])
+
+
+@pytest.mark.parametrize("vocab", [2049, 100000])
+def test_many_rows_of_equal_logits(vocab):
+    x = np.full((100, vocab), -1.5, dtype=np.float32)
+    x[:, ::2] += 1e-4
+    half = (vocab + 1) // 2
+    tokens, _, _ = _run(x, 1.0, 1 + np.arange(100) * (half // 100), 1.0, 0.0, 1.0 - 2.0 ** -24)
+    assert tokens.tolist() == [2 * i * (half // 100) for i in range(100)]
+
+
 def test_defaults_and_parameters_by_row():
     rng = np.random.default_rng(0)
     x = _logits(rng, 40, 5000)
