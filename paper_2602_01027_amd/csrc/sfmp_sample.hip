@@ -62,6 +62,8 @@ __device__ __forceinline__ float logit_of(uint32_t bits) {
   return x;
 }
 
+typedef __attribute__((address_space(1))) u32x4 GlobalRun;
+
 // Calls f(number, logit) for the tokens [from, to) of a row; the threads take runs of 16 aligned bytes in turn.
 template <int T, int THREADS, typename F>
 __device__ __forceinline__ void for_each_logit(const void* row, int from, int to, F f) {
@@ -69,11 +71,30 @@ __device__ __forceinline__ void for_each_logit(const void* row, int from, int to
   const int lead = (int)((reinterpret_cast<uintptr_t>(row) & 15) / SIZE);  // elements between the aligned address and the row
   const uint8_t* const base = (const uint8_t*)row - lead * SIZE;
   const int first = (from + lead + RUN - 1) / RUN, last = max((to + lead) / RUN, first);  // whole runs
-#pragma unroll 4
-  for (int v = first + threadIdx.x; v < last; v += THREADS) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(base + (int64_t)v * 16);
+  const GlobalRun* const runs = (const GlobalRun*)reinterpret_cast<uintptr_t>(base);
+  // four runs at a time, the next four requested before
+  constexpr int AHEAD = 4;
+  u32x4 now[AHEAD], next[AHEAD];
+  auto request = [&](u32x4 (&w)[AHEAD], int v) {
 #pragma unroll
-    for (int j = 0; j < RUN; ++j) f(v * RUN - lead + j, logit_of<T>(SIZE == 4 ? w[j] : (j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu));
+    for (int k = 0; k < AHEAD; ++k)
+      if (v + k * THREADS < last) w[k] = runs[v + k * THREADS];
+  };
+  int v = first + threadIdx.x;
+  request(now, v);
+  for (; v < last; v += AHEAD * THREADS) {
+    request(next, v + AHEAD * THREADS);
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) {
+      if (v + k * THREADS < last) {
+#pragma unroll
+        for (int j = 0; j < RUN; ++j) {
+          const u32x4 w = now[k];
+          f((v + k * THREADS) * RUN - lead + j, logit_of<T>(SIZE == 4 ? w[j] : (j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu));
+        }
+      }
+      now[k] = next[k];
+    }
   }
   // before the first and behind the last
   const int head = min(first * RUN - lead, to), tail = max(last * RUN - lead, head);
@@ -94,12 +115,16 @@ struct Row {
   const void* logits;
   float m, inverse;
   bool plain;  // m and 1 / T are finite
-  __device__ __forceinline__ Row(const void* p, float largest, float t) : logits(p), m(largest), inverse(1.0f / fmaxf(t, 0.0f)) {
-    plain = inverse < INFINITY && fabsf(m) < INFINITY;
+  __device__ __forceinline__ Row(const void* p, float largest, float t) : logits(p) {
+    // (the same for all lanes, which the compiler has to be told)
+    m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(largest)));
+    inverse = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(1.0f / fmaxf(t, 0.0f))));
+    plain = __builtin_amdgcn_readfirstlane(inverse < INFINITY && fabsf(m) < INFINITY);
   }
   // (l - m) / T; not above kLeast for a NaN
+  template <bool PLAIN = false>
   __device__ __forceinline__ float y(float l) const {
-    if (plain) return (l - m) * inverse;
+    if (PLAIN) return (l - m) * inverse;
     return l == m ? 0.0f : l == -INFINITY ? -INFINITY : (l - m) * inverse;
   }
   static __device__ __forceinline__ uint32_t weight(float y) { return (uint32_t)rintf(expf(y) * 2147483648.0f); }
@@ -158,13 +183,16 @@ __global__ __launch_bounds__(kSliceThreads) void sample_bins_kernel(SampleArgs a
   const Row row = make_row<T>(a, r);
   __syncthreads();
   if (row.m == -INFINITY) return;
-  for_each_logit<T, kSliceThreads>(row.logits, slice_from(a, s), slice_from(a, s + 1), [&](int, float l) {
-    const float y = row.y(l);
-    if (y > kLeast) {
-      const uint32_t w = Row::weight(y);
-      if (w) atomicAdd(&bins[Row::bin(y)], (1ull << kCountBit) + w);
-    }
-  });
+  auto add = [&](float y) {
+    if (!(y > kLeast)) return;
+    const uint32_t w = Row::weight(y);
+    if (w) atomicAdd(&bins[Row::bin(y)], (1ull << kCountBit) + w);
+  };
+  const int from = slice_from(a, s), to = slice_from(a, s + 1);
+  if (row.plain)
+    for_each_logit<T, kSliceThreads>(row.logits, from, to, [&](int, float l) { add(row.template y<true>(l)); });
+  else
+    for_each_logit<T, kSliceThreads>(row.logits, from, to, [&](int, float l) { add(row.y(l)); });
   __syncthreads();
   for (int i = threadIdx.x; i < kBins; i += kSliceThreads)
     if (const unsigned long long x = bins[i]) {
@@ -189,7 +217,6 @@ struct PickShared {
   uint64_t found;
   float wave_max[kPickThreads / 64];
   uint32_t listed, counted;
-  int last_bin, digit;
 };
 
 // Sum over the threads before this one, and over all.
@@ -222,12 +249,17 @@ struct Wanted {
   float top_p, floor;
   bool by_top_p, by_min_p;
   unsigned long long total, min_before;  // (before the bin of min-p's floor)
-  int from[4], to[4];  // ranges of bins (from > to: none)
-  uint32_t tokens;     // in them
+  int from[4];          // ranges of bins
+  uint32_t span[4];     // bins of a range behind its first
+  uint32_t tokens;      // in them
+  __device__ __forceinline__ void range(int x, int first, int last) {
+    from[x] = __builtin_amdgcn_readfirstlane(first);
+    span[x] = __builtin_amdgcn_readfirstlane(last - first);
+  }
   __device__ __forceinline__ bool has(int bin) const {
     bool y = false;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) y |= bin >= from[x] && bin <= to[x];
+    for (int x = 0; x < 4; ++x) y |= (uint32_t)(bin - from[x]) <= span[x];
     return y;
   }
 };
@@ -305,10 +337,10 @@ template <int THREADS>
 __device__ __forceinline__ Wanted find_wanted(const SampleArgs& a, int r, const Bins<THREADS>& bins, PickShared* sh) {
   Wanted w = filters_of(a, r, sh->counted, sh->total);
 #pragma unroll
-  for (int x = 0; x < 4; ++x) w.from[x] = 1, w.to[x] = 0;
+  for (int x = 0; x < 4; ++x) w.from[x] = 1 << 30, w.span[x] = 0;  // (none)
   const float u = a.uniform[r];
   unsigned long long least = w.total, most = w.total;  // both ends of the kept weight
-  if (threadIdx.x == 0) sh->listed = 0, sh->last_bin = 0;
+  if (threadIdx.x == 0) sh->listed = 0;
   const int min_bin = w.floor > kLeast ? Row::bin(w.floor) : kBins - 1;
   if (w.by_min_p) bins.mark_bin(min_bin, &sh->mark[5]);
   if (w.top_k) {
@@ -316,7 +348,7 @@ __device__ __forceinline__ Wanted find_wanted(const SampleArgs& a, int r, const 
     bins.mark_first([&](uint32_t c, unsigned long long) { return c >= k; }, &sh->mark[0]);
     __syncthreads();
     const Mark x = sh->mark[0];
-    w.from[0] = w.to[0] = x.bin;
+    w.range(0, x.bin, x.bin);
     least = x.before + 1, most = x.through;
   }
   if (w.by_top_p) {
@@ -325,13 +357,13 @@ __device__ __forceinline__ Wanted find_wanted(const SampleArgs& a, int r, const 
     bins.mark_first([&](uint32_t, unsigned long long m) { return (double)m >= high; }, &sh->mark[2]);
     __syncthreads();
     const Mark x = sh->mark[1], y = sh->mark[2];
-    w.from[1] = x.bin, w.to[1] = y.bin;
+    w.range(1, x.bin, y.bin);
     least = min(least, x.before + 1), most = min(most, y.through);
   }
   if (w.by_min_p) {
     __syncthreads();
     const Mark x = sh->mark[5];
-    w.from[2] = w.to[2] = min_bin;
+    w.range(2, min_bin, min_bin);
     w.min_before = x.before;
     least = min(least, max(x.before, 1ull)), most = min(most, x.through);
   }
@@ -340,34 +372,48 @@ __device__ __forceinline__ Wanted find_wanted(const SampleArgs& a, int r, const 
   bins.mark_first([&](uint32_t, unsigned long long m) { return m > low; }, &sh->mark[3]);
   bins.mark_first([&](uint32_t, unsigned long long m) { return m > high; }, &sh->mark[4]);
   __syncthreads();
-  w.from[3] = sh->mark[3].bin, w.to[3] = sh->mark[4].bin;
+  w.range(3, sh->mark[3].bin, sh->mark[4].bin);
   uint32_t tokens = 0;
-  int last = 0;
 #pragma unroll
   for (int j = 0; j < Bins<THREADS>::EACH; ++j) {
     const int bin = Bins<THREADS>::EACH * threadIdx.x + j;
     if (w.has(bin)) {
       const uint32_t before = j ? bins.count[j - 1] : bins.count_before;
       tokens += bins.count[j] - before;
-      last = bin;
       sh->mass[bin] = j ? bins.mass[j - 1] : bins.mass_before;
       sh->count[bin] = before;
     }
   }
   if (tokens) atomicAdd(&sh->listed, tokens);
-  if (last) atomicMax(&sh->last_bin, last);
   __syncthreads();
-  w.tokens = sh->listed;
+  w.tokens = __builtin_amdgcn_readfirstlane(sh->listed);
   return w;
 }
 
-// The logit below which no token is in the wanted bins (with a margin for rounding).
-__device__ __forceinline__ float reach_of(const Row& row, int last_bin) {
-  const float reach = row.m - (float)(last_bin + 2) / kBinsPerUnit / row.inverse * 1.0001f - fabsf(row.m) * 1e-6f;
-  return reach == reach && row.m < INFINITY ? reach : -INFINITY;
-}
-__device__ __forceinline__ bool is_wanted(const Row& row, float l, float reach, const Wanted& w) {
-  if (l < reach) return false;
+// The wanted bins as intervals of logits, with a margin for rounding: most tokens are told apart without their bin.
+struct Reach {
+  float middle[4], half[4];
+  __device__ __forceinline__ Reach(const Row& row, const Wanted& w) {
+    const float unit = 1.0f / (kBinsPerUnit * row.inverse), margin = fabsf(row.m) * 2e-6f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const bool none = w.from[x] >= kBins;
+      const float high = row.m - (float)(w.from[x] - 1) * unit, low = row.m - (float)(w.from[x] + (int)w.span[x] + 2) * unit;
+      const float c = !row.plain || none ? 0.0f : 0.5f * (high + low);
+      const float h = none ? -1.0f : !row.plain ? INFINITY : 0.5001f * (high - low) + margin + fabsf(c) * 1e-6f;
+      middle[x] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c)));
+      half[x] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(h)));
+    }
+  }
+  __device__ __forceinline__ bool may_hold(float l) const {
+    bool y = false;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) y |= fabsf(l - middle[x]) <= half[x];
+    return y;
+  }
+};
+__device__ __forceinline__ bool is_wanted(const Row& row, float l, const Reach& reach, const Wanted& w) {
+  if (!reach.may_hold(l)) return false;
   const float y = row.y(l);
   return y > kLeast && w.has(Row::bin(y)) && Row::weight(y);
 }
@@ -377,14 +423,29 @@ __device__ __forceinline__ float logit_of_entry(uint64_t e) {
   return __uint_as_float(f & 0x80000000u ? f : ~f & 0x7FFFFFFFu);
 }
 
-// Sorts list[0, n) upwards, n a power of two (at least 128).  With strides up to 64 the elements of a wavefront's threads lie
-// within 128 of its own: no barrier of the workgroup is needed between those steps.
+// Sorts list[0, n) upwards, n a power of two from 64 to kListed, all entries different (but for the ~0 behind the last).
 template <int THREADS>
 __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
+  if (n <= 256) {
+    // by rank: THREADS / n threads count the smaller ones of an entry
+    const int shift = __builtin_ctz(THREADS) - __builtin_ctz(n), parts = 1 << shift;
+    const int e = threadIdx.x >> shift, q = threadIdx.x & (parts - 1);
+    const uint64_t x = list[e];
+    int rank = 0;
+#pragma unroll 4
+    for (int j = q; j < n; j += parts) rank += list[j] < x || (j < e && list[j] == x);
+    for (int s = 1; s < parts; s *= 2) rank += __shfl_xor(rank, s);
+    __syncthreads();
+    if (q == 0) list[rank] = x;
+    __syncthreads();
+    return;
+  }
+  // With strides up to 64 the elements of a wavefront's threads lie within 128 of its own: no barrier of the workgroup is needed
+  // between those steps.
   for (int size = 2; size <= n; size *= 2)
     for (int stride = size / 2; stride > 0; stride /= 2) {
       for (int t = threadIdx.x; t < n / 2; t += THREADS) {
-        const int i = 2 * stride * (t / stride) + t % stride, j = i + stride;
+        const int i = 2 * t - (t & (stride - 1)), j = i + stride;
         const uint64_t x = list[i], y = list[j];
         if ((x > y) == ((i & size) == 0)) list[i] = y, list[j] = x;
       }
@@ -401,7 +462,7 @@ template <int THREADS>
 __device__ __forceinline__ void choose_from_list(const SampleArgs& a, int r, const Row& row, const Wanted& w, PickShared* sh) {
   constexpr int EACH = kListed / THREADS;
   const int i = threadIdx.x, n = (int)w.tokens;
-  int size = 128;
+  int size = 64;
   while (size < n) size *= 2;
   for (int j = n + i; j < size; j += THREADS) sh->list[j] = ~0ull;
   const int min_bin = w.from[2];
@@ -609,7 +670,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArg
   const Wanted w = find_wanted<kSliceThreads>(a, r, bins, sh);
   if (s == 0 && threadIdx.x == 0) a.wanted[r] = w;
   if (w.tokens > kListed) return;
-  const float reach = reach_of(row, sh->last_bin);
+  const Reach reach(row, w);
   for_each_logit<T, kSliceThreads>(row.logits, slice_from(a, s), slice_from(a, s + 1), [&](int token, float l) {
     if (is_wanted(row, l, reach, w)) {
       const int bin = Row::bin(row.y(l));
@@ -624,14 +685,16 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   extern __shared__ __align__(16) uint8_t lds[];
   PickShared* const sh = reinterpret_cast<PickShared*>(lds);
   const int r = blockIdx.x;
+  const Listed* const list = a.list + (int64_t)r * kListed;
+  const Listed mine = list[threadIdx.x];  // (requested before it is known how many there are)
+  const Wanted w = a.wanted[r];
   const Row row = make_row<T>(a, r);
   if (row.m == -INFINITY) return store_none(a, r);
-  const Wanted w = a.wanted[r];
   if (w.tokens > kListed) {
     choose_crowded<T>(a, r, row, w, sh);
   } else {
     for (int j = threadIdx.x; j < (int)w.tokens; j += kPickThreads) {
-      const Listed x = a.list[(int64_t)r * kListed + j];
+      const Listed x = j < kPickThreads ? mine : list[j];
       sh->list[j] = x.entry;
       const int bin = Row::bin(row.y(logit_of_entry(x.entry)));
       sh->mass[bin] = x.mass_before;
@@ -659,14 +722,17 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   for (int w = 0; w < kPickThreads / 64; ++w) m = fmaxf(m, sh->wave_max[w]);
   const Row row(logits, m, a.temperature ? a.temperature[r] : 1.0f);
   if (row.m == -INFINITY) return store_none(a, r);
-  for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) {
-    const float y = row.y(l);
+  auto add = [&](float y) {
     if (!(y > kLeast)) return;
     const uint32_t w = Row::weight(y);
     if (!w) return;
     atomicAdd(&sh->mass[Row::bin(y)], (unsigned long long)w);
     atomicAdd(&sh->count[Row::bin(y)], 1u);
-  });
+  };
+  if (row.plain)
+    for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) { add(row.template y<true>(l)); });
+  else
+    for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) { add(row.y(l)); });
   __syncthreads();
   Bins<kPickThreads> bins;
 #pragma unroll
@@ -679,7 +745,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   if (w.tokens > kListed) {
     choose_crowded<T>(a, r, row, w, sh);
   } else {
-    const float reach = reach_of(row, sh->last_bin);
+    const Reach reach(row, w);
     __syncthreads();
     if (i == 0) sh->listed = 0;
     __syncthreads();
