@@ -8,9 +8,10 @@ namespace {
 template <int D, int NT>
 constexpr int kWaves = D * NT >= 256 ? 4 : 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-// Weights are rounded to fp16 after multiplication by 2^14: a product with V then keeps its 11 bits down to 2^-28 of the largest.
-constexpr float kWeightUnit = 16384.0f;
-constexpr float kLeastReference = 7.8886090522101181e-31f;  // 2^-100
+// Weights are rounded to fp16 in units of 2^-14: they keep their 11 bits down to 2^-28 of the largest.
+constexpr float kWeightUnit = 16384.0f, kWeightBits = 14.0f;
+// Sums are rescaled when a page's largest score (in units of ln 2) exceeds what they are relative to by more than this.
+constexpr float kSlack = 16.0f;
 
 struct AttentionArgs {
   KvView v;
@@ -53,7 +54,7 @@ __device__ __forceinline__ half8 operand_of(uint32_t lo, uint32_t hi) {
 template <int D, int NT>
 struct Partial {
   floatx4 o[NT][D / 16];
-  float m[NT], l[NT];  // running maximum of the scores (in units of ln 2) and sum of 2^(score - m)
+  float m[NT], l[NT];  // what the sums are relative to, in units of ln 2 (-infinity: no token yet), and the sum of 2^(score - m)
 };
 
 // The rows of a unit (one sequence, one key/value head, 16 * NT of its query rows).
@@ -64,6 +65,35 @@ struct Rows {
   int at[NT];        // position of the row in the sequence
   int first, last;   // smallest and largest of them
 };
+
+// Query values as fp16, and what they have to be multiplied by.  bf16 rows are brought into the range of fp16 by a power of
+// two (largest element in [2^10, 2^11)): elements down to 2^-25 of it stay exact, below the error is under 2^-35 of it.
+// The lanes of a row are those that differ in the bits s1 and s2.
+template <int N>
+__device__ __forceinline__ float bring_to_fp16(const u32x4 (&raw)[N], half8 (&q)[N], bool bf16, int s1, int s2) {
+  if (!bf16) {
+#pragma unroll
+    for (int s = 0; s < N; ++s) q[s] = __builtin_bit_cast(half8, raw[s]);
+    return 1.0f;
+  }
+  uint32_t largest = 0;
+#pragma unroll
+  for (int s = 0; s < N; ++s)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) largest = max(largest, max(raw[s][j] & 0x7FFFu, raw[s][j] >> 16 & 0x7FFFu));
+  largest = max(largest, (uint32_t)__shfl_xor((int)largest, s1));
+  largest = max(largest, (uint32_t)__shfl_xor((int)largest, s2));
+  const int exponent = min(max((int)(largest >> 7), 11), 254);  // (biased; both powers of two stay normal)
+  const float up = __uint_as_float((uint32_t)(127 + 127 + 10 - exponent) << 23);
+#pragma unroll
+  for (int s = 0; s < N; ++s)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      q[s][2 * j] = (_Float16)(__uint_as_float(raw[s][j] << 16) * up);
+      q[s][2 * j + 1] = (_Float16)(__uint_as_float(raw[s][j] & 0xFFFF0000u) * up);
+    }
+  return __uint_as_float((uint32_t)(exponent - 10) << 23);
+}
 
 template <int D, int NT>
 __device__ __forceinline__ void load_rows(const AttentionArgs& a, const KvEntry& e, int head, int tile, Rows<D, NT>& r) {
@@ -82,30 +112,7 @@ __device__ __forceinline__ void load_rows(const AttentionArgs& a, const KvEntry&
 #pragma unroll
     for (int s = 0; s < D / 32; ++s)
       raw[s] = *reinterpret_cast<const u32x4*>(src + 64 * (s / 2) + 16 * g + 8 * (s % 2));
-    if (!a.bf16) {
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s) r.q[nt][s] = __builtin_bit_cast(half8, raw[s]);
-    } else {
-      // bf16 rows are brought into the range of fp16 by a power of two (largest element in [2^10, 2^11)): elements
-      // down to 2^-25 of it stay exact, below the error is under 2^-35 of it
-      uint32_t largest = 0;
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) largest = max(largest, max(raw[s][j] & 0x7FFFu, raw[s][j] >> 16 & 0x7FFFu));
-      largest = max(largest, (uint32_t)__shfl_xor((int)largest, 16));
-      largest = max(largest, (uint32_t)__shfl_xor((int)largest, 32));
-      const int exponent = min(max((int)(largest >> 7), 11), 254);  // (biased; both powers of two stay normal)
-      const float up = __uint_as_float((uint32_t)(127 + 127 + 10 - exponent) << 23);
-      r.factor[nt] *= __uint_as_float((uint32_t)(exponent - 10) << 23);
-#pragma unroll
-      for (int s = 0; s < D / 32; ++s)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          r.q[nt][s][2 * j] = (_Float16)(__uint_as_float(raw[s][j] << 16) * up);
-          r.q[nt][s][2 * j + 1] = (_Float16)(__uint_as_float(raw[s][j] & 0xFFFF0000u) * up);
-        }
-    }
+    r.factor[nt] *= bring_to_fp16<D / 32>(raw, r.q[nt], a.bf16, 16, 32);
   }
   r.first = e.length - e.n + tile * NT * 16 / a.group;
   r.last = e.length - e.n + min((tile + 1) * NT * 16 - 1, count - 1) / a.group;
@@ -165,7 +172,6 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
     for (int dt = 0; dt < D / 16; ++dt) p.o[nt][dt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
   }
   if (begin >= end) return;
-  float reference = kLeastReference;  // largest scale of V so far: weights are multiplied by scale / reference
   // Numbers and scales of 64 pages at a time, one per lane
   int held_page = 0;
   float held_k = 0.0f, held_v = 0.0f;
@@ -212,102 +218,106 @@ __device__ __forceinline__ void accumulate(const AttentionArgs& a, const KvEntry
     const bool masked = page * kPage + kPage - 1 > r.first || (a.window > 0 && page * kPage <= r.last - a.window);
     if (page * kPage + kPage > e.length) {
       // tokens that were never written: whatever the bytes are, they must not meet the weight 0 as a NaN
+      int written = e.length - token;
+      asm volatile("" : "+v"(written));
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        const int left = e.length - (token + 4 * w);
+        const int left = written - 4 * w;
         const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) c.v[dt][w] &= keep;
       }
     }
 
-    // running maximum and reference
-    float factor[NT], now[NT];
-    bool changed = scale_v > reference;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      factor[nt] = scale_k * r.factor[nt];
-      float m = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[nt][t][x] *= factor[nt];
-      if (masked) {
-        const int from = a.window > 0 ? r.at[nt] - a.window : -1;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int j = token + 4 * t + x;
-            if (j > r.at[nt] || j <= from) s[nt][t][x] = -INFINITY;
-          }
-      }
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) m = fmaxf(m, s[nt][t][x]);
-      m = fmaxf(m, __shfl_xor(m, 16));
-      m = fmaxf(m, __shfl_xor(m, 32));
-      now[nt] = fmaxf(p.m[nt], m);
-      changed |= now[nt] != p.m[nt];
-    }
-    if (__any(changed)) {
-      float shrink = 1.0f;
-      if (scale_v > reference) {
-        shrink = reference / scale_v;
-        reference = scale_v;
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float alpha = now[nt] == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(p.m[nt] - now[nt]);
-        p.m[nt] = now[nt];
-        p.l[nt] *= alpha;
-        const float both = alpha * shrink;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; ++dt) p.o[nt][dt] *= both;
-      }
-    }
-    const float unit = scale_v * (kWeightUnit / reference);
+    // Weights of the page relative to its own largest one (in fp16, in units of 2^-14), the page relative to those before
     half8 w[NT][2];
+    float scale[NT], now[NT], sum[NT], beta[NT];
+    bool changed = false;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const float m = p.m[nt] == -INFINITY ? 0.0f : p.m[nt];
-      float sum = 0.0f;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const float y = __builtin_amdgcn_exp2f(s[nt][t][x] - m);
-          sum += y;
-          w[nt][t / 2][4 * (t % 2) + x] = (_Float16)(y * unit);
-          s[nt][t][x] = y;
-        }
-      if (masked && unit != unit) {  // a scale that is NaN reaches the rows that see the page, and no others
+      const float factor = scale_k * r.factor[nt];
+      if (masked) {
+        int to = r.at[nt] - token, from = a.window > 0 ? to - a.window : -1 - token;
+        asm volatile("" : "+v"(to), "+v"(from));  // (or the compiler computes all of it for every page)
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            if (s[nt][t][x] == 0.0f) w[nt][t / 2][4 * (t % 2) + x] = (_Float16)0.0f;
+            if (4 * t + x > to || 4 * t + x <= from) s[nt][t][x] = -INFINITY;
       }
-      p.l[nt] += sum;
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) top = fmaxf(top, s[nt][t][x]);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const bool sees = top != -INFINITY;
+      const float score = sees ? top * factor : -INFINITY, shift = kWeightBits - (sees ? score : 0.0f);
+      now[nt] = score > p.m[nt] + kSlack ? score : p.m[nt];
+      changed |= now[nt] != p.m[nt];
+      float times = factor;
+      if (__any(!(factor > 0.0f))) {  // a scale of K that is 0 or NaN: not to be multiplied with -infinity
+        const float value = factor > 0.0f ? 1.0f : factor;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (!(factor > 0.0f) && s[nt][t][x] != -INFINITY) s[nt][t][x] = value;
+        if (!(factor > 0.0f)) times = 1.0f;
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[nt][t][x] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nt][t][x], times, shift));
+      sum[nt] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          sum[nt] += s[nt][t][x];
+          w[nt][t / 2][4 * (t % 2) + x] = (_Float16)s[nt][t][x];
+        }
+      beta[nt] = sees ? __builtin_amdgcn_exp2f(score - now[nt]) : 0.0f;
+      scale[nt] = sees ? scale_v * (1.0f / kWeightUnit) * beta[nt] : 0.0f;  // (a scale that is NaN reaches the rows that see the page)
+    }
+    if (__any(changed)) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float alpha = p.m[nt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(p.m[nt] - now[nt]);
+        p.m[nt] = now[nt];
+        p.l[nt] *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) p.o[nt][dt] *= alpha;
+      }
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int nt = 0; nt < NT; ++nt) p.l[nt] = __builtin_fmaf(sum[nt], beta[nt], p.l[nt]);
+    // The product of a page is taken by itself and added with the scale of V: sums of pages whose scales are far apart keep what an
+    // fp32 sum keeps
 #pragma unroll
-      for (int dt = 0; dt < D / 16; ++dt) {
+    for (int dt = 0; dt < D / 16; ++dt) {
+      floatx4 page_o[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) page_o[nt] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
         const half8 val = operand_of<FMT>(c.v[dt][2 * u], c.v[dt][2 * u + 1]);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-          p.o[nt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[nt][u], p.o[nt][dt], 0, 0, 0);
+        for (int nt = 0; nt < NT; ++nt) page_o[nt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[nt][u], page_o[nt], 0, 0, 0);
       }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) p.o[nt][dt][x] = __builtin_fmaf(page_o[nt][x], scale[nt], p.o[nt][dt][x]);
+    }
     if (more) load_values<D>(block, c);
   }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     p.l[nt] += __shfl_xor(p.l[nt], 16);
     p.l[nt] += __shfl_xor(p.l[nt], 32);
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) p.o[nt][dt] *= reference * (1.0f / kWeightUnit);
+    p.l[nt] *= 1.0f / kWeightUnit;
   }
 }
 
@@ -328,23 +338,6 @@ __device__ __forceinline__ void store_partial(uint8_t* at, const Partial<D, NT>&
     ml[(NT + nt) * 64 + lane] = p.l[nt];
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) o[(nt * (D / 16) + dt) * 64 + lane] = p.o[nt][dt];
-  }
-}
-
-template <int D, int NT>
-__device__ __forceinline__ void merge_partial(const uint8_t* at, Partial<D, NT>& p) {
-  const int lane = threadIdx.x & 63;
-  const floatx4* const o = reinterpret_cast<const floatx4*>(at);
-  const float* const ml = reinterpret_cast<const float*>(at + kPartialVectors<D, NT> * 16);
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const float m2 = ml[nt * 64 + lane], l2 = ml[(NT + nt) * 64 + lane];
-    const float top = fmaxf(p.m[nt], m2), base = top == -INFINITY ? 0.0f : top;
-    const float f1 = __builtin_amdgcn_exp2f(p.m[nt] - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
-    p.m[nt] = top;
-    p.l[nt] = p.l[nt] * f1 + l2 * f2;
-#pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) p.o[nt][dt] = p.o[nt][dt] * f1 + o[(nt * (D / 16) + dt) * 64 + lane] * f2;
   }
 }
 
@@ -385,6 +378,45 @@ __device__ __forceinline__ void store_rows(const AttentionArgs& a, const KvEntry
   }
 }
 
+// 16 rows and 16 dims of the sum of partial results.
+struct Slice {
+  floatx4 o;
+  float m, l;
+};
+// The slice of `count` partial results, `at(i)` their addresses.  A wavefront's work: adding up is spread over the wavefronts
+// by slices.
+template <int D, int NT, typename F>
+__device__ __forceinline__ Slice add_partials(int count, int nt, int dt, F at) {
+  const int lane = threadIdx.x & 63;
+  auto ml = [&](int i) { return reinterpret_cast<const float*>(at(i) + kPartialVectors<D, NT> * 16) + nt * 64 + lane; };
+  Slice s{floatx4{0.0f, 0.0f, 0.0f, 0.0f}, -INFINITY, 0.0f};
+#pragma unroll 4
+  for (int i = 0; i < count; ++i) s.m = fmaxf(s.m, *ml(i));
+  const float base = s.m == -INFINITY ? 0.0f : s.m;
+#pragma unroll 4
+  for (int i = 0; i < count; ++i) {
+    const float f = __builtin_amdgcn_exp2f(*ml(i) - base);
+    s.l += ml(i)[NT * 64] * f;
+    s.o += reinterpret_cast<const floatx4*>(at(i))[(nt * (D / 16) + dt) * 64 + lane] * f;
+  }
+  return s;
+}
+template <int D, int NT>
+__device__ __forceinline__ void store_slice(const AttentionArgs& a, const KvEntry& e, int head, int tile, int nt, int dt, const Slice& s) {
+  const RowResult r = row_result(a, e, head, (tile * NT + nt) * 16 + (threadIdx.x & 15), D, s.m, s.l, dt == 0);
+  if (r.there) store_dims(a, r, dt, s.o);
+}
+template <int D, int NT>
+__device__ __forceinline__ void store_partial_slice(uint8_t* at, int nt, int dt, const Slice& s) {
+  const int lane = threadIdx.x & 63;
+  reinterpret_cast<floatx4*>(at)[(nt * (D / 16) + dt) * 64 + lane] = s.o;
+  if (dt == 0) {
+    float* const ml = reinterpret_cast<float*>(at + kPartialVectors<D, NT> * 16);
+    ml[nt * 64 + lane] = s.m;
+    ml[(NT + nt) * 64 + lane] = s.l;
+  }
+}
+
 // One workgroup per unit: its wavefronts take ranges of the pages and are joined in LDS.
 template <int D, int FMT, int NT>
 __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_unit_kernel(AttentionArgs a) {
@@ -400,12 +432,12 @@ __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_unit_kernel(Atten
   const int begin = min(all.begin + wave * each, all.end), end = min(begin + each, all.end);
   Partial<D, NT> p;
   accumulate<D, FMT, NT>(a, e, head, begin, end, r, p);
-  if (wave > 0) store_partial<D, NT>(lds + (wave - 1) * BYTES, p);
+  store_partial<D, NT>(lds + wave * BYTES, p);
   __syncthreads();
-  if (wave > 0) return;
-#pragma unroll 1
-  for (int at = 0; at < WAVES - 1; ++at) merge_partial<D, NT>(lds + at * BYTES, p);
-  store_rows<D, NT>(a, e, head, tile, p);
+  for (int slice = wave; slice < NT * D / 16; slice += WAVES) {
+    const int nt = slice / (D / 16), dt = slice % (D / 16);
+    store_slice<D, NT>(a, e, head, tile, nt, dt, add_partials<D, NT>(WAVES, nt, dt, [&](int i) { return lds + i * BYTES; }));
+  }
 }
 
 // ---- the work cut into equal parts ---------------------------------------------------------------------------------
@@ -416,18 +448,27 @@ __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_unit_kernel(Atten
 // A unit that lies inside one workgroup is finished there; one that is cut leaves a partial result per workgroup, which
 // join_kernel adds up in order.
 
-constexpr int kMostPlanned = 1024;  // batch entries
+constexpr int kMostPlanned = 512;        // batch entries
+constexpr int kMostPlannedPrompts = 256;  // (two workgroups share a compute unit's LDS)
 
+template <int MOST>
 struct Plan {
-  int before[kMostPlanned + 1];  // pages of all units of the entries before
+  int before[MOST + 1];  // pages of all units of the entries before
   int sums[16];
-  int left[8];  // of a wavefront whose part starts inside a unit: 1 if the unit ends in it, 2 if not
-  KvEntry entry[kMostPlanned];
+  // Of every wavefront: whether its part starts inside a unit (1: which ends in it, 2: which does not), and whether it ends
+  // inside one that starts in it; then that unit, or, of the first wavefront, the one that it starts in
+  struct {
+    int left, right, entry, head, tile;
+  } wave[9];
+  KvEntry entry[MOST];
 };
 
 struct CutArgs {
-  uint8_t* partials;  // [workgroup][2]: of a unit that began before the workgroup's part, of one that ends behind it
+  uint8_t* partials;   // [workgroup][2]: of a unit that began before the workgroup's part, of one that ends behind it
+  KvEntry* entries;    // [batch]
+  int32_t* before;     // [batch + 1]; what the first workgroup found
   int32_t workgroups, waves;
+  int32_t least;       // pages of a wavefront
 };
 
 // Pages that the units of an entry read: all of them the same ones.
@@ -440,8 +481,8 @@ __device__ __forceinline__ int tiles_of_entry(const AttentionArgs& a, const KvEn
 }
 
 // Fills the plan; all threads of the workgroup.  Returns the pages of all units.
-template <int THREADS>
-__device__ int make_plan(const AttentionArgs& a, int rows, Plan* plan) {
+template <int THREADS, int MOST>
+__device__ int make_plan(const AttentionArgs& a, int rows, Plan<MOST>* plan) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int carry = 0;
   for (int base = 0; base < a.v.batch; base += THREADS) {
@@ -481,119 +522,498 @@ struct Share {
 };
 __device__ __forceinline__ Share share_of(const CutArgs& c, int total) {
   Share s;
-  s.of_wave = max((total + c.workgroups * c.waves - 1) / (c.workgroups * c.waves), 1);
+  s.of_wave = max((total + c.workgroups * c.waves - 1) / (c.workgroups * c.waves), c.least);
   s.of_workgroup = s.of_wave * c.waves;
   return s;
+}
+
+// The batch entry that the page `at` of all belongs to: the last one that starts at or before it.
+template <int MOST>
+__device__ __forceinline__ int entry_of_page(const AttentionArgs& a, const Plan<MOST>& plan, int at) {
+  const int lane = threadIdx.x & 63;
+  int held = -1;
+  for (int base = 0; base < a.v.batch; base += 64) {
+    const uint64_t starts = __ballot(base + lane < a.v.batch && plan.before[min(base + lane, a.v.batch)] <= at);
+    held += __popcll(starts);
+    if (~starts) break;
+  }
+  return held;
+}
+// For the kernels that join partial results
+template <int THREADS, int MOST>
+__device__ __forceinline__ void keep_plan(const AttentionArgs& a, const CutArgs& c, const Plan<MOST>& plan) {
+  if (blockIdx.x) return;
+  for (int b = threadIdx.x; b <= a.v.batch; b += THREADS) {
+    c.before[b] = plan.before[b];
+    if (b < a.v.batch) c.entries[b] = plan.entry[b];
+  }
 }
 
 template <int D, int FMT, int NT>
 __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_cut_kernel(AttentionArgs a, CutArgs c) {
   extern __shared__ __align__(16) uint8_t lds[];
   constexpr int WAVES = kWaves<D, NT>, BYTES = kPartialBytes<D, NT>;
-  Plan& plan = *reinterpret_cast<Plan*>(lds + (WAVES - 1) * BYTES);
-  int* const left = plan.left;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Plan<kMostPlanned>& plan = *reinterpret_cast<Plan<kMostPlanned>*>(lds + 2 * WAVES * BYTES);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int total = make_plan<64 * WAVES>(a, 16 * NT, &plan);
   const Share share = share_of(c, total);
   const int from = (int)min((int64_t)blockIdx.x * share.of_workgroup, (int64_t)total);
   int at = min(from + wave * share.of_wave, total);
   const int to = min(at + share.of_wave, total);
   uint8_t* const partials = c.partials + (int64_t)blockIdx.x * 2 * BYTES;
-  int kind = 0;
-  enum { kNone, kFromBefore, kFromHere };  // (of a unit that this wavefront has to complete)
-  int open = kNone;
-  Partial<D, NT> p;
-  KvEntry e;
-  int head = 0, tile = 0;
+  keep_plan<64 * WAVES>(a, c, plan);
+  int left = 0, right = 0, held = 0, head = 0, tile = 0;
   while (at < to) {
-    int lo = 0, hi = a.v.batch;  // the last entry that starts at or before `at`
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      (plan.before[mid] <= at ? lo : hi) = mid;
-    }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    e = plan.entry[lo];
+    held = entry_of_page(a, plan, at);
+    const KvEntry e = plan.entry[held];
     const PageRange pages = pages_of_entry(a, e);
     const int each = pages.end - pages.begin, tiles = tiles_of_entry(a, e, 16 * NT);
-    const int unit = (at - plan.before[lo]) / each, first = (at - plan.before[lo]) - unit * each;
+    const int unit = (at - plan.before[held]) / each, first = (at - plan.before[held]) - unit * each;
     const int count = min(each - first, to - at);
     head = unit / tiles, tile = unit - head * tiles;
     Rows<D, NT> r;
     load_rows<D, NT>(a, e, head, tile, r);
+    Partial<D, NT> p;
     accumulate<D, FMT, NT>(a, e, head, pages.begin + first, pages.begin + first + count, r, p);
     at += count;
-    const bool begins = first == 0, ends = first + count == each;
-    if (begins && ends) {
+    const bool ends = first + count == each;
+    if (first == 0 && ends) {
       store_rows<D, NT>(a, e, head, tile, p);
-    } else if (begins) {
-      open = kFromHere;
-    } else if (wave > 0) {
-      store_partial<D, NT>(lds + (wave - 1) * BYTES, p);
-      kind = ends ? 1 : 2;
-    } else if (ends) {
-      store_partial<D, NT>(partials, p);
     } else {
-      open = kFromBefore;
+      store_partial<D, NT>(lds + (2 * wave + (first == 0)) * BYTES, p);
+      if (first == 0)
+        right = 1;
+      else
+        left = ends ? 1 : 2;
+      if (first == 0 || wave == 0) {  // (a part that starts inside a unit may end inside another: the first wavefront notes both)
+        auto& mine = plan.wave[first == 0 ? wave : WAVES];
+        mine.entry = held, mine.head = head, mine.tile = tile;
+      }
     }
   }
-  if ((threadIdx.x & 63) == 0) left[wave] = kind;
+  if (lane == 0) plan.wave[wave].left = left, plan.wave[wave].right = right;
   __syncthreads();
-  if (open == kNone) return;
-  bool ended = false;
-#pragma unroll 1
-  for (int w = wave + 1; w < WAVES && !ended && left[w]; ++w) {
-    merge_partial<D, NT>(lds + (w - 1) * BYTES, p);
-    ended = left[w] == 1;
+  // Every unit that is cut by the borders of wavefronts: from one that it starts in (or the workgroup's first) to one that it
+  // ends in (or the last)
+  const auto& flags = plan.wave[lane % WAVES];
+  const uint32_t all = (1u << WAVES) - 1, ending = __ballot(flags.left == 1) & all, going = __ballot(flags.left == 2) & all;
+  const uint32_t starting = __ballot(flags.right) & all;
+  for (uint32_t todo = starting << 1 | ((ending | going) & 1); todo; todo &= todo - 1) {
+    const int w = __builtin_ctz(todo) - 1;
+    const bool from_before = w < 0;
+    // wavefronts behind that continue the unit, until one that it ends in
+    const int next = w + 1 + (from_before && !(ending & 1));
+    const int run = __builtin_ctz(~(going >> next));
+    const bool here = from_before && (ending & 1), ended = here || (next + run < WAVES && (ending >> (next + run) & 1));
+    const int last = here ? 0 : next + run - 1 + ended;
+    const uint8_t* const start = lds + (from_before ? 0 : 2 * w + 1) * BYTES;
+    const int base = from_before ? 0 : w;
+    const auto& of = plan.wave[from_before ? WAVES : w];
+    for (int slice = wave; slice < NT * D / 16; slice += WAVES) {
+      const int nt = slice / (D / 16), dt = slice % (D / 16);
+      const Slice s = add_partials<D, NT>(last - base + 1, nt, dt, [&](int i) { return i ? lds + 2 * (base + i) * BYTES : start; });
+      if (!from_before && ended)
+        store_slice<D, NT>(a, plan.entry[of.entry], of.head, of.tile, nt, dt, s);
+      else
+        store_partial_slice<D, NT>(partials + (from_before ? 0 : BYTES), nt, dt, s);
+    }
   }
-  if (open == kFromBefore)
-    store_partial<D, NT>(partials, p);
-  else if (ended)
-    store_rows<D, NT>(a, e, head, tile, p);
-  else
-    store_partial<D, NT>(partials + BYTES, p);
 }
 
-// One workgroup per head and batch entry: adds up the partial results of its units that were cut, and stores zeros for an
-// entry without pages.  Wavefront w takes the dims 16 w + 0..15.
-template <int D, int NT>
-__global__ __launch_bounds__(4 * D) void join_kernel(AttentionArgs a, CutArgs c) {
+// Adds up the partial results of the units that were cut by the borders of workgroups, and stores zeros for entries without
+// pages.  Workgroup = (entry, head); PARTS = 1: wavefront w takes the dims 16 w + 0..15 and adds up its partial results one
+// after the other.  PARTS = 8, where a unit is cut into many: a workgroup takes 32 dims, eight wavefronts share the
+// partial results of 16 of them.
+template <int D, int NT, int PARTS>
+__global__ __launch_bounds__((PARTS == 1 ? 4 * D : 1024)) void join_kernel(AttentionArgs a, CutArgs c) {
   constexpr int BYTES = kPartialBytes<D, NT>;
-  __shared__ Plan plan;
-  const int total = make_plan<4 * D>(a, 16 * NT, &plan);
-  const Share share = share_of(c, total);
-  const int b = blockIdx.x, head = blockIdx.y, dt = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const KvEntry e = plan.entry[b];
+  __shared__ __align__(16) floatx4 part_o[PARTS == 1 ? 1 : 16 * 64];
+  __shared__ float part_m[PARTS == 1 ? 1 : 16 * 64], part_l[PARTS == 1 ? 1 : 16 * 64];
+  const int b = blockIdx.x, head = blockIdx.y, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int dt = PARTS == 1 ? wave : blockIdx.z * 2 + wave / PARTS, part = PARTS == 1 ? 0 : wave % PARTS;
+  const KvEntry e = c.entries[b];
+  const int before = c.before[b];
+  const Share share = share_of(c, c.before[a.v.batch]);
   const PageRange pages = pages_of_entry(a, e);
   const int each = pages.end - pages.begin, tiles = tiles_of_entry(a, e, 16 * NT);
   for (int tile = 0; tile < tiles; ++tile) {
-    const int start = plan.before[b] + (head * tiles + tile) * each;
+    const int start = before + (head * tiles + tile) * each;
     const int w0 = start / share.of_workgroup, w1 = (start + each - 1) / share.of_workgroup;
     if (each > 0 && w0 == w1) continue;
+    const int all = each > 0 ? w1 - w0 + 1 : 0, one = (all + PARTS - 1) / PARTS;
+    const int from = min(part * one, all), count = min(one, all - from);
+    auto at = [&](int i) { return c.partials + ((int64_t)(w0 + from + i) * 2 + (from + i == 0)) * BYTES; };
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float m = -INFINITY, l = 0.0f;
-      floatx4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (each > 0) {
-        auto ml_of = [&](int w) {
-          return reinterpret_cast<const float*>(c.partials + ((int64_t)w * 2 + (w == w0)) * BYTES + kPartialVectors<D, NT> * 16) + nt * 64 + lane;
-        };
-        auto o_of = [&](int w) {
-          return reinterpret_cast<const floatx4*>(c.partials + ((int64_t)w * 2 + (w == w0)) * BYTES) + (nt * (D / 16) + dt) * 64 + lane;
-        };
-#pragma unroll 8
-        for (int w = w0; w <= w1; ++w) m = fmaxf(m, *ml_of(w));
-        const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll 8
-        for (int w = w0; w <= w1; ++w) {
-          const float f = __builtin_amdgcn_exp2f(*ml_of(w) - base);
-          l += ml_of(w)[NT * 64] * f;
-          o += *o_of(w) * f;
+      Slice s = add_partials<D, NT>(count, nt, dt, at);
+      if constexpr (PARTS > 1) {
+        __syncthreads();
+        part_o[wave * 64 + lane] = s.o, part_m[wave * 64 + lane] = s.m, part_l[wave * 64 + lane] = s.l;
+        __syncthreads();
+        if (part) continue;
+        for (int x = 1; x < PARTS; ++x) {
+          const int y = (wave + x) * 64 + lane;
+          const float top = fmaxf(s.m, part_m[y]), base = top == -INFINITY ? 0.0f : top;
+          const float f1 = __builtin_amdgcn_exp2f(s.m - base), f2 = __builtin_amdgcn_exp2f(part_m[y] - base);
+          s.m = top;
+          s.l = s.l * f1 + part_l[y] * f2;
+          s.o = s.o * f1 + part_o[y] * f2;
         }
       }
-      const RowResult r = row_result(a, e, head, (tile * NT + nt) * 16 + (lane & 15), D, m, l, dt == 0);
-      if (r.there) store_dims(a, r, dt, o);
+      store_slice<D, NT>(a, e, head, tile, nt, dt, s);
     }
   }
+}
+
+// ---- many rows -----------------------------------------------------------------------------------------------------
+//
+// Four wavefronts of 32 query rows each share the pages: every page is converted to fp16 once, into LDS, and read from there
+// as matrix operands by all four.  While a page is multiplied, the next one is converted into the other half of the LDS
+// and the one after it is on its way from memory.  Keys and queries are multiplied as 32 x 32 x 16; with the bits 2
+// and 3 of a key's row exchanged the result is, lane by lane, the other operand of the product with the values.
+
+constexpr int kPromptRows = 128;  // of a workgroup
+
+template <int D>
+struct PromptTile {
+  static constexpr int KEY_PITCH = D * 2 + 16, VALUE_PITCH = kPage * 2 + 16;  // (rows of a column on different banks)
+  __align__(16) uint8_t keys[kPage * KEY_PITCH];
+  __align__(16) uint8_t values[D * VALUE_PITCH];
+};
+
+template <int D>
+constexpr int kPromptPartialBytes = kPromptRows * (D + 2) * 4;  // floatx4 [4 wavefronts][D / 8][64], then m and l [128]
+
+// Whole tiles: which (entry, tile, head) a workgroup is.  Tiles far down a prompt read the most pages: they come first, and the
+// second half of the workgroups that the GPU holds at once runs the other way, so that a compute unit gets a long and a short one.
+struct PromptUnit {
+  int b, tile, head;
+};
+__device__ __forceinline__ PromptUnit prompt_unit(const AttentionArgs& a, int tiles, int units, int x) {
+  constexpr int kRound = 256;
+  if (x / kRound % 2) x = min(x / kRound * kRound + kRound, units) - 1 - x % kRound;
+  PromptUnit u;
+  u.head = x % a.v.heads;
+  x /= a.v.heads;
+  u.b = x % a.v.batch;
+  u.tile = tiles - 1 - x / a.v.batch;
+  return u;
+}
+
+// What a lane of a prompt workgroup has accumulated: of row l % 32 of its wavefront the dims 32 x + 8 (r / 4) + 4 (l / 32) + r % 4.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+template <int D>
+struct PromptSums {
+  floatx16 o[D / 32];
+  float m, l;
+};
+
+// Pages [from, to) of a tile as far as its rows see them; all threads of the workgroup, the LDS free on entry and exit.
+template <int D, int FMT>
+__device__ __forceinline__ void attend_tile(const AttentionArgs& a, const KvEntry& e, int kv_head, int tile_number, int from_page, int to_page,
+                                            PromptTile<D>* tiles, PromptSums<D>& sums) {
+  constexpr int STEPS = D / 16, OT = D / 32, LOADS = D / 64;
+  const int count = e.n * a.group;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i32 = lane & 31, h = lane >> 5;
+  const int row0 = tile_number * kPromptRows, row = row0 + wave * 32 + i32;
+
+  // Pages of the workgroup, and rows of the wavefront
+  const int before = e.length - e.n;
+  const PageRange all = e.slot < 0 ? PageRange{0, 0} : pages_seen(a, before + row0 / a.group, before + min(row0 + kPromptRows - 1, count - 1) / a.group);
+  const int begin = max(all.begin, from_page), end = min(all.end, to_page);
+  const int wave_first = before + min(row0 + wave * 32, count - 1) / a.group, wave_last = before + min(row0 + wave * 32 + 31, count - 1) / a.group;
+  const bool wave_used = row0 + wave * 32 < count;
+
+  half8 q[STEPS];
+  float row_factor = a.scale * kLog2e;
+  const int at = before + min(row, count - 1) / a.group;
+  {
+    const int token = min(row, count - 1) / a.group, head = kv_head * a.group + min(row, count - 1) - token * a.group;
+    const uint16_t* const src = a.Q + (int64_t)(e.row0 + token) * a.q_stride + (int64_t)head * D + 8 * h;
+    u32x4 raw[STEPS];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) raw[s] = *reinterpret_cast<const u32x4*>(src + 16 * s);
+    row_factor *= bring_to_fp16<STEPS>(raw, q, a.bf16, 32, 32);
+  }
+
+  // 16 codes of the keys and of the values per thread and load; keys go to the row that has the bits 2 and 3 exchanged
+  auto exchanged = [](int row) { return (row & ~12) | (row & 4) << 1 | (row & 8) >> 1; };
+  u32x4 codes_k[LOADS], codes_v[LOADS];
+  int held_page = 0;
+  float held_k = 0.0f, held_v = 0.0f;
+  auto hold = [&](int page) {
+    held_page = max(kv_page(a.v, e.slot, min(page + lane, end - 1)), 0);
+    const float* const s = kv_scale(a.v, held_page, kv_head, 0);
+    held_k = s[0];
+    held_v = s[1];
+  };
+  auto request = [&](int page) {
+    const uint8_t* const block = kv_block<D>(a.v, __builtin_amdgcn_readlane(held_page, (page - begin) % 64), kv_head, 0);
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      codes_k[x] = *reinterpret_cast<const u32x4*>(block + x * 4096 + threadIdx.x * 16);
+      codes_v[x] = *reinterpret_cast<const u32x4*>(block + kPage * D + x * 4096 + threadIdx.x * 16);
+    }
+  };
+  auto convert = [&](int page, PromptTile<D>& tile) {
+#pragma unroll
+    for (int x = 0; x < LOADS; ++x) {
+      const int byte = x * 4096 + threadIdx.x * 16;
+      half8* const k = reinterpret_cast<half8*>(tile.keys + exchanged(byte / D) * PromptTile<D>::KEY_PITCH + byte % D * 2);
+      k[0] = operand_of<FMT>(codes_k[x][0], codes_k[x][1]);
+      k[1] = operand_of<FMT>(codes_k[x][2], codes_k[x][3]);
+      if (page * kPage + kPage > e.length) {  // tokens that were never written must not meet the weight 0 as a NaN
+        int written = e.length - (page * kPage + byte % kPage);
+        asm volatile("" : "+v"(written));
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int left = written - 4 * w;
+          codes_v[x][w] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+        }
+      }
+      half8* const v = reinterpret_cast<half8*>(tile.values + byte / kPage * PromptTile<D>::VALUE_PITCH + byte % kPage * 2);
+      v[0] = operand_of<FMT>(codes_v[x][0], codes_v[x][1]);
+      v[1] = operand_of<FMT>(codes_v[x][2], codes_v[x][3]);
+    }
+  };
+
+  floatx16 (&o)[OT] = sums.o;
+#pragma unroll
+  for (int x = 0; x < OT; ++x)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[x][r] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+  float next_k = 0.0f, next_v = 0.0f;
+  if (begin < end) {
+    hold(begin);
+    request(begin);
+    next_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_k), 0));
+    next_v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_v), 0));
+    convert(begin, tiles[0]);
+    if (begin + 1 < end) request(begin + 1);
+    __syncthreads();
+  }
+  for (int page = begin; page < end; ++page) {
+    const PromptTile<D>& tile = tiles[(page - begin) & 1];
+    const float scale_k = next_k, scale_v = next_v;
+    const bool skip = !wave_used || page * kPage > wave_last || (a.window > 0 && page * kPage + kPage - 1 <= wave_first - a.window);
+    floatx16 s[2];
+    if (!skip) {
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][r] = 0.0f;
+#pragma unroll
+      for (int x = 0; x < STEPS; ++x)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          const half8 k = *reinterpret_cast<const half8*>(tile.keys + (32 * kt + i32) * PromptTile<D>::KEY_PITCH + (16 * x + 8 * h) * 2);
+          s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[x], s[kt], 0, 0, 0);
+        }
+    }
+    if (page + 1 < end) {
+      const int ahead = (page + 1 - begin) % 64;
+      next_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_k), ahead));
+      next_v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_v), ahead));
+      convert(page + 1, tiles[(page + 1 - begin) & 1]);
+      if (page + 2 < end) {
+        if ((page + 2 - begin) % 64 == 0) hold(page + 2);
+        request(page + 2);
+      }
+    }
+    if (!skip) {
+      const float factor = scale_k * row_factor;
+      const bool masked = page * kPage + kPage - 1 > wave_first || (a.window > 0 && page * kPage <= wave_last - a.window);
+      // s[kt][8 u + j] is the key 32 kt + 16 u + 8 h + j
+      const int token = page * kPage + 8 * h;
+      if (masked) {
+        int to = at - token, from = a.window > 0 ? to - a.window : -1 - token;
+        asm volatile("" : "+v"(to), "+v"(from));  // (or the compiler computes all of it for every page)
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int j = 32 * kt + 16 * (r / 8) + r % 8;
+            if (j > to || j <= from) s[kt][r] = -INFINITY;
+          }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kt][r]);
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const bool sees = top != -INFINITY;
+      const float score = sees ? top * factor : -INFINITY, shift = kWeightBits - (sees ? score : 0.0f);
+      float times = factor;
+      if (__any(!(factor > 0.0f))) {  // a scale of K that is 0 or NaN: not to be multiplied with -infinity
+        const float value = factor > 0.0f ? 1.0f : factor;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (!(factor > 0.0f) && s[kt][r] != -INFINITY) s[kt][r] = value;
+        if (!(factor > 0.0f)) times = 1.0f;
+      }
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][r], times, shift));
+      // (the sums are kept relative to a score that the largest exceeds by no more than kSlack)
+      const float now = score > m + kSlack ? score : m;
+      if (__any(now != m)) {
+        const float alpha = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - now);
+        m = now;
+        l *= alpha;
+#pragma unroll
+        for (int x = 0; x < OT; ++x) o[x] *= alpha;
+      }
+      const float beta = sees ? __builtin_amdgcn_exp2f(score - now) : 0.0f;
+      const float scale = sees ? scale_v * (1.0f / kWeightUnit) * beta : 0.0f;  // (NaN: as above)
+      half8 w[4];
+      float sum = 0.0f;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          sum += s[kt][r];
+          w[2 * kt + r / 8][r % 8] = (_Float16)s[kt][r];
+        }
+      l = __builtin_fmaf(sum, beta, l);
+      // (the product of a page by itself, as above)
+#pragma unroll
+      for (int x = 0; x < OT; ++x) {
+        floatx16 page_o;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) page_o[r] = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const half8 v = *reinterpret_cast<const half8*>(tile.values + (32 * x + i32) * PromptTile<D>::VALUE_PITCH + (16 * u + 8 * h) * 2);
+          page_o = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[u], page_o, 0, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[x][r] = __builtin_fmaf(page_o[r], scale, o[x][r]);
+      }
+    }
+    __syncthreads();
+  }
+  l += __shfl_xor(l, 32);
+  sums.m = m;
+  sums.l = l * (1.0f / kWeightUnit);
+}
+
+// A row of a tile, and where the dims 4 (l / 32) ... of it go.
+__device__ __forceinline__ RowResult prompt_row(const AttentionArgs& a, const KvEntry& e, int kv_head, int tile, int D, float m, float l, bool with_lse) {
+  const int lane = threadIdx.x & 63, h = lane >> 5, row = tile * kPromptRows + (threadIdx.x >> 6) * 32 + (lane & 31);
+  RowResult r{row < e.n * a.group, nullptr, 0.0f};
+  if (!r.there) return r;
+  const int token = row / a.group, head = kv_head * a.group + row - token * a.group;
+  const bool empty = m == -INFINITY && l == 0.0f;
+  r.inverse = empty ? 0.0f : 1.0f / l;
+  r.dst = a.O + (int64_t)(e.row0 + token) * a.o_stride + (int64_t)head * D + 4 * h;
+  if (a.lse && with_lse && h == 0)
+    a.lse[(int64_t)(e.row0 + token) * a.q_heads + head] = empty ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  return r;
+}
+template <int D>
+__device__ __forceinline__ void store_tile(const AttentionArgs& a, const KvEntry& e, int kv_head, int tile, const PromptSums<D>& s) {
+  const RowResult r = prompt_row(a, e, kv_head, tile, D, s.m, s.l, true);
+  if (!r.there) return;
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)  // 8 dims and the two halves of them: in units of 16, as store_dims counts
+      store_dims(a, RowResult{true, r.dst + 32 * x + 8 * q, r.inverse}, 0, floatx4{s.o[x][4 * q], s.o[x][4 * q + 1], s.o[x][4 * q + 2], s.o[x][4 * q + 3]});
+}
+template <int D>
+__device__ __forceinline__ void store_tile_partial(uint8_t* to, const PromptSums<D>& s) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  floatx4* const po = reinterpret_cast<floatx4*>(to) + wave * (D / 8) * 64 + lane;
+#pragma unroll
+  for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      po[(4 * x + q) * 64] = floatx4{s.o[x][4 * q], s.o[x][4 * q + 1], s.o[x][4 * q + 2], s.o[x][4 * q + 3]};
+  float* const ml = reinterpret_cast<float*>(to + kPromptRows * D * 4) + wave * 32 + (lane & 31);
+  if (lane < 32) ml[0] = s.m, ml[kPromptRows] = s.l;
+}
+
+// One workgroup per tile.
+template <int D, int FMT>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_prompt_kernel(AttentionArgs a, int tiles, int units) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  const PromptUnit u = prompt_unit(a, tiles, units, blockIdx.x);
+  const KvEntry e = kv_entry(a.v, u.b);
+  if (u.tile * kPromptRows >= e.n * a.group) return;
+  PromptSums<D> s;
+  attend_tile<D, FMT>(a, e, u.head, u.tile, 0, a.max_pages, reinterpret_cast<PromptTile<D>*>(lds), s);
+  store_tile<D>(a, e, u.head, u.tile, s);
+}
+
+// The work cut into equal parts, as above: few tiles with many pages each.  (All tiles of an entry count as many pages; a tile skips
+// those behind its last row.)
+template <int D, int FMT>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_prompt_cut_kernel(AttentionArgs a, CutArgs c) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  Plan<kMostPlannedPrompts>& plan = *reinterpret_cast<Plan<kMostPlannedPrompts>*>(lds + 2 * sizeof(PromptTile<D>));
+  const int total = make_plan<256>(a, kPromptRows, &plan);
+  const Share share = share_of(c, total);
+  keep_plan<256>(a, c, plan);
+  int at = (int)min((int64_t)blockIdx.x * share.of_workgroup, (int64_t)total);
+  const int to = min(at + share.of_workgroup, total);
+  uint8_t* const partials = c.partials + (int64_t)blockIdx.x * 2 * kPromptPartialBytes<D>;
+  while (at < to) {
+    const int held = entry_of_page(a, plan, at);
+    const KvEntry e = plan.entry[held];
+    const PageRange pages = pages_of_entry(a, e);
+    const int each = pages.end - pages.begin, tiles = tiles_of_entry(a, e, kPromptRows);
+    const int unit = (at - plan.before[held]) / each, first = (at - plan.before[held]) - unit * each;
+    const int count = min(each - first, to - at), head = unit / tiles, tile = unit - head * tiles;
+    PromptSums<D> s;
+    attend_tile<D, FMT>(a, e, head, tile, pages.begin + first, pages.begin + first + count, reinterpret_cast<PromptTile<D>*>(lds), s);
+    at += count;
+    if (first == 0 && count == each)
+      store_tile<D>(a, e, head, tile, s);
+    else
+      store_tile_partial<D>(partials + (first == 0 ? kPromptPartialBytes<D> : 0), s);
+  }
+}
+
+// Adds up the partial results of the tiles that were cut, and stores zeros for entries without pages.  Lanes as above; a workgroup
+// takes 32 dims.
+template <int D>
+__global__ __launch_bounds__(256) void join_prompt_kernel(AttentionArgs a, CutArgs c) {
+  const int tile = blockIdx.x / (D / 32), x = blockIdx.x % (D / 32), head = blockIdx.y, b = blockIdx.z;
+  const KvEntry e = c.entries[b];
+  const int tiles = tiles_of_entry(a, e, kPromptRows);
+  if (tile >= tiles) return;
+  const Share share = share_of(c, c.before[a.v.batch]);
+  const PageRange pages = pages_of_entry(a, e);
+  const int each = pages.end - pages.begin, start = c.before[b] + (head * tiles + tile) * each;
+  const int w0 = start / share.of_workgroup, w1 = each ? (start + each - 1) / share.of_workgroup : w0 - 1;
+  if (w0 == w1) return;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  auto at = [&](int w) { return c.partials + ((int64_t)w * 2 + (w == w0)) * kPromptPartialBytes<D>; };
+  auto ml = [&](int w) { return reinterpret_cast<const float*>(at(w) + kPromptRows * D * 4) + wave * 32 + (lane & 31); };
+  float m = -INFINITY, l = 0.0f;
+#pragma unroll 4
+  for (int w = w0; w <= w1; ++w) m = fmaxf(m, *ml(w));
+  const float base = m == -INFINITY ? 0.0f : m;
+  floatx4 o[4];
+#pragma unroll
+  for (int q = 0; q < 4; ++q) o[q] = floatx4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+  for (int w = w0; w <= w1; ++w) {
+    const float f = __builtin_amdgcn_exp2f(*ml(w) - base);
+    l += ml(w)[kPromptRows] * f;
+    const floatx4* const po = reinterpret_cast<const floatx4*>(at(w)) + wave * (D / 8) * 64 + lane;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) o[q] += po[(4 * x + q) * 64] * f;
+  }
+  const RowResult r = prompt_row(a, e, head, tile, D, m, l, x == 0);
+  if (!r.there) return;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) store_dims(a, RowResult{true, r.dst + 32 * x + 8 * q, r.inverse}, 0, o[q]);
 }
 
 // ---- launches ------------------------------------------------------------------------------------------------------
@@ -603,7 +1023,7 @@ int launch_units(const AttentionArgs& a, int max_rows, hipStream_t stream) {
   const void* const fn = (const void*)attend_unit_kernel<D, FMT, NT>;
   if (int e = allow_full_lds(fn, "attend_unit_kernel")) return e;
   const int64_t tiles = ((int64_t)max_rows * a.group + 16 * NT - 1) / (16 * NT);
-  constexpr int threads = 64 * kWaves<D, NT>, lds = (kWaves<D, NT> - 1) * kPartialBytes<D, NT>;
+  constexpr int threads = 64 * kWaves<D, NT>, lds = kWaves<D, NT> * kPartialBytes<D, NT>;
   attend_unit_kernel<D, FMT, NT><<<dim3((uint32_t)tiles, a.v.heads, a.v.batch), threads, lds, stream>>>(a);
   return kv_launched("attend_unit_kernel");
 }
@@ -612,9 +1032,14 @@ template <int D, int FMT, int NT>
 int launch_cut(const AttentionArgs& a, const CutArgs& c, hipStream_t stream) {
   const void* const fn = (const void*)attend_cut_kernel<D, FMT, NT>;
   if (int e = allow_full_lds(fn, "attend_cut_kernel")) return e;
-  constexpr int threads = 64 * kWaves<D, NT>, lds = (kWaves<D, NT> - 1) * kPartialBytes<D, NT> + sizeof(Plan);
+  constexpr int threads = 64 * kWaves<D, NT>, lds = 2 * kWaves<D, NT> * kPartialBytes<D, NT> + (int)sizeof(Plan<kMostPlanned>);
+  static_assert(lds <= 160 * 1024, "LDS of a compute unit");
   attend_cut_kernel<D, FMT, NT><<<c.workgroups, threads, lds, stream>>>(a, c);
-  join_kernel<D, NT><<<dim3(a.v.batch, a.v.heads), 4 * D, 0, stream>>>(a, c);
+  // (with fewer units than a few, each is cut into many parts)
+  if ((int64_t)a.v.batch * a.v.heads * 8 <= c.workgroups)
+    join_kernel<D, NT, 8><<<dim3(a.v.batch, a.v.heads, D / 32), 1024, 0, stream>>>(a, c);
+  else
+    join_kernel<D, NT, 1><<<dim3(a.v.batch, a.v.heads), 4 * D, 0, stream>>>(a, c);
   return kv_launched("attend_cut_kernel");
 }
 
@@ -623,29 +1048,75 @@ struct AttentionForm {
   int nt;          // tiles of 16 rows that a unit holds
   int workgroups;  // 0: one per unit
   int waves;       // of one
-  int64_t partial_bytes;
+  bool may_cut;    // (with a window or without)
+  int64_t cut_bytes;
+  bool prompt;     // tiles of kPromptRows rows: then
+  int tiles, units;
+  int least;       // pages of a wavefront (of a prompt's workgroup)
 };
+
+// From this many rows of an entry and key/value head on, attend_prompt_kernel.
+constexpr int kPromptFrom = 64;
 
 int waves_of(int dim, int nt) { return dim * nt >= 256 ? 4 : 8; }
 
-AttentionForm choose_form(int dim, int heads, int group, int batch, int max_rows, int max_tokens) {
+AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows, int max_rows, int max_tokens, int window) {
   AttentionForm f{};
   const int64_t rows = (int64_t)max_rows * group;
+  if (rows > kPromptFrom) {
+    const int64_t most = (rows + kPromptRows - 1) / kPromptRows, pages = ((int64_t)max_tokens + kPage - 1) / kPage;
+    // workgroups with work: about the rows of all entries, and a part of a tile each
+    const int64_t busy = (((int64_t)all_rows * group) / kPromptRows + batch) * heads;
+    f.prompt = true;
+    f.tiles = (int)most;
+    f.units = (int)(most * batch * heads);
+    f.waves = 1;
+    f.least = 8;
+    const int slots = dim == 256 ? 256 : 512;
+    f.may_cut = busy < slots && batch <= kMostPlannedPrompts && pages > 16;
+    f.cut_bytes = (int64_t)slots * 2 * kPromptRows * (dim + 2) * 4;
+    if (f.may_cut) f.workgroups = slots;
+    return f;
+  }
+  f.least = 1;
   f.nt = dim < 256 && rows > 16 ? 2 : 1;
   f.waves = waves_of(dim, f.nt);
-  const int64_t tiles = (rows + 16 * f.nt - 1) / (16 * f.nt), units = tiles * heads * batch, pages = (max_tokens + kPage - 1) / kPage;
-  const int64_t alone = (units + 255) / 256 * ((pages + f.waves - 1) / f.waves);
-  const int64_t cut = (units * pages + 256 * f.waves - 1) / (256 * f.waves);
-  if (batch <= kMostPlanned && tiles <= 4 && alone > cut + 8) {
-    f.workgroups = 256;
-    f.partial_bytes = (int64_t)f.workgroups * 2 * (f.nt * (dim / 16) * 64 * 16 + 2 * f.nt * 64 * 4);
-  }
+  const int64_t all_pages = ((int64_t)max_tokens + kPage - 1) / kPage, seen = ((int64_t)window + max_rows) / kPage + 2;
+  const int64_t pages = window > 0 && seen < all_pages ? seen : all_pages;
+  const int64_t tiles = (rows + 16 * f.nt - 1) / (16 * f.nt), units = tiles * heads * batch;
+  // Pages that a wavefront reads one after the other where each unit has a workgroup, and where the work is cut into equal parts.
+  // Fitted to both forms over 1 to 200 sequences of 128 to 16384 tokens, of one length and of lengths down to a 16th: (4.3, 2.7),
+  // (10, 5.0) us with 128 dims, int8.  The first form waits for its longest unit, the second reads what there is: the host knows
+  // the longest sequence alone, and counts half of it for each.
+  const double cut = (double)((units * pages + 256 * f.waves - 1) / (256 * f.waves)) * (batch > 1 ? 0.5 : 1.0);
+  const double start = f.waves == 8 ? 10.0 : 14.0, of_parts = start + (dim == 64 ? 2.9 : 5.0) * cut;
+  auto of_units = [&](int64_t p) { return 4.3 + (dim == 64 ? 1.25 : 2.7) * (double)((units + 255) / 256 * ((p + f.waves - 1) / f.waves)); };
+  f.may_cut = batch <= kMostPlanned && tiles <= 4 && of_units(all_pages) > start;
+  f.cut_bytes = (int64_t)256 * 2 * (f.nt * (dim / 16) * 64 * 16 + 2 * f.nt * 64 * 4);
+  if (f.may_cut && of_parts < of_units(pages)) f.workgroups = 256;
   return f;
 }
 
 template <int D, int FMT>
+int launch_prompt(const AttentionArgs& a, const AttentionForm& f, const CutArgs& c, hipStream_t stream) {
+  constexpr int lds = 2 * (int)sizeof(PromptTile<D>), cut_lds = lds + (int)sizeof(Plan<kMostPlannedPrompts>);
+  static_assert((D == 256 ? 1 : 2) * cut_lds <= 160 * 1024, "LDS of a compute unit");
+  if (f.workgroups) {
+    if (int e = allow_full_lds((const void*)attend_prompt_cut_kernel<D, FMT>, "attend_prompt_cut_kernel")) return e;
+    attend_prompt_cut_kernel<D, FMT><<<c.workgroups, 256, cut_lds, stream>>>(a, c);
+    join_prompt_kernel<D><<<dim3(f.tiles * (D / 32), a.v.heads, a.v.batch), 256, 0, stream>>>(a, c);
+  } else {
+    if (int e = allow_full_lds((const void*)attend_prompt_kernel<D, FMT>, "attend_prompt_kernel")) return e;
+    attend_prompt_kernel<D, FMT><<<f.units, 256, lds, stream>>>(a, f.tiles, f.units);
+  }
+  return kv_launched("attend_prompt_kernel");
+}
+
+template <int D, int FMT>
 int launch_attention(const AttentionArgs& a, const AttentionForm& f, int max_rows, void* workspace, hipStream_t stream) {
-  const CutArgs c{(uint8_t*)workspace, f.workgroups, f.waves};
+  uint8_t* const entries = (uint8_t*)workspace + f.cut_bytes;
+  const CutArgs c{(uint8_t*)workspace, (KvEntry*)entries, (int32_t*)(entries + kMostPlanned * sizeof(KvEntry)), f.workgroups, f.waves, f.least};
+  if (f.prompt) return launch_prompt<D, FMT>(a, f, c, stream);
   if constexpr (D < 256)
     if (f.nt == 2) return f.workgroups ? launch_cut<D, FMT, 2>(a, c, stream) : launch_units<D, FMT, 2>(a, max_rows, stream);
   return f.workgroups ? launch_cut<D, FMT, 1>(a, c, stream) : launch_units<D, FMT, 1>(a, max_rows, stream);
@@ -668,8 +1139,8 @@ extern "C" int sfmp_kv_attention_workspace(const sfmp_kv_layout_t* layout, int32
   if ((tiles && pages > INT32_MAX / tiles) || (int64_t)batch * layout->kv_heads * pages * tiles > INT32_MAX) return SFMP_ERR_SHAPE;
   *bytes = 256;
   if (batch && max_rows) {
-    const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch, max_rows, max_tokens);
-    *bytes = round_up_256(f.partial_bytes + 1);
+    const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch, rows, max_rows, max_tokens, 0);
+    if (f.may_cut) *bytes = round_up_256(f.cut_bytes + kMostPlanned * (sizeof(KvEntry) + 4) + 4);
   }
   return SFMP_OK;
 }
@@ -705,7 +1176,7 @@ extern "C" int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, 
   a.bf16 = dtype == SFMP_TYPE_BF16;
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (batch->max_rows == 0) return SFMP_OK;
-  const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, a.group, batch->batch, batch->max_rows, max_tokens);
+  const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, a.group, batch->batch, batch->rows, batch->max_rows, max_tokens, window);
   auto with_dim = [&](auto fmt) {
     if (layout->head_dim == 64) return launch_attention<64, fmt()>(a, f, batch->max_rows, workspace_dev, stream);
     if (layout->head_dim == 128) return launch_attention<128, fmt()>(a, f, batch->max_rows, workspace_dev, stream);
