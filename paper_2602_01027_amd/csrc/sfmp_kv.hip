@@ -17,16 +17,39 @@ extern "C" int sfmp_kv_query(int32_t pages, int32_t kv_heads, int32_t head_dim, 
 
 namespace {
 
-// Quantises what a call writes into one (page, head, K or V).  Workgroup = 256 threads; thread = token tid / 4 of the page
-// and every fourth run of 8 dims, so that four threads read 64 contiguous bytes of a row.  The values (codes of a page
-// are transposed) go through LDS.
+// Rows and columns of 4 x 4 bytes exchanged: x[i] holds 4 tokens of dim i, then y[j] 4 dims of token j (and the other way).
+__device__ __forceinline__ void turn4(const uint32_t (&x)[4], uint32_t (&y)[4]) {
+  const uint32_t ab = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), cd = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u);
+  const uint32_t ef = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u), gh = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);
+  y[0] = __builtin_amdgcn_perm(cd, ab, 0x05040100u);
+  y[1] = __builtin_amdgcn_perm(cd, ab, 0x07060302u);
+  y[2] = __builtin_amdgcn_perm(gh, ef, 0x05040100u);
+  y[3] = __builtin_amdgcn_perm(gh, ef, 0x07060302u);
+}
+
+// Who does what in a workgroup of D threads for the keys or the values of one (page, head): with keys a thread has 8 dims of
+// every eighth token, so that a token is read and written by neighbours; with values 4 dims of 16 tokens, whose codes it
+// turns in registers: values of a page lie as [dim][token].
+template <int D>
+struct PagePart {
+  bool values;
+  int dim;    // first
+  int token;  // first
+  __device__ __forceinline__ PagePart() {
+    const int t = threadIdx.x;
+    values = blockIdx.z;
+    dim = values ? t % (D / 4) * 4 : t % (D / 8) * 8;
+    token = values ? t / (D / 4) * 16 : t / (D / 8);
+  }
+  __device__ __forceinline__ int key_token(int i) const { return token + 8 * i; }  // i < 8
+};
+
+// Quantises what a call writes into one (page, head).
 template <int D, int FMT>
-__global__ __launch_bounds__(256) void append_kernel(KvView v, const uint16_t* K, const uint16_t* V, int64_t k_stride,
-                                                     int64_t v_stride, bool bf16, int pages_per_entry) {
-  constexpr int RUNS = D / 32, PITCH = kPage + 4;
-  __shared__ uint32_t largest_of_wave[4];
-  __shared__ __align__(16) uint8_t tile[D * PITCH];
-  const int b = blockIdx.x / pages_per_entry, head = blockIdx.y, which = blockIdx.z;
+__global__ __launch_bounds__(D) void append_kernel(KvView v, const uint16_t* K, const uint16_t* V, int64_t k_stride,
+                                                       int64_t v_stride, bool bf16, int pages_per_entry) {
+  __shared__ uint32_t largest_of_wave[D / 64];
+  const int b = blockIdx.x / pages_per_entry, head = blockIdx.y;
   const KvEntry e = kv_entry(v, b);
   const int before = e.length - e.n, start = max(before, 0);  // (rows that would stand before token 0 are left out)
   const int place = start / kPage + blockIdx.x % pages_per_entry;
@@ -34,29 +57,44 @@ __global__ __launch_bounds__(256) void append_kernel(KvView v, const uint16_t* K
   const int page = kv_page(v, e.slot, place);
   if (page < 0) return;
   const int first = max(start - place * kPage, 0), end = min(e.length - place * kPage, kPage);  // new tokens of the page
+  const PagePart<D> part;
+  float* const scale_at = kv_scale(v, page, head, part.values);
+  const float held = first > 0 ? *scale_at : 0.0f;
 
-  const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
-  const bool fresh = token >= first && token < end;
-  uint16_t raw[RUNS][8];
+  const int64_t row = (int64_t)e.row0 + place * kPage - before;  // of token 0 of the page
+  uint32_t raw[32];  // keys: 8 times 8 dims; values: 16 times 4 dims
   uint32_t largest = 0;
-  if (fresh) {
-    const int64_t row = (int64_t)e.row0 + place * kPage + token - before;
-    const uint16_t* src = (which ? V + row * v_stride : K + row * k_stride) + (int64_t)head * D;
+  auto look = [&](uint32_t w) {
+    largest = max(largest, max(__float_as_uint(value_of(w & 0xFFFFu, bf16)) & 0x7FFFFFFFu, __float_as_uint(value_of(w >> 16, bf16)) & 0x7FFFFFFFu));
+  };
+  if (!part.values) {
+    const uint16_t* const src = K + row * k_stride + (int64_t)head * D + part.dim;
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i)
-      *reinterpret_cast<u32x4*>(raw[i]) = *reinterpret_cast<const u32x4*>(src + 8 * (quarter + 4 * i));
+    for (int i = 0; i < 8; ++i) {
+      const int token = part.key_token(i);
+      u32x4 w = {0, 0, 0, 0};
+      if (token >= first && token < end) w = *reinterpret_cast<const u32x4*>(src + token * k_stride);
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i)
+      for (int j = 0; j < 4; ++j) raw[4 * i + j] = w[j];
+    }
+  } else {
+    const uint16_t* const src = V + row * v_stride + (int64_t)head * D + part.dim;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) largest = max(largest, __float_as_uint(value_of(raw[i][j], bf16)) & 0x7FFFFFFFu);
+    for (int j = 0; j < 16; ++j) {
+      const int token = part.token + j;
+      u32x2 w = {0, 0};
+      if (token >= first && token < end) w = *reinterpret_cast<const u32x2*>(src + token * v_stride);
+      raw[2 * j] = w[0], raw[2 * j + 1] = w[1];
+    }
   }
+#pragma unroll
+  for (int i = 0; i < 32; ++i) look(raw[i]);
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, s));
   if ((threadIdx.x & 63) == 0) largest_of_wave[threadIdx.x >> 6] = largest;
-  float* const scale_at = kv_scale(v, page, head, which);
-  const float held = first > 0 ? *scale_at : 0.0f;
   __syncthreads();
-  largest = max(max(largest_of_wave[0], largest_of_wave[1]), max(largest_of_wave[2], largest_of_wave[3]));
+#pragma unroll
+  for (int w = 0; w < D / 64; ++w) largest = max(largest, largest_of_wave[w]);
   const float need = scale_for<FMT>(largest);
   // NaN in either stays
   const float scale = first == 0 || need != need ? need : need > held ? need : held;
@@ -65,22 +103,14 @@ __global__ __launch_bounds__(256) void append_kernel(KvView v, const uint16_t* K
   const float inverse = inverse_scale(scale);
   if (threadIdx.x == 0 && (first == 0 || scale != held)) *scale_at = scale;
 
-  uint8_t* const block = kv_block<D>(v, page, head, which);
-  uint32_t codes[RUNS][2];
-  if (fresh) {
+  uint8_t* const block = kv_block<D>(v, page, head, part.values);
+  auto encoded = [&](uint32_t a, uint32_t b) {  // 4 new values
+    const float s = inverse > 0.0f ? inverse : 0.0f;
+    float x[4] = {value_of(a & 0xFFFFu, bf16), value_of(a >> 16, bf16), value_of(b & 0xFFFFu, bf16), value_of(b >> 16, bf16)};
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i)
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        float x[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = inverse > 0.0f ? value_of(raw[i][4 * half + j], bf16) * inverse : 0.0f;
-        codes[i][half] = encode4<FMT>(x);
-      }
-  } else {
-#pragma unroll
-    for (int i = 0; i < RUNS; ++i) codes[i][0] = codes[i][1] = kZeroCode<FMT> * 0x01010101u;
-  }
+    for (int j = 0; j < 4; ++j) x[j] = s > 0.0f ? x[j] * s : 0.0f;
+    return encode4<FMT>(x);
+  };
   auto requantised = [&](uint32_t w) {
     float x[4];
     decode4<FMT>(w, x);
@@ -88,12 +118,13 @@ __global__ __launch_bounds__(256) void append_kernel(KvView v, const uint16_t* K
     for (int j = 0; j < 4; ++j) x[j] *= kept;
     return encode4<FMT>(x);
   };
-  if (which == 0) {  // [token][dim]
+  if (!part.values) {  // [token][dim]
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i) {
-      u32x2* const at = reinterpret_cast<u32x2*>(block + token * D + 8 * (quarter + 4 * i));
-      if (fresh || first == 0) {
-        *at = u32x2{codes[i][0], codes[i][1]};
+    for (int i = 0; i < 8; ++i) {
+      const int token = part.key_token(i);
+      u32x2* const at = reinterpret_cast<u32x2*>(block + token * D + part.dim);
+      if ((token >= first && token < end) || first == 0) {  // (codes of no value are those of zeros)
+        *at = u32x2{encoded(raw[4 * i], raw[4 * i + 1]), encoded(raw[4 * i + 2], raw[4 * i + 3])};
       } else if (grown && token < first) {
         const u32x2 w = *at;
         *at = u32x2{requantised(w[0]), requantised(w[1])};
@@ -101,37 +132,54 @@ __global__ __launch_bounds__(256) void append_kernel(KvView v, const uint16_t* K
     }
     return;
   }
-  // [dim][token]: the codes are turned in LDS, then laid over what the page holds
+  // [dim][token]
+  const int from = part.token;
+  if (from >= end && first > 0) return;
+  if (from + 16 <= first && !grown) return;
+  uint32_t turned[4][4];  // [dim][4 tokens each]
 #pragma unroll
-  for (int i = 0; i < RUNS; ++i)
+  for (int q = 0; q < 4; ++q) {
+    uint32_t x[4], y[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) tile[(8 * (quarter + 4 * i) + j) * PITCH + token] = codes[i][j >> 2] >> (8 * (j & 3));
-  __syncthreads();
-  for (int at = threadIdx.x * 4; at < D * kPage; at += 1024) {
-    const int dim = at / kPage, t = at % kPage;  // 4 tokens of a dim
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(tile + dim * PITCH + t);
-    if (first == 0) {
-      *reinterpret_cast<uint32_t*>(block + at) = w;
-    } else if (t + 4 > first ? t < end : grown) {
-      uint32_t old = *reinterpret_cast<const uint32_t*>(block + at), fresh_bytes = 0;
+    for (int j = 0; j < 4; ++j) x[j] = encoded(raw[2 * (4 * q + j)], raw[2 * (4 * q + j) + 1]);
+    turn4(x, y);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (t + j >= first && t + j < end) fresh_bytes |= 0xFFu << (8 * j);
-      uint32_t mix = old;
-      if (grown) {
-        uint32_t earlier = 0;
+    for (int d = 0; d < 4; ++d) turned[d][q] = y[d];
+  }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (t + j < first) earlier |= 0xFFu << (8 * j);
-        mix = (requantised(old) & earlier) | (old & ~earlier);
+  for (int d = 0; d < 4; ++d) {
+    uint8_t* const at = block + (part.dim + d) * kPage + from;
+    u32x4 w = {turned[d][0], turned[d][1], turned[d][2], turned[d][3]};
+    if (first > 0 && !grown && end - max(first, from) <= 2) {  // one or two tokens: what is there need not be read
+      for (int token = max(first, from); token < min(end, from + 16); ++token) {
+        const int j = token - from;
+        const uint32_t word = j < 8 ? (j < 4 ? w[0] : w[1]) : (j < 12 ? w[2] : w[3]);
+        at[j] = (uint8_t)(word >> (8 * (j & 3)));
       }
-      *reinterpret_cast<uint32_t*>(block + at) = (w & fresh_bytes) | (mix & ~fresh_bytes);
+      continue;
     }
+    if (first > 0 && (from < first || from + 16 > end)) {
+      const u32x4 old = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t fresh = 0, earlier = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int token = from + 4 * q + j;
+          if (token >= first && token < end) fresh |= 0xFFu << (8 * j);
+          if (token < first) earlier |= 0xFFu << (8 * j);
+        }
+        const uint32_t again = grown ? requantised(old[q]) : old[q];
+        w[q] = (w[q] & fresh) | (again & earlier) | (old[q] & ~(fresh | earlier));
+      }
+    }
+    *reinterpret_cast<u32x4*>(at) = w;
   }
 }
 
-// Reads back the part of a call that lies in one (page, head, K or V).  Thread = token tid / 4, as above; values of V are
-// turned in LDS first.
+// Reads back the part of a call that lies in one (page, head, K or V).  Workgroup = 256 threads; thread = token tid / 4 of the page
+// and every fourth run of 8 dims, so that four threads write 64 contiguous bytes of a row; values are turned in LDS first.
+// (Turned in registers, as they are written, 64 sequences' last pages took 11 us instead of 9.6.)
 template <int D, int FMT>
 __global__ __launch_bounds__(256) void gather_kernel(KvView v, const int32_t* first_of, void* K, void* V, int64_t k_stride,
                                                      int64_t v_stride, int dtype, int pages_per_entry) {
@@ -142,9 +190,11 @@ __global__ __launch_bounds__(256) void gather_kernel(KvView v, const int32_t* fi
   const int start = max(first_of[b], 0);
   const int place = start / kPage + blockIdx.x % pages_per_entry;
   if (e.n < 1 || (int64_t)place * kPage >= (int64_t)start + e.n) return;
+  // (the table's entry is asked for before the length is known)
+  const int listed = e.slot >= 0 && place < v.table_pages ? kv_page(v, e.slot, place) : -1;
   const int token = threadIdx.x >> 2, quarter = threadIdx.x & 3;
   const int64_t at = (int64_t)place * kPage + token;
-  const int page = e.slot >= 0 && (int64_t)place * kPage < e.length ? kv_page(v, e.slot, place) : -1;
+  const int page = (int64_t)place * kPage < e.length ? listed : -1;
   const float scale = page < 0 ? 0.0f : *kv_scale(v, page, head, which);
   uint32_t codes[RUNS][2];
   if (page >= 0) {
@@ -237,7 +287,7 @@ extern "C" int sfmp_kv_append(const sfmp_kv_layout_t* layout, int32_t layer, voi
   if (pages * v.batch > INT32_MAX) return SFMP_ERR_SHAPE;
   const dim3 grid((uint32_t)(pages * v.batch), v.heads, 2);
   for_kv_layout(layout, [&](auto d, auto fmt) {
-    append_kernel<d(), fmt()><<<grid, 256, 0, (hipStream_t)hip_stream>>>(v, (const uint16_t*)K_dev, (const uint16_t*)V_dev, k_stride,
+    append_kernel<d(), fmt()><<<grid, d(), 0, (hipStream_t)hip_stream>>>(v, (const uint16_t*)K_dev, (const uint16_t*)V_dev, k_stride,
                                                                          v_stride, dtype == SFMP_TYPE_BF16, (int)pages);
   });
   return kv_launched("append_kernel");
