@@ -668,11 +668,14 @@ __global__ __launch_bounds__((PARTS == 1 ? 4 * D : 1024)) void join_kernel(Atten
 // ---- many rows -----------------------------------------------------------------------------------------------------
 //
 // Four wavefronts of 32 query rows each share the pages: every page is converted to fp16 once, into LDS, and read from there
-// as matrix operands by all four.  While a page is multiplied, the next one is converted into the other half of the LDS
-// and the one after it is on its way from memory.  Keys and queries are multiplied as 32 x 32 x 16; with the bits 2
+// as matrix operands by all four.  While a page is multiplied, the next one is converted into another part of the LDS
+// and the one after it is on its way from memory.  Two such groups in a workgroup take every other page of the same rows and
+// are added up at the end: on every SIMD one wavefront multiplies while the other takes exponentials.  Keys and queries are multiplied as 32 x 32 x 16; with the bits 2
 // and 3 of a key's row exchanged the result is, lane by lane, the other operand of the product with the values.
 
 constexpr int kPromptRows = 128;  // of a workgroup
+template <int D>
+constexpr int kGroups = D == 256 ? 1 : 2;  // (256 dims: LDS for one)
 
 template <int D>
 struct PromptTile {
@@ -684,14 +687,13 @@ struct PromptTile {
 template <int D>
 constexpr int kPromptPartialBytes = kPromptRows * (D + 2) * 4;  // floatx4 [4 wavefronts][D / 8][64], then m and l [128]
 
-// Whole tiles: which (entry, tile, head) a workgroup is.  Tiles far down a prompt read the most pages: they come first, and the
-// second half of the workgroups that the GPU holds at once runs the other way, so that a compute unit gets a long and a short one.
+// Whole tiles: which (entry, tile, head) a workgroup is.  Tiles far down a prompt read the most pages: they come first, so that the
+// short ones fill up what the long ones leave.  The heads of a tile are neighbours: on the XCDs in turn, each XCD's L2 holds
+// the pages of its heads.
 struct PromptUnit {
   int b, tile, head;
 };
-__device__ __forceinline__ PromptUnit prompt_unit(const AttentionArgs& a, int tiles, int units, int x) {
-  constexpr int kRound = 256;
-  if (x / kRound % 2) x = min(x / kRound * kRound + kRound, units) - 1 - x % kRound;
+__device__ __forceinline__ PromptUnit prompt_unit(const AttentionArgs& a, int tiles, int x) {
   PromptUnit u;
   u.head = x % a.v.heads;
   x /= a.v.heads;
@@ -708,13 +710,15 @@ struct PromptSums {
   float m, l;
 };
 
-// Pages [from, to) of a tile as far as its rows see them; all threads of the workgroup, the LDS free on entry and exit.
-template <int D, int FMT>
+// Pages [from, to) of a tile as far as its rows see them; all threads of the workgroup, the LDS free on entry and exit.  The sums are
+// left with the first 256 threads.
+template <int D, int FMT, int GROUPS>
 __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const KvEntry& e, int kv_head, int tile_number, int from_page, int to_page,
                                             PromptTile<D>* tiles, PromptSums<D>& sums) {
-  constexpr int STEPS = D / 16, OT = D / 32, LOADS = D / 64;
+  constexpr int STEPS = D / 16, OT = D / 32, LOADS = D / 32;
   const int count = e.n * a.group;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, i32 = lane & 31, h = lane >> 5;
+  const int group = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8), tid = threadIdx.x & 255;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = threadIdx.x & 63, i32 = lane & 31, h = lane >> 5;
   const int row0 = tile_number * kPromptRows, row = row0 + wave * 32 + i32;
 
   // Pages of the workgroup, and rows of the wavefront
@@ -736,9 +740,10 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const KvEntr
     row_factor *= bring_to_fp16<STEPS>(raw, q, a.bf16, 32, 32);
   }
 
-  // 16 codes of the keys and of the values per thread and load; keys go to the row that has the bits 2 and 3 exchanged
+  // 8 codes of the keys and of the values per thread and load, so that neighbours write 16 contiguous bytes each; keys go to the
+  // row that has the bits 2 and 3 exchanged
   auto exchanged = [](int row) { return (row & ~12) | (row & 4) << 1 | (row & 8) >> 1; };
-  u32x4 codes_k[LOADS], codes_v[LOADS];
+  u32x2 codes_k[LOADS], codes_v[LOADS];
   int held_page = 0;
   float held_k = 0.0f, held_v = 0.0f;
   auto hold = [&](int page) {
@@ -751,29 +756,27 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const KvEntr
     const uint8_t* const block = kv_block<D>(a.v, __builtin_amdgcn_readlane(held_page, (page - begin) % 64), kv_head, 0);
 #pragma unroll
     for (int x = 0; x < LOADS; ++x) {
-      codes_k[x] = *reinterpret_cast<const u32x4*>(block + x * 4096 + threadIdx.x * 16);
-      codes_v[x] = *reinterpret_cast<const u32x4*>(block + kPage * D + x * 4096 + threadIdx.x * 16);
+      codes_k[x] = *reinterpret_cast<const u32x2*>(block + x * 2048 + tid * 8);
+      codes_v[x] = *reinterpret_cast<const u32x2*>(block + kPage * D + x * 2048 + tid * 8);
     }
   };
   auto convert = [&](int page, PromptTile<D>& tile) {
+    if (page * kPage + kPage > e.length) {  // tokens that were never written must not meet the weight 0 as a NaN
+      int written = e.length - (page * kPage + tid * 8 % kPage);
+      asm volatile("" : "+v"(written));
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        const int left = written - 4 * w;
+        const uint32_t keep = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+#pragma unroll
+        for (int x = 0; x < LOADS; ++x) codes_v[x][w] &= keep;
+      }
+    }
 #pragma unroll
     for (int x = 0; x < LOADS; ++x) {
-      const int byte = x * 4096 + threadIdx.x * 16;
-      half8* const k = reinterpret_cast<half8*>(tile.keys + exchanged(byte / D) * PromptTile<D>::KEY_PITCH + byte % D * 2);
-      k[0] = operand_of<FMT>(codes_k[x][0], codes_k[x][1]);
-      k[1] = operand_of<FMT>(codes_k[x][2], codes_k[x][3]);
-      if (page * kPage + kPage > e.length) {  // tokens that were never written must not meet the weight 0 as a NaN
-        int written = e.length - (page * kPage + byte % kPage);
-        asm volatile("" : "+v"(written));
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int left = written - 4 * w;
-          codes_v[x][w] &= left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
-        }
-      }
-      half8* const v = reinterpret_cast<half8*>(tile.values + byte / kPage * PromptTile<D>::VALUE_PITCH + byte % kPage * 2);
-      v[0] = operand_of<FMT>(codes_v[x][0], codes_v[x][1]);
-      v[1] = operand_of<FMT>(codes_v[x][2], codes_v[x][3]);
+      const int byte = x * 2048 + tid * 8;
+      *reinterpret_cast<half8*>(tile.keys + exchanged(byte / D) * PromptTile<D>::KEY_PITCH + byte % D * 2) = operand_of<FMT>(codes_k[x][0], codes_k[x][1]);
+      *reinterpret_cast<half8*>(tile.values + byte / kPage * PromptTile<D>::VALUE_PITCH + byte % kPage * 2) = operand_of<FMT>(codes_v[x][0], codes_v[x][1]);
     }
   };
 
@@ -784,19 +787,24 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const KvEntr
     for (int r = 0; r < 16; ++r) o[x][r] = 0.0f;
   float m = -INFINITY, l = 0.0f;
   float next_k = 0.0f, next_v = 0.0f;
-  if (begin < end) {
-    hold(begin);
-    request(begin);
-    next_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_k), 0));
-    next_v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_v), 0));
-    convert(begin, tiles[0]);
-    if (begin + 1 < end) request(begin + 1);
-    __syncthreads();
+  tiles += 2 * group;
+  auto scales_of = [&](int page) {
+    next_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_k), (page - begin) % 64));
+    next_v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_v), (page - begin) % 64));
+  };
+  if (begin < end) hold(begin);
+  if (begin + group < end) {
+    request(begin + group);
+    scales_of(begin + group);
+    convert(begin + group, tiles[0]);
+    if (begin + group + GROUPS < end) request(begin + group + GROUPS);
   }
-  for (int page = begin; page < end; ++page) {
-    const PromptTile<D>& tile = tiles[(page - begin) & 1];
+  __syncthreads();
+  for (int step = 0; begin + step * GROUPS < end; ++step) {
+    const int page = begin + group + step * GROUPS;
+    const PromptTile<D>& tile = tiles[step & 1];
     const float scale_k = next_k, scale_v = next_v;
-    const bool skip = !wave_used || page * kPage > wave_last || (a.window > 0 && page * kPage + kPage - 1 <= wave_first - a.window);
+    const bool skip = page >= end || !wave_used || page * kPage > wave_last || (a.window > 0 && page * kPage + kPage - 1 <= wave_first - a.window);
     floatx16 s[2];
     if (!skip) {
 #pragma unroll
@@ -811,14 +819,13 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const KvEntr
           s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[x], s[kt], 0, 0, 0);
         }
     }
-    if (page + 1 < end) {
-      const int ahead = (page + 1 - begin) % 64;
-      next_k = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_k), ahead));
-      next_v = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(held_v), ahead));
-      convert(page + 1, tiles[(page + 1 - begin) & 1]);
-      if (page + 2 < end) {
-        if ((page + 2 - begin) % 64 == 0) hold(page + 2);
-        request(page + 2);
+    if (page + GROUPS < end) {
+      scales_of(page + GROUPS);
+      convert(page + GROUPS, tiles[(step + 1) & 1]);
+      const int ahead = page + 2 * GROUPS;
+      if (ahead < end) {
+        if ((ahead - begin) % 64 < GROUPS) hold(ahead - group);
+        request(ahead);
       }
     }
     if (!skip) {
@@ -898,8 +905,36 @@ __device__ __forceinline__ void attend_tile(const AttentionArgs& a, const KvEntr
     __syncthreads();
   }
   l += __shfl_xor(l, 32);
+  l *= 1.0f / kWeightUnit;
+  if constexpr (GROUPS == 2) {
+    floatx4* const other_o = reinterpret_cast<floatx4*>(tiles - 2 * group) + wave * (D / 8) * 64 + lane;
+    float* const other_ml = reinterpret_cast<float*>(tiles - 2 * group) + kPromptRows * D + tid;
+    if (group == 1) {
+#pragma unroll
+      for (int x = 0; x < OT; ++x)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) other_o[(4 * x + q) * 64] = floatx4{o[x][4 * q], o[x][4 * q + 1], o[x][4 * q + 2], o[x][4 * q + 3]};
+      other_ml[0] = m, other_ml[256] = l;
+    }
+    __syncthreads();
+    if (group == 0) {
+      const float m2 = other_ml[0], top = fmaxf(m, m2), base = top == -INFINITY ? 0.0f : top;
+      const float f1 = __builtin_amdgcn_exp2f(m - base), f2 = __builtin_amdgcn_exp2f(m2 - base);
+      m = top;
+      l = l * f1 + other_ml[256] * f2;
+#pragma unroll
+      for (int x = 0; x < OT; ++x)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const floatx4 y = other_o[(4 * x + q) * 64];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[x][4 * q + j] = o[x][4 * q + j] * f1 + y[j] * f2;
+        }
+    }
+    __syncthreads();
+  }
   sums.m = m;
-  sums.l = l * (1.0f / kWeightUnit);
+  sums.l = l;
 }
 
 // A row of a tile, and where the dims 4 (l / 32) ... of it go.
@@ -940,14 +975,14 @@ __device__ __forceinline__ void store_tile_partial(uint8_t* to, const PromptSums
 
 // One workgroup per tile.
 template <int D, int FMT>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_prompt_kernel(AttentionArgs a, int tiles, int units) {
+__global__ __launch_bounds__((256 * kGroups<D>)) void attend_prompt_kernel(AttentionArgs a, int tiles) {
   extern __shared__ __align__(16) uint8_t lds[];
-  const PromptUnit u = prompt_unit(a, tiles, units, blockIdx.x);
+  const PromptUnit u = prompt_unit(a, tiles, blockIdx.x);
   const KvEntry e = kv_entry(a.v, u.b);
   if (u.tile * kPromptRows >= e.n * a.group) return;
   PromptSums<D> s;
-  attend_tile<D, FMT>(a, e, u.head, u.tile, 0, a.max_pages, reinterpret_cast<PromptTile<D>*>(lds), s);
-  store_tile<D>(a, e, u.head, u.tile, s);
+  attend_tile<D, FMT, kGroups<D>>(a, e, u.head, u.tile, 0, a.max_pages, reinterpret_cast<PromptTile<D>*>(lds), s);
+  if (threadIdx.x < 256) store_tile<D>(a, e, u.head, u.tile, s);
 }
 
 // The work cut into equal parts, as above: few tiles with many pages each.  (All tiles of an entry count as many pages; a tile skips
@@ -970,7 +1005,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_prompt_cut_kerne
     const int unit = (at - plan.before[held]) / each, first = (at - plan.before[held]) - unit * each;
     const int count = min(each - first, to - at), head = unit / tiles, tile = unit - head * tiles;
     PromptSums<D> s;
-    attend_tile<D, FMT>(a, e, head, tile, pages.begin + first, pages.begin + first + count, reinterpret_cast<PromptTile<D>*>(lds), s);
+    attend_tile<D, FMT, 1>(a, e, head, tile, pages.begin + first, pages.begin + first + count, reinterpret_cast<PromptTile<D>*>(lds), s);
     at += count;
     if (first == 0 && count == each)
       store_tile<D>(a, e, head, tile, s);
@@ -1073,7 +1108,7 @@ AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows
     f.waves = 1;
     f.least = 8;
     const int slots = dim == 256 ? 256 : 512;
-    f.may_cut = busy < slots && batch <= kMostPlannedPrompts && pages > 16;
+    f.may_cut = busy < 512 && batch <= kMostPlannedPrompts && pages > 16;
     f.cut_bytes = (int64_t)slots * 2 * kPromptRows * (dim + 2) * 4;
     if (f.may_cut) f.workgroups = slots;
     return f;
@@ -1099,15 +1134,16 @@ AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows
 
 template <int D, int FMT>
 int launch_prompt(const AttentionArgs& a, const AttentionForm& f, const CutArgs& c, hipStream_t stream) {
-  constexpr int lds = 2 * (int)sizeof(PromptTile<D>), cut_lds = lds + (int)sizeof(Plan<kMostPlannedPrompts>);
-  static_assert((D == 256 ? 1 : 2) * cut_lds <= 160 * 1024, "LDS of a compute unit");
+  constexpr int threads = 256 * kGroups<D>, lds = 2 * kGroups<D> * (int)sizeof(PromptTile<D>);
+  constexpr int cut_lds = 2 * (int)sizeof(PromptTile<D>) + (int)sizeof(Plan<kMostPlannedPrompts>);
+  static_assert((D == 256 ? 1 : 2) * cut_lds <= 160 * 1024 && kPromptRows * D * 4 + 2048 <= lds, "LDS of a compute unit");
   if (f.workgroups) {
     if (int e = allow_full_lds((const void*)attend_prompt_cut_kernel<D, FMT>, "attend_prompt_cut_kernel")) return e;
     attend_prompt_cut_kernel<D, FMT><<<c.workgroups, 256, cut_lds, stream>>>(a, c);
     join_prompt_kernel<D><<<dim3(f.tiles * (D / 32), a.v.heads, a.v.batch), 256, 0, stream>>>(a, c);
   } else {
     if (int e = allow_full_lds((const void*)attend_prompt_kernel<D, FMT>, "attend_prompt_kernel")) return e;
-    attend_prompt_kernel<D, FMT><<<f.units, 256, lds, stream>>>(a, f.tiles, f.units);
+    attend_prompt_kernel<D, FMT><<<f.units, threads, lds, stream>>>(a, f.tiles);
   }
   return kv_launched("attend_prompt_kernel");
 }
