@@ -399,7 +399,8 @@ int sfmp_kv_gather(const sfmp_kv_layout_t* layout, int32_t layer, const void* co
  * logarithm of the sum of w.  A row that sees no token (p < 0, an empty sequence) gets O = 0, lse = -infinity.  Scores,
  * softmax statistics and sums are held in fp32; products are taken on the matrix cores from exact fp16 values of the
  * codes and of Q (bf16: each row scaled by a power of two); the softmax weights are rounded to fp16 before the product
- * with V, which adds to a result about as much error as its own rounding to fp16.  max_tokens: at least the longest
+ * with V, relative to the largest of their row in the page (2^-11 of itself, for weights under 2^-28 of that largest one 2^-39 of
+ * it), which adds to a result less error than its own rounding to fp16.  max_tokens: at least the longest
  * sequence of the batch; tokens past it are not read.  The same call on the same inputs gives the same bits; a sequence's
  * result may differ in its last bits with the batch it is in (the work is cut by the whole batch).
  * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads, strides, max_tokens < 1, window < 0, scale not finite or not positive, or

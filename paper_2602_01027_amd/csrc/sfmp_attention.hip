@@ -1070,7 +1070,7 @@ int launch_cut(const AttentionArgs& a, const CutArgs& c, hipStream_t stream) {
   constexpr int threads = 64 * kWaves<D, NT>, lds = 2 * kWaves<D, NT> * kPartialBytes<D, NT> + (int)sizeof(Plan<kMostPlanned>);
   static_assert(lds <= 160 * 1024, "LDS of a compute unit");
   attend_cut_kernel<D, FMT, NT><<<c.workgroups, threads, lds, stream>>>(a, c);
-  // (with fewer units than a few, each is cut into many parts)
+  // (8 units of 65536 tokens 30.9 us against 36.0, 16 units 57.1 and 58.3, 32 the same, 64 of 16384 tokens 56.4 against 55.8)
   if ((int64_t)a.v.batch * a.v.heads * 8 <= c.workgroups)
     join_kernel<D, NT, 8><<<dim3(a.v.batch, a.v.heads, D / 32), 1024, 0, stream>>>(a, c);
   else
@@ -1097,28 +1097,44 @@ int waves_of(int dim, int nt) { return dim * nt >= 256 ? 4 : 8; }
 
 AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows, int max_rows, int max_tokens, int window) {
   AttentionForm f{};
-  const int64_t rows = (int64_t)max_rows * group;
-  if (rows > kPromptFrom) {
-    const int64_t most = (rows + kPromptRows - 1) / kPromptRows, pages = ((int64_t)max_tokens + kPage - 1) / kPage;
-    // workgroups with work: about the rows of all entries, and a part of a tile each
-    const int64_t busy = (((int64_t)all_rows * group) / kPromptRows + batch) * heads;
+  const int64_t rows = (int64_t)max_rows * group, all_pages = ((int64_t)max_tokens + kPage - 1) / kPage;
+  const int64_t seen = ((int64_t)window + max_rows) / kPage + 2, pages = window > 0 && seen < all_pages ? seen : all_pages;
+  f.nt = dim < 256 && rows > 16 ? 2 : 1;
+  const int64_t tiles = (rows + 16 * f.nt - 1) / (16 * f.nt), units = tiles * heads * batch;
+  // Tiles of 128 rows for more than 64 (a page is converted once for all of them), but not where every small tile finds a compute
+  // unit and reads few pages.  Small against large tiles, us: 68 rows, 8 heads of 128 dims, one sequence of 512 tokens 10.2 and 15.9,
+  // of 1024 13.9 and 18.3, of 2048 23.6 and 20.8; 64 sequences of 512 tokens 56 and 34; 65 rows, 16 heads of 64 dims, 2048 tokens
+  // 12.5 and 17.7; 100 rows, 4 heads of 256 dims, 2048 tokens 28.6 and 31.6, of 4096 49 and 36.
+  if (rows > kPromptFrom && (units > 256 || all_pages > (dim == 64 ? 64 : dim == 128 ? 16 : 32))) {
+    const int64_t most = (rows + kPromptRows - 1) / kPromptRows;
     f.prompt = true;
     f.tiles = (int)most;
     f.units = (int)(most * batch * heads);
     f.waves = 1;
-    f.least = 8;
+    // Time (us) of a workgroup for each tile and of equal parts, fitted to 1 to 64 sequences of 512 to 32768 tokens, 64 to 2048 of
+    // them new, of one length and of lengths down to an eighth.  The host knows the rows of all entries, and the longest alone: the
+    // first form waits for it, the second reads what there is, and 0.6 of it is counted for each.  A tile ends at its last row, which
+    // only helps the first form, and only where other tiles wait.
     const int slots = dim == 256 ? 256 : 512;
-    f.may_cut = busy < 512 && batch <= kMostPlannedPrompts && pages > 16;
+    const double tiles_used = batch == 1 ? (double)most * heads : ((double)all_rows * group / kPromptRows + 0.5 * batch) * heads;
+    const double whole_start = dim == 64 ? 6.5 : dim == 128 ? 9.0 : 9.5, whole_page = dim == 64 ? 0.78 : dim == 128 ? 1.09 : 3.9;
+    const double cut_start = dim == 64 ? 10.0 : dim == 128 ? 14.0 : 18.0, cut_page = dim == 64 ? 1.9 : dim == 128 ? 2.7 : 4.0;
+    // (least: more parts to join against fewer workgroups with work: 17 tiles of 2048 tokens 23.7 us with 4 pages, 26.6 with 8, of
+    // 8192 tokens 40.8 and 35.3)
+    f.least = all_pages <= 64 ? 4 : 8;
+    auto cut_is_faster = [&](int64_t p) {
+      const double each = (batch > 1 ? 0.6 : 1.0) * tiles_used * (double)p / slots;
+      const double cut = cut_start + cut_page * (each > f.least ? each : f.least);
+      const double whole = tiles_used > 256 ? whole_page * ((double)p - max_rows / (2.0 * kPage)) * (tiles_used / 256) : whole_page * (double)p;
+      return cut < whole_start + whole;
+    };
+    f.may_cut = tiles_used < 512 && batch <= kMostPlannedPrompts && cut_is_faster(all_pages);
+    if (f.may_cut && cut_is_faster(pages)) f.workgroups = slots;
     f.cut_bytes = (int64_t)slots * 2 * kPromptRows * (dim + 2) * 4;
-    if (f.may_cut) f.workgroups = slots;
     return f;
   }
   f.least = 1;
-  f.nt = dim < 256 && rows > 16 ? 2 : 1;
   f.waves = waves_of(dim, f.nt);
-  const int64_t all_pages = ((int64_t)max_tokens + kPage - 1) / kPage, seen = ((int64_t)window + max_rows) / kPage + 2;
-  const int64_t pages = window > 0 && seen < all_pages ? seen : all_pages;
-  const int64_t tiles = (rows + 16 * f.nt - 1) / (16 * f.nt), units = tiles * heads * batch;
   // Pages that a wavefront reads one after the other where each unit has a workgroup, and where the work is cut into equal parts.
   // Fitted to both forms over 1 to 200 sequences of 128 to 16384 tokens, of one length and of lengths down to a 16th: (4.3, 2.7),
   // (10, 5.0) us with 128 dims, int8.  The first form waits for its longest unit, the second reads what there is: the host knows

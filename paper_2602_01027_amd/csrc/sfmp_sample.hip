@@ -759,16 +759,19 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
 }
 
 int slices_of(int32_t rows, int32_t vocab) {
-  // slices of 4096 tokens or more, two thousand workgroups at most; 2^15 tokens at most
+  // slices of 4096 tokens or more, 512 workgroups at most (each adds a histogram of its own to the row's: 32 rows of 131072
+  // tokens 43.8 us, with 1024 workgroups 56.5, with 256 46.3); 2^15 tokens at most
   int64_t s = vocab / 4096;
-  if (s * rows > 2048) s = 2048 / rows;
+  if (s * rows > 512) s = 512 / rows;
   const int64_t least = ((int64_t)vocab + kMostSlice - 1) / kMostSlice;
   if (s < least) s = least;
   return (int)s;
 }
 
-// From this many rows on, one workgroup per row.
-constexpr int kWholeRows = 96;
+// One workgroup per row: its time grows with the vocabulary and hardly with the rows, that of four launches over slices with both.
+// One row of 8000 tokens 21.5 us against 28.7, of 32000 26.9 and 29.4, of 131072 58.5 and 29.0; 32 rows of 50257 tokens
+// 37.7 and 41.8, of 131072 62.9 and 43.8; 128 of them 80.1 and 82.0.
+bool whole_rows(int32_t rows, int32_t vocab) { return rows >= 110 || (int64_t)vocab * (110 - rows) < 4200000; }
 
 struct SampleWorkspace {
   int64_t max_at, mass_at, count_at, list_at, wanted_at, listed_at, bytes;
@@ -776,7 +779,7 @@ struct SampleWorkspace {
 SampleWorkspace sample_workspace(int32_t rows, int32_t vocab) {
   SampleWorkspace w{};
   w.bytes = 256;
-  if (rows == 0 || rows >= kWholeRows) return w;
+  if (rows == 0 || whole_rows(rows, vocab)) return w;
   w.count_at = round_up_256((int64_t)rows * kBins * 8);
   w.list_at = w.count_at + round_up_256((int64_t)rows * kBins * 4);
   w.wanted_at = w.list_at + round_up_256((int64_t)rows * kListed * sizeof(Listed));
@@ -788,7 +791,7 @@ SampleWorkspace sample_workspace(int32_t rows, int32_t vocab) {
 
 template <int T>
 int launch_sample(const SampleArgs& a, hipStream_t stream) {
-  if (a.rows >= kWholeRows) {
+  if (whole_rows(a.rows, a.vocab)) {
     if (int e = allow_full_lds((const void*)sample_row_kernel<T>, "sample_row_kernel")) return e;
     sample_row_kernel<T><<<a.rows, kPickThreads, sizeof(PickShared), stream>>>(a);
   } else {

@@ -251,6 +251,33 @@ def test_attention_without_slots_and_with_room_in_max_tokens():
     _attend("fp8", 64, 2, 2, "bfloat16", CHUNKS, slots=False, max_tokens=9000, apart=0)
 
 
+MANY = [(40, 40), (1, 130), (33, 64), (40, 65), (17, 128), (0, 100), (39, 129), (40, 300)] * 4
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,group,entries,max_tokens,window",
+                         [(2, 4, TOKENS, 20000, 0), (2, 4, TOKENS, 20000, 100), (8, 2, TOKENS, 60000, 0),      # parts of all pages, joined
+                          (2, 6, DRAFTS, 20000, 0), (8, 6, DRAFTS, 60000, 0), (2, 6, DRAFTS, 20000, 80),       # the same, tiles of 32 rows
+                          (4, 4, MANY, None, 0), (4, 4, MANY, None, 50),                                      # large tiles, one workgroup each
+                          (2, 4, CHUNKS, 9000, 0), (2, 4, CHUNKS, 9000, 90), (4, 4, MANY, 9000, 0)])          # parts of large tiles
+def test_attention_in_every_form(fmt, dim, heads, group, entries, max_tokens, window):
+    # how a call is cut depends on what its longest sequence may be: the same small sequences under any promise
+    _attend(fmt, dim, heads, group, "float16" if dim == 128 else "bfloat16", entries, window=window, max_tokens=max_tokens, seed=dim + heads)
+
+
+@pytest.mark.parametrize("max_tokens", [None, 9000])
+def test_attention_of_large_tiles_with_scales_far_apart(max_tokens):
+    # (values of 2^7 at most: a weight below 2^-28 of its page's largest is a multiple of 2^-39 of it, which the bound's last term
+    # covers for values up to 2^9)
+    def change(pool, tables, order):
+        rng = np.random.default_rng(6)
+        pool["scales"][..., 1] = 2.0 ** rng.choice([-120, -100, -60, -30, -12, 0], size=pool["scales"].shape[:3])
+        pool["scales"][:, ::5, :, 1] = 0.0
+        pool["scales"][:, 1::6, :, 0] = 0.0
+    _attend("int8", 128, 4, 4, "bfloat16", MANY, change=change, max_tokens=max_tokens, seed=78)
+
+
 @pytest.mark.parametrize("fmt", ["int8", "fp8"])
 @pytest.mark.parametrize("entries", [TOKENS, CHUNKS])
 def test_attention_with_scales_far_apart(fmt, entries):

@@ -98,6 +98,18 @@ def test_many_rows(dtype, rows, vocab, apart, offset):
     assert sure > 40 and np.array_equal(tokens, all_[:96])
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,vocab,apart,offset", [(1, 38183, 0, 0), (40, 100003, 1, 2), (64, 131072, 0, 0), (2, 1000003, 5, 1)])
+def test_slices_of_every_length(dtype, rows, vocab, apart, offset):
+    # few to many slices of a row, of 4096 to 32768 tokens
+    rng = np.random.default_rng(rows + vocab)
+    x = _logits(rng, rows, vocab)
+    t, k = rng.choice([0.0, 0.6, 1.0, 2.0], rows), rng.choice([0, 1, 50, 2000], rows)
+    p, m, u = rng.choice([0.2, 0.95, 1.0], rows), rng.choice([0.0, 0.03], rows), rng.random(rows)
+    sure, _ = _check(x, t, k, p, m, u, dtype=dtype, apart=apart, offset=offset)
+    assert sure >= rows // 3
+
+
 @pytest.mark.parametrize("vocab", [2049, 100000])
 def test_many_rows_of_equal_logits(vocab):
     x = np.full((100, vocab), -1.5, dtype=np.float32)
