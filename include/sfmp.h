@@ -453,7 +453,8 @@ int sfmp_kv_compact(const sfmp_kv_layout_t* layout, void* codes_dev, float* scal
  * takes the first token of the order.  NaN logits count as -infinity; a row without a logit above -infinity gives -1
  * and the log-probability -infinity.  Sums of weights are whole numbers: the result does not depend on how the row was cut.
  * temperature, top_k, top_p, min_p: fp32 / int32 / fp32 / fp32 [rows], each may be NULL (1, all, all, all).  tokens: int32
- * [rows].  logprobs: NULL, or fp32 [rows], ln of w_token over the sum of all w of the row.
+ * [rows].  logprobs: NULL, or fp32 [rows], ln of w_token over the sum of all w of the row
+ * (0 with T <= 0, where the first token has all the weight).
  * SFMP_ERR_SHAPE: rows < 0, vocab < 1 or above 2^24, stride < vocab.  Alignment: logits to their element size. */
 int sfmp_sample_workspace(int32_t rows, int32_t vocab, int64_t* bytes);
 int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32_t vocab, int64_t stride,
