@@ -417,7 +417,8 @@ __device__ __forceinline__ void store_partial_slice(uint8_t* at, int nt, int dt,
   }
 }
 
-// One workgroup per unit: its wavefronts take ranges of the pages and are joined in LDS.
+// One workgroup per unit: its wavefronts take ranges of the pages and are joined in LDS.  One launch and the shortest chain of loads there
+// is (length, page number, codes): 8 heads of 128 dims, 500 tokens 7.0 us (the smallest kernels here take 2.3).
 template <int D, int FMT, int NT>
 __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_unit_kernel(AttentionArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -549,6 +550,8 @@ __device__ __forceinline__ void keep_plan(const AttentionArgs& a, const CutArgs&
   }
 }
 
+// Bound by HBM: 131071 tokens of 8 heads of 128 dims (268 MB) 51.5 us, 5.2 TB/s with start and end, 6.2 TB/s while it streams; 64 sequences of
+// 130 to 8190 tokens (261 MB, fp8) 56.6 us.  Requesting two pages ahead instead of one spilled registers and was slower.
 template <int D, int FMT, int NT>
 __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_cut_kernel(AttentionArgs a, CutArgs c) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -623,7 +626,7 @@ __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_cut_kernel(Attent
 // Adds up the partial results of the units that were cut by the borders of workgroups, and stores zeros for entries without
 // pages.  Workgroup = (entry, head); PARTS = 1: wavefront w takes the dims 16 w + 0..15 and adds up its partial results one
 // after the other.  PARTS = 8, where a unit is cut into many: a workgroup takes 32 dims, eight wavefronts share the
-// partial results of 16 of them.
+// partial results of 16 of them.  5.1 to 5.5 us (with one wavefront per 16 dims alone 10.4 for 131071 tokens).
 template <int D, int NT, int PARTS>
 __global__ __launch_bounds__((PARTS == 1 ? 4 * D : 1024)) void join_kernel(AttentionArgs a, CutArgs c) {
   constexpr int BYTES = kPartialBytes<D, NT>;
@@ -670,8 +673,13 @@ __global__ __launch_bounds__((PARTS == 1 ? 4 * D : 1024)) void join_kernel(Atten
 // Four wavefronts of 32 query rows each share the pages: every page is converted to fp16 once, into LDS, and read from there
 // as matrix operands by all four.  While a page is multiplied, the next one is converted into another part of the LDS
 // and the one after it is on its way from memory.  Two such groups in a workgroup take every other page of the same rows and
-// are added up at the end: on every SIMD one wavefront multiplies while the other takes exponentials.  Keys and queries are multiplied as 32 x 32 x 16; with the bits 2
-// and 3 of a key's row exchanged the result is, lane by lane, the other operand of the product with the values.
+// are added up at the end: on every SIMD one wavefront multiplies while the other takes exponentials.  Keys and queries are
+// multiplied as 32 x 32 x 16; with the bits 2 and 3 of a key's row exchanged the result is, lane by lane, the other operand of the product
+// with the values.
+//
+// 2048 rows of 32 heads over themselves, 8 key heads of 128 dims: 55 us, 617 TFLOP/s of products that count (with one group 59 us; a large
+// fp16 product of the library reaches 1110 here).  A step of two pages per SIMD takes 2.8 us: two fifths of it are matrix
+// instructions, the rest what the two wavefronts do not overlap of converting the next page, exponentials and LDS.
 
 constexpr int kPromptRows = 128;  // of a workgroup
 template <int D>
@@ -986,7 +994,8 @@ __global__ __launch_bounds__((256 * kGroups<D>)) void attend_prompt_kernel(Atten
 }
 
 // The work cut into equal parts, as above: few tiles with many pages each.  (All tiles of an entry count as many pages; a tile skips
-// those behind its last row.)
+// those behind its last row.)  6 chunks of 65 to 701 rows over 900 to 8001 tokens, 16 heads of 64 dims: 48 us, and 9 to join; one workgroup
+// for each tile takes 97, as long as the longest.  One group of wavefronts: with two, 57.
 template <int D, int FMT>
 __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_prompt_cut_kernel(AttentionArgs a, CutArgs c) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -1090,7 +1099,8 @@ struct AttentionForm {
   int least;       // pages of a wavefront (of a prompt's workgroup)
 };
 
-// From this many rows of an entry and key/value head on, attend_prompt_kernel.
+// With more rows of an entry and key/value head than these, attend_prompt_kernel (48 rows, 8 heads of 128 dims, us: one sequence of 512
+// tokens 10.3 against 15.9, of 8192 25.8 and 31.8, 8 of 2048 28.7 and 29.1; 64 of 2048 100 and 91).
 constexpr int kPromptFrom = 64;
 
 int waves_of(int dim, int nt) { return dim * nt >= 256 ? 4 : 8; }

@@ -44,7 +44,11 @@ struct PagePart {
   __device__ __forceinline__ int key_token(int i) const { return token + 8 * i; }  // i < 8
 };
 
-// Quantises what a call writes into one (page, head).
+// Quantises what a call writes into one (page, head): s = max |x| / 127 (or the power of two that brings it under 448), codes rint(x / s).
+// Tokens that the page held before keep their codes unless the scale grows: then they are read and rounded anew,
+// rint(code s_old / s_new).  Bound by latency at a token per sequence (length, page number, rows, maximum over the workgroup, one after
+// the other): 64 sequences, 8 heads of 128 dims 7.4 us, 2.1 MB of pages touched; a prompt of 2048 tokens 7.8 us, 12.6 MB.  One
+// workgroup for each K and V of a (page, head), so that the maximum needs no second launch.
 template <int D, int FMT>
 __global__ __launch_bounds__(D) void append_kernel(KvView v, const uint16_t* K, const uint16_t* V, int64_t k_stride,
                                                        int64_t v_stride, bool bf16, int pages_per_entry) {
@@ -179,7 +183,8 @@ __global__ __launch_bounds__(D) void append_kernel(KvView v, const uint16_t* K, 
 
 // Reads back the part of a call that lies in one (page, head, K or V).  Workgroup = 256 threads; thread = token tid / 4 of the page
 // and every fourth run of 8 dims, so that four threads write 64 contiguous bytes of a row; values are turned in LDS first.
-// (Turned in registers, as they are written, 64 sequences' last pages took 11 us instead of 9.6.)
+// (Turned in registers, as they are written, 64 sequences' last pages took 11 us instead of 9.6.)  Bound by latency, too: 64 last pages
+// 8.4 - 9.3 us, 2048 tokens of 8 heads of 128 dims 6.3 us for 12.6 MB.
 template <int D, int FMT>
 __global__ __launch_bounds__(256) void gather_kernel(KvView v, const int32_t* first_of, void* K, void* V, int64_t k_stride,
                                                      int64_t v_stride, int dtype, int pages_per_entry) {

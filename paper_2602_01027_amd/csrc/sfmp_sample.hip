@@ -148,7 +148,8 @@ __device__ __forceinline__ uint32_t falling_key(float l) {
 
 __device__ __forceinline__ int slice_from(const SampleArgs& a, int s) { return (int)((int64_t)a.vocab * s / a.slices); }
 
-// Largest logit of every slice; clears the histograms.
+// Largest logit of every slice; clears the histograms.  One row of 131072 fp16 tokens, 32 slices: 4.1 us, this and the next three bound by
+// latency (a launch, a few dependent loads, a few barriers each; the logits are 0.26 MB).
 template <int T>
 __global__ __launch_bounds__(kSliceThreads) void sample_max_kernel(SampleArgs a) {
   __shared__ float of_wave[kSliceThreads / 64];
@@ -172,7 +173,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_max_kernel(SampleArgs a)
 }
 
 // Adds a slice to the histogram of its row.  A bin of a slice is one 64-bit word in LDS: its count above bit 46, its
-// weight below (a slice has at most 2^15 tokens of at most 2^31).
+// weight below (a slice has at most 2^15 tokens of at most 2^31).  The same row: 6.2 us.
 constexpr int kCountBit = 46;
 constexpr int kMostSlice = 1 << 15;
 template <int T>
@@ -652,7 +653,8 @@ __device__ __forceinline__ void store_none(const SampleArgs& a, int r) {
 }
 
 // Slices: the tokens of the wanted bins into the row's list, with the sums before their bins; the workgroup of the first
-// slice leaves what the choice needs to know beside.
+// slice leaves what the choice needs to know beside.  Every workgroup adds up the row's histogram for itself (48 KiB from the L2, instead
+// of a launch for it): 8.7 us.
 template <int T>
 __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -679,7 +681,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArg
   });
 }
 
-// One workgroup per row: the choice.
+// One workgroup per row: the choice.  12 us: a chain of loads, a sort and some fifteen barriers.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -705,7 +707,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   store_choice(a, r, row, w, sh);
 }
 
-// One workgroup per row: everything.
+// One workgroup per row: everything.  256 rows of 100003 fp32 logits (102 MB) 78 us: 16 us for the maximum, which reads HBM at 6.4 TB/s,
+// 25 us for the histogram (some 20 instructions and two LDS atomics per logit: bound by the vector units), 16 us for collecting (the
+// row comes out of a cache by then), the rest latency.  Keeping a part of the row in registers between the passes was slower.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
