@@ -110,6 +110,19 @@ __device__ __forceinline__ float max_of_wave(float x) {
   return x;
 }
 
+// What a row is asked for.  Where an array is not given, another address is read in its place: without branches all five loads are
+// under way together, from the kernel's start.
+struct Asked {
+  float temperature, top_p, min_p, uniform;
+  int32_t top_k;
+};
+__device__ __forceinline__ Asked asked_of(const SampleArgs& a, int r) {
+  const float* const any = a.uniform + r;
+  const float t = *(a.temperature ? a.temperature + r : any), p = *(a.top_p ? a.top_p + r : any), q = *(a.min_p ? a.min_p + r : any);
+  const int32_t k = *(a.top_k ? a.top_k + r : reinterpret_cast<const int32_t*>(any));
+  return Asked{a.temperature ? t : 1.0f, a.top_p ? p : 1.0f, a.min_p ? q : 0.0f, *any, a.top_k ? k : 0};
+}
+
 // What the weights of a row are computed from.
 struct Row {
   const void* logits;
@@ -132,11 +145,10 @@ struct Row {
 };
 
 template <int T>
-__device__ __forceinline__ Row make_row(const SampleArgs& a, int r) {
+__device__ __forceinline__ Row make_row(const SampleArgs& a, int r, float t) {
   const int lane = threadIdx.x & 63;
   float m = -INFINITY;
   for (int s = lane; s < a.slices; s += 64) m = fmaxf(m, a.slice_max[(int64_t)r * a.slices + s]);
-  const float t = a.temperature ? a.temperature[r] : 1.0f;
   return Row((const uint8_t*)a.logits + r * a.stride * (T == SFMP_TYPE_FP32 ? 4 : 2), max_of_wave(m), t);
 }
 
@@ -181,7 +193,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_bins_kernel(SampleArgs a
   __shared__ unsigned long long bins[kBins];
   const int s = blockIdx.x, r = blockIdx.y;
   for (int i = threadIdx.x; i < kBins; i += kSliceThreads) bins[i] = 0;
-  const Row row = make_row<T>(a, r);
+  const Row row = make_row<T>(a, r, a.temperature ? a.temperature[r] : 1.0f);
   __syncthreads();
   if (row.m == -INFINITY) return;
   auto add = [&](float y) {
@@ -247,7 +259,7 @@ __device__ __forceinline__ unsigned long long sum_before(unsigned long long x, P
 // The filters of a row, and the bins that the end of each and the chosen token can lie in.
 struct Wanted {
   int top_k;  // 0: all
-  float top_p, floor;
+  float top_p, floor, uniform;
   bool by_top_p, by_min_p;
   unsigned long long total, min_before;  // (before the bin of min-p's floor)
   int from[4];          // ranges of bins
@@ -264,16 +276,16 @@ struct Wanted {
     return y;
   }
 };
-__device__ __forceinline__ Wanted filters_of(const SampleArgs& a, int r, uint32_t counted, unsigned long long total) {
+__device__ __forceinline__ Wanted filters_of(const Asked& x, uint32_t counted, unsigned long long total) {
   Wanted w;
   w.total = total;
   w.min_before = 0;
-  const bool greedy = a.temperature && a.temperature[r] <= 0.0f;
-  w.top_k = greedy ? 1 : a.top_k ? a.top_k[r] : 0;
+  w.uniform = x.uniform;
+  w.top_k = x.temperature <= 0.0f ? 1 : x.top_k;
   if (w.top_k <= 0 || (uint32_t)w.top_k >= counted) w.top_k = 0;  // (counted: tokens whose weight is not 0)
-  w.top_p = a.top_p ? a.top_p[r] : 1.0f;
+  w.top_p = x.top_p;
   w.by_top_p = w.top_p < 1.0f;
-  const float min_p = a.min_p ? a.min_p[r] : 0.0f;
+  const float min_p = x.min_p;
   w.by_min_p = min_p > 0.0f;
   w.floor = w.by_min_p ? logf(fminf(min_p, 1.0f)) : -INFINITY;
   return w;
@@ -335,11 +347,11 @@ struct Bins {
 // Which bins are wanted.  A position inside a bin leaves the weight kept by top-k uncertain by that bin, which may make two
 // bins of one for the filters after it.  Leaves the sums before the wanted bins in sh->mass and sh->count.
 template <int THREADS>
-__device__ __forceinline__ Wanted find_wanted(const SampleArgs& a, int r, const Bins<THREADS>& bins, PickShared* sh) {
-  Wanted w = filters_of(a, r, sh->counted, sh->total);
+__device__ __forceinline__ Wanted find_wanted(const Asked& asked, const Bins<THREADS>& bins, PickShared* sh) {
+  Wanted w = filters_of(asked, sh->counted, sh->total);
 #pragma unroll
   for (int x = 0; x < 4; ++x) w.from[x] = 1 << 30, w.span[x] = 0;  // (none)
-  const float u = a.uniform[r];
+  const float u = w.uniform;
   unsigned long long least = w.total, most = w.total;  // both ends of the kept weight
   if (threadIdx.x == 0) sh->listed = 0;
   const int min_bin = w.floor > kLeast ? Row::bin(w.floor) : kBins - 1;
@@ -460,7 +472,7 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
 // The choice, from the list of the tokens in the wanted bins (w.tokens of them in sh->list), the sums before these bins
 // being in sh->mass and sh->count.
 template <int THREADS>
-__device__ __forceinline__ void choose_from_list(const SampleArgs& a, int r, const Row& row, const Wanted& w, PickShared* sh) {
+__device__ __forceinline__ void choose_from_list(const Row& row, const Wanted& w, PickShared* sh) {
   constexpr int EACH = kListed / THREADS;
   const int i = threadIdx.x, n = (int)w.tokens;
   int size = 64;
@@ -532,7 +544,7 @@ __device__ __forceinline__ void choose_from_list(const SampleArgs& a, int r, con
     __syncthreads();
     kept = min(kept, sh->min_mass);
   }
-  const unsigned long long passed = min((unsigned long long)((double)a.uniform[r] * (double)kept), kept - 1);
+  const unsigned long long passed = min((unsigned long long)((double)w.uniform * (double)kept), kept - 1);
 #pragma unroll
   for (int x = 0; x < EACH; ++x)
     if (weight[x] && through[x] > passed && through[x] - weight[x] <= passed) sh->found = sh->list[EACH * i + x];
@@ -616,7 +628,7 @@ __device__ __noinline__ unsigned long long place_of(const SampleArgs& a, const R
 }
 
 template <int T>
-__device__ void choose_crowded(const SampleArgs& a, int r, const Row& row, const Wanted& w, PickShared* sh) {
+__device__ void choose_crowded(const SampleArgs& a, const Row& row, const Wanted& w, PickShared* sh) {
   unsigned long long kept = w.total;
   if (w.top_k) kept = place_of<T>(a, row, Sought{Sought::kCount, (uint32_t)w.top_k, 0.0, 0}, sh);
   if (w.by_top_p) kept = min(kept, place_of<T>(a, row, Sought{Sought::kAtLeast, 0, (double)w.top_p * (double)kept, 0}, sh));
@@ -634,7 +646,7 @@ __device__ void choose_crowded(const SampleArgs& a, int r, const Row& row, const
     __syncthreads();
     kept = min(kept, sh->min_mass);
   }
-  const unsigned long long passed = min((unsigned long long)((double)a.uniform[r] * (double)kept), kept - 1);
+  const unsigned long long passed = min((unsigned long long)((double)w.uniform * (double)kept), kept - 1);
   place_of<T>(a, row, Sought{Sought::kAbove, 0, 0.0, passed}, sh);
 }
 
@@ -660,16 +672,17 @@ __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArg
   extern __shared__ __align__(16) uint8_t lds[];
   PickShared* const sh = reinterpret_cast<PickShared*>(lds);
   const int s = blockIdx.x, r = blockIdx.y;
+  const Asked asked = asked_of(a, r);
   Bins<kSliceThreads> bins;
   {
     const int64_t at = (int64_t)r * kBins + Bins<kSliceThreads>::EACH * threadIdx.x;
 #pragma unroll
     for (int j = 0; j < Bins<kSliceThreads>::EACH; ++j) bins.mass[j] = a.mass[at + j], bins.count[j] = a.count[at + j];
   }
-  const Row row = make_row<T>(a, r);
+  const Row row = make_row<T>(a, r, asked.temperature);
   if (row.m == -INFINITY) return;
   bins.add_up(sh);
-  const Wanted w = find_wanted<kSliceThreads>(a, r, bins, sh);
+  const Wanted w = find_wanted<kSliceThreads>(asked, bins, sh);
   if (s == 0 && threadIdx.x == 0) a.wanted[r] = w;
   if (w.tokens > kListed) return;
   const Reach reach(row, w);
@@ -690,10 +703,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   const Listed* const list = a.list + (int64_t)r * kListed;
   const Listed mine = list[threadIdx.x];  // (requested before it is known how many there are)
   const Wanted w = a.wanted[r];
-  const Row row = make_row<T>(a, r);
+  const Row row = make_row<T>(a, r, a.temperature ? a.temperature[r] : 1.0f);
   if (row.m == -INFINITY) return store_none(a, r);
   if (w.tokens > kListed) {
-    choose_crowded<T>(a, r, row, w, sh);
+    choose_crowded<T>(a, row, w, sh);
   } else {
     for (int j = threadIdx.x; j < (int)w.tokens; j += kPickThreads) {
       const Listed x = j < kPickThreads ? mine : list[j];
@@ -702,7 +715,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
       sh->mass[bin] = x.mass_before;
       sh->count[bin] = x.count_before;
     }
-    choose_from_list<kPickThreads>(a, r, row, w, sh);
+    choose_from_list<kPickThreads>(row, w, sh);
   }
   store_choice(a, r, row, w, sh);
 }
@@ -716,6 +729,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   PickShared* const sh = reinterpret_cast<PickShared*>(lds);
   const int r = blockIdx.x, i = threadIdx.x;
   const void* const logits = (const uint8_t*)a.logits + r * a.stride * (T == SFMP_TYPE_FP32 ? 4 : 2);
+  const Asked asked = asked_of(a, r);
   for (int j = i; j < kBins; j += kPickThreads) sh->mass[j] = 0, sh->count[j] = 0;
   float m = -INFINITY;
   for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) { m = fmaxf(m, l); });
@@ -724,7 +738,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kPickThreads / 64; ++w) m = fmaxf(m, sh->wave_max[w]);
-  const Row row(logits, m, a.temperature ? a.temperature[r] : 1.0f);
+  const Row row(logits, m, asked.temperature);
   if (row.m == -INFINITY) return store_none(a, r);
   auto add = [&](float y) {
     if (!(y > kLeast)) return;
@@ -745,9 +759,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
     bins.count[j] = sh->count[Bins<kPickThreads>::EACH * i + j];
   }
   bins.add_up(sh);
-  const Wanted w = find_wanted<kPickThreads>(a, r, bins, sh);
+  const Wanted w = find_wanted<kPickThreads>(asked, bins, sh);
   if (w.tokens > kListed) {
-    choose_crowded<T>(a, r, row, w, sh);
+    choose_crowded<T>(a, row, w, sh);
   } else {
     const Reach reach(row, w);
     __syncthreads();
@@ -757,7 +771,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
       if (is_wanted(row, l, reach, w)) sh->list[atomicAdd(&sh->listed, 1u)] = entry_of(token, l);
     });
     __syncthreads();
-    choose_from_list<kPickThreads>(a, r, row, w, sh);
+    choose_from_list<kPickThreads>(row, w, sh);
   }
   store_choice(a, r, row, w, sh);
 }
