@@ -65,15 +65,14 @@ __device__ __forceinline__ float logit_of(uint32_t bits) {
 typedef __attribute__((address_space(1))) u32x4 GlobalRun;
 
 // Calls f(number, logit) for the tokens [from, to) of a row; the threads take runs of 16 aligned bytes in turn.
-template <int T, int THREADS, typename F>
+template <int T, int THREADS, int AHEAD = 4, typename F>
 __device__ __forceinline__ void for_each_logit(const void* row, int from, int to, F f) {
   constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
   const int lead = (int)((reinterpret_cast<uintptr_t>(row) & 15) / SIZE);  // elements between the aligned address and the row
   const uint8_t* const base = (const uint8_t*)row - lead * SIZE;
   const int first = (from + lead + RUN - 1) / RUN, last = max((to + lead) / RUN, first);  // whole runs
   const GlobalRun* const runs = (const GlobalRun*)reinterpret_cast<uintptr_t>(base);
-  // four runs at a time, the next four requested before
-  constexpr int AHEAD = 4;
+  // AHEAD runs at a time, as many more requested before
   u32x4 now[AHEAD], next[AHEAD];
   auto request = [&](u32x4 (&w)[AHEAD], int v) {
 #pragma unroll
@@ -84,13 +83,15 @@ __device__ __forceinline__ void for_each_logit(const void* row, int from, int to
   request(now, v);
   for (; v < last; v += AHEAD * THREADS) {
     request(next, v + AHEAD * THREADS);
+    int at = v;
+    asm volatile("" : "+v"(at));  // (the numbers are made where they are used, not kept as RUN * AHEAD counters)
 #pragma unroll
     for (int k = 0; k < AHEAD; ++k) {
       if (v + k * THREADS < last) {
 #pragma unroll
         for (int j = 0; j < RUN; ++j) {
           const u32x4 w = now[k];
-          f((v + k * THREADS) * RUN - lead + j, logit_of<T>(SIZE == 4 ? w[j] : (j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu));
+          f((at + k * THREADS) * RUN - lead + j, logit_of<T>(SIZE == 4 ? w[j] : (j & 1) ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu));
         }
       }
       now[k] = next[k];
@@ -568,7 +569,7 @@ struct Sought {
 // Leaves the token's entry in sh->found, returns the running sum with it.  kPickThreads threads; sh->mass and sh->count
 // are used for the digits.
 template <int T>
-__device__ __noinline__ unsigned long long place_of(const SampleArgs& a, const Row& row, const Sought& sought, PickShared* sh) {
+__device__ __forceinline__ unsigned long long place_of(const SampleArgs& a, const Row& row, const Sought& sought, PickShared* sh) {
   constexpr int kDigitBits = 12;
   static_assert(kBins == 1 << kDigitBits, "digits are counted like bins");
   const int i = threadIdx.x;
@@ -580,7 +581,7 @@ __device__ __noinline__ unsigned long long place_of(const SampleArgs& a, const R
     for (int j = i; j < kBins; j += kPickThreads) sh->mass[j] = 0, sh->count[j] = 0;
     __syncthreads();
     const int next = max(shift - kDigitBits, 0);
-    for_each_logit<T, kPickThreads>(row.logits, 0, a.vocab, [&](int token, float l) {
+    for_each_logit<T, kPickThreads, 1>(row.logits, 0, a.vocab, [&](int token, float l) {
       const float y = row.y(l);
       if (!(y > kLeast)) return;
       const uint32_t w = Row::weight(y);
@@ -627,27 +628,41 @@ __device__ __noinline__ unsigned long long place_of(const SampleArgs& a, const R
   return mass_before + Row::weight(row.y(logit_of_entry(prefix)));
 }
 
+// (One place where the search stands in the code, and no call: a call's stack costs every launch of the kernel 7 us, whether a row is
+// crowded or not.)
 template <int T>
-__device__ void choose_crowded(const SampleArgs& a, const Row& row, const Wanted& w, PickShared* sh) {
+__device__ __forceinline__ void choose_crowded(const SampleArgs& a, const Row& row, const Wanted& w, PickShared* sh) {
   unsigned long long kept = w.total;
-  if (w.top_k) kept = place_of<T>(a, row, Sought{Sought::kCount, (uint32_t)w.top_k, 0.0, 0}, sh);
-  if (w.by_top_p) kept = min(kept, place_of<T>(a, row, Sought{Sought::kAtLeast, 0, (double)w.top_p * (double)kept, 0}, sh));
-  if (w.by_min_p) {
-    if (threadIdx.x == 0) sh->min_mass = 0;
-    __syncthreads();
-    unsigned long long mine = 0;
-    for_each_logit<T, kPickThreads>(row.logits, 0, a.vocab, [&](int, float l) {
-      const float y = row.y(l);
-      if (y >= w.floor && y > kLeast) mine += Row::weight(y);
-    });
+#pragma clang loop unroll(disable)
+  for (int filter = 0; filter < 4; ++filter) {
+    Sought sought{Sought::kCount, (uint32_t)w.top_k, 0.0, 0};
+    if (filter == 0) {
+      if (!w.top_k) continue;
+    } else if (filter == 1) {
+      if (!w.by_top_p) continue;
+      sought.by = Sought::kAtLeast;
+      sought.aim = (double)w.top_p * (double)kept;
+    } else if (filter == 2) {
+      if (!w.by_min_p) continue;
+      if (threadIdx.x == 0) sh->min_mass = 0;
+      __syncthreads();
+      unsigned long long mine = 0;
+      for_each_logit<T, kPickThreads, 1>(row.logits, 0, a.vocab, [&](int, float l) {
+        const float y = row.y(l);
+        if (y >= w.floor && y > kLeast) mine += Row::weight(y);
+      });
 #pragma unroll
-    for (int s = 1; s < 64; s *= 2) mine += __shfl_xor(mine, s);
-    if ((threadIdx.x & 63) == 0) atomicAdd(&sh->min_mass, mine);
-    __syncthreads();
-    kept = min(kept, sh->min_mass);
+      for (int s = 1; s < 64; s *= 2) mine += __shfl_xor(mine, s);
+      if ((threadIdx.x & 63) == 0) atomicAdd(&sh->min_mass, mine);
+      __syncthreads();
+      kept = min(kept, sh->min_mass);
+      continue;
+    } else {
+      sought.by = Sought::kAbove;
+      sought.passed = min((unsigned long long)((double)w.uniform * (double)kept), kept - 1);
+    }
+    kept = min(kept, place_of<T>(a, row, sought, sh));
   }
-  const unsigned long long passed = min((unsigned long long)((double)w.uniform * (double)kept), kept - 1);
-  place_of<T>(a, row, Sought{Sought::kAbove, 0, 0.0, passed}, sh);
 }
 
 __device__ __forceinline__ void store_choice(const SampleArgs& a, int r, const Row& row, const Wanted& w, const PickShared* sh) {
@@ -750,7 +765,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   if (row.plain)
     for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) { add(row.template y<true>(l)); });
   else
-    for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int, float l) { add(row.y(l)); });
+    for_each_logit<T, kPickThreads, 1>(logits, 0, a.vocab, [&](int, float l) { add(row.y(l)); });
   __syncthreads();
   Bins<kPickThreads> bins;
 #pragma unroll
