@@ -161,7 +161,7 @@ __device__ __forceinline__ uint32_t falling_key(float l) {
 
 __device__ __forceinline__ int slice_from(const SampleArgs& a, int s) { return (int)((int64_t)a.vocab * s / a.slices); }
 
-// Largest logit of every slice; clears the histograms.  One row of 131072 fp16 tokens, 32 slices: 4.1 us, this and the next three bound by
+// Largest logit of every slice; clears the histograms.  One row of 131072 fp16 tokens, 32 slices: 3.3 us, this and the next three bound by
 // latency (a launch, a few dependent loads, a few barriers each; the logits are 0.26 MB).
 template <int T>
 __global__ __launch_bounds__(kSliceThreads) void sample_max_kernel(SampleArgs a) {
@@ -186,7 +186,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_max_kernel(SampleArgs a)
 }
 
 // Adds a slice to the histogram of its row.  A bin of a slice is one 64-bit word in LDS: its count above bit 46, its
-// weight below (a slice has at most 2^15 tokens of at most 2^31).  The same row: 6.2 us.
+// weight below (a slice has at most 2^15 tokens of at most 2^31).  The same row: 6.3 us.
 constexpr int kCountBit = 46;
 constexpr int kMostSlice = 1 << 15;
 template <int T>
@@ -681,7 +681,7 @@ __device__ __forceinline__ void store_none(const SampleArgs& a, int r) {
 
 // Slices: the tokens of the wanted bins into the row's list, with the sums before their bins; the workgroup of the first
 // slice leaves what the choice needs to know beside.  Every workgroup adds up the row's histogram for itself (48 KiB from the L2, instead
-// of a launch for it): 8.7 us.
+// of a launch for it): 8.4 us.
 template <int T>
 __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -709,7 +709,7 @@ __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArg
   });
 }
 
-// One workgroup per row: the choice.  12 us: a chain of loads, a sort and some fifteen barriers.
+// One workgroup per row: the choice.  5.4 us: a chain of loads, a sort and some fifteen barriers.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -735,9 +735,10 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   store_choice(a, r, row, w, sh);
 }
 
-// One workgroup per row: everything.  256 rows of 100003 fp32 logits (102 MB) 78 us: 16 us for the maximum, which reads HBM at 6.4 TB/s,
-// 25 us for the histogram (some 20 instructions and two LDS atomics per logit: bound by the vector units), 16 us for collecting (the
-// row comes out of a cache by then), the rest latency.  Keeping a part of the row in registers between the passes was slower.
+// One workgroup per row: everything.  256 rows of 100003 fp32 logits (102 MB) 62 us: about 20 us each for the maximum, which reads HBM, and for the histogram (some 20
+// instructions and two LDS atomics per logit), 15 for collecting (the row comes out of a cache by then), the rest a chain of barriers:
+// with 1000 tokens 13 us.  Neither a shorter exponential nor one atomic for both sums made a difference; keeping a part of the row in
+// registers between the passes was slower.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -793,7 +794,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
 
 int slices_of(int32_t rows, int32_t vocab) {
   // slices of 4096 tokens or more, 512 workgroups at most (each adds a histogram of its own to the row's: 32 rows of 131072
-  // tokens 43.8 us, with 1024 workgroups 56.5, with 256 46.3); 2^15 tokens at most
+  // tokens 36.7 us, with 1024 workgroups 47.5, with 256 39.9); 2^15 tokens at most
   int64_t s = vocab / 4096;
   if (s * rows > 512) s = 512 / rows;
   const int64_t least = ((int64_t)vocab + kMostSlice - 1) / kMostSlice;
@@ -802,8 +803,8 @@ int slices_of(int32_t rows, int32_t vocab) {
 }
 
 // One workgroup per row: its time grows with the vocabulary and hardly with the rows, that of four launches over slices with both.
-// One row of 8000 tokens 21.5 us against 28.7, of 32000 26.9 and 29.4, of 131072 58.5 and 29.0; 32 rows of 50257 tokens
-// 37.7 and 41.8, of 131072 62.9 and 43.8; 128 of them 80.1 and 82.0.
+// One row of 8000 tokens 14.7 us against 24.8, of 32000 19.0 and 23.4, of 131072 46.5 and 22.6; 32 rows of 50257 tokens
+// 29.8 and 35.5, of 131072 52.6 and 37.4; 128 of them 67.7 and 72.8.
 bool whole_rows(int32_t rows, int32_t vocab) { return rows >= 110 || (int64_t)vocab * (110 - rows) < 4200000; }
 
 struct SampleWorkspace {
