@@ -185,10 +185,11 @@ __global__ __launch_bounds__(kSliceThreads) void sample_max_kernel(SampleArgs a)
   }
 }
 
-// Adds a slice to the histogram of its row.  A bin of a slice is one 64-bit word in LDS: its count above bit 46, its
-// weight below (a slice has at most 2^15 tokens of at most 2^31).  The same row: 6.3 us.
-constexpr int kCountBit = 46;
+// Adds a slice to the histogram of its row.  A bin of a slice is one 64-bit word in LDS: its count from bit 47 on, its
+// weight below.  All of a slice may lie in one bin, with the largest weight each: 2^15 tokens of 2^31.  The same row: 6.3 us.
+constexpr int kCountBit = 47;
 constexpr int kMostSlice = 1 << 15;
+static_assert((uint64_t)kMostSlice << 31 < 1ull << kCountBit && kMostSlice < 1 << (64 - kCountBit), "weight and count of a whole slice in one bin");
 template <int T>
 __global__ __launch_bounds__(kSliceThreads) void sample_bins_kernel(SampleArgs a) {
   __shared__ unsigned long long bins[kBins];

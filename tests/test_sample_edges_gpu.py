@@ -1,0 +1,61 @@
+"""Choice of the next token on the GPU where sums, slices and parameters end."""
+import math
+
+import numpy as np
+import pytest
+
+from test_sample_gpu import _check, _logits, _run
+
+pytestmark = pytest.mark.gpu
+
+# Rows of 262144 (of 57 to 93 in a call) and 524288 tokens (of 31 to 101) are cut into slices of 32768, the longest there are, and
+# with a token more or less into slices of both neighbouring lengths.
+WIDE = [(64, 262144), (64, 262143), (64, 262145), (31, 524288), (31, 524285)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16"])
+@pytest.mark.parametrize("rows,vocab", WIDE)
+def test_equal_logits_in_the_longest_slices(rows, vocab, dtype):
+    # a slice lies in one bin as a whole, every token with the largest weight: the choice is exact, the number of the token
+    x = np.full((rows, vocab), 3.25, dtype=np.float32)
+    u = ((np.arange(rows) + 0.5) / rows).astype(np.float32)
+    tokens, logprobs, _ = _run(x, 1.0, 0, 1.0, 0.0, u, dtype=dtype)
+    assert tokens.tolist() == [int(float(v) * vocab) for v in u]
+    # (as the test of equal logits in short slices: a logarithm and a sum in fp32)
+    assert np.allclose(logprobs, -math.log(vocab), rtol=1e-6)
+    k = 1 + np.arange(rows) * (vocab // rows)
+    tokens, logprobs, _ = _run(x, 1.0, k, 1.0, 0.0, 1.0 - 2.0 ** -24, dtype=dtype)
+    assert tokens.tolist() == (k - 1).tolist() and np.allclose(logprobs, -math.log(vocab), rtol=1e-6)
+    # top-p on top of it: the shortest prefix that holds a half of k equal weights
+    tokens, _, _ = _run(x, 1.0, k, 0.5, 0.0, 1.0 - 2.0 ** -24, dtype=dtype)
+    assert tokens.tolist() == ((k + 1) // 2 - 1).tolist()
+
+
+@pytest.mark.parametrize("rows,vocab", WIDE[:1] + WIDE[3:4])
+def test_one_slice_above_the_others(rows, vocab):
+    x = np.zeros((rows, vocab), dtype=np.float32)
+    place = np.arange(rows) % (vocab // 32768) * 32768
+    for r in range(rows):
+        x[r, place[r]:place[r] + 32768] = 1.0
+    tokens, logprobs, _ = _run(x, 1.0, 0, 1.0, 0.0, 0.0)
+    assert tokens.tolist() == place.tolist()
+    assert np.allclose(logprobs, -math.log(32768 + (vocab - 32768) / math.e), rtol=1e-6)
+    # the weight of the slice in the whole is 0.28 or less: behind it the others follow by their numbers
+    share = 32768 / (32768 + (vocab - 32768) / math.e)
+    u = np.float32(0.9)
+    rest = int((float(u) - share) / (1 - share) * (vocab - 32768))
+    tokens, _, _ = _run(x, 1.0, 0, 1.0, 0.0, u)
+    # (a weight of 1/e in units of 2^-31: 2^-31 of the sum off, a token of 2^19 at most)
+    want = rest + np.where(rest >= place, 32768, 0)
+    assert (np.abs(tokens - want) <= 1).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("rows,vocab", WIDE[:3])
+def test_every_filter_over_the_longest_slices(rows, vocab, dtype):
+    rng = np.random.default_rng(vocab)
+    x = _logits(rng, rows, vocab)
+    t, k = rng.choice([0.0, 0.6, 1.0, 2.0], rows), rng.choice([0, 1, 50, 2000], rows)
+    p, m, u = rng.choice([0.2, 0.95, 1.0], rows), rng.choice([0.0, 0.03], rows), rng.random(rows)
+    sure, _ = _check(x, t, k, p, m, u, dtype=dtype)
+    assert sure >= rows // 3
