@@ -9,6 +9,7 @@
 //
 // Few rows are cut into slices over many workgroups, which takes three launches (largest logit; histogram; collection) and
 // a fourth for the choice.  Many rows have one workgroup each, which does all of it.
+#include <float.h>
 #include <math.h>
 
 #include "sfmp_device.h"
@@ -405,7 +406,9 @@ __device__ __forceinline__ Wanted find_wanted(const Asked& asked, const Bins<THR
   return w;
 }
 
-// The wanted bins as intervals of logits, with a margin for rounding: most tokens are told apart without their bin.
+// The wanted bins as intervals of logits, with a margin for rounding: most tokens are told apart without their bin.  Where a bin's
+// width in logits is no normal number (a temperature of infinity, or near the least one) or an interval passes the range of fp32, the
+// bin alone decides.
 struct Reach {
   float middle[4], half[4];
   __device__ __forceinline__ Reach(const Row& row, const Wanted& w) {
@@ -414,8 +417,9 @@ struct Reach {
     for (int x = 0; x < 4; ++x) {
       const bool none = w.from[x] >= kBins;
       const float high = row.m - (float)(w.from[x] - 1) * unit, low = row.m - (float)(w.from[x] + (int)w.span[x] + 2) * unit;
-      const float c = !row.plain || none ? 0.0f : 0.5f * (high + low);
-      const float h = none ? -1.0f : !row.plain ? INFINITY : 0.5001f * (high - low) + margin + fabsf(c) * 1e-6f;
+      float c = 0.5f * (high + low), h = 0.5001f * (high - low) + margin + fabsf(c) * 1e-6f;
+      if (!row.plain || !(unit >= FLT_MIN && fabsf(c) < INFINITY && h < INFINITY)) c = 0.0f, h = INFINITY;
+      if (none) h = -1.0f;
       middle[x] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(c)));
       half[x] = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(h)));
     }
@@ -471,12 +475,12 @@ __device__ __forceinline__ void sort_list(uint64_t* list, int n) {
     }
 }
 
-// The choice, from the list of the tokens in the wanted bins (w.tokens of them in sh->list), the sums before these bins
+// The choice, from the list of the tokens in the wanted bins (the first n of sh->list), the sums before these bins
 // being in sh->mass and sh->count.
 template <int THREADS>
-__device__ __forceinline__ void choose_from_list(const Row& row, const Wanted& w, PickShared* sh) {
+__device__ __forceinline__ void choose_from_list(const Row& row, const Wanted& w, int n, PickShared* sh) {
   constexpr int EACH = kListed / THREADS;
-  const int i = threadIdx.x, n = (int)w.tokens;
+  const int i = threadIdx.x;
   int size = 64;
   while (size < n) size *= 2;
   for (int j = n + i; j < size; j += THREADS) sh->list[j] = ~0ull;
@@ -705,7 +709,8 @@ __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArg
   for_each_logit<T, kSliceThreads>(row.logits, slice_from(a, s), slice_from(a, s + 1), [&](int token, float l) {
     if (is_wanted(row, l, reach, w)) {
       const int bin = Row::bin(row.y(l));
-      a.list[(int64_t)r * kListed + atomicAdd(&a.listed[r], 1u)] = Listed{entry_of(token, l), sh->mass[bin], sh->count[bin], 0};
+      const uint32_t at = atomicAdd(&a.listed[r], 1u);
+      if (at < kListed) a.list[(int64_t)r * kListed + at] = Listed{entry_of(token, l), sh->mass[bin], sh->count[bin], 0};
     }
   });
 }
@@ -719,19 +724,21 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
   const Listed* const list = a.list + (int64_t)r * kListed;
   const Listed mine = list[threadIdx.x];  // (requested before it is known how many there are)
   const Wanted w = a.wanted[r];
+  const uint32_t listed = a.listed[r];
   const Row row = make_row<T>(a, r, a.temperature ? a.temperature[r] : 1.0f);
   if (row.m == -INFINITY) return store_none(a, r);
   if (w.tokens > kListed) {
     choose_crowded<T>(a, row, w, sh);
   } else {
-    for (int j = threadIdx.x; j < (int)w.tokens; j += kPickThreads) {
+    const int n = (int)min(w.tokens, listed);  // (as many as were collected: logits that another stream changes meanwhile leave fewer)
+    for (int j = threadIdx.x; j < n; j += kPickThreads) {
       const Listed x = j < kPickThreads ? mine : list[j];
       sh->list[j] = x.entry;
       const int bin = Row::bin(row.y(logit_of_entry(x.entry)));
       sh->mass[bin] = x.mass_before;
       sh->count[bin] = x.count_before;
     }
-    choose_from_list<kPickThreads>(row, w, sh);
+    choose_from_list<kPickThreads>(row, w, n, sh);
   }
   store_choice(a, r, row, w, sh);
 }
@@ -785,10 +792,13 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
     if (i == 0) sh->listed = 0;
     __syncthreads();
     for_each_logit<T, kPickThreads>(logits, 0, a.vocab, [&](int token, float l) {
-      if (is_wanted(row, l, reach, w)) sh->list[atomicAdd(&sh->listed, 1u)] = entry_of(token, l);
+      if (is_wanted(row, l, reach, w)) {
+        const uint32_t at = atomicAdd(&sh->listed, 1u);
+        if (at < kListed) sh->list[at] = entry_of(token, l);
+      }
     });
     __syncthreads();
-    choose_from_list<kPickThreads>(row, w, sh);
+    choose_from_list<kPickThreads>(row, w, (int)min(w.tokens, sh->listed), sh);
   }
   store_choice(a, r, row, w, sh);
 }

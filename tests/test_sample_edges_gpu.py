@@ -59,3 +59,50 @@ def test_every_filter_over_the_longest_slices(rows, vocab, dtype):
     p, m, u = rng.choice([0.2, 0.95, 1.0], rows), rng.choice([0.0, 0.03], rows), rng.random(rows)
     sure, _ = _check(x, t, k, p, m, u, dtype=dtype)
     assert sure >= rows // 3
+
+
+def _uniform(x, u):
+    """Tokens of rows whose finite logits all weigh the same: by falling logit, equal ones by rising number."""
+    out = []
+    for row, v in zip(x, np.broadcast_to(np.asarray(u, dtype=np.float32), len(x))):
+        n = int(np.isfinite(row).sum())
+        out.append(int(np.lexsort((np.arange(row.size), -row.astype(np.float64)))[int(float(v) * n)]))
+    return out
+
+
+@pytest.mark.parametrize("temperature", [1e30, 3e38, math.inf])
+@pytest.mark.parametrize("rows,vocab,finite", [(4, 100, 100), (4, 2048, 2048), (4, 2049, 2049), (4, 5000, 1500), (3, 131072, 700), (3, 131072, 2048),
+                                               (2, 131072, 2049), (120, 1000, 1000), (64, 262144, 90)])
+def test_temperatures_at_which_all_weigh_the_same(temperature, rows, vocab, finite):
+    rng = np.random.default_rng(vocab + finite)
+    x = np.full((rows, vocab), -math.inf, dtype=np.float32)
+    for r in range(rows):
+        x[r, rng.permutation(vocab)[:finite]] = rng.choice(rng.normal(0.0, 3.0, 50), finite)
+    u = rng.random(rows).astype(np.float32)
+    tokens, logprobs, _ = _run(x, temperature, 0, 1.0, 0.0, u)
+    assert tokens.tolist() == _uniform(x, u)
+    assert np.allclose(logprobs, -math.log(finite), rtol=1e-6)
+    tokens, _, _ = _run(x, temperature, 1 + rng.integers(0, finite, rows), [1.0, 0.7][rows % 2], 0.5, 0.0)
+    assert tokens.tolist() == _uniform(x, 0.0)
+    tokens, _, _ = _run(x, temperature, finite, 1.0, 0.999, 1.0 - 2.0 ** -24)
+    assert tokens.tolist() == _uniform(x, 1.0 - 2.0 ** -24)
+
+
+@pytest.mark.parametrize("temperature", [1e-38, 4e-38, 1e-36, 1e-30])
+def test_temperatures_near_the_least(temperature):
+    # logits that lie a few temperatures apart, some of them no normal numbers; weights 1, 1/e, 1/e^2
+    t = float(np.float32(temperature))
+    x = np.float32(t) * np.array([[-1.0, 0.0, -2.0, -1e3], [0.0, -2.0, -1.0, -40.0]], dtype=np.float32)
+    share = np.cumsum(np.exp([0.0, -1.0, -2.0])) / np.exp([0.0, -1.0, -2.0]).sum()
+    for u, at in ((0.1, 0), (0.99 * share[0], 0), (1.01 * share[0], 1), (0.999 * share[1], 1), (1.001 * share[1], 2), (1.0 - 2.0 ** -24, 2)):
+        tokens, logprobs, _ = _run(x, t, 0, 1.0, 0.0, u)
+        assert tokens.tolist() == [[1, 0, 2][at], [0, 2, 1][at]], u
+        # (a product of a denormal number and its temperature: 2^-22 of it)
+        assert np.allclose(logprobs, -at - math.log(np.exp([0.0, -1.0, -2.0]).sum()), atol=1e-5)
+
+
+def test_intervals_that_pass_the_range_of_fp32():
+    x = np.array([[3.4e38, 3.3e38, 0.5e38, 0.0], [-3.3e38, -3.4e38, -3.35e38, -math.inf]], dtype=np.float32)
+    for t in (1e37, 1e38, 3.4e38):
+        _check(x, t, 0, 1.0, 0.0, [0.3, 0.9])
+        _check(x, t, 2, 1.0, 0.0, [0.9, 0.6])
