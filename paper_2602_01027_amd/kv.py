@@ -111,8 +111,12 @@ def _batch(tables: DeviceKvTables, slots, row_start, rows: int, max_rows: int) -
 
 
 def _workspace(t):
-    if t is None:
+    """(address, bytes) of a contiguous GPU tensor of any type; None and an empty one are left to the library's check."""
+    import torch
+    if t is None or (isinstance(t, torch.Tensor) and t.numel() == 0):
         return None, 0
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError("workspace has to be a contiguous tensor on the GPU")
     return C.c_void_p(t.data_ptr()), t.numel() * t.element_size()
 
 
