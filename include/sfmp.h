@@ -405,7 +405,8 @@ int sfmp_kv_gather(const sfmp_kv_layout_t* layout, int32_t layer, const void* co
  * result may differ in its last bits with the batch it is in (the work is cut by the whole batch).
  * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads, strides, max_tokens < 1, window < 0, scale not finite or not positive, or
  * batch * kv_heads * ceil(max_tokens / 64) * ceil(max_rows * q_heads / kv_heads / 16) >= 2^31.  SFMP_ERR_WORKSPACE as for sfmp_gemm; the
- * workspace's contents are irrelevant on entry. */
+ * workspace's contents are irrelevant on entry.  sfmp_kv_attention_workspace: bytes that are enough for every call with this layout and
+ * q_heads, and with no more batch entries, rows, max_rows and max_tokens than these, with any window. */
 int sfmp_kv_attention_workspace(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t q_heads,
                                 int32_t max_rows, int32_t max_tokens, int64_t* bytes);
 int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, const void* codes_dev, const float* scales_dev,
@@ -455,7 +456,8 @@ int sfmp_kv_compact(const sfmp_kv_layout_t* layout, void* codes_dev, float* scal
  * temperature, top_k, top_p, min_p: fp32 / int32 / fp32 / fp32 [rows], each may be NULL (1, all, all, all).  tokens: int32
  * [rows].  logprobs: NULL, or fp32 [rows], ln of w_token over the sum of all w of the row
  * (0 with T <= 0, where the first token has all the weight).
- * SFMP_ERR_SHAPE: rows < 0, vocab < 1 or above 2^24, stride < vocab.  Alignment: logits to their element size. */
+ * SFMP_ERR_SHAPE: rows < 0, vocab < 1 or above 2^24, stride < vocab.  Alignment: logits to their element size.
+ * sfmp_sample_workspace: bytes that are enough for every call of no more rows and no larger vocabulary. */
 int sfmp_sample_workspace(int32_t rows, int32_t vocab, int64_t* bytes);
 int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32_t vocab, int64_t stride,
                 const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,

@@ -1102,8 +1102,23 @@ struct AttentionForm {
 // With more rows of an entry and key/value head than these, attend_prompt_kernel (48 rows, 8 heads of 128 dims, us: one sequence of 512
 // tokens 10.3 against 15.9, of 8192 25.8 and 31.8, 8 of 2048 28.7 and 29.1; 64 of 2048 100 and 91).
 constexpr int kPromptFrom = 64;
+constexpr int kMostCutTiles = 4;  // of an entry, in equal parts
 
 int waves_of(int dim, int nt) { return dim * nt >= 256 ? 4 : 8; }
+
+// Time (us) that equal parts take at least, and that a workgroup for each unit of p pages takes (choose_form).
+double parts_start(int waves) { return waves == 8 ? 10.0 : 14.0; }
+double time_of_units(int dim, int waves, int64_t units, int64_t p) {
+  return 4.3 + (dim == 64 ? 1.25 : 2.7) * (double)((units + 255) / 256 * ((p + waves - 1) / waves));
+}
+// Partial results of the 256 workgroups, or of a prompt's parts.
+int64_t cut_bytes_of(int dim, int nt) { return (int64_t)256 * 2 * (nt * (dim / 16) * 64 * 16 + 2 * nt * 64 * 4); }
+int prompt_slots(int dim) { return dim == 256 ? 256 : 512; }
+int64_t prompt_cut_bytes(int dim) { return (int64_t)prompt_slots(dim) * 2 * kPromptRows * (dim + 2) * 4; }
+// (a page is converted once for all rows of a large tile: choose_form)
+bool in_large_tiles(int dim, int64_t rows, int64_t units, int64_t all_pages) {
+  return rows > kPromptFrom && (units > 256 || all_pages > (dim == 64 ? 64 : dim == 128 ? 16 : 32));
+}
 
 AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows, int max_rows, int max_tokens, int window) {
   AttentionForm f{};
@@ -1115,7 +1130,7 @@ AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows
   // unit and reads few pages.  Small against large tiles, us: 68 rows, 8 heads of 128 dims, one sequence of 512 tokens 10.2 and 15.9,
   // of 1024 13.9 and 18.3, of 2048 23.6 and 20.8; 64 sequences of 512 tokens 56 and 34; 65 rows, 16 heads of 64 dims, 2048 tokens
   // 12.5 and 17.7; 100 rows, 4 heads of 256 dims, 2048 tokens 28.6 and 31.6, of 4096 49 and 36.
-  if (rows > kPromptFrom && (units > 256 || all_pages > (dim == 64 ? 64 : dim == 128 ? 16 : 32))) {
+  if (in_large_tiles(dim, rows, units, all_pages)) {
     const int64_t most = (rows + kPromptRows - 1) / kPromptRows;
     f.prompt = true;
     f.tiles = (int)most;
@@ -1125,7 +1140,7 @@ AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows
     // them new, of one length and of lengths down to an eighth.  The host knows the rows of all entries, and the longest alone: the
     // first form waits for it, the second reads what there is, and 0.6 of it is counted for each.  A tile ends at its last row, which
     // only helps the first form, and only where other tiles wait.
-    const int slots = dim == 256 ? 256 : 512;
+    const int slots = prompt_slots(dim);
     const double tiles_used = batch == 1 ? (double)most * heads : ((double)all_rows * group / kPromptRows + 0.5 * batch) * heads;
     const double whole_start = dim == 64 ? 6.5 : dim == 128 ? 9.0 : 9.5, whole_page = dim == 64 ? 0.78 : dim == 128 ? 1.09 : 3.9;
     const double cut_start = dim == 64 ? 10.0 : dim == 128 ? 14.0 : 18.0, cut_page = dim == 64 ? 1.9 : dim == 128 ? 2.7 : 4.0;
@@ -1140,7 +1155,7 @@ AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows
     };
     f.may_cut = tiles_used < 512 && batch <= kMostPlannedPrompts && cut_is_faster(all_pages);
     if (f.may_cut && cut_is_faster(pages)) f.workgroups = slots;
-    f.cut_bytes = (int64_t)slots * 2 * kPromptRows * (dim + 2) * 4;
+    f.cut_bytes = prompt_cut_bytes(dim);
     return f;
   }
   f.least = 1;
@@ -1150,12 +1165,49 @@ AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows
   // (10, 5.0) us with 128 dims, int8.  The first form waits for its longest unit, the second reads what there is: the host knows
   // the longest sequence alone, and counts half of it for each.
   const double cut = (double)((units * pages + 256 * f.waves - 1) / (256 * f.waves)) * (batch > 1 ? 0.5 : 1.0);
-  const double start = f.waves == 8 ? 10.0 : 14.0, of_parts = start + (dim == 64 ? 2.9 : 5.0) * cut;
-  auto of_units = [&](int64_t p) { return 4.3 + (dim == 64 ? 1.25 : 2.7) * (double)((units + 255) / 256 * ((p + f.waves - 1) / f.waves)); };
-  f.may_cut = batch <= kMostPlanned && tiles <= 4 && of_units(all_pages) > start;
-  f.cut_bytes = (int64_t)256 * 2 * (f.nt * (dim / 16) * 64 * 16 + 2 * f.nt * 64 * 4);
-  if (f.may_cut && of_parts < of_units(pages)) f.workgroups = 256;
+  const double start = parts_start(f.waves), of_parts = start + (dim == 64 ? 2.9 : 5.0) * cut;
+  f.may_cut = batch <= kMostPlanned && tiles <= kMostCutTiles && time_of_units(dim, f.waves, units, all_pages) > start;
+  f.cut_bytes = cut_bytes_of(dim, f.nt);
+  if (f.may_cut && of_parts < time_of_units(dim, f.waves, units, pages)) f.workgroups = 256;
   return f;
+}
+
+int64_t bytes_with_plan(int64_t cut_bytes) { return round_up_256(cut_bytes + kMostPlanned * (sizeof(KvEntry) + 4) + 4); }
+
+// What a call needs: that of its form.
+int64_t workspace_of_call(const AttentionForm& f) { return f.may_cut ? bytes_with_plan(f.cut_bytes) : 256; }
+
+// What every call of no more entries, rows and tokens can do with: forms follow each other back and forth as a call grows, but each has its
+// conditions, all of which grow with it, or hold up to a number of entries and of tiles.
+int64_t workspace_up_to(int dim, int heads, int group, int batch, int max_rows, int max_tokens) {
+  const int64_t rows = (int64_t)max_rows * group, all_pages = ((int64_t)max_tokens + kPage - 1) / kPage;
+  const int64_t entries = batch < kMostPlanned ? batch : kMostPlanned;
+  int64_t most = 256;
+  for (int nt = 1; nt <= (dim < 256 && rows > 16 ? 2 : 1); ++nt) {
+    const int64_t widest = dim < 256 && nt == 1 ? 1 : kMostCutTiles, all = (rows + 16 * nt - 1) / (16 * nt), tiles = all < widest ? all : widest;
+    const int waves = waves_of(dim, nt);
+    if (time_of_units(dim, waves, tiles * heads * entries, all_pages) > parts_start(waves)) {
+      const int64_t bytes = bytes_with_plan(cut_bytes_of(dim, nt));
+      most = bytes > most ? bytes : most;
+    }
+  }
+  const int nt = dim < 256 ? 2 : 1;
+  if (in_large_tiles(dim, rows, (rows + 16 * nt - 1) / (16 * nt) * heads * batch, all_pages)) {
+    const int64_t bytes = bytes_with_plan(prompt_cut_bytes(dim));
+    most = bytes > most ? bytes : most;
+  }
+  return most;
+}
+
+int check_sizes(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t q_heads, int32_t max_rows, int32_t max_tokens) {
+  if (int e = check_kv_layout(layout)) return e;
+  if (batch < 0 || batch > 65535 || rows < 0 || rows > kMaxRows || max_rows < 0 || max_rows > rows || q_heads < 1 ||
+      q_heads % layout->kv_heads || q_heads > 65536 || max_tokens < 1 || max_tokens > kMaxTablePages * kPage)
+    return SFMP_ERR_SHAPE;
+  const int64_t pages = ((int64_t)max_tokens + kPage - 1) / kPage;
+  const int64_t tiles = ((int64_t)max_rows * (q_heads / layout->kv_heads) + 15) / 16;
+  if ((tiles && pages > INT32_MAX / tiles) || (int64_t)batch * layout->kv_heads * pages * tiles > INT32_MAX) return SFMP_ERR_SHAPE;
+  return SFMP_OK;
 }
 
 template <int D, int FMT>
@@ -1192,18 +1244,8 @@ using namespace sfmp;
 extern "C" int sfmp_kv_attention_workspace(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t q_heads,
                                            int32_t max_rows, int32_t max_tokens, int64_t* bytes) {
   if (!bytes) return SFMP_ERR_NULL;
-  if (int e = check_kv_layout(layout)) return e;
-  if (batch < 0 || batch > 65535 || rows < 0 || rows > kMaxRows || max_rows < 0 || max_rows > rows || q_heads < 1 ||
-      q_heads % layout->kv_heads || q_heads > 65536 || max_tokens < 1 || max_tokens > kMaxTablePages * kPage)
-    return SFMP_ERR_SHAPE;
-  const int64_t pages = ((int64_t)max_tokens + kPage - 1) / kPage;
-  const int64_t tiles = ((int64_t)max_rows * (q_heads / layout->kv_heads) + 15) / 16;
-  if ((tiles && pages > INT32_MAX / tiles) || (int64_t)batch * layout->kv_heads * pages * tiles > INT32_MAX) return SFMP_ERR_SHAPE;
-  *bytes = 256;
-  if (batch && max_rows) {
-    const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch, rows, max_rows, max_tokens, 0);
-    if (f.may_cut) *bytes = round_up_256(f.cut_bytes + kMostPlanned * (sizeof(KvEntry) + 4) + 4);
-  }
+  if (int e = check_sizes(layout, batch, rows, q_heads, max_rows, max_tokens)) return e;
+  *bytes = batch && max_rows ? workspace_up_to(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch, max_rows, max_tokens) : 256;
   return SFMP_OK;
 }
 
@@ -1214,8 +1256,7 @@ extern "C" int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, 
                                  void* workspace_dev, int64_t workspace_bytes, void* hip_stream) {
   AttentionArgs a;
   if (int e = make_kv_view(layout, layer, codes_dev, scales_dev, tables, batch, &a.v)) return e;
-  int64_t need = 0;
-  if (int e = sfmp_kv_attention_workspace(layout, batch->batch, batch->rows, q_heads, batch->max_rows, max_tokens, &need)) return e;
+  if (int e = check_sizes(layout, batch->batch, batch->rows, q_heads, batch->max_rows, max_tokens)) return e;
   if (dtype != SFMP_TYPE_FP16 && dtype != SFMP_TYPE_BF16) return SFMP_ERR_LAYOUT;
   const int64_t width = (int64_t)q_heads * layout->head_dim;
   if (window < 0 || !(scale > 0.0f) || !(scale < INFINITY) || q_stride < width || o_stride < width || q_stride % 8 || o_stride % 8 ||
@@ -1224,21 +1265,24 @@ extern "C" int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, 
   if (batch->rows == 0 || batch->batch == 0) return SFMP_OK;
   if (!Q_dev || !O_dev) return SFMP_ERR_NULL;
   if (!kv_aligned(Q_dev, 16) || !kv_aligned(O_dev, 16) || !kv_aligned(lse_dev, 4)) return SFMP_ERR_ALIGN;
-  if (!workspace_dev || !kv_aligned(workspace_dev, 256) || workspace_bytes < need) return SFMP_ERR_WORKSPACE;
+  const int group = q_heads / layout->kv_heads;
+  const AttentionForm f = batch->max_rows ? choose_form(layout->head_dim, layout->kv_heads, group, batch->batch, batch->rows, batch->max_rows,
+                                                        max_tokens, window)
+                                          : AttentionForm{};
+  if (!workspace_dev || !kv_aligned(workspace_dev, 256) || workspace_bytes < workspace_of_call(f)) return SFMP_ERR_WORKSPACE;
   a.Q = (const uint16_t*)Q_dev;
   a.O = (uint16_t*)O_dev;
   a.lse = lse_dev;
   a.q_stride = q_stride;
   a.o_stride = o_stride;
   a.q_heads = q_heads;
-  a.group = q_heads / layout->kv_heads;
+  a.group = group;
   a.window = window;
   a.max_pages = (max_tokens + kPage - 1) / kPage;
   a.scale = scale;
   a.bf16 = dtype == SFMP_TYPE_BF16;
   const hipStream_t stream = (hipStream_t)hip_stream;
   if (batch->max_rows == 0) return SFMP_OK;
-  const AttentionForm f = choose_form(layout->head_dim, layout->kv_heads, a.group, batch->batch, batch->rows, batch->max_rows, max_tokens, window);
   auto with_dim = [&](auto fmt) {
     if (layout->head_dim == 64) return launch_attention<64, fmt()>(a, f, batch->max_rows, workspace_dev, stream);
     if (layout->head_dim == 128) return launch_attention<128, fmt()>(a, f, batch->max_rows, workspace_dev, stream);

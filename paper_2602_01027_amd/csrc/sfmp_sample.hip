@@ -803,11 +803,12 @@ __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) 
   store_choice(a, r, row, w, sh);
 }
 
+constexpr int kMostSlices = 512;
 int slices_of(int32_t rows, int32_t vocab) {
   // slices of 4096 tokens or more, 512 workgroups at most (each adds a histogram of its own to the row's: 32 rows of 131072
   // tokens 36.7 us, with 1024 workgroups 47.5, with 256 39.9); 2^15 tokens at most
   int64_t s = vocab / 4096;
-  if (s * rows > 512) s = 512 / rows;
+  if (s * rows > kMostSlices) s = kMostSlices / rows;
   const int64_t least = ((int64_t)vocab + kMostSlice - 1) / kMostSlice;
   if (s < least) s = least;
   return (int)s;
@@ -821,17 +822,29 @@ bool whole_rows(int32_t rows, int32_t vocab) { return rows >= 110 || (int64_t)vo
 struct SampleWorkspace {
   int64_t max_at, mass_at, count_at, list_at, wanted_at, listed_at, bytes;
 };
-SampleWorkspace sample_workspace(int32_t rows, int32_t vocab) {
+SampleWorkspace sample_workspace(int32_t rows, int64_t slices) {  // (of all rows)
   SampleWorkspace w{};
   w.bytes = 256;
-  if (rows == 0 || whole_rows(rows, vocab)) return w;
+  if (rows == 0) return w;
   w.count_at = round_up_256((int64_t)rows * kBins * 8);
   w.list_at = w.count_at + round_up_256((int64_t)rows * kBins * 4);
   w.wanted_at = w.list_at + round_up_256((int64_t)rows * kListed * sizeof(Listed));
   w.listed_at = w.wanted_at + round_up_256((int64_t)rows * sizeof(Wanted));
   w.max_at = w.listed_at + round_up_256((int64_t)rows * 4);
-  w.bytes = w.max_at + round_up_256((int64_t)rows * slices_of(rows, vocab) * 4);
+  w.bytes = w.max_at + round_up_256(slices * 4);
   return w;
+}
+// What a call needs
+SampleWorkspace workspace_of_call(int32_t rows, int32_t vocab) {
+  return whole_rows(rows, vocab) ? sample_workspace(0, 0) : sample_workspace(rows, (int64_t)rows * slices_of(rows, vocab));
+}
+// What every call of no more rows and tokens can do with: the most rows of such a vocabulary that are cut (whole_rows), and as many
+// slices as calls up to there have.
+int64_t workspace_up_to(int32_t rows, int32_t vocab) {
+  int32_t cut = rows < 109 ? rows : 109;
+  while (cut > 0 && whole_rows(cut, vocab)) --cut;
+  const int64_t least = (int64_t)cut * (((int64_t)vocab + kMostSlice - 1) / kMostSlice);
+  return sample_workspace(cut, least > kMostSlices ? least : kMostSlices).bytes;
 }
 
 template <int T>
@@ -854,6 +867,10 @@ int launch_sample(const SampleArgs& a, hipStream_t stream) {
   return SFMP_ERR_HIP;
 }
 
+int check_rows(int32_t rows, int32_t vocab) {
+  return rows < 0 || rows > 65535 || vocab < 1 || vocab > (1 << 24) ? SFMP_ERR_SHAPE : SFMP_OK;
+}
+
 }  // namespace
 }  // namespace sfmp
 
@@ -861,8 +878,8 @@ using namespace sfmp;
 
 extern "C" int sfmp_sample_workspace(int32_t rows, int32_t vocab, int64_t* bytes) {
   if (!bytes) return SFMP_ERR_NULL;
-  if (rows < 0 || rows > 65535 || vocab < 1 || vocab > (1 << 24)) return SFMP_ERR_SHAPE;
-  *bytes = sample_workspace(rows, vocab).bytes;
+  if (int e = check_rows(rows, vocab)) return e;
+  *bytes = workspace_up_to(rows, vocab);
   return SFMP_OK;
 }
 
@@ -870,8 +887,7 @@ extern "C" int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, 
                            const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev,
                            const float* min_p_dev, const float* uniform_dev, int32_t* tokens_dev, float* logprobs_dev,
                            void* workspace_dev, int64_t workspace_bytes, void* hip_stream) {
-  int64_t need = 0;
-  if (int e = sfmp_sample_workspace(rows, vocab, &need)) return e;
+  if (int e = check_rows(rows, vocab)) return e;
   if (dtype != SFMP_TYPE_FP16 && dtype != SFMP_TYPE_BF16 && dtype != SFMP_TYPE_FP32) return SFMP_ERR_LAYOUT;
   if (stride < vocab || stride > INT64_MAX / 8 / 65536) return SFMP_ERR_SHAPE;
   if (rows == 0) return SFMP_OK;
@@ -880,8 +896,8 @@ extern "C" int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, 
   if (off(logits_dev, dtype == SFMP_TYPE_FP32 ? 4 : 2) || off(temperature_dev, 4) || off(top_k_dev, 4) || off(top_p_dev, 4) ||
       off(min_p_dev, 4) || off(uniform_dev, 4) || off(tokens_dev, 4) || off(logprobs_dev, 4))
     return SFMP_ERR_ALIGN;
-  if (!workspace_dev || off(workspace_dev, 256) || workspace_bytes < need) return SFMP_ERR_WORKSPACE;
-  const SampleWorkspace w = sample_workspace(rows, vocab);
+  const SampleWorkspace w = workspace_of_call(rows, vocab);
+  if (!workspace_dev || off(workspace_dev, 256) || workspace_bytes < w.bytes) return SFMP_ERR_WORKSPACE;
   uint8_t* const at = (uint8_t*)workspace_dev;
   const SampleArgs a{logits_dev, rows, vocab, slices_of(rows, vocab), stride, temperature_dev, top_k_dev, top_p_dev, min_p_dev,
                      uniform_dev, tokens_dev, logprobs_dev, (float*)(at + w.max_at), (Listed*)(at + w.list_at), (Wanted*)(at + w.wanted_at),

@@ -158,6 +158,7 @@ def sfmp_kv_gather(cache: DeviceKvCache, layer: int, tables: DeviceKvTables, slo
 
 
 def sfmp_kv_attention_workspace(layout: SfmpKvLayout, batch: int, rows: int, q_heads: int, max_rows: int, max_tokens: int) -> int:
+    """Bytes that are enough for these sizes and for smaller ones."""
     n = C.c_int64(0)
     _check(load_library().sfmp_kv_attention_workspace(C.byref(layout), int(batch), int(rows), int(q_heads), int(max_rows),
                                                       int(max_tokens), C.byref(n)))
@@ -239,6 +240,7 @@ def sfmp_kv_compact(cache: DeviceKvCache, tables: DeviceKvTables, status, worksp
 
 
 def sfmp_sample_workspace(rows: int, vocab: int) -> int:
+    """Bytes that are enough for so many rows of so many tokens and for fewer."""
     n = C.c_int64(0)
     _check(load_library().sfmp_sample_workspace(int(rows), int(vocab), C.byref(n)))
     return int(n.value)

@@ -1,4 +1,7 @@
 """What the binding of the cache and sampling calls does with arguments before the library sees them (no GPU)."""
+import math
+import random
+
 import pytest
 
 import paper_2602_01027_amd as S
@@ -10,3 +13,40 @@ def test_a_workspace_has_to_be_contiguous_memory_of_the_gpu():
         with pytest.raises(ValueError, match="workspace has to be"):
             S.kv._workspace(bad)
     assert S.kv._workspace(None) == (None, 0) and S.kv._workspace(torch.zeros(0)) == (None, 0)
+
+
+def test_a_workspace_is_enough_for_smaller_calls():
+    """Forms that need none and forms that need much follow each other as a call grows: 512 sequences of 8192 tokens are cut into parts, 513 are
+    not; 77 rows of 131072 tokens are cut into slices, 78 are not."""
+    L = S.sfmp_kv_query(16, 8, 128)
+    assert S.sfmp_kv_attention_workspace(L, 513, 513, 32, 1, 8192) >= S.sfmp_kv_attention_workspace(L, 512, 512, 32, 1, 8192) > 4 << 20
+    assert S.sfmp_sample_workspace(78, 131072) >= S.sfmp_sample_workspace(77, 131072) > 7 << 20
+    assert S.sfmp_sample_workspace(1, 1000) == 256 and S.sfmp_kv_attention_workspace(L, 1, 1, 32, 1, 64) == 256
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_workspaces_never_fall_as_calls_grow(dim):
+    rng = random.Random(dim)
+    log = lambda lo, hi: int(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.99))))  # noqa: E731
+    seen = set()
+    for _ in range(4000):
+        heads, group = rng.choice((1, 2, 8, 16)), rng.choice((1, 2, 4, 5, 8, 16, 40))
+        L = S.sfmp_kv_query(16, heads, dim)
+        big = [log(1, 700), log(1, 300), log(1, 40000)]  # entries, rows of one, tokens
+        for k in range(3):
+            if rng.random() < 0.2:
+                big[k] = rng.choice(((255, 256, 257, 511, 512, 513), (16, 17, 32, 64, 65), (64, 1024, 1025, 2048, 2049))[k])
+        small = [max(1, log(1, n)) if rng.random() < 0.6 else max(1, n - 1) for n in big]
+        size = lambda b, r, t: S.sfmp_kv_attention_workspace(L, b, b * r, heads * group, r, t)  # noqa: E731
+        assert size(*small) <= size(*big), (heads, group, small, big)
+        assert S.sfmp_kv_attention_workspace(L, small[0], small[0] + small[1] - 1, heads * group, small[1], small[2]) <= size(*big)
+        seen.add(size(*small))
+    assert len(seen) >= 3
+
+
+def test_workspaces_of_sampling_never_fall_as_calls_grow():
+    rng = random.Random(3)
+    for _ in range(4000):
+        rows, vocab = rng.randint(1, 130), int(math.exp(rng.uniform(0, math.log(1 << 24))))
+        assert S.sfmp_sample_workspace(rng.randint(0, rows), rng.randint(1, vocab)) <= S.sfmp_sample_workspace(rows, vocab)
+        assert S.sfmp_sample_workspace(rows - 1, vocab) <= S.sfmp_sample_workspace(rows, vocab)

@@ -1,5 +1,9 @@
 """The cache and sampling calls on the GPU where sizes and arguments end."""
+import numpy as np
 import pytest
+
+from kv_util import U16, attention_bound, make_pool, make_tables, upload
+from oracle import sfmp_kv_oracle as O
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -29,3 +33,44 @@ def test_workspaces_that_are_not_contiguous_gpu_memory_are_refused():
             with pytest.raises(ValueError, match="workspace has to be"):
                 call(bad)
     torch.cuda.synchronize()
+
+
+def test_one_workspace_for_a_batch_that_shrinks():
+    # made for the largest step of a program (whose form needs none), used by the smaller ones (whose forms cut the work into parts)
+    torch, S = _torch()
+    rng = np.random.default_rng(12)
+    n, dim, heads, group, tokens = 520, 64, 2, 2, 9000
+    lengths = rng.integers(1, 130, n)
+    lengths[0] = 1000
+    pool = make_pool(rng, 1, int((-(-lengths // 64)).sum()), heads, dim, "int8")
+    tables = make_tables(rng, lengths, 16, pool["codes"].shape[1])
+    cache, dt = upload(S, pool, tables, "int8")
+    most = 40  # rows of an entry
+    size = S.sfmp_kv_attention_workspace(cache.layout, n, n * most, heads * group, most, tokens)
+    canary = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    for batch, rows in ((n, 1), (512, 1), (100, 1), (3, 1), (1, 1), (3, 8), (2, most), (100, 12), (n, 3), (300, most)):
+        start = (np.arange(batch + 1) * rows).astype(np.int32)
+        q = rng.normal(size=(batch * rows, heads * group, dim)).astype(np.float16)
+        Q, got = torch.from_numpy(q).to(DEV), torch.full((batch * rows, heads * group, dim), float("nan"), dtype=torch.float16, device=DEV)
+        S.sfmp_kv_attention(cache, 0, dt, None if batch == n else torch.arange(batch, dtype=torch.int32, device=DEV), torch.from_numpy(start).to(DEV),
+                            Q, got, rows, tokens, 0.125, canary[:size])
+        a = got.float().cpu().numpy()
+        for b in sorted({0, batch - 1, batch // 2}):
+            k, v = O.dense(pool, 0, tables, b, "int8", dim)
+            r = slice(b * rows, (b + 1) * rows)
+            want, _, spread, products = O.attention(q[r].astype(np.float64), k, v, 0.125)
+            assert (np.abs(a[r] - want) <= attention_bound(U16, want, spread, products)).all(), (batch, rows, b)
+    assert (canary[size:] == 0x5A).all()
+    # likewise rows of logits
+    rows, vocab = 130, 140000
+    size = S.sfmp_sample_workspace(rows, vocab)
+    canary = torch.full((size + 4096,), 0x5A, dtype=torch.uint8, device=DEV)
+    logits = torch.from_numpy(rng.normal(0.0, 3.0, size=(rows, vocab)).astype(np.float32)).to(DEV)
+    u = torch.from_numpy(rng.random(rows).astype(np.float32)).to(DEV)
+    tokens = torch.empty(rows, dtype=torch.int32, device=DEV)
+    S.sfmp_sample(logits, None, None, None, None, u, tokens, None, canary[:size])
+    for n in (109, 80, 79, 64, 33, 1):
+        few = torch.empty(n, dtype=torch.int32, device=DEV)
+        S.sfmp_sample(logits[:n], None, None, None, None, u[:n], few, None, canary[:size])
+        assert torch.equal(few, tokens[:n])
+    assert (canary[size:] == 0x5A).all()
