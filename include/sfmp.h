@@ -403,8 +403,8 @@ int sfmp_kv_gather(const sfmp_kv_layout_t* layout, int32_t layer, const void* co
  * it), which adds to a result less error than its own rounding to fp16.  max_tokens: at least the longest
  * sequence of the batch; tokens past it are not read.  The same call on the same inputs gives the same bits; a sequence's
  * result may differ in its last bits with the batch it is in (the work is cut by the whole batch).
- * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads, strides, max_tokens < 1, window < 0, scale not finite or not positive, or
- * batch * kv_heads * ceil(max_tokens / 64) * ceil(max_rows * q_heads / kv_heads / 16) >= 2^31.  SFMP_ERR_WORKSPACE as for sfmp_gemm; the
+ * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads, strides, max_tokens < 1, window < 0, scale not finite or not positive,
+ * max_rows * q_heads / kv_heads > 2^30, or batch * kv_heads * ceil(max_tokens / 64) * ceil(max_rows * q_heads / kv_heads / 16) >= 2^31.  SFMP_ERR_WORKSPACE as for sfmp_gemm; the
  * workspace's contents are irrelevant on entry.  sfmp_kv_attention_workspace: bytes that are enough for every call with this layout and
  * q_heads, and with no more batch entries, rows, max_rows and max_tokens than these, with any window. */
 int sfmp_kv_attention_workspace(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t q_heads,

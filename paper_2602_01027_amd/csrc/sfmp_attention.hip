@@ -1,5 +1,6 @@
 // Attention over the 8-bit paged cache.
 #include "sfmp_kv.h"
+#include "sfmp_parts.h"
 
 namespace sfmp {
 namespace {
@@ -518,15 +519,7 @@ __device__ int make_plan(const AttentionArgs& a, int rows, Plan<MOST>* plan) {
 }
 
 // Pages of every workgroup and wavefront.
-struct Share {
-  int of_wave, of_workgroup;
-};
-__device__ __forceinline__ Share share_of(const CutArgs& c, int total) {
-  Share s;
-  s.of_wave = max((total + c.workgroups * c.waves - 1) / (c.workgroups * c.waves), c.least);
-  s.of_workgroup = s.of_wave * c.waves;
-  return s;
-}
+__device__ __forceinline__ Parts parts_of(const CutArgs& c, int total) { return Parts(total, c.workgroups, c.waves, c.least); }
 
 // The batch entry that the page `at` of all belongs to: the last one that starts at or before it.
 template <int MOST>
@@ -559,10 +552,9 @@ __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_cut_kernel(Attent
   Plan<kMostPlanned>& plan = *reinterpret_cast<Plan<kMostPlanned>*>(lds + 2 * WAVES * BYTES);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int total = make_plan<64 * WAVES>(a, 16 * NT, &plan);
-  const Share share = share_of(c, total);
-  const int from = (int)min((int64_t)blockIdx.x * share.of_workgroup, (int64_t)total);
-  int at = min(from + wave * share.of_wave, total);
-  const int to = min(at + share.of_wave, total);
+  const Part part = parts_of(c, total).part(blockIdx.x, wave);
+  int at = part.begin;
+  const int to = part.end;
   uint8_t* const partials = c.partials + (int64_t)blockIdx.x * 2 * BYTES;
   keep_plan<64 * WAVES>(a, c, plan);
   int left = 0, right = 0, held = 0, head = 0, tile = 0;
@@ -636,12 +628,12 @@ __global__ __launch_bounds__((PARTS == 1 ? 4 * D : 1024)) void join_kernel(Atten
   const int dt = PARTS == 1 ? wave : blockIdx.z * 2 + wave / PARTS, part = PARTS == 1 ? 0 : wave % PARTS;
   const KvEntry e = c.entries[b];
   const int before = c.before[b];
-  const Share share = share_of(c, c.before[a.v.batch]);
+  const Parts parts = parts_of(c, c.before[a.v.batch]);
   const PageRange pages = pages_of_entry(a, e);
   const int each = pages.end - pages.begin, tiles = tiles_of_entry(a, e, 16 * NT);
   for (int tile = 0; tile < tiles; ++tile) {
     const int start = before + (head * tiles + tile) * each;
-    const int w0 = start / share.of_workgroup, w1 = (start + each - 1) / share.of_workgroup;
+    const int w0 = parts.workgroup_of(start), w1 = each > 0 ? parts.workgroup_of(start + each - 1) : w0;
     if (each > 0 && w0 == w1) continue;
     const int all = each > 0 ? w1 - w0 + 1 : 0, one = (all + PARTS - 1) / PARTS;
     const int from = min(part * one, all), count = min(one, all - from);
@@ -1001,10 +993,10 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_prompt_cut_kerne
   extern __shared__ __align__(16) uint8_t lds[];
   Plan<kMostPlannedPrompts>& plan = *reinterpret_cast<Plan<kMostPlannedPrompts>*>(lds + 2 * sizeof(PromptTile<D>));
   const int total = make_plan<256>(a, kPromptRows, &plan);
-  const Share share = share_of(c, total);
   keep_plan<256>(a, c, plan);
-  int at = (int)min((int64_t)blockIdx.x * share.of_workgroup, (int64_t)total);
-  const int to = min(at + share.of_workgroup, total);
+  const Part part = parts_of(c, total).whole(blockIdx.x);
+  int at = part.begin;
+  const int to = part.end;
   uint8_t* const partials = c.partials + (int64_t)blockIdx.x * 2 * kPromptPartialBytes<D>;
   while (at < to) {
     const int held = entry_of_page(a, plan, at);
@@ -1031,10 +1023,10 @@ __global__ __launch_bounds__(256) void join_prompt_kernel(AttentionArgs a, CutAr
   const KvEntry e = c.entries[b];
   const int tiles = tiles_of_entry(a, e, kPromptRows);
   if (tile >= tiles) return;
-  const Share share = share_of(c, c.before[a.v.batch]);
+  const Parts parts = parts_of(c, c.before[a.v.batch]);
   const PageRange pages = pages_of_entry(a, e);
   const int each = pages.end - pages.begin, start = c.before[b] + (head * tiles + tile) * each;
-  const int w0 = start / share.of_workgroup, w1 = each ? (start + each - 1) / share.of_workgroup : w0 - 1;
+  const int w0 = parts.workgroup_of(start), w1 = each ? parts.workgroup_of(start + each - 1) : w0 - 1;
   if (w0 == w1) return;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   auto at = [&](int w) { return c.partials + ((int64_t)w * 2 + (w == w0)) * kPromptPartialBytes<D>; };
@@ -1205,8 +1197,8 @@ int check_sizes(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int
       q_heads % layout->kv_heads || q_heads > 65536 || max_tokens < 1 || max_tokens > kMaxTablePages * kPage)
     return SFMP_ERR_SHAPE;
   const int64_t pages = ((int64_t)max_tokens + kPage - 1) / kPage;
-  const int64_t tiles = ((int64_t)max_rows * (q_heads / layout->kv_heads) + 15) / 16;
-  if ((tiles && pages > INT32_MAX / tiles) || (int64_t)batch * layout->kv_heads * pages * tiles > INT32_MAX) return SFMP_ERR_SHAPE;
+  const int64_t unit_rows = (int64_t)max_rows * (q_heads / layout->kv_heads), tiles = (unit_rows + 15) / 16;
+  if (unit_rows > kMaxRows || (tiles && pages > INT32_MAX / tiles) || (int64_t)batch * layout->kv_heads * pages * tiles > INT32_MAX) return SFMP_ERR_SHAPE;
   return SFMP_OK;
 }
 

@@ -50,3 +50,13 @@ def test_workspaces_of_sampling_never_fall_as_calls_grow():
         rows, vocab = rng.randint(1, 130), int(math.exp(rng.uniform(0, math.log(1 << 24))))
         assert S.sfmp_sample_workspace(rng.randint(0, rows), rng.randint(1, vocab)) <= S.sfmp_sample_workspace(rows, vocab)
         assert S.sfmp_sample_workspace(rows - 1, vocab) <= S.sfmp_sample_workspace(rows, vocab)
+
+
+def test_rows_of_a_head_stay_below_2_to_the_30():
+    # (rows of an entry times query heads of a key head are counted in 32 bits)
+    L = S.sfmp_kv_query(16, 1, 64)
+    assert S.sfmp_kv_attention_workspace(L, 1, 2 ** 28, 4, 2 ** 28, 64) > 0
+    for rows, heads in ((2 ** 28 + 1, 4), (2 ** 30, 2), (2 ** 29, 4), (2 ** 26, 64)):
+        with pytest.raises(S.SfmpError) as e:
+            S.sfmp_kv_attention_workspace(L, 1, rows, heads, rows, 64)
+        assert e.value.code == -2
