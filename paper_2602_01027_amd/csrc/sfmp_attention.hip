@@ -1269,7 +1269,8 @@ extern "C" int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, 
   a.o_stride = o_stride;
   a.q_heads = q_heads;
   a.group = group;
-  a.window = window;
+  // (a window longer than any sequence is none: positions less a window stay within 32 bits, also those of rows before the first token)
+  a.window = window >= tables->table_pages * kPage ? 0 : window;
   a.max_pages = (max_tokens + kPage - 1) / kPage;
   a.scale = scale;
   a.bf16 = dtype == SFMP_TYPE_BF16;

@@ -74,3 +74,28 @@ def test_one_workspace_for_a_batch_that_shrinks():
         S.sfmp_sample(logits[:n], None, None, None, None, u[:n], few, None, canary[:size])
         assert torch.equal(few, tokens[:n])
     assert (canary[size:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 100, 64 * 2 ** 20])
+@pytest.mark.parametrize("entries,max_tokens", [([(8, 3), (2, 2), (30, 20)], None), ([(8, 3), (1, 700), (3, 0)], 20000), ([(300, 40), (200, 190)], None),
+                                                ([(70, 20), (200, 190)], 9000)])
+def test_windows_that_reach_past_every_sequence(entries, max_tokens, window):
+    # rows that stand before the first token, and a window whose end lies 2^31 before the others: the same bits as without a window
+    torch, S = _torch()
+    rng = np.random.default_rng(21)
+    heads, group, dim = 2, 2, 128
+    lengths, counts = [t for _, t in entries], [n for n, _ in entries]
+    tokens = max_tokens or max(lengths)
+    pages = sum(-(-t // 64) for t in lengths)
+    cache, dt = upload(S, make_pool(rng, 1, pages, heads, dim, "int8"), make_tables(rng, lengths, -(-max(lengths) // 64), pages), "int8")
+    start = torch.from_numpy(np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)).to(DEV)
+    q = torch.from_numpy(rng.normal(size=(sum(counts), heads * group, dim)).astype(np.float16)).to(DEV)
+    ws = torch.empty(S.sfmp_kv_attention_workspace(cache.layout, len(entries), sum(counts), heads * group, max(counts), tokens), dtype=torch.uint8,
+                     device=DEV)
+    results = []
+    for w in (0, window):
+        out, lse = torch.full_like(q, float("nan")), torch.full(q.shape[:2], float("nan"), device=DEV)
+        S.sfmp_kv_attention(cache, 0, dt, None, start, q, out, max(counts), tokens, 0.09, ws, window=w, lse=lse)
+        results.append((out, lse))
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+    assert not torch.isneginf(results[0][1][-1]).any() or lengths[-1] == 0
