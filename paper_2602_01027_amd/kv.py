@@ -30,11 +30,20 @@ class DeviceKvTables:
     refs: object
 
 
+def _int(x, what: str) -> int:
+    """A number that the C call takes as int32 (ctypes would cut it off)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        raise ValueError(f"{what} has to fit 32 bits, got {x}")
+    return x
+
+
 def sfmp_kv_query(pages: int, kv_heads: int, head_dim: int, format: str = "int8", layers: int = 1) -> SfmpKvLayout:
     """Layout of a pool; format "int8", "fp8" or the header's integer."""
     out = SfmpKvLayout()
-    fmt = KV_FORMATS[format] if isinstance(format, str) else int(format)
-    _check(load_library().sfmp_kv_query(int(pages), int(kv_heads), int(head_dim), fmt, int(layers), C.byref(out)))
+    fmt = KV_FORMATS[format] if isinstance(format, str) else _int(format, "format")
+    _check(load_library().sfmp_kv_query(_int(pages, "pages"), _int(kv_heads, "kv_heads"), _int(head_dim, "head_dim"), fmt,
+                                        _int(layers, "layers"), C.byref(out)))
     return out
 
 
@@ -101,13 +110,13 @@ def _tables(layout: SfmpKvLayout, t: DeviceKvTables):
     table = _tensor(t.page_table, "page_table", "int32", None, None)
     sequences, width = (0, 0) if t.page_table is None else t.page_table.shape
     return SfmpKvTables(table, _tensor(t.lengths, "lengths", "int32", sequences), _tensor(t.refs, "refs", "int32", layout.pages),
-                        sequences, width)
+                        _int(sequences, "sequences"), _int(width, "table_pages"))
 
 
 def _batch(tables: DeviceKvTables, slots, row_start, rows: int, max_rows: int) -> SfmpKvBatch:
     batch = slots.shape[0] if slots is not None else row_start.shape[0] - 1 if row_start is not None else rows
-    return SfmpKvBatch(_tensor(slots, "slots", "int32", None), _tensor(row_start, "row_start", "int32", batch + 1), batch, rows,
-                       int(max_rows), 0)
+    return SfmpKvBatch(_tensor(slots, "slots", "int32", None), _tensor(row_start, "row_start", "int32", batch + 1), _int(batch, "batch"),
+                       _int(rows, "rows"), _int(max_rows, "max_rows"), 0)
 
 
 def _workspace(t):
@@ -136,7 +145,7 @@ def sfmp_kv_append(cache: DeviceKvCache, layer: int, tables: DeviceKvTables, slo
     if V.shape != K.shape or v_dtype != dtype:
         raise ValueError("K and V have to be of one shape and type")
     t, b = _tables(L, tables), _batch(tables, slots, row_start, K.shape[0], max_rows)
-    _check(load_library().sfmp_kv_append(layout, layer, codes, scales, C.byref(t), C.byref(b), k, v, dtype, k_stride, v_stride,
+    _check(load_library().sfmp_kv_append(layout, _int(layer, "layer"), codes, scales, C.byref(t), C.byref(b), k, v, dtype, k_stride, v_stride,
                                          _stream_ptr(stream)))
 
 
@@ -153,15 +162,15 @@ def sfmp_kv_gather(cache: DeviceKvCache, layer: int, tables: DeviceKvTables, slo
     if V.shape != K.shape or v_dtype != dtype:
         raise ValueError("K and V have to be of one shape and type")
     t, b = _tables(L, tables), _batch(tables, slots, row_start, K.shape[0], max_rows)
-    _check(load_library().sfmp_kv_gather(layout, layer, codes, scales, C.byref(t), C.byref(b), _tensor(first, "first", "int32", b.batch),
-                                         k, v, dtype, k_stride, v_stride, _stream_ptr(stream)))
+    _check(load_library().sfmp_kv_gather(layout, _int(layer, "layer"), codes, scales, C.byref(t), C.byref(b),
+                                         _tensor(first, "first", "int32", b.batch), k, v, dtype, k_stride, v_stride, _stream_ptr(stream)))
 
 
 def sfmp_kv_attention_workspace(layout: SfmpKvLayout, batch: int, rows: int, q_heads: int, max_rows: int, max_tokens: int) -> int:
     """Bytes that are enough for these sizes and for smaller ones."""
     n = C.c_int64(0)
-    _check(load_library().sfmp_kv_attention_workspace(C.byref(layout), int(batch), int(rows), int(q_heads), int(max_rows),
-                                                      int(max_tokens), C.byref(n)))
+    _check(load_library().sfmp_kv_attention_workspace(C.byref(layout), _int(batch, "batch"), _int(rows, "rows"), _int(q_heads, "q_heads"),
+                                                      _int(max_rows, "max_rows"), _int(max_tokens, "max_tokens"), C.byref(n)))
     return int(n.value)
 
 
@@ -183,8 +192,8 @@ def sfmp_kv_attention(cache: DeviceKvCache, layer: int, tables: DeviceKvTables, 
         raise ValueError("Q and O have to be of one shape and type")
     t, b = _tables(L, tables), _batch(tables, slots, row_start, Q.shape[0], max_rows)
     at, size = _workspace(workspace)
-    _check(load_library().sfmp_kv_attention(layout, layer, codes, scales, C.byref(t), C.byref(b), q, Q.shape[1], dtype, q_stride,
-                                            int(max_tokens), int(window), float(scale), o, o_stride,
+    _check(load_library().sfmp_kv_attention(layout, _int(layer, "layer"), codes, scales, C.byref(t), C.byref(b), q, _int(Q.shape[1], "q_heads"),
+                                            dtype, q_stride, _int(max_tokens, "max_tokens"), _int(window, "window"), float(scale), o, o_stride,
                                             _tensor(lse, "lse", "float32", Q.shape[0], Q.shape[1]), at, size, _stream_ptr(stream)))
 
 
@@ -242,7 +251,7 @@ def sfmp_kv_compact(cache: DeviceKvCache, tables: DeviceKvTables, status, worksp
 def sfmp_sample_workspace(rows: int, vocab: int) -> int:
     """Bytes that are enough for so many rows of so many tokens and for fewer."""
     n = C.c_int64(0)
-    _check(load_library().sfmp_sample_workspace(int(rows), int(vocab), C.byref(n)))
+    _check(load_library().sfmp_sample_workspace(_int(rows, "rows"), _int(vocab, "vocab"), C.byref(n)))
     return int(n.value)
 
 
@@ -257,7 +266,7 @@ def sfmp_sample(logits, temperature, top_k, top_p, min_p, uniform, tokens, logpr
         raise ValueError("logits has to be a tensor on the GPU")
     if logits.dtype not in _types() or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits has to be fp16, bf16 or fp32 [rows, vocab] with contiguous rows")
-    n, vocab = logits.shape
+    n, vocab = _int(logits.shape[0], "rows"), _int(logits.shape[1], "vocab")
     at, size = _workspace(workspace)
     _check(load_library().sfmp_sample(logits.data_ptr() or None, _types()[logits.dtype], n, vocab, logits.stride(0) if n > 1 else vocab,
                                       _tensor(temperature, "temperature", "float32", n), _tensor(top_k, "top_k", "int32", n),

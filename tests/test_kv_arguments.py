@@ -60,3 +60,15 @@ def test_rows_of_a_head_stay_below_2_to_the_30():
         with pytest.raises(S.SfmpError) as e:
             S.sfmp_kv_attention_workspace(L, 1, rows, heads, rows, 64)
         assert e.value.code == -2
+
+
+@pytest.mark.parametrize("past", [2 ** 31, 2 ** 32, 2 ** 32 + 1, -2 ** 31 - 1, 2 ** 64 + 4])
+def test_numbers_that_do_not_fit_32_bits_are_refused_not_cut_off(past):
+    L = S.sfmp_kv_query(4, 2, 64)
+    calls = [lambda k=k: S.sfmp_kv_query(*[past if i == k else (4, 2, 64, 0, 1)[i] for i in range(5)]) for k in range(5)]
+    calls += [lambda k=k: S.sfmp_kv_attention_workspace(L, *[past if i == k else (1, 4, 2, 4, 100)[i] for i in range(5)]) for k in range(5)]
+    calls += [lambda: S.sfmp_sample_workspace(past, 100), lambda: S.sfmp_sample_workspace(1, past),
+              lambda: S.kv._batch(None, None, None, 1, past), lambda: S.kv._batch(None, None, None, past, 1)]
+    for call in calls:
+        with pytest.raises(ValueError, match="fit 32 bits"):
+            call()

@@ -99,3 +99,20 @@ def test_windows_that_reach_past_every_sequence(entries, max_tokens, window):
         results.append((out, lse))
     assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
     assert not torch.isneginf(results[0][1][-1]).any() or lengths[-1] == 0
+
+
+def test_numbers_of_a_call_that_do_not_fit_32_bits_are_refused():
+    torch, S = _torch()
+    layout = S.sfmp_kv_query(4, 2, 64)
+    cache, tables = S.make_kv_cache(layout), S.make_kv_tables(layout, 2, 3)
+    x = torch.zeros((2, 2, 64), dtype=torch.float16, device=DEV)
+    i, w = torch.zeros(2, dtype=torch.int32, device=DEV), torch.zeros(1 << 16, dtype=torch.uint8, device=DEV)
+    for past in (2 ** 32, 2 ** 32 + 1, -2 ** 32):
+        for layer, max_rows, tokens, window in ((past, 1, 64, 0), (0, past, 64, 0), (0, 1, past, 0), (0, 1, 64, past)):
+            with pytest.raises(ValueError, match="fit 32 bits"):
+                S.sfmp_kv_attention(cache, layer, tables, i, None, x, x.clone(), max_rows, tokens, 1.0, w, window=window)
+        for layer, max_rows in ((past, 1), (0, past)):
+            with pytest.raises(ValueError, match="fit 32 bits"):
+                S.sfmp_kv_append(cache, layer, tables, i, None, x, x, max_rows)
+            with pytest.raises(ValueError, match="fit 32 bits"):
+                S.sfmp_kv_gather(cache, layer, tables, i, i, None, x, x.clone(), max_rows)
