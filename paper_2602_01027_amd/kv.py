@@ -113,8 +113,16 @@ def _tables(layout: SfmpKvLayout, t: DeviceKvTables):
                         _int(sequences, "sequences"), _int(width, "table_pages"))
 
 
+def _length(t, what: str) -> int:
+    """Elements of a vector."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dim() != 1:
+        raise ValueError(f"{what} has to be a vector on the GPU, got {type(t).__name__ if not isinstance(t, torch.Tensor) else list(t.shape)}")
+    return t.shape[0]
+
+
 def _batch(tables: DeviceKvTables, slots, row_start, rows: int, max_rows: int) -> SfmpKvBatch:
-    batch = slots.shape[0] if slots is not None else row_start.shape[0] - 1 if row_start is not None else rows
+    batch = _length(slots, "slots") if slots is not None else _length(row_start, "row_start") - 1 if row_start is not None else rows
     return SfmpKvBatch(_tensor(slots, "slots", "int32", None), _tensor(row_start, "row_start", "int32", batch + 1), _int(batch, "batch"),
                        _int(rows, "rows"), _int(max_rows, "max_rows"), 0)
 
@@ -209,7 +217,7 @@ def sfmp_kv_reserve(cache: DeviceKvCache, tables: DeviceKvTables, slots, counts,
     if rc is not None:
         return _check(rc)
     layout, codes, scales = _cache(cache)
-    t, n = _tables(cache.layout, tables), slots.shape[0]
+    t, n = _tables(cache.layout, tables), _length(slots, "slots")
     at, size = _workspace(workspace)
     _check(load_library().sfmp_kv_reserve(layout, codes, scales, C.byref(t), _tensor(slots, "slots", "int32", n),
                                           _tensor(counts, "counts", "int32", n), n, _tensor(status, "status", "int32", 1), at, size,
@@ -221,7 +229,7 @@ def sfmp_kv_fork(cache: DeviceKvCache, tables: DeviceKvTables, parents, children
     rc = _launcher().kv_fork(cache, tables, parents, children, stream)
     if rc is not None:
         return _check(rc)
-    t, n = _tables(cache.layout, tables), parents.shape[0]
+    t, n = _tables(cache.layout, tables), _length(parents, "parents")
     _check(load_library().sfmp_kv_fork(C.byref(cache.layout), C.byref(t), _tensor(parents, "parents", "int32", n),
                                        _tensor(children, "children", "int32", n), n, _stream_ptr(stream)))
 
@@ -231,7 +239,7 @@ def sfmp_kv_free(cache: DeviceKvCache, tables: DeviceKvTables, slots, keep=None,
     rc = _launcher().kv_free(cache, tables, slots, keep, stream)
     if rc is not None:
         return _check(rc)
-    t, n = _tables(cache.layout, tables), slots.shape[0]
+    t, n = _tables(cache.layout, tables), _length(slots, "slots")
     _check(load_library().sfmp_kv_free(C.byref(cache.layout), C.byref(t), _tensor(slots, "slots", "int32", n),
                                        _tensor(keep, "keep", "int32", n), n, _stream_ptr(stream)))
 

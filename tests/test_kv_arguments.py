@@ -72,3 +72,11 @@ def test_numbers_that_do_not_fit_32_bits_are_refused_not_cut_off(past):
     for call in calls:
         with pytest.raises(ValueError, match="fit 32 bits"):
             call()
+
+
+def test_slots_and_row_starts_have_to_be_vectors():
+    import torch
+    for bad in ([0], 3, torch.zeros((), dtype=torch.int32), torch.zeros((1, 1), dtype=torch.int32)):
+        for slots, row_start in ((bad, None), (None, bad)):
+            with pytest.raises(ValueError, match="has to be a vector"):
+                S.kv._batch(None, slots, row_start, 1, 1)

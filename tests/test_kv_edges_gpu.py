@@ -116,3 +116,15 @@ def test_numbers_of_a_call_that_do_not_fit_32_bits_are_refused():
                 S.sfmp_kv_append(cache, layer, tables, i, None, x, x, max_rows)
             with pytest.raises(ValueError, match="fit 32 bits"):
                 S.sfmp_kv_gather(cache, layer, tables, i, i, None, x, x.clone(), max_rows)
+
+
+def test_calls_on_pages_refuse_what_is_no_vector():
+    torch, S = _torch()
+    layout = S.sfmp_kv_query(4, 2, 64)
+    cache, tables = S.make_kv_cache(layout), S.make_kv_tables(layout, 2, 3)
+    i, w = torch.zeros(1, dtype=torch.int32, device=DEV), torch.zeros(1 << 16, dtype=torch.uint8, device=DEV)
+    for bad in (None, [0], 0, i[0], i[None]):
+        for call in (lambda: S.sfmp_kv_reserve(cache, tables, bad, None, i, w), lambda: S.sfmp_kv_fork(cache, tables, bad, i),
+                     lambda: S.sfmp_kv_free(cache, tables, bad)):
+            with pytest.raises(ValueError, match="has to be a vector"):
+                call()
