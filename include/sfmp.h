@@ -403,7 +403,8 @@ int sfmp_kv_gather(const sfmp_kv_layout_t* layout, int32_t layer, const void* co
  * it), which adds to a result less error than its own rounding to fp16.  max_tokens: at least the longest
  * sequence of the batch; tokens past it are not read.  The same call on the same inputs gives the same bits; a sequence's
  * result may differ in its last bits with the batch it is in (the work is cut by the whole batch).
- * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads, strides, max_tokens < 1, window < 0, scale not finite or not positive,
+ * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads (no multiple of kv_heads, or above 65536), strides,
+ * batch > 65535, max_tokens < 1 or above 2^26, window < 0, scale not finite or not positive,
  * max_rows * q_heads / kv_heads > 2^30, or batch * kv_heads * ceil(max_tokens / 64) * ceil(max_rows * q_heads / kv_heads / 16) >= 2^31.  SFMP_ERR_WORKSPACE as for sfmp_gemm; the
  * workspace's contents are irrelevant on entry.  sfmp_kv_attention_workspace: bytes that are enough for every call with this layout and
  * q_heads, and with no more batch entries, rows, max_rows and max_tokens than these, with any window. */
@@ -454,9 +455,11 @@ int sfmp_kv_compact(const sfmp_kv_layout_t* layout, void* codes_dev, float* scal
  * takes the first token of the order.  NaN logits count as -infinity; a row without a logit above -infinity gives -1
  * and the log-probability -infinity.  Sums of weights are whole numbers: the result does not depend on how the row was cut.
  * temperature, top_k, top_p, min_p: fp32 / int32 / fp32 / fp32 [rows], each may be NULL (1, all, all, all).  tokens: int32
- * [rows].  logprobs: NULL, or fp32 [rows], ln of w_token over the sum of all w of the row
- * (0 with T <= 0, where the first token has all the weight).
- * SFMP_ERR_SHAPE: rows < 0, vocab < 1 or above 2^24, stride < vocab.  Alignment: logits to their element size.
+ * [rows].  logprobs: NULL, or fp32 [rows], (l_token - m) / T less ln of the sum of all w of the
+ * row.  With w in whole units, and tokens below 2^-32 of the most probable one left out, that sum is off by at most vocab * 2^-32, and so is
+ * the log-probability: 3e-5 for 131072 tokens, which can be much of the value where one token has nearly all the weight.  With T <= 0 the
+ * tokens that share the largest logit weigh 1 each and the others nothing: 0, or where n tokens share it -ln n (the first is chosen all the same).
+ * SFMP_ERR_SHAPE: rows < 0 or above 65535, vocab < 1 or above 2^24, stride < vocab.  Alignment: logits to their element size.
  * sfmp_sample_workspace: bytes that are enough for every call of no more rows and no larger vocabulary. */
 int sfmp_sample_workspace(int32_t rows, int32_t vocab, int64_t* bytes);
 int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32_t vocab, int64_t stride,

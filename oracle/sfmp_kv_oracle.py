@@ -209,7 +209,8 @@ def compact(pool, tables):
 
 def sample(logits, temperature, top_k, top_p, min_p, u):
     """One row of logits (values that fp32 holds).  Returns (token, log-probability, margin): margin is how near, in shares of the
-    whole weight, a threshold or the random number came to deciding otherwise."""
+    whole weight, a threshold or the random number came to deciding otherwise.  At temperature 0 all tokens of the largest logit weigh
+    the same in the log-probability, though the first is chosen."""
     x = np.where(np.isnan(logits), -math.inf, logits.astype(np.float64))
     m = x.max()
     if m == -math.inf:

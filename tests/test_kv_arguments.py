@@ -2,8 +2,10 @@
 import math
 import random
 
+import numpy as np
 import pytest
 
+from oracle import sfmp_kv_oracle as O
 import paper_2602_01027_amd as S
 
 
@@ -80,3 +82,21 @@ def test_slots_and_row_starts_have_to_be_vectors():
         for slots, row_start in ((bad, None), (None, bad)):
             with pytest.raises(ValueError, match="has to be a vector"):
                 S.kv._batch(None, slots, row_start, 1, 1)
+
+
+def test_sizes_past_the_limits_of_the_header():
+    L = S.sfmp_kv_query(16, 8, 128)
+    size = lambda batch=1, q_heads=8, tokens=64: S.sfmp_kv_attention_workspace(L, batch, batch, q_heads, 1, tokens)  # noqa: E731
+    assert size(batch=65535) and size(q_heads=65536) and size(tokens=2 ** 26) and S.sfmp_sample_workspace(65535, 2 ** 24)
+    for past in (lambda: size(batch=65536), lambda: size(q_heads=65544), lambda: size(q_heads=12), lambda: size(tokens=2 ** 26 + 1), lambda: size(tokens=0),
+                 lambda: S.sfmp_sample_workspace(65536, 10), lambda: S.sfmp_sample_workspace(1, 2 ** 24 + 1), lambda: S.sfmp_sample_workspace(-1, 10),
+                 lambda: S.sfmp_sample_workspace(1, 0)):
+        with pytest.raises(S.SfmpError) as e:
+            past()
+        assert e.value.code == -2
+
+
+def test_log_probability_of_a_tie_at_temperature_0():
+    x = np.array([1.0, 7.0, 7.0, -3.0, 7.0, 6.99])
+    assert O.sample(x, 0.0, 0, 1.0, 0.0, 0.9)[:2] == (1, pytest.approx(-math.log(3)))
+    assert O.sample(x[:2], 0.0, 0, 1.0, 0.0, 0.9)[:2] == (1, 0.0)

@@ -106,3 +106,34 @@ def test_intervals_that_pass_the_range_of_fp32():
     for t in (1e37, 1e38, 3.4e38):
         _check(x, t, 0, 1.0, 0.0, [0.3, 0.9])
         _check(x, t, 2, 1.0, 0.0, [0.9, 0.6])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("rows,vocab", [(3, 1000), (3, 131072), (120, 5000)])
+def test_log_probabilities_of_ties_at_temperature_0(rows, vocab, dtype):
+    # -ln of the number of tokens that share the largest logit, 0 where there is one
+    rng = np.random.default_rng(vocab)
+    x = rng.normal(size=(rows, vocab)).astype(np.float32)
+    ties = rng.choice([1, 2, 7, 900], rows)
+    first = []
+    for r in range(rows):
+        at = rng.permutation(vocab)[:ties[r]]
+        x[r, at] = 9.5
+        first.append(int(at.min()))
+    tokens, logprobs, _ = _run(x, 0.0, 0, 1.0, 0.0, 0.7, dtype=dtype)
+    assert tokens.tolist() == first
+    assert (logprobs[ties == 1] == 0).all() and np.allclose(logprobs, -np.log(ties), rtol=1e-6)
+
+
+@pytest.mark.parametrize("rows", [2, 120])
+def test_log_probability_where_the_others_are_below_the_unit(rows):
+    # one token with nearly all the weight: off by what the others lose or gain in whole units of 2^-31, 2^-32 for each at most
+    vocab = 70000
+    for other in (-24.0, -22.3, -22.0, -21.0, -20.0):
+        x = np.full((rows, vocab), other, dtype=np.float32)
+        x[:, 5] = 0.0
+        tokens, logprobs, _ = _run(x, 1.0, 0, 1.0, 0.0, 0.0)
+        want = -math.log1p((vocab - 1) * math.exp(other))
+        assert (tokens == 5).all() and (np.abs(logprobs - want) <= vocab * 2.0 ** -32 + 1e-6 * abs(want)).all()
+        units = (vocab - 1) * round(math.exp(other) * 2 ** 31) * 2.0 ** -31
+        assert np.allclose(logprobs, -math.log1p(units), rtol=1e-6, atol=0.0)
