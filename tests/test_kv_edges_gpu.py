@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from kv_util import U16, attention_bound, make_pool, make_tables, upload
+from kv_util import U16, UB16, attention_bound, make_pool, make_tables, upload
 from oracle import sfmp_kv_oracle as O
 
 pytestmark = pytest.mark.gpu
@@ -128,3 +128,49 @@ def test_calls_on_pages_refuse_what_is_no_vector():
                      lambda: S.sfmp_kv_free(cache, tables, bad)):
             with pytest.raises(ValueError, match="has to be a vector"):
                 call()
+
+
+def _weights_floor(q, k, v, scale):
+    """What weights held in units of 2^-38 of their page's largest add to a result: 2^-39 of that largest weight for every token of the
+    page, times the token's value."""
+    n, heads, dim = q.shape
+    t, group = k.shape[0], heads // k.shape[1]
+    out = np.zeros((n, heads, dim))
+    for i in range(n):
+        p = t - n + i
+        for h in range(heads):
+            z = scale * (k[:p + 1, h // group] @ q[i, h].astype(np.float64))
+            w = np.exp(z - z.max())
+            for page in range(0, p + 1, 64):
+                part = slice(page, min(page + 64, p + 1))
+                out[i, h] += 2.0 ** -39 * w[part].max() / w.sum() * np.abs(v[part, h // group]).sum(0)
+    return out
+
+
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("entries,max_tokens", [([(1, 500), (1, 1000), (1, 130)], 1000), ([(1, 500), (1, 1000), (1, 130)], 40000),
+                                                ([(40, 300), (33, 97), (70, 200)], 2000), ([(40, 300), (33, 97), (70, 200)], 9000)])
+@pytest.mark.parametrize("powers", [[60], [12, 30], [-30, 0, 60, 90]])
+def test_attention_over_values_of_great_magnitude(fmt, entries, max_tokens, powers):
+    # the least weights' rounding in proportion to the values that they multiply, where an absolute term does not cover it
+    torch, S = _torch()
+    rng = np.random.default_rng(len(powers) + max_tokens)
+    heads, group, dim = 2, 2, 128
+    lengths, counts = [t for _, t in entries], [n for n, _ in entries]
+    pages = sum(-(-t // 64) for t in lengths)
+    pool, tables = make_pool(rng, 1, pages, heads, dim, fmt), make_tables(rng, lengths, -(-max(lengths) // 64), pages)
+    pool["scales"][..., 1] = 2.0 ** rng.choice(powers, size=pool["scales"].shape[:3])
+    cache, dt = upload(S, pool, tables, fmt)
+    start = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    Q = torch.from_numpy(rng.normal(0.0, 4.0, size=(sum(counts), heads * group, dim)).astype(np.float32)).bfloat16().to(DEV)
+    q, out = Q.float().cpu().numpy(), torch.full_like(Q, float("nan"))
+    ws = torch.empty(S.sfmp_kv_attention_workspace(cache.layout, len(entries), sum(counts), heads * group, max(counts), max_tokens), dtype=torch.uint8,
+                     device=DEV)
+    S.sfmp_kv_attention(cache, 0, dt, None, torch.from_numpy(start).to(DEV), Q, out, max(counts), max_tokens, 0.09, ws)
+    got = out.float().cpu().numpy().astype(np.float64)
+    for b in range(len(entries)):
+        k, v = O.dense(pool, 0, tables, b, fmt, dim)
+        r = slice(start[b], start[b + 1])
+        want, _, spread, products = O.attention(q[r], k, v, 0.09)
+        bound = attention_bound(UB16, want, spread, products) + _weights_floor(q[r], k, v, 0.09)
+        assert (np.abs(got[r] - want) <= bound).all(), (b, (np.abs(got[r] - want) / bound).max())
