@@ -406,7 +406,8 @@ int sfmp_kv_gather(const sfmp_kv_layout_t* layout, int32_t layer, const void* co
  * SFMP_ERR_SHAPE (beside the bounds above: table_pages > 2^20, rows > 2^30): q_heads (no multiple of kv_heads, or above 65536), strides,
  * batch > 65535, max_tokens < 1 or above 2^26, window < 0, scale not finite or not positive,
  * max_rows * q_heads / kv_heads > 2^30, or batch * kv_heads * ceil(max_tokens / 64) * ceil(max_rows * q_heads / kv_heads / 16) >= 2^31.  SFMP_ERR_WORKSPACE as for sfmp_gemm; the
- * workspace's contents are irrelevant on entry.  sfmp_kv_attention_workspace: bytes that are enough for every call with this layout and
+ * workspace's contents are irrelevant on entry.  Weights stand relative to a score that the largest exceeds by less than a factor of 2^16 while they are
+ * added up: |V| times the tokens seen has to stay below 2^111.  sfmp_kv_attention_workspace: bytes that are enough for every call with this layout and
  * q_heads, and with no more batch entries, rows, max_rows and max_tokens than these, with any window. */
 int sfmp_kv_attention_workspace(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t q_heads,
                                 int32_t max_rows, int32_t max_tokens, int64_t* bytes);

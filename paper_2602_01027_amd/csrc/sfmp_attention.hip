@@ -9,7 +9,9 @@ namespace {
 template <int D, int NT>
 constexpr int kWaves = D * NT >= 256 ? 4 : 8;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
-// Weights are rounded to fp16 in units of 2^-14: they keep their 11 bits down to 2^-28 of the largest.
+// Weights are rounded to fp16, which the matrix cores take them in (their sum is not), in units of 2^-14: they keep their 11 bits down to 2^-28 of the
+// largest.  It adds up to a seventh to the error of an fp16 result (2.1e-4 of it in the 2-norm, with unrounded weights, 2.4e-4 at most in
+// the cases measured) and none that shows to a bf16 one (1.7e-3).
 constexpr float kWeightUnit = 16384.0f, kWeightBits = 14.0f;
 // Sums are rescaled when a page's largest score (in units of ln 2) exceeds what they are relative to by more than this.
 constexpr float kSlack = 16.0f;
@@ -543,8 +545,8 @@ __device__ __forceinline__ void keep_plan(const AttentionArgs& a, const CutArgs&
   }
 }
 
-// Bound by HBM: 131071 tokens of 8 heads of 128 dims (268 MB) 51.5 us, 5.2 TB/s with start and end, 6.2 TB/s while it streams; 64 sequences of
-// 130 to 8190 tokens (261 MB, fp8) 56.6 us.  Requesting two pages ahead instead of one spilled registers and was slower.
+// Bound by HBM: 131071 tokens of 8 heads of 128 dims (268 MB) 51.8 us, 5.2 TB/s with start and end (vector instructions issue in a quarter of
+// that time, the matrix pipes are busy for 7 %); 64 sequences of 130 to 8190 tokens (261 MB, fp8) 56 us.  Requesting two pages ahead instead of one spilled registers and was slower.
 template <int D, int FMT, int NT>
 __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_cut_kernel(AttentionArgs a, CutArgs c) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -670,8 +672,8 @@ __global__ __launch_bounds__((PARTS == 1 ? 4 * D : 1024)) void join_kernel(Atten
 // with the values.
 //
 // 2048 rows of 32 heads over themselves, 8 key heads of 128 dims: 55 us, 617 TFLOP/s of products that count (with one group 59 us; a large
-// fp16 product of the library reaches 1110 here).  A step of two pages per SIMD takes 2.8 us: two fifths of it are matrix
-// instructions, the rest what the two wavefronts do not overlap of converting the next page, exponentials and LDS.
+// fp16 product of the library reaches 1110 here).  By the counters of a launch the matrix pipes are busy for 27 % of its cycles, vector instructions
+// (conversion of pages, masks, exponentials, rescaling) issue for 41 %, the LDS is busy for 22 %: they overlap in part.
 
 constexpr int kPromptRows = 128;  // of a workgroup
 template <int D>

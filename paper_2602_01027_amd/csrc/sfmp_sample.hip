@@ -686,7 +686,7 @@ __device__ __forceinline__ void store_none(const SampleArgs& a, int r) {
 
 // Slices: the tokens of the wanted bins into the row's list, with the sums before their bins; the workgroup of the first
 // slice leaves what the choice needs to know beside.  Every workgroup adds up the row's histogram for itself (48 KiB from the L2, instead
-// of a launch for it): 8.4 us.
+// of a launch for it): 8.9 us.
 template <int T>
 __global__ __launch_bounds__(kSliceThreads) void sample_collect_kernel(SampleArgs a) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -745,7 +745,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a)
 
 // One workgroup per row: everything.  256 rows of 100003 fp32 logits (102 MB) 62 us: about 20 us each for the maximum, which reads HBM, and for the histogram (some 20
 // instructions and two LDS atomics per logit), 15 for collecting (the row comes out of a cache by then), the rest a chain of barriers:
-// with 1000 tokens 13 us.  Neither a shorter exponential nor one atomic for both sums made a difference; keeping a part of the row in
+// with 1000 tokens 13 us.  Vector instructions issue for half of a launch's cycles, the LDS is busy for 15 %, half of that conflicts.  Neither a shorter exponential nor one atomic for both sums made a difference; keeping a part of the row in
 // registers between the passes was slower.
 template <int T>
 __global__ __launch_bounds__(kPickThreads) void sample_row_kernel(SampleArgs a) {
