@@ -546,7 +546,8 @@ __device__ __forceinline__ void keep_plan(const AttentionArgs& a, const CutArgs&
 }
 
 // Bound by HBM: 131071 tokens of 8 heads of 128 dims (268 MB) 51.8 us, 5.2 TB/s with start and end (vector instructions issue in a quarter of
-// that time, the matrix pipes are busy for 7 %); 64 sequences of 130 to 8190 tokens (261 MB, fp8) 56 us.  Requesting two pages ahead instead of one spilled registers and was slower.
+// that time, the matrix pipes are busy for 7 %); 64 sequences of 130 to 8190 tokens (261 MB, fp8) 56 us.  Requesting two pages ahead instead of
+// one spilled registers and was slower.
 template <int D, int FMT, int NT>
 __global__ __launch_bounds__((64 * kWaves<D, NT>)) void attend_cut_kernel(AttentionArgs a, CutArgs c) {
   extern __shared__ __align__(16) uint8_t lds[];
