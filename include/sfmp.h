@@ -416,6 +416,50 @@ int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, const void*
                       int32_t dtype, int64_t q_stride, int32_t max_tokens, int32_t window, float scale, void* O_dev,
                       int64_t o_stride, float* lse_dev, void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
 
+/* Device.  The same with first tokens that stay visible behind the window: a row at position p sees the tokens j <= p with
+ * j > p - window or j < sinks (window 0: all tokens j <= p, whatever `sinks`).  The pages that lie between are not read, so that an endless
+ * sequence costs what its window and its first pages do.  Positions count from the sequence's first token; keys keep the rotation that they were
+ * appended with.  Everything else, errors and workspace (sfmp_kv_attention_workspace) too, as sfmp_kv_attention; SFMP_ERR_SHAPE if sinks < 0. */
+int sfmp_kv_attention_sinks(const sfmp_kv_layout_t* layout, int32_t layer, const void* codes_dev, const float* scales_dev,
+                            const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch, const void* Q_dev, int32_t q_heads,
+                            int32_t dtype, int64_t q_stride, int32_t max_tokens, int32_t window, int32_t sinks, float scale,
+                            void* O_dev, int64_t o_stride, float* lse_dev, void* workspace_dev, int64_t workspace_bytes,
+                            void* hip_stream);
+
+/* Device.  Attention of a batch whose sequences share their first pages, group by group (samples or beams of a prompt, questions about a
+ * document, requests behind one instruction: what sfmp_kv_fork makes): the shared pages are read once for all rows of a group instead of once
+ * for each sequence.
+ *
+ * Group g is the batch entries group_start[g] .. group_start[g+1]-1 (int32 [groups + 1], ascending; entries outside of all groups attend for
+ * themselves).  sfmp_kv_share, called once for all layers when the step's tokens have been reserved, finds the pages that the sequences of each
+ * group hold in common before they differ, and divides the work; sfmp_kv_attention_shared then computes what sfmp_kv_attention_sinks does
+ * (window 0: sfmp_kv_attention), with the same O, lse, errors and numerics but for the order of its sums.  The same call on the same
+ * inputs gives the same bits.
+ *   prefix_dev: NULL, or int32 [groups], the tokens of these pages (a multiple of 64; of a group of one sequence all its full pages; 0 for an
+ *   empty group).
+ *   plan_dev: written by sfmp_kv_share, read by sfmp_kv_attention_shared; 256-byte aligned.  It holds for calls with the same batch, groups, q_heads,
+ *   max_tokens, window, sinks and pool layout until lengths, tables, slots, row or group starts change.  A plan that was made
+ *   with other numbers than the call's is not used: O and lse stay as they were.  One with the numbers of the call but of other contents
+ *   gives unspecified results.
+ * Where there is nothing to gain (no more sequences than groups, more than 64 rows of a sequence and key head, short contexts) the call runs as
+ * sfmp_kv_attention_sinks, and sfmp_kv_share only finds what prefix_dev asks for.
+ * Errors as sfmp_kv_attention_sinks; SFMP_ERR_SHAPE for groups < 0 or above 65535, SFMP_ERR_WORKSPACE for a plan that is missing, not aligned or too
+ * small too.  sfmp_kv_share_plan, sfmp_kv_attention_shared_workspace: bytes of plan and workspace that are enough for every call with this
+ * layout and q_heads, and with no more batch entries, rows, groups, max_rows and max_tokens than these. */
+int sfmp_kv_share_plan(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t groups, int32_t q_heads, int32_t max_rows,
+                       int32_t max_tokens, int64_t* bytes);
+int sfmp_kv_share(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch,
+                  const int32_t* group_start_dev, int32_t groups, int32_t q_heads, int32_t max_tokens, int32_t window,
+                  int32_t sinks, int32_t* prefix_dev, void* plan_dev, int64_t plan_bytes, void* hip_stream);
+int sfmp_kv_attention_shared_workspace(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t groups,
+                                       int32_t q_heads, int32_t max_rows, int32_t max_tokens, int64_t* bytes);
+int sfmp_kv_attention_shared(const sfmp_kv_layout_t* layout, int32_t layer, const void* codes_dev, const float* scales_dev,
+                             const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch, const int32_t* group_start_dev,
+                             int32_t groups, const void* Q_dev, int32_t q_heads, int32_t dtype, int64_t q_stride,
+                             int32_t max_tokens, int32_t window, int32_t sinks, float scale, void* O_dev, int64_t o_stride,
+                             float* lse_dev, const void* plan_dev, int64_t plan_bytes, void* workspace_dev,
+                             int64_t workspace_bytes, void* hip_stream);
+
 /* Device.  Page management without the host: no call reads anything back, so a decode loop with all of them can be
  * captured in a graph.  n sequences per call, each at most once; the arrays are int32 [n] on the device.
  *

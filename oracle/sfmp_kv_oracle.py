@@ -109,8 +109,8 @@ def dense(pool, layer, tables, slot, fmt, dim):
     return out[0], out[1]
 
 
-def attention(Q, K, V, scale, window=0):
-    """Rows Q [n, q_heads, dim], the last of a sequence with keys and values [t, heads, dim].  Returns (O, lse, spread, products):
+def attention(Q, K, V, scale, window=0, sinks=0):
+    """A row at position p sees the tokens j <= p, with a window those with j > p - window or j < sinks.  Rows Q [n, q_heads, dim], the last of a sequence with keys and values [t, heads, dim].  Returns (O, lse, spread, products):
     spread [n, q_heads, dim] is sum w |V| / sum w, products [n, q_heads] the largest scale * sum |Q K| of a seen token
     (what rounding errors are in proportion to)."""
     n, heads, dim = Q.shape
@@ -122,8 +122,9 @@ def attention(Q, K, V, scale, window=0):
         lo = max(0, p - window + 1) if window else 0
         if p < lo:
             continue
+        seen = np.r_[0:min(sinks, lo), lo:p + 1]
         for h in range(heads):
-            k, v = K[lo:p + 1, h // group], V[lo:p + 1, h // group]
+            k, v = K[seen, h // group], V[seen, h // group]
             with np.errstate(invalid="ignore"):
                 z = scale * (k @ Q[i, h].astype(np.float64))
             products[i, h] = scale * np.max(np.abs(k) @ np.abs(Q[i, h].astype(np.float64)))

@@ -63,7 +63,9 @@ EXPORTS = ("sfmp_strerror", "sfmp_pack_query", "sfmp_layout_set_quant", "sfmp_pa
            "sfmp_lut_pack", "sfmp_lut_gemv_workspace", "sfmp_lut_gemv",
            "sfmp_kv_query", "sfmp_kv_append", "sfmp_kv_gather", "sfmp_kv_attention_workspace", "sfmp_kv_attention",
            "sfmp_kv_pages_workspace", "sfmp_kv_reserve", "sfmp_kv_fork", "sfmp_kv_free", "sfmp_kv_compact",
-           "sfmp_sample_workspace", "sfmp_sample")
+           "sfmp_sample_workspace", "sfmp_sample",
+           "sfmp_kv_attention_sinks", "sfmp_kv_share_plan", "sfmp_kv_share", "sfmp_kv_attention_shared_workspace",
+           "sfmp_kv_attention_shared")
 
 
 def lib_path() -> str:
@@ -111,6 +113,11 @@ def load_library():
     lib.sfmp_kv_compact.argtypes = [KP, vp, vp, TP, vp, vp, i64, vp]
     lib.sfmp_sample_workspace.argtypes = [i32, i32, NP]
     lib.sfmp_sample.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+    lib.sfmp_kv_attention_sinks.argtypes = [KP, i32, vp, vp, TP, BP, vp, i32, i32, i64, i32, i32, i32, f32, vp, i64, vp, vp, i64, vp]
+    lib.sfmp_kv_share_plan.argtypes = lib.sfmp_kv_attention_shared_workspace.argtypes = [KP, i32, i32, i32, i32, i32, i32, NP]
+    lib.sfmp_kv_share.argtypes = [KP, TP, BP, vp, i32, i32, i32, i32, i32, vp, vp, i64, vp]
+    lib.sfmp_kv_attention_shared.argtypes = [KP, i32, vp, vp, TP, BP, vp, i32, vp, i32, i32, i64, i32, i32, i32, f32, vp, i64, vp, vp, i64, vp,
+                                             i64, vp]
     for name in EXPORTS:
         if name != "sfmp_strerror":
             getattr(lib, name).restype = C.c_int
@@ -122,6 +129,7 @@ class _NoExtension:
     """Stands in for the extension where there is none to use: leaves every call to the ctypes path."""
     gemm = gemm_static = gemv_batched = gemm_batched = staticmethod(lambda *args: None)
     kv_append = kv_gather = kv_attention = kv_reserve = kv_fork = kv_free = kv_compact = sample = gemm
+    kv_attention_sinks = kv_share = kv_attention_shared = gemm
 
 
 _LAUNCHER = None  # (library, extension module bound to it)
@@ -167,7 +175,7 @@ def _launcher():
                                                             lib.sfmp_gemm_batched)))
         module.bind_kv(SfmpKvLayout, *(C.cast(f, C.c_void_p).value for f in (
             lib.sfmp_kv_append, lib.sfmp_kv_gather, lib.sfmp_kv_attention, lib.sfmp_kv_reserve, lib.sfmp_kv_fork, lib.sfmp_kv_free,
-            lib.sfmp_kv_compact, lib.sfmp_sample)))
+            lib.sfmp_kv_compact, lib.sfmp_sample, lib.sfmp_kv_attention_sinks, lib.sfmp_kv_share, lib.sfmp_kv_attention_shared)))
     except ImportError as e:
         warnings.warn(f"launches are marshalled by ctypes, some 8 us of host time more per call: {e}; build it with "
                       "`python -m paper_2602_01027_amd.build` (or __graft_entry__.build())", RuntimeWarning, stacklevel=3)

@@ -1,0 +1,653 @@
+// Attention of a batch whose sequences share their first pages, group by group: the shared pages are read once for the rows of
+// the whole group.
+//
+// A row's softmax falls into that over the pages it shares and that over its sequence's own.  Of each part there are the largest score m, the
+// sum l of 2^(score - m) and the sum o of 2^(score - m) V; both parts together have m = max(m1, m2), l = l1 2^(m1 - m) + l2 2^(m2 - m), o
+// likewise.  So the rows of a group, which lie one behind the other, are one tall matrix over the shared pages, and every sequence goes on by
+// itself behind them.  All of it is one row of (unit, page) steps, shared ones first, that is cut into parts as equal in time as the two kinds allow:
+// a plan, made once for all layers of a step, says which workgroup starts where.  A launch does the parts, a second one adds up what they
+// left, by rows.
+#include "sfmp_attention.h"
+
+namespace sfmp {
+namespace {
+
+constexpr int32_t kPlanMagic = 0x5348504C;
+constexpr int kMostOwnRows = 64;     // rows of an entry and key head
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanHeadBytes = 256;
+constexpr int kMostParts = 2048;     // of shared pages, and of own ones
+
+// Numbers that a plan and the calls that use it have to agree in.
+struct PlanKey {
+  int32_t magic, batch, rows, groups, heads, q_heads, dim, max_rows, max_tokens, window, sinks, pages, sequences, table_pages, with_slots, with_starts;
+};
+struct PlanHead {
+  PlanKey key;
+  int32_t usable;            // 0: more units than the workspace holds (group starts that do not ascend)
+  int32_t group_workgroups;  // those that work on shared pages: the first ones
+  int32_t of_group_part, of_own_part;   // steps of a part
+  int32_t group_steps, own_steps;
+};
+// Rows of a group over the pages that its sequences share.
+struct GroupPlan {
+  int32_t slot;              // of a sequence that holds the pages
+  int32_t common;            // pages that all rows of the group see in full (but for a window)
+  int32_t row0, n;
+  int32_t first, last;       // smallest and largest position
+  int32_t each, tiles;       // places of the pages that the rows see, tiles of rows
+  int32_t before, unit0;     // steps and units of the groups before
+  int32_t unused[6];
+};
+// A sequence behind them.
+struct EntryPlan {
+  KvEntry entry;
+  int32_t group;             // -1: none
+  int32_t common;
+  int32_t each, tiles, before, unit0;
+  int32_t unused[6];
+};
+// Where a part starts: group or entry, its unit (head * tiles + tile), place of the page.
+struct PartStart {
+  int32_t of, unit, first, unused;
+};
+static_assert(sizeof(PlanKey) == 64 && sizeof(PlanHead) <= kPlanHeadBytes && sizeof(GroupPlan) == 64 && sizeof(EntryPlan) == 64 && sizeof(PartStart) == 16, "");
+
+// How a call runs.
+struct SharedForm {
+  bool shared;               // else as sfmp_kv_attention
+  int tile_rows;             // of a unit of shared pages: 16, 32 (a wavefront's) or kPromptRows (a workgroup's)
+  int workgroups;
+  int group_parts, own_parts;        // at most
+  int group_least, own_least;        // steps of a part
+  int64_t group_units, own_units;    // at most
+  float group_cost;                  // time of a step of shared pages, in that of an own one of a wavefront
+};
+
+struct SharedArgs {
+  PlanHead* head;
+  GroupPlan* groups;
+  EntryPlan* entries;
+  int32_t* row_entry;        // [rows] its batch entry
+  int32_t* row_at;           // [rows] its position
+  PartStart* group_starts;
+  PartStart* own_starts;
+  PlanKey key;
+  const int32_t* group_start;
+  int32_t* prefix;           // or null
+  int32_t tile_rows, workgroups, group_least, own_least;
+  int64_t group_units, own_units;
+  float group_cost;
+  // partial results: o [slot][rows][dim], m and l [slot][rows][2].  The slot of a unit in a part is the sum of their numbers: from one
+  // (part, unit) to the next in the row of steps, one of them or both go up by one.
+  float* group_o;
+  float* group_ml;
+  float* own_o;
+  float* own_ml;
+};
+
+// ---- the plan ------------------------------------------------------------------------------------------------------
+
+// Pages of the list that are shared ones, and those that are not.
+template <bool SINKS>
+__device__ __forceinline__ PageRange<SINKS> pages_below(const PageRange<SINKS>& p, int common) {
+  if constexpr (SINKS) {
+    const int edge = min(p.edge, common), w0 = p.edge + p.gap, w1 = min(p.end + p.gap, common);
+    return PageRange<true>{0, edge + max(w1 - w0, 0), edge, w0 - edge};
+  } else {
+    return PageRange<false>{p.begin, max(min(p.end, common), p.begin)};
+  }
+}
+template <bool SINKS>
+__device__ __forceinline__ PageRange<SINKS> pages_from(const PageRange<SINKS>& p, int common) {
+  if constexpr (SINKS) {
+    const int s0 = min(p.edge, common), w0 = max(p.edge + p.gap, common), w1 = p.end + p.gap;
+    return PageRange<true>{s0, p.edge + max(w1 - w0, 0), p.edge, w0 - p.edge};
+  } else {
+    const int begin = max(p.begin, common);
+    return PageRange<false>{begin, max(p.end, begin)};
+  }
+}
+template <bool SINKS>
+__device__ __forceinline__ PageRange<SINKS> pages_of_group(const AttentionArgs& a, const GroupPlan& g) {
+  if (g.n < 1 || g.common < 1) return no_pages<SINKS>();
+  return pages_below<SINKS>(pages_seen<SINKS>(a, g.first, g.last), g.common);
+}
+template <bool SINKS>
+__device__ __forceinline__ PageRange<SINKS> own_pages(const AttentionArgs& a, const KvEntry& e, int common) {
+  return pages_from<SINKS>(pages_of_entry<SINKS>(a, e), common);
+}
+
+// What the sequences of a group share, a workgroup per group; the last one takes the entries that belong to none.  Bound by chains of loads (group,
+// slot, length, table) and, for many sequences, by reading their rows of the page table.
+template <bool SINKS>
+__global__ __launch_bounds__(kPlanThreads) void share_groups_kernel(AttentionArgs a, SharedArgs p) {
+  __shared__ int whole, seen, first, last, end_row, differs;
+  const int g = blockIdx.x, tid = threadIdx.x, batch = a.v.batch, groups = p.key.groups;
+  const bool none = g == groups;
+  auto start_of = [&](int i) { return min(max(p.group_start[i], 0), batch); };
+  // (none: the entries before the first group and behind the last)
+  const int from = none ? 0 : start_of(g), to = none ? start_of(0) : max(start_of(g + 1), from);
+  const int from2 = none ? start_of(groups) : to, to2 = none ? batch : to;
+  if (tid == 0) whole = seen = kMaxTablePages, first = INT32_MAX, last = INT32_MIN, end_row = 0, differs = INT32_MAX;
+  __syncthreads();
+  const int row0 = from < to ? kv_entry(a.v, from).row0 : 0, slot0 = from < to ? kv_entry(a.v, from).slot : -1;
+  for (int side = 0; side < 2; ++side) {
+    const int end = side ? to2 : to;
+    for (int b = (side ? max(from2, to) : from) + tid; b < end; b += kPlanThreads) {
+      const KvEntry e = kv_entry(a.v, b);
+      atomicMin(&whole, e.length / kPage);
+      if (e.n > 0) {
+        atomicMin(&seen, max(e.length - e.n + 1, 0) / kPage);
+        atomicMin(&first, e.length - e.n);
+        atomicMax(&last, e.length - 1);
+        atomicMax(&end_row, e.row0 + e.n);
+        for (int i = 0; p.entries && i < e.n; ++i) p.row_entry[e.row0 + i] = b, p.row_at[e.row0 + i] = e.length - e.n + i;
+      }
+      if (!p.entries) continue;
+      p.entries[b].entry = e;
+      p.entries[b].group = none ? -1 : g;
+      if (none) p.entries[b].common = 0;
+    }
+  }
+  __syncthreads();
+  if (none) return;
+  // The first place in which two of the sequences differ: 256 places at a time, four sequences side by side
+  const int most = from < to ? min(whole, a.v.table_pages) : 0;
+  for (int base = 0; base < most; base += kPlanThreads / 4) {
+    const int place = base + tid % (kPlanThreads / 4);
+    if (place < most) {
+      const int32_t id = a.v.table[(int64_t)slot0 * a.v.table_pages + place];
+      bool other = false;
+#pragma unroll 8
+      for (int b = from + 1 + tid / (kPlanThreads / 4); b < to; b += 4) {
+        const int slot = a.v.slots ? a.v.slots[b] : b;  // (inside the table: a sequence outside has no page, and `most` is 0)
+        other |= a.v.table[(int64_t)slot * a.v.table_pages + place] != id;
+      }
+      if (other) atomicMin(&differs, place);
+    }
+    __syncthreads();
+    if (differs != INT32_MAX) break;
+  }
+  const int found = min(most, differs);
+  if (p.prefix && tid == 0) p.prefix[g] = found * kPage;
+  if (!p.entries) return;
+  const int common = to - from < 2 ? 0 : min(min(found, seen), a.max_pages);
+  for (int b = from + tid; b < to; b += kPlanThreads) p.entries[b].common = common;
+  if (tid == 0) {
+    GroupPlan plan{};
+    plan.slot = slot0, plan.common = common, plan.row0 = row0;
+    plan.n = (int)min((int64_t)max(end_row - row0, 0), (int64_t)(to - from) * a.v.max_rows);
+    plan.first = first, plan.last = last;
+    const PageRange<SINKS> pages = pages_of_group<SINKS>(a, plan);
+    plan.each = pages.end - pages.begin;
+    plan.tiles = plan.each ? (int)(((int64_t)plan.n * a.group + p.tile_rows - 1) / p.tile_rows) : 0;
+    p.groups[g] = plan;
+  }
+}
+
+// Sums over the threads before this one, and over all of them.
+__device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* sums, int64_t* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t up = x;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const int64_t y = __shfl_up(up, s);
+    if (lane >= s) up += y;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = up;
+  __syncthreads();
+  int64_t ahead = 0;
+  *all = 0;
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    if (w < wave) ahead += sums[w];
+    *all += sums[w];
+  }
+  return ahead + up - x;
+}
+
+// The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part.
+template <bool SINKS>
+__global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
+  __shared__ int64_t sums[kPlanThreads / 64];
+  const int tid = threadIdx.x, heads = a.v.heads;
+  int64_t group_steps = 0, group_units = 0, own_steps = 0, own_units = 0, all;
+  for (int base = 0; base < p.key.groups; base += kPlanThreads) {
+    const int g = base + tid;
+    const int64_t units = g < p.key.groups ? (int64_t)p.groups[g].tiles * heads : 0, steps = units ? units * p.groups[g].each : 0;
+    const int64_t s = scan_before(steps, sums, &all) + group_steps;
+    group_steps += all;
+    const int64_t u = scan_before(units, sums, &all) + group_units;
+    group_units += all;
+    if (g < p.key.groups) p.groups[g].before = (int)s, p.groups[g].unit0 = (int)u;
+  }
+  for (int base = 0; base < a.v.batch; base += kPlanThreads) {
+    const int b = base + tid;
+    int64_t units = 0, steps = 0;
+    if (b < a.v.batch) {
+      const KvEntry e = p.entries[b].entry;
+      const PageRange<SINKS> pages = own_pages<SINKS>(a, e, p.entries[b].common);
+      const int each = pages.end - pages.begin, tiles = each > 0 ? tiles_of_entry(a, e, 16) : 0;
+      units = (int64_t)tiles * heads;
+      steps = units * each;
+      p.entries[b].each = each, p.entries[b].tiles = tiles;
+    }
+    const int64_t s = scan_before(steps, sums, &all) + own_steps;
+    own_steps += all;
+    const int64_t u = scan_before(units, sums, &all) + own_units;
+    own_units += all;
+    if (b < a.v.batch) p.entries[b].before = (int)s, p.entries[b].unit0 = (int)u;
+  }
+  // Workgroups for shared pages and for own ones, in the proportion of their times
+  const bool usable = group_units <= p.group_units && own_units <= p.own_units && group_steps <= INT32_MAX && own_steps <= INT32_MAX;
+  const bool wide = p.tile_rows == kPromptRows;
+  const float group_time = (float)group_steps * p.group_cost, own_time = (float)own_steps;
+  int64_t group_workgroups = 0;
+  if (group_steps) {
+    group_workgroups = own_steps ? (int64_t)((float)p.workgroups * group_time / (group_time + own_time) + 0.5f) : p.workgroups;
+    group_workgroups = min(max(group_workgroups, (int64_t)1), (int64_t)p.workgroups - (own_steps > 0));
+  }
+  const int64_t group_parts = max(wide ? group_workgroups : 4 * group_workgroups, (int64_t)1), own_parts = max(4 * (p.workgroups - group_workgroups), (int64_t)1);
+  const int of_group = (int)max((group_steps + group_parts - 1) / group_parts, (int64_t)p.group_least);
+  const int of_own = (int)max((own_steps + own_parts - 1) / own_parts, (int64_t)p.own_least);
+  __syncthreads();
+  if (tid < 16) reinterpret_cast<int32_t*>(&p.head->key)[tid] = reinterpret_cast<const int32_t*>(&p.key)[tid];
+  if (tid == 0) {
+    p.head->usable = usable;
+    p.head->group_workgroups = (int)group_workgroups;
+    p.head->of_group_part = of_group, p.head->of_own_part = of_own;
+    p.head->group_steps = usable ? (int)group_steps : 0, p.head->own_steps = usable ? (int)own_steps : 0;
+  }
+  if (!usable) return;
+  for (int64_t part = tid; part < group_parts && part * of_group < group_steps; part += kPlanThreads) {
+    const int at = (int)part * of_group;
+    int lo = 0, hi = p.key.groups;  // the last group that starts at or before the step
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      (p.groups[mid].before <= at ? lo : hi) = mid;
+    }
+    const int each = max(p.groups[lo].each, 1), inside = at - p.groups[lo].before;
+    p.group_starts[part] = PartStart{lo, inside / each, inside % each, 0};
+  }
+  for (int64_t part = tid; part < own_parts && part * of_own < own_steps; part += kPlanThreads) {
+    const int at = (int)part * of_own;
+    int lo = 0, hi = a.v.batch;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      (p.entries[mid].before <= at ? lo : hi) = mid;
+    }
+    const int each = max(p.entries[lo].each, 1), inside = at - p.entries[lo].before;
+    p.own_starts[part] = PartStart{lo, inside / each, inside % each, 0};
+  }
+}
+
+// ---- attention -----------------------------------------------------------------------------------------------------
+
+// The rows of a group as those of one entry.
+struct GroupRows {
+  int32_t slot, length, row0, n, first, last;
+  const int32_t* at;
+};
+__device__ __forceinline__ int position_of(const GroupRows& e, int token) { return e.at[e.row0 + token]; }
+__device__ __forceinline__ int least_position(const GroupRows& e, int, int) { return e.first; }
+__device__ __forceinline__ int largest_position(const GroupRows& e, int, int) { return e.last; }
+
+// Whether the plan is one for this call (the same in all lanes).
+__device__ __forceinline__ bool plan_fits(const SharedArgs& p) {
+  const int lane = threadIdx.x & 63;
+  const bool other = lane < 16 && reinterpret_cast<const int32_t*>(p.head)[lane] != reinterpret_cast<const int32_t*>(&p.key)[lane];
+  return !__any(other);
+}
+
+template <int D, int NT>
+__device__ __forceinline__ void store_partial_rows(float* o, float* ml, int rows, const Partial<D, NT>& p) {
+  const int i16 = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = 16 * nt + i16;
+    if (row >= rows) continue;
+    if (g == 0) ml[2 * row] = p.m[nt], ml[2 * row + 1] = p.l[nt];
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<floatx4*>(o + row * D + 16 * dt + 4 * g) = p.o[nt][dt];
+  }
+}
+
+// NTP: tiles of 16 rows that a wavefront takes over shared pages; 0: a workgroup takes 128.
+template <int D, int NTP>
+constexpr int kWavesPerSimd = D == 256 || (D == 128 && NTP == 2) ? 1 : 2;
+
+template <int D, int FMT, int NTP, bool SINKS>
+__global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_kernel(AttentionArgs a, SharedArgs p) {
+  extern __shared__ __align__(16) uint8_t lds[];
+  if (!plan_fits(p)) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int group_workgroups = p.head->group_workgroups;
+  if ((int)blockIdx.x < group_workgroups) {
+    const int part = NTP ? blockIdx.x * 4 + wave : blockIdx.x;
+    const int64_t begin = (int64_t)part * p.head->of_group_part;
+    int left = (int)min((int64_t)p.head->of_group_part, (int64_t)p.head->group_steps - begin);
+    if (left <= 0) return;
+    const PartStart start = p.group_starts[part];
+    int g = start.of, unit = start.unit, first = start.first;
+    while (left > 0) {
+      if (g >= p.key.groups) break;
+      const GroupPlan plan = p.groups[g];
+      if (unit >= plan.tiles * a.v.heads) {  // the next group
+        ++g, unit = 0;
+        continue;
+      }
+      const GroupRows e{plan.slot, plan.common * kPage, plan.row0, plan.n, plan.first, plan.last, p.row_at};
+      const PageRange<SINKS> pages = pages_of_group<SINKS>(a, plan);
+      const int head = unit / plan.tiles, tile = unit - head * plan.tiles, count = min(plan.each - first, left);
+      const int64_t slot = (int64_t)part + plan.unit0 + unit;
+      if constexpr (NTP > 0) {
+        Rows<D, NTP> r;
+        load_rows<D, NTP>(a, e, head, tile, r);
+        Partial<D, NTP> sums;
+        accumulate<D, FMT, NTP, SINKS>(a, e, head, pages, pages.begin + first, pages.begin + first + count, r, sums);
+        store_partial_rows<D, NTP>(p.group_o + slot * (16 * NTP * D), p.group_ml + slot * (16 * NTP * 2), plan.n * a.group - tile * 16 * NTP, sums);
+      } else {
+        PromptSums<D> s;
+        attend_tile<D, FMT, 1, SINKS>(a, e, head, tile, pages, pages.begin + first, pages.begin + first + count, reinterpret_cast<PromptTile<D>*>(lds), s);
+        const int lane = threadIdx.x & 63, row = wave * 32 + (lane & 31), h = lane >> 5;
+        if (row < plan.n * a.group - tile * kPromptRows) {
+          float* const o = p.group_o + (slot * kPromptRows + row) * D + 4 * h;
+#pragma unroll
+          for (int x = 0; x < D / 32; ++x)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<floatx4*>(o + 32 * x + 8 * q) = floatx4{s.o[x][4 * q], s.o[x][4 * q + 1], s.o[x][4 * q + 2], s.o[x][4 * q + 3]};
+          float* const ml = p.group_ml + (slot * kPromptRows + row) * 2;
+          if (h == 0) ml[0] = s.m, ml[1] = s.l;
+        }
+      }
+      left -= count;
+      first = 0;
+      ++unit;
+    }
+    return;
+  }
+  const int part = ((int)blockIdx.x - group_workgroups) * 4 + wave;
+  const int64_t begin = (int64_t)part * p.head->of_own_part;
+  int left = (int)min((int64_t)p.head->of_own_part, (int64_t)p.head->own_steps - begin);
+  if (left <= 0) return;
+  const PartStart start = p.own_starts[part];
+  int b = start.of, unit = start.unit, first = start.first;
+  while (left > 0) {
+    if (b >= a.v.batch) break;
+    const EntryPlan plan = p.entries[b];
+    if (unit >= plan.tiles * a.v.heads) {
+      ++b, unit = 0;
+      continue;
+    }
+    const KvEntry e = plan.entry;
+    const PageRange<SINKS> pages = own_pages<SINKS>(a, e, plan.common);
+    const int head = unit / plan.tiles, tile = unit - head * plan.tiles, count = min(plan.each - first, left);
+    const int64_t slot = (int64_t)part + plan.unit0 + unit;
+    Rows<D, 1> r;
+    load_rows<D, 1>(a, e, head, tile, r);
+    Partial<D, 1> sums;
+    accumulate<D, FMT, 1, SINKS>(a, e, head, pages, pages.begin + first, pages.begin + first + count, r, sums);
+    store_partial_rows<D, 1>(p.own_o + slot * (16 * D), p.own_ml + slot * 32, e.n * a.group - tile * 16, sums);
+    left -= count;
+    first = 0;
+    ++unit;
+  }
+}
+
+// Adds up the partial results of a row and head, a wavefront each: of the parts of its group's unit, then of its own one's.
+template <int D>
+__global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, SharedArgs p) {
+  if (!plan_fits(p) || !p.head->usable) return;
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= (int64_t)a.v.rows * a.q_heads) return;
+  const int row = (int)(at / a.q_heads), q_head = (int)(at - (int64_t)row * a.q_heads), head = q_head / a.group, h = q_head - head * a.group;
+  const int b = p.row_entry[row];
+  if ((uint32_t)b >= (uint32_t)a.v.batch) return;
+  const EntryPlan plan = p.entries[b];
+  if (row < plan.entry.row0 || row >= plan.entry.row0 + plan.entry.n) return;  // (a row of no entry)
+  // parts [0, group_parts) and [group_parts, parts)
+  int group_parts = 0, own_parts = 0;
+  int64_t group_at = 0, own_at = 0;  // rows of the first partial results; those of the next parts lie a slot further each
+  if (plan.group >= 0 && plan.common > 0) {
+    const GroupPlan g = p.groups[plan.group];
+    const int i = (row - g.row0) * a.group + h, tile = i / p.tile_rows, unit = head * g.tiles + tile;
+    if (g.each > 0 && row >= g.row0 && row - g.row0 < g.n) {
+      const int from = g.before + unit * g.each, w0 = from / p.head->of_group_part;
+      group_parts = (from + g.each - 1) / p.head->of_group_part - w0 + 1;
+      group_at = ((int64_t)w0 + g.unit0 + unit) * p.tile_rows + i - tile * p.tile_rows;
+    }
+  }
+  if (plan.each > 0) {
+    const int i = (row - plan.entry.row0) * a.group + h, tile = i / 16, unit = head * plan.tiles + tile;
+    const int from = plan.before + unit * plan.each, w0 = from / p.head->of_own_part;
+    own_parts = (from + plan.each - 1) / p.head->of_own_part - w0 + 1;
+    own_at = ((int64_t)w0 + plan.unit0 + unit) * 16 + i - tile * 16;
+  }
+  const int parts = group_parts + own_parts;
+  auto ml_of = [&](int i) {
+    return i < group_parts ? p.group_ml + 2 * (group_at + (int64_t)i * p.tile_rows) : p.own_ml + 2 * (own_at + (int64_t)(i - group_parts) * 16);
+  };
+  float m = -INFINITY;
+  for (int i = lane; i < parts; i += 64) m = fmaxf(m, ml_of(i)[0]);
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
+  const float base = m == -INFINITY ? 0.0f : m;
+  constexpr int EACH = D / 64;
+  float o[EACH] = {}, l = 0.0f;
+  for (int i0 = 0; i0 < parts; i0 += 64) {
+    float f = 0.0f, li = 0.0f;
+    if (i0 + lane < parts) {
+      const float* const x = ml_of(i0 + lane);
+      f = __builtin_amdgcn_exp2f(x[0] - base);
+      li = x[1] * f;
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) li += __shfl_xor(li, s);
+    l += li;
+    const int count = min(parts - i0, 64);
+    for (int i = 0; i < count; ++i) {
+      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
+      const float* const x = (i0 + i < group_parts ? p.group_o + (group_at + (int64_t)(i0 + i) * p.tile_rows) * D
+                                                   : p.own_o + (own_at + (int64_t)(i0 + i - group_parts) * 16) * D) + lane * EACH;
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) o[j] = __builtin_fmaf(x[j], fi, o[j]);
+    }
+  }
+  const bool empty = m == -INFINITY && l == 0.0f;  // (not where every score is a NaN)
+  const float inverse = empty ? 0.0f : 1.0f / l;
+  uint16_t* const dst = a.O + (int64_t)row * a.o_stride + (int64_t)q_head * D + lane * EACH;
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) dst[j] = bits_of(o[j] * inverse, a.bf16);
+  if (a.lse && lane == 0) a.lse[at] = empty ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ---- launches ------------------------------------------------------------------------------------------------------
+
+SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int groups, int max_rows, int max_tokens) {
+  SharedForm f{};
+  const int64_t own_rows = (int64_t)max_rows * group, mean = groups ? ((int64_t)rows * group + groups - 1) / groups : 0;
+  f.shared = groups > 0 && groups < batch && max_rows > 0 && own_rows <= kMostOwnRows && (int64_t)rows * heads * group <= INT32_MAX;
+  if (!f.shared) return f;
+  f.tile_rows = dim == 256 ? (mean <= 16 ? 16 : kPromptRows) : mean <= 32 ? 32 : kPromptRows;
+  f.workgroups = dim == 256 || (dim == 128 && f.tile_rows == 32) ? 256 : 512;
+  f.group_parts = f.tile_rows == kPromptRows ? f.workgroups : 4 * f.workgroups;
+  f.own_parts = 4 * f.workgroups;
+  f.group_least = f.tile_rows == kPromptRows ? 4 : 1;
+  f.own_least = 1;
+  f.group_units = ((int64_t)batch * own_rows / f.tile_rows + groups) * heads;
+  f.own_units = (int64_t)batch * ((own_rows + 15) / 16) * heads;
+  f.group_cost = f.tile_rows == kPromptRows ? 2.2f : 1.0f;
+  return f;
+}
+
+// Bytes of plan and workspace that a call needs.
+int64_t plan_bytes(const SharedForm& f, int batch, int rows, int groups) {
+  if (!f.shared) return kPlanHeadBytes;
+  return kPlanHeadBytes + (int64_t)groups * sizeof(GroupPlan) + (int64_t)batch * sizeof(EntryPlan) + 2 * kMostParts * sizeof(PartStart) +
+         round_up_256((int64_t)rows * 4) * 2;
+}
+int64_t shared_workspace(const SharedForm& f, int dim) {
+  return ((f.group_parts + f.group_units) * f.tile_rows + (f.own_parts + f.own_units) * 16) * (dim + 2) * 4;
+}
+// ... and those that every call of no more entries, rows and groups can do with: the rows of partial results are the most with large tiles.
+int64_t plan_bytes_up_to(int batch, int rows, int groups) {
+  SharedForm f{};
+  f.shared = batch > 1 && groups > 0;
+  return plan_bytes(f, batch, rows, groups);
+}
+int64_t shared_workspace_up_to(int dim, int heads, int group, int batch, int groups, int max_rows) {
+  if (batch < 2 || groups < 1 || max_rows < 1 || group > kMostOwnRows) return 0;
+  const int64_t own_rows = (int64_t)max_rows * group < kMostOwnRows ? max_rows * group : kMostOwnRows;
+  SharedForm f{};
+  f.tile_rows = kPromptRows;
+  f.group_parts = 512, f.own_parts = kMostParts;
+  f.group_units = ((int64_t)batch * own_rows / kPromptRows + 1 + (groups < batch ? groups : batch - 1)) * heads;
+  f.own_units = (int64_t)batch * ((own_rows + 15) / 16) * heads;
+  return shared_workspace(f, dim);
+}
+
+SharedArgs shared_args(const SharedForm& f, const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch,
+                       const int32_t* group_start, int groups, int q_heads, int max_tokens, int window, int sinks, void* plan) {
+  SharedArgs p{};
+  uint8_t* at = (uint8_t*)plan;
+  auto take = [&](int64_t bytes) { uint8_t* const x = at; at += bytes; return x; };
+  p.head = (PlanHead*)take(kPlanHeadBytes);
+  if (f.shared) {
+    p.groups = (GroupPlan*)take((int64_t)groups * sizeof(GroupPlan));
+    p.entries = (EntryPlan*)take((int64_t)batch->batch * sizeof(EntryPlan));
+    p.group_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
+    p.own_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
+    p.row_entry = (int32_t*)take(round_up_256((int64_t)batch->rows * 4));
+    p.row_at = (int32_t*)take(round_up_256((int64_t)batch->rows * 4));
+  }
+  p.key = PlanKey{kPlanMagic, batch->batch, batch->rows, groups, layout->kv_heads, q_heads, layout->head_dim, batch->max_rows, max_tokens, window, sinks,
+                  layout->pages, tables->sequences, tables->table_pages, batch->slots_dev != nullptr, batch->row_start_dev != nullptr};
+  p.group_start = group_start;
+  p.tile_rows = f.tile_rows, p.workgroups = f.workgroups, p.group_least = f.group_least, p.own_least = f.own_least;
+  p.group_units = f.group_units, p.own_units = f.own_units, p.group_cost = f.group_cost;
+  return p;
+}
+
+template <int D, int FMT, int NTP, bool SINKS>
+int launch_shared(const AttentionArgs& a, const SharedArgs& p, hipStream_t stream) {
+  constexpr int lds = NTP ? 0 : 2 * (int)sizeof(PromptTile<D>);
+  static_assert(kWavesPerSimd<D, NTP> * lds <= 160 * 1024, "LDS of a compute unit");
+  if (lds)
+    if (int e = allow_full_lds((const void*)attend_shared_kernel<D, FMT, NTP, SINKS>, "attend_shared_kernel")) return e;
+  attend_shared_kernel<D, FMT, NTP, SINKS><<<p.workgroups, 256, lds, stream>>>(a, p);
+  const int64_t joins = ((int64_t)a.v.rows * a.q_heads + 3) / 4;
+  join_shared_kernel<D><<<(uint32_t)joins, 256, 0, stream>>>(a, p);
+  return kv_launched("attend_shared_kernel");
+}
+
+template <int D, int FMT, bool SINKS>
+int launch_shared_rows(const AttentionArgs& a, const SharedArgs& p, hipStream_t stream) {
+  if (p.tile_rows == kPromptRows) return launch_shared<D, FMT, 0, SINKS>(a, p, stream);
+  return launch_shared<D, FMT, (D == 256 ? 1 : 2), SINKS>(a, p, stream);
+}
+
+template <bool SINKS>
+int launch_shared_kind(int dim, int format, const AttentionArgs& a, const SharedArgs& p, hipStream_t stream) {
+  if (format == SFMP_KV_INT8) {
+    if (dim == 64) return launch_shared_rows<64, SFMP_KV_INT8, SINKS>(a, p, stream);
+    if (dim == 128) return launch_shared_rows<128, SFMP_KV_INT8, SINKS>(a, p, stream);
+    return launch_shared_rows<256, SFMP_KV_INT8, SINKS>(a, p, stream);
+  }
+  if (dim == 64) return launch_shared_rows<64, SFMP_KV_FP8, SINKS>(a, p, stream);
+  if (dim == 128) return launch_shared_rows<128, SFMP_KV_FP8, SINKS>(a, p, stream);
+  return launch_shared_rows<256, SFMP_KV_FP8, SINKS>(a, p, stream);
+}
+
+// What both calls take and check.
+int check_shared(const sfmp_kv_layout_t* layout, const sfmp_kv_batch_t* batch, const int32_t* group_start, int32_t groups, int32_t q_heads,
+                 int32_t max_tokens, int32_t window, int32_t sinks) {
+  if (int e = check_sizes(layout, batch->batch, batch->rows, q_heads, batch->max_rows, max_tokens)) return e;
+  if (groups < 0 || groups > 65535 || window < 0 || sinks < 0) return SFMP_ERR_SHAPE;
+  if (groups && !group_start) return SFMP_ERR_NULL;
+  if (!kv_aligned(group_start, 4)) return SFMP_ERR_ALIGN;
+  return SFMP_OK;
+}
+
+int check_group_sizes(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t groups, int32_t q_heads, int32_t max_rows, int32_t max_tokens) {
+  if (int e = check_sizes(layout, batch, rows, q_heads, max_rows, max_tokens)) return e;
+  return groups < 0 || groups > 65535 ? SFMP_ERR_SHAPE : SFMP_OK;
+}
+
+}  // namespace
+}  // namespace sfmp
+
+using namespace sfmp;
+
+extern "C" int sfmp_kv_share_plan(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t groups, int32_t q_heads, int32_t max_rows,
+                                  int32_t max_tokens, int64_t* bytes) {
+  if (!bytes) return SFMP_ERR_NULL;
+  if (int e = check_group_sizes(layout, batch, rows, groups, q_heads, max_rows, max_tokens)) return e;
+  *bytes = round_up_256(plan_bytes_up_to(batch, rows, groups));
+  return SFMP_OK;
+}
+
+extern "C" int sfmp_kv_attention_shared_workspace(const sfmp_kv_layout_t* layout, int32_t batch, int32_t rows, int32_t groups, int32_t q_heads,
+                                                  int32_t max_rows, int32_t max_tokens, int64_t* bytes) {
+  if (!bytes) return SFMP_ERR_NULL;
+  if (int e = check_group_sizes(layout, batch, rows, groups, q_heads, max_rows, max_tokens)) return e;
+  if (int e = sfmp_kv_attention_workspace(layout, batch, rows, q_heads, max_rows, max_tokens, bytes)) return e;
+  const int64_t shared = round_up_256(shared_workspace_up_to(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch, groups, max_rows));
+  if (shared > *bytes) *bytes = shared;
+  return SFMP_OK;
+}
+
+extern "C" int sfmp_kv_share(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch,
+                             const int32_t* group_start_dev, int32_t groups, int32_t q_heads, int32_t max_tokens, int32_t window, int32_t sinks,
+                             int32_t* prefix_dev, void* plan_dev, int64_t plan_bytes_given, void* hip_stream) {
+  AttentionArgs a{};
+  // (no pool is touched: any aligned address does for the check)
+  if (int e = make_kv_view(layout, 0, (const void*)(uintptr_t)256, (const float*)(uintptr_t)256, tables, batch, &a.v)) return e;
+  if (int e = check_shared(layout, batch, group_start_dev, groups, q_heads, max_tokens, window, sinks)) return e;
+  if (!kv_aligned(prefix_dev, 4)) return SFMP_ERR_ALIGN;
+  const SharedForm f = choose_shared(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch->batch, batch->rows, groups, batch->max_rows,
+                                     max_tokens);
+  if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
+  if (groups == 0 || (!f.shared && !prefix_dev)) return SFMP_OK;
+  a.group = q_heads / layout->kv_heads;
+  a.window = window >= tables->table_pages * kPage ? 0 : window;
+  a.sinks = sinks;
+  a.max_pages = (max_tokens + kPage - 1) / kPage;
+  SharedArgs p = shared_args(f, layout, tables, batch, group_start_dev, groups, q_heads, max_tokens, window, sinks, plan_dev);
+  p.prefix = prefix_dev;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const bool sinks_seen = a.window && a.sinks;
+  (sinks_seen ? share_groups_kernel<true> : share_groups_kernel<false>)<<<groups + 1, kPlanThreads, 0, stream>>>(a, p);
+  if (f.shared) (sinks_seen ? share_parts_kernel<true> : share_parts_kernel<false>)<<<1, kPlanThreads, 0, stream>>>(a, p);
+  return kv_launched("share_groups_kernel");
+}
+
+extern "C" int sfmp_kv_attention_shared(const sfmp_kv_layout_t* layout, int32_t layer, const void* codes_dev, const float* scales_dev,
+                                        const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch, const int32_t* group_start_dev, int32_t groups,
+                                        const void* Q_dev, int32_t q_heads, int32_t dtype, int64_t q_stride, int32_t max_tokens, int32_t window,
+                                        int32_t sinks, float scale, void* O_dev, int64_t o_stride, float* lse_dev, const void* plan_dev,
+                                        int64_t plan_bytes_given, void* workspace_dev, int64_t workspace_bytes, void* hip_stream) {
+  AttentionArgs a;
+  if (int e = make_kv_view(layout, layer, codes_dev, scales_dev, tables, batch, &a.v)) return e;
+  if (int e = check_shared(layout, batch, group_start_dev, groups, q_heads, max_tokens, window, sinks)) return e;
+  const SharedForm f = choose_shared(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch->batch, batch->rows, groups, batch->max_rows,
+                                     max_tokens);
+  if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
+  if (!f.shared)
+    return sfmp_kv_attention_sinks(layout, layer, codes_dev, scales_dev, tables, batch, Q_dev, q_heads, dtype, q_stride, max_tokens, window, sinks, scale,
+                                   O_dev, o_stride, lse_dev, workspace_dev, workspace_bytes, hip_stream);
+  if (int e = check_attention(layout, tables, batch, Q_dev, q_heads, dtype, q_stride, max_tokens, window, sinks, scale, O_dev, o_stride, lse_dev, &a)) return e;
+  if (batch->rows == 0 || batch->batch == 0) return SFMP_OK;
+  if (!workspace_dev || !kv_aligned(workspace_dev, 256) || workspace_bytes < shared_workspace(f, layout->head_dim)) return SFMP_ERR_WORKSPACE;
+  SharedArgs p = shared_args(f, layout, tables, batch, group_start_dev, groups, q_heads, max_tokens, window, sinks, (void*)plan_dev);
+  const int64_t group_rows = (f.group_parts + f.group_units) * f.tile_rows, own_rows = (f.own_parts + f.own_units) * 16;
+  p.group_o = (float*)workspace_dev;
+  p.own_o = p.group_o + group_rows * layout->head_dim;
+  p.group_ml = p.own_o + own_rows * layout->head_dim;
+  p.own_ml = p.group_ml + group_rows * 2;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  if (a.window && a.sinks) return launch_shared_kind<true>(layout->head_dim, layout->format, a, p, stream);
+  return launch_shared_kind<false>(layout->head_dim, layout->format, a, p, stream);
+}

@@ -235,6 +235,9 @@ PyObject* gemm_batched(PyObject*, PyObject* const* a, Py_ssize_t n) {
 struct KvApi {
   decltype(&sfmp_kv_append) append = nullptr;
   decltype(&sfmp_kv_gather) gather = nullptr;
+  decltype(&sfmp_kv_attention_sinks) attention_sinks = nullptr;
+  decltype(&sfmp_kv_share) share = nullptr;
+  decltype(&sfmp_kv_attention_shared) attention_shared = nullptr;
   decltype(&sfmp_kv_attention) attention = nullptr;
   decltype(&sfmp_kv_reserve) reserve = nullptr;
   decltype(&sfmp_kv_fork) fork = nullptr;
@@ -440,13 +443,16 @@ PyObject* kv_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 // kv_attention(cache, layer, tables, slots, row_start, Q, O, max_rows, max_tokens, scale, workspace, window, lse, stream)
+// kv_attention_sinks(... window, sinks, lse, stream)
+template <bool SINKS>
 PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (wrong_count(n, 14)) return nullptr;
+  constexpr int G = SINKS ? 1 : 0;
+  if (wrong_count(n, 14 + G)) return nullptr;
   Held held;
   CacheArg c;
   RowsArg q, o;
   sfmp_kv_batch_t b;
-  int32_t layer, max_tokens, window;
+  int32_t layer, max_tokens, window, sinks = 0;
   int64_t bytes = 0;
   const void *workspace = nullptr, *lse = nullptr;
   void* stream = nullptr;
@@ -461,11 +467,87 @@ PyObject* kv_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const float scale = (float)PyFloat_AS_DOUBLE(a[9]);
   SFMP_READ(workspace_of(a[10], &workspace, &bytes));
   SFMP_READ(int_of(a[11], &window));
-  SFMP_READ(checked(a[12], at::kFloat, {q.rows, q.heads}, &lse));
+  if constexpr (SINKS) SFMP_READ(int_of(a[12], &sinks));
+  SFMP_READ(checked(a[12 + G], at::kFloat, {q.rows, q.heads}, &lse));
+  SFMP_READ(stream_handle(a[13 + G], &stream));
+  return call([&] {
+    if constexpr (SINKS)
+      return kv.attention_sinks(&c.layout, layer, c.codes, (const float*)c.scales, &c.tables, &b, q.at, q.heads, q.type, q.stride,
+                                max_tokens, window, sinks, scale, (void*)o.at, o.stride, (float*)lse, (void*)workspace, bytes, stream);
+    else
+      return kv.attention(&c.layout, layer, c.codes, (const float*)c.scales, &c.tables, &b, q.at, q.heads, q.type, q.stride,
+                          max_tokens, window, scale, (void*)o.at, o.stride, (float*)lse, (void*)workspace, bytes, stream);
+  });
+}
+
+// First batch entries of the groups, and their end.
+Read groups_of(PyObject* starts, const void** at, int32_t* groups) {
+  if (Read r = length_of(starts, groups)) return r;
+  if (*groups < 1) return kOther;
+  if (Read r = checked(starts, at::kInt, {*groups}, at)) return r;
+  --*groups;
+  return kTaken;
+}
+
+// kv_share(cache, tables, slots, row_start, group_start, rows, q_heads, max_rows, max_tokens, plan, window, sinks, prefix, stream)
+PyObject* kv_share(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (wrong_count(n, 14)) return nullptr;
+  Held held;
+  CacheArg c;
+  sfmp_kv_batch_t b;
+  int32_t rows, groups, q_heads, max_tokens, window, sinks;
+  int64_t bytes = 0;
+  const void *starts = nullptr, *plan = nullptr, *prefix = nullptr;
+  void* stream = nullptr;
+  SFMP_READ(read_cache(a[0], a[1], &held, &c));
+  SFMP_READ(int_of(a[5], &rows));
+  SFMP_READ(read_batch(a[2], a[3], rows, a[7], &b));
+  SFMP_READ(groups_of(a[4], &starts, &groups));
+  SFMP_READ(int_of(a[6], &q_heads));
+  SFMP_READ(int_of(a[8], &max_tokens));
+  SFMP_READ(workspace_of(a[9], &plan, &bytes));
+  SFMP_READ(int_of(a[10], &window));
+  SFMP_READ(int_of(a[11], &sinks));
+  SFMP_READ(checked(a[12], at::kInt, {groups}, &prefix));
   SFMP_READ(stream_handle(a[13], &stream));
   return call([&] {
-    return kv.attention(&c.layout, layer, c.codes, (const float*)c.scales, &c.tables, &b, q.at, q.heads, q.type, q.stride,
-                        max_tokens, window, scale, (void*)o.at, o.stride, (float*)lse, (void*)workspace, bytes, stream);
+    return kv.share(&c.layout, &c.tables, &b, (const int32_t*)starts, groups, q_heads, max_tokens, window, sinks, (int32_t*)prefix, (void*)plan,
+                    bytes, stream);
+  });
+}
+
+// kv_attention_shared(cache, layer, tables, slots, row_start, group_start, Q, O, max_rows, max_tokens, scale, plan, workspace, window, sinks, lse,
+// stream)
+PyObject* kv_attention_shared(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (wrong_count(n, 17)) return nullptr;
+  Held held;
+  CacheArg c;
+  RowsArg q, o;
+  sfmp_kv_batch_t b;
+  int32_t layer, groups, max_tokens, window, sinks;
+  int64_t bytes = 0, plan_bytes = 0;
+  const void *starts = nullptr, *plan = nullptr, *workspace = nullptr, *lse = nullptr;
+  void* stream = nullptr;
+  SFMP_READ(read_cache(a[0], a[2], &held, &c));
+  SFMP_READ(int_of(a[1], &layer));
+  SFMP_READ(rows_of(a[6], false, -1, c.layout.head_dim, &q));
+  SFMP_READ(rows_of(a[7], false, q.heads, c.layout.head_dim, &o));
+  if (q.rows != o.rows || q.type != o.type) Py_RETURN_NONE;
+  SFMP_READ(read_batch(a[3], a[4], q.rows, a[8], &b));
+  SFMP_READ(groups_of(a[5], &starts, &groups));
+  SFMP_READ(int_of(a[9], &max_tokens));
+  if (!PyFloat_CheckExact(a[10])) Py_RETURN_NONE;
+  const float scale = (float)PyFloat_AS_DOUBLE(a[10]);
+  SFMP_READ(workspace_of(a[11], &plan, &plan_bytes));
+  SFMP_READ(workspace_of(a[12], &workspace, &bytes));
+  SFMP_READ(int_of(a[13], &window));
+  SFMP_READ(int_of(a[14], &sinks));
+  SFMP_READ(checked(a[15], at::kFloat, {q.rows, q.heads}, &lse));
+  SFMP_READ(stream_handle(a[16], &stream));
+  return call([&] {
+    return kv.attention_shared(&c.layout, layer, c.codes, (const float*)c.scales, &c.tables, &b, (const int32_t*)starts, groups, q.at, q.heads, q.type,
+                               q.stride, max_tokens, window, sinks, scale, (void*)o.at, o.stride, (float*)lse, plan, plan_bytes, (void*)workspace, bytes,
+                               stream);
   });
 }
 
@@ -558,11 +640,11 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// bind_kv(SfmpKvLayout, addresses of the eight C functions); after bind()
+// bind_kv(SfmpKvLayout, addresses of the eleven C functions); after bind()
 PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (wrong_count(n, 9)) return nullptr;
-  void* f[8];
-  for (int i = 0; i < 8; ++i) {
+  if (wrong_count(n, 12)) return nullptr;
+  void* f[11];
+  for (int i = 0; i < 11; ++i) {
     f[i] = PyLong_AsVoidPtr(a[1 + i]);
     if (!f[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null function");
@@ -579,6 +661,9 @@ PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   kv.free_pages = (decltype(kv.free_pages))f[5];
   kv.compact = (decltype(kv.compact))f[6];
   kv.sample = (decltype(kv.sample))f[7];
+  kv.attention_sinks = (decltype(kv.attention_sinks))f[8];
+  kv.share = (decltype(kv.share))f[9];
+  kv.attention_shared = (decltype(kv.attention_shared))f[10];
   Py_RETURN_NONE;
 }
 
@@ -617,7 +702,10 @@ PyMethodDef methods[] = {
     {"bind_kv", (PyCFunction)(void (*)(void))bind_kv, METH_FASTCALL, nullptr},
     {"kv_append", (PyCFunction)(void (*)(void))kv_rows<false>, METH_FASTCALL, nullptr},
     {"kv_gather", (PyCFunction)(void (*)(void))kv_rows<true>, METH_FASTCALL, nullptr},
-    {"kv_attention", (PyCFunction)(void (*)(void))kv_attention, METH_FASTCALL, nullptr},
+    {"kv_attention", (PyCFunction)(void (*)(void))kv_attention<false>, METH_FASTCALL, nullptr},
+    {"kv_attention_sinks", (PyCFunction)(void (*)(void))kv_attention<true>, METH_FASTCALL, nullptr},
+    {"kv_share", (PyCFunction)(void (*)(void))kv_share, METH_FASTCALL, nullptr},
+    {"kv_attention_shared", (PyCFunction)(void (*)(void))kv_attention_shared, METH_FASTCALL, nullptr},
     {"kv_reserve", (PyCFunction)(void (*)(void))kv_reserve, METH_FASTCALL, nullptr},
     {"kv_fork", (PyCFunction)(void (*)(void))kv_tables<true>, METH_FASTCALL, nullptr},
     {"kv_free", (PyCFunction)(void (*)(void))kv_tables<false>, METH_FASTCALL, nullptr},

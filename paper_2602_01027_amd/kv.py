@@ -205,6 +205,94 @@ def sfmp_kv_attention(cache: DeviceKvCache, layer: int, tables: DeviceKvTables, 
                                             _tensor(lse, "lse", "float32", Q.shape[0], Q.shape[1]), at, size, _stream_ptr(stream)))
 
 
+def sfmp_kv_attention_sinks(cache: DeviceKvCache, layer: int, tables: DeviceKvTables, slots, row_start, Q, O, max_rows: int,
+                            max_tokens: int, scale: float, workspace, window: int, sinks: int, lse=None, stream=None) -> None:
+    """sfmp_kv_attention with first tokens that stay visible: a row sees the last `window` tokens and the first `sinks` ones."""
+    rc = _launcher().kv_attention_sinks(cache, layer, tables, slots, row_start, Q, O, max_rows, max_tokens, scale, workspace, window,
+                                        sinks, lse, stream)
+    if rc is not None:
+        return _check(rc)
+    layout, codes, scales = _cache(cache)
+    q, dtype, q_stride, o, o_stride = _attended(Q, O, cache.layout.head_dim)
+    t, b = _tables(cache.layout, tables), _batch(tables, slots, row_start, Q.shape[0], max_rows)
+    at, size = _workspace(workspace)
+    _check(load_library().sfmp_kv_attention_sinks(
+        layout, _int(layer, "layer"), codes, scales, C.byref(t), C.byref(b), q, _int(Q.shape[1], "q_heads"), dtype, q_stride,
+        _int(max_tokens, "max_tokens"), _int(window, "window"), _int(sinks, "sinks"), float(scale), o, o_stride,
+        _tensor(lse, "lse", "float32", Q.shape[0], Q.shape[1]), at, size, _stream_ptr(stream)))
+
+
+def _attended(Q, O, dim: int):
+    """(address of Q, type, row stride, address of O, row stride) of rows of one shape and type."""
+    import torch
+    types = (torch.float16, torch.bfloat16)
+    q, dtype, q_stride = _rows(Q, "Q", types, None, dim)
+    o, o_dtype, o_stride = _rows(O, "O", types, None, dim)
+    if O.shape != Q.shape or o_dtype != dtype:
+        raise ValueError("Q and O have to be of one shape and type")
+    return q, dtype, q_stride, o, o_stride
+
+
+def _groups(group_start):
+    """(address, groups) of the first batch entry of every group and their end."""
+    n = _length(group_start, "group_start")
+    if n < 1:
+        raise ValueError("group_start has to hold the end of the last group")
+    return _tensor(group_start, "group_start", "int32", n), _int(n - 1, "groups")
+
+
+def _sizes_with_groups(call, layout, batch, rows, groups, q_heads, max_rows, max_tokens) -> int:
+    n = C.c_int64(0)
+    _check(call(C.byref(layout), _int(batch, "batch"), _int(rows, "rows"), _int(groups, "groups"), _int(q_heads, "q_heads"),
+                _int(max_rows, "max_rows"), _int(max_tokens, "max_tokens"), C.byref(n)))
+    return int(n.value)
+
+
+def sfmp_kv_share_plan(layout: SfmpKvLayout, batch: int, rows: int, groups: int, q_heads: int, max_rows: int, max_tokens: int) -> int:
+    """Bytes of a plan that are enough for these sizes and for smaller ones."""
+    return _sizes_with_groups(load_library().sfmp_kv_share_plan, layout, batch, rows, groups, q_heads, max_rows, max_tokens)
+
+
+def sfmp_kv_attention_shared_workspace(layout: SfmpKvLayout, batch: int, rows: int, groups: int, q_heads: int, max_rows: int,
+                                       max_tokens: int) -> int:
+    """Bytes that are enough for these sizes and for smaller ones."""
+    return _sizes_with_groups(load_library().sfmp_kv_attention_shared_workspace, layout, batch, rows, groups, q_heads, max_rows, max_tokens)
+
+
+def sfmp_kv_share(cache: DeviceKvCache, tables: DeviceKvTables, slots, row_start, group_start, rows: int, q_heads: int, max_rows: int,
+                  max_tokens: int, plan, window: int = 0, sinks: int = 0, prefix=None, stream=None) -> None:
+    """Finds the first pages that the batch entries group_start[g] .. group_start[g + 1] - 1 (int32 [groups + 1]) hold in common, for every group,
+    and plans sfmp_kv_attention_shared of `rows` rows with these arguments; prefix: int32 [groups] or None, the tokens of the pages."""
+    rc = _launcher().kv_share(cache, tables, slots, row_start, group_start, rows, q_heads, max_rows, max_tokens, plan, window, sinks, prefix,
+                              stream)
+    if rc is not None:
+        return _check(rc)
+    starts, groups = _groups(group_start)
+    t, b = _tables(cache.layout, tables), _batch(tables, slots, row_start, rows, max_rows)
+    at, size = _workspace(plan)
+    _check(load_library().sfmp_kv_share(C.byref(cache.layout), C.byref(t), C.byref(b), starts, groups, _int(q_heads, "q_heads"),
+                                        _int(max_tokens, "max_tokens"), _int(window, "window"), _int(sinks, "sinks"),
+                                        _tensor(prefix, "prefix", "int32", groups), at, size, _stream_ptr(stream)))
+
+
+def sfmp_kv_attention_shared(cache: DeviceKvCache, layer: int, tables: DeviceKvTables, slots, row_start, group_start, Q, O, max_rows: int,
+                             max_tokens: int, scale: float, plan, workspace, window: int = 0, sinks: int = 0, lse=None, stream=None) -> None:
+    """sfmp_kv_attention_sinks (window 0: sfmp_kv_attention) of a batch planned by sfmp_kv_share: the pages that a group shares are read once."""
+    rc = _launcher().kv_attention_shared(cache, layer, tables, slots, row_start, group_start, Q, O, max_rows, max_tokens, scale, plan, workspace,
+                                         window, sinks, lse, stream)
+    if rc is not None:
+        return _check(rc)
+    layout, codes, scales = _cache(cache)
+    starts, groups = _groups(group_start)
+    q, dtype, q_stride, o, o_stride = _attended(Q, O, cache.layout.head_dim)
+    t, b = _tables(cache.layout, tables), _batch(tables, slots, row_start, Q.shape[0], max_rows)
+    (plan_at, plan_size), (at, size) = _workspace(plan), _workspace(workspace)
+    _check(load_library().sfmp_kv_attention_shared(
+        layout, _int(layer, "layer"), codes, scales, C.byref(t), C.byref(b), starts, groups, q, _int(Q.shape[1], "q_heads"), dtype, q_stride,
+        _int(max_tokens, "max_tokens"), _int(window, "window"), _int(sinks, "sinks"), float(scale), o, o_stride,
+        _tensor(lse, "lse", "float32", Q.shape[0], Q.shape[1]), plan_at, plan_size, at, size, _stream_ptr(stream)))
+
+
 def sfmp_kv_pages_workspace(layout: SfmpKvLayout) -> int:
     n = C.c_int64(0)
     _check(load_library().sfmp_kv_pages_workspace(C.byref(layout), C.byref(n)))
