@@ -471,6 +471,9 @@ int sfmp_kv_attention_shared(const sfmp_kv_layout_t* layout, int32_t layer, cons
  * table too short.  n <= SFMP_KV_MAX_BATCH.
  * sfmp_kv_fork: children[i] becomes a copy of parents[i] that holds the same pages (several may share a parent).  A
  * child must be empty (length 0) and no sequence may be both a parent and a child.
+ * sfmp_kv_reorder: sequence slots[i] becomes what sequence slots[parents[i]] was before the call: it holds the same pages (several may have one
+ * parent; a sequence that is nobody's parent is gone, and the pages that it alone held are free).  parents[i] outside 0 .. n-1: it becomes
+ * empty.  What a beam search does with its sequences after sfmp_beam_select.  n <= SFMP_KV_MAX_BATCH.
  * sfmp_kv_free: sequence slots[i] keeps its first keep[i] tokens (keep NULL: none) and gives back the other pages.
  * sfmp_kv_compact: moves the live pages with numbers >= n_live, n_live being the number of live pages, in ascending order into the free pages
  * below it, in all layers, and renumbers page table and refs: afterwards the pages n_live .. pages-1 are free.
@@ -483,6 +486,8 @@ int sfmp_kv_reserve(const sfmp_kv_layout_t* layout, void* codes_dev, float* scal
                     void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
 int sfmp_kv_fork(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const int32_t* parents_dev,
                  const int32_t* children_dev, int32_t n, void* hip_stream);
+int sfmp_kv_reorder(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const int32_t* slots_dev,
+                    const int32_t* parents_dev, int32_t n, void* hip_stream);
 int sfmp_kv_free(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const int32_t* slots_dev,
                  const int32_t* keep_dev, int32_t n, void* hip_stream);
 int sfmp_kv_compact(const sfmp_kv_layout_t* layout, void* codes_dev, float* scales_dev, const sfmp_kv_tables_t* tables,
@@ -511,6 +516,28 @@ int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32_t voc
                 const float* temperature_dev, const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev,
                 const float* uniform_dev, int32_t* tokens_dev, float* logprobs_dev, void* workspace_dev,
                 int64_t workspace_bytes, void* hip_stream);
+
+/* Device.  One step of a beam search.  Request r has the rows r * beams .. r * beams + beams - 1 of logits (dtype SFMP_TYPE_FP16, _BF16 or _FP32; row i
+ * at logits + i * stride elements, vocab of them) and of scores (fp32, the sums of log-probabilities so far).  Token t continues row i with the value
+ *     scores[i] + (l_t - m) - ln sum_j exp(l_j - m),   m the row's largest logit,
+ * and ranks by weights[i] times it (weights NULL: 1; 1 / length to compare beams of different lengths: positive, finite).  A row with ended[i]
+ * not 0 (ended NULL: none) has one continuation: end_token, with the value scores[i].  The `choices` continuations of a request that rank
+ * highest, of equal ones those of the lower row and then of the lower token, are written in that order: next_scores fp32, parents int32 (the row of
+ * logits; what sfmp_kv_reorder takes where choices = beams) and tokens int32, each [requests][choices].
+ * NaN logits count as -infinity, +infinity as the largest number of fp32; tokens of -infinity and rows whose score is -infinity or NaN (or that have
+ * no logit above -infinity) have no continuation.  Where a request has fewer than `choices`, the rest is -infinity, -1, -1.  (A request that starts
+ * from one prompt has the scores 0, -infinity, -infinity, ...)
+ * Values are held and compared in 64 bits and rounded once; the sum of exponentials is off by some 2^-24 of it divided by the square root of the
+ * tokens that make it up, the largest `choices` of each piece of the row not counted: those enter in 64 bits.  Rows of equal logits have equal
+ * values, whatever their alignment.  The same call on the same inputs gives the same bits.
+ * SFMP_ERR_SHAPE: requests < 0, beams outside 1 .. 32, requests * beams > 65535, choices outside 1 .. 64, vocab outside 1 .. 2^24, stride < vocab,
+ * with ended an end_token outside the vocabulary.  Alignment: logits to their element size.  The workspace is 256-byte aligned, its contents
+ * irrelevant on entry; sfmp_beam_select_workspace: bytes that are enough for every call of no more requests, beams, tokens and choices. */
+int sfmp_beam_select_workspace(int32_t requests, int32_t beams, int32_t vocab, int32_t choices, int64_t* bytes);
+int sfmp_beam_select(const void* logits_dev, int32_t dtype, int32_t requests, int32_t beams, int32_t vocab, int64_t stride,
+                     const float* scores_dev, const float* weights_dev, const int32_t* ended_dev, int32_t end_token, int32_t choices,
+                     float* next_scores_dev, int32_t* parents_dev, int32_t* tokens_dev, void* workspace_dev,
+                     int64_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -243,3 +243,48 @@ def sample(logits, temperature, top_k, top_p, min_p, u):
     at = int((sums <= r).sum())
     margin = min(margin, np.abs(sums[:kept] - r).min() / total if u > 0 and kept > 1 else 1.0)
     return int(order[at]), float(yo[at] - math.log(total)), float(margin)
+
+
+def reorder(tables, slots, parents):
+    """Works in place: sequence slots[i] becomes what slots[parents[i]] was (a parent outside of the call: empty)."""
+    table, lengths, refs = tables["table"], tables["lengths"], tables["refs"]
+    before = {s: (table[s].copy(), int(lengths[s])) for s in slots}
+    for s in slots:
+        for page in before[s][0][:pages_of(before[s][1])]:
+            refs[page] -= 1
+    for s, p in zip(slots, parents):
+        row, length = before[slots[p]] if 0 <= p < len(slots) else (table[s], 0)
+        n = pages_of(length)
+        table[s, :n] = row[:n]
+        lengths[s] = length
+        for page in row[:n]:
+            refs[page] += 1
+
+
+def beam_select(logits, scores, choices, weights=None, ended=None, end_token=0):
+    """One request: logits [beams, vocab].  Returns ([(value, row, token)] in order, at most `choices`; the logarithm's argument of every row, and
+    the sum of |l - m| w in proportion to it, which rounded exponentials err in proportion to)."""
+    found, sums, slopes = [], np.ones(len(logits)), np.zeros(len(logits))
+    weights = np.ones(len(logits)) if weights is None else weights
+    for b, row in enumerate(logits):
+        score = float(scores[b])
+        if not score > -math.inf:
+            continue
+        if ended is not None and ended[b]:
+            found.append((-score * float(weights[b]), b, end_token, score))
+            continue
+        x = np.asarray(row, dtype=np.float64)
+        x = np.minimum(np.where(np.isnan(x), -math.inf, x), float(np.finfo(np.float32).max))
+        m = x.max()
+        if m == -math.inf:
+            continue
+        w = np.exp(x - m)
+        sums[b] = w.sum()
+        there = w > 0
+        slopes[b] = (w[there] * (m - x[there])).sum() / sums[b]
+        for t in np.argsort(-x, kind="stable")[:choices]:
+            if x[t] > -math.inf:
+                value = score + ((x[t] - m) - math.log(sums[b]))
+                found.append((-value * float(weights[b]), b, int(t), value))
+    found.sort(key=lambda f: f[:3])
+    return [(v, b, t) for _, b, t, v in found[:choices]], sums, slopes

@@ -65,7 +65,7 @@ EXPORTS = ("sfmp_strerror", "sfmp_pack_query", "sfmp_layout_set_quant", "sfmp_pa
            "sfmp_kv_pages_workspace", "sfmp_kv_reserve", "sfmp_kv_fork", "sfmp_kv_free", "sfmp_kv_compact",
            "sfmp_sample_workspace", "sfmp_sample",
            "sfmp_kv_attention_sinks", "sfmp_kv_share_plan", "sfmp_kv_share", "sfmp_kv_attention_shared_workspace",
-           "sfmp_kv_attention_shared")
+           "sfmp_kv_attention_shared", "sfmp_kv_reorder", "sfmp_beam_select_workspace", "sfmp_beam_select")
 
 
 def lib_path() -> str:
@@ -118,6 +118,9 @@ def load_library():
     lib.sfmp_kv_share.argtypes = [KP, TP, BP, vp, i32, i32, i32, i32, i32, vp, vp, i64, vp]
     lib.sfmp_kv_attention_shared.argtypes = [KP, i32, vp, vp, TP, BP, vp, i32, vp, i32, i32, i64, i32, i32, i32, f32, vp, i64, vp, vp, i64, vp,
                                              i64, vp]
+    lib.sfmp_kv_reorder.argtypes = [KP, TP, vp, vp, i32, vp]
+    lib.sfmp_beam_select_workspace.argtypes = [i32, i32, i32, i32, NP]
+    lib.sfmp_beam_select.argtypes = [vp, i32, i32, i32, i32, i64, vp, vp, vp, i32, i32, vp, vp, vp, vp, i64, vp]
     for name in EXPORTS:
         if name != "sfmp_strerror":
             getattr(lib, name).restype = C.c_int
@@ -129,7 +132,7 @@ class _NoExtension:
     """Stands in for the extension where there is none to use: leaves every call to the ctypes path."""
     gemm = gemm_static = gemv_batched = gemm_batched = staticmethod(lambda *args: None)
     kv_append = kv_gather = kv_attention = kv_reserve = kv_fork = kv_free = kv_compact = sample = gemm
-    kv_attention_sinks = kv_share = kv_attention_shared = gemm
+    kv_attention_sinks = kv_share = kv_attention_shared = kv_reorder = beam_select = gemm
 
 
 _LAUNCHER = None  # (library, extension module bound to it)
@@ -175,7 +178,8 @@ def _launcher():
                                                             lib.sfmp_gemm_batched)))
         module.bind_kv(SfmpKvLayout, *(C.cast(f, C.c_void_p).value for f in (
             lib.sfmp_kv_append, lib.sfmp_kv_gather, lib.sfmp_kv_attention, lib.sfmp_kv_reserve, lib.sfmp_kv_fork, lib.sfmp_kv_free,
-            lib.sfmp_kv_compact, lib.sfmp_sample, lib.sfmp_kv_attention_sinks, lib.sfmp_kv_share, lib.sfmp_kv_attention_shared)))
+            lib.sfmp_kv_compact, lib.sfmp_sample, lib.sfmp_kv_attention_sinks, lib.sfmp_kv_share, lib.sfmp_kv_attention_shared,
+            lib.sfmp_kv_reorder, lib.sfmp_beam_select)))
     except ImportError as e:
         warnings.warn(f"launches are marshalled by ctypes, some 8 us of host time more per call: {e}; build it with "
                       "`python -m paper_2602_01027_amd.build` (or __graft_entry__.build())", RuntimeWarning, stacklevel=3)

@@ -13,7 +13,8 @@ LIB = os.path.join(HERE, "libsfmp.so")
 TORCH_LIB = os.path.join(HERE, "_sfmp_torch.so")  # argument marshalling for torch tensors (host code only)
 PROBE_LIB = os.path.join(HERE, "libsfmp_probe.so")  # the benchmark's streaming-read probe, not part of the product
 SOURCES = ["sfmp_host.cpp", "sfmp_unpack.hip", "sfmp_decode.hip", "sfmp_prefill.hip", "sfmp_lut.hip", "sfmp_api.hip",
-           "sfmp_kv.hip", "sfmp_kv_pages.hip", "sfmp_attention.hip", "sfmp_attention_sinks.hip", "sfmp_attention_shared.hip", "sfmp_sample.hip"]
+           "sfmp_kv.hip", "sfmp_kv_pages.hip", "sfmp_attention.hip", "sfmp_attention_sinks.hip", "sfmp_attention_shared.hip", "sfmp_sample.hip",
+           "sfmp_beam.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-fp32 instructions are switched off for all device code of this library
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",

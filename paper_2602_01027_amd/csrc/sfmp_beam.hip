@@ -1,0 +1,540 @@
+// One step of a beam search: the best continuations of every request over its beams and the vocabulary.
+//
+// A continuation's value is score + (l - m) - ln sum exp(l - m) of its beam's row of logits.  Inside a row the order is that of the logits, so that a
+// workgroup which holds a piece of a row in registers needs no more of it than its largest logits, as many as are wanted of the request, and its sum of
+// exponentials: the row is read once.  A second launch, a workgroup per request, makes values of what the pieces of all beams have left and picks
+// the best.
+//
+// Continuations of different beams can lie closer together than fp32 tells apart (scores of -50 in steps of 4e-6), so that values are fp64,
+// and of the sum, which fp32 exponentials make to some 2^-24 of each term, the listed terms - the largest ones - are made again in fp64.
+#include <float.h>
+#include <math.h>
+
+#include "sfmp_device.h"
+#include "sfmp_internal.h"
+
+namespace sfmp {
+namespace {
+
+constexpr int kThreads = 512;        // of a piece
+constexpr int kGroups = kThreads / 2;
+constexpr int kMostBeams = 32, kMostChoices = 64;
+constexpr int kMostListed = 16384;   // entries of the lists of a request
+
+struct Piece {
+  double sum;    // of exp(l - top)
+  float top;     // its largest logit; -infinity: none
+  int32_t unused;
+};
+
+struct BeamArgs {
+  const void* logits;
+  int64_t stride;
+  int32_t requests, beams, vocab, choices, pieces, chunks_each;
+  const float* scores;
+  const float* weights;
+  const int32_t* ended;
+  int32_t end_token;
+  float* next_scores;
+  int32_t* parents;
+  int32_t* tokens;
+  Piece* piece;      // [rows][pieces]
+  uint64_t* listed;  // [rows][pieces][choices], falling; 0: none
+};
+
+// Numbers in the order of the values (0 stays free: below all of them; -0 is 0)
+__device__ __forceinline__ uint32_t key_of(float x) {
+  const uint32_t u = __float_as_uint(x + 0.0f);
+  return u ^ ((int32_t)u < 0 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float logit_of_key(uint32_t key) {
+  return __uint_as_float(key ^ ((int32_t)key < 0 ? 0x80000000u : 0xFFFFFFFFu));
+}
+__device__ __forceinline__ uint64_t key_of(double x) {
+  const uint64_t u = (uint64_t)__double_as_longlong(x + 0.0);
+  return u ^ ((int64_t)u < 0 ? ~0ull : 1ull << 63);
+}
+
+// NaN as -infinity, +infinity as the largest number
+__device__ __forceinline__ float in_range(float x) { return x != x ? -INFINITY : fminf(x, FLT_MAX); }
+
+template <int T>
+__device__ __forceinline__ float logit_at(const u32x4& w, int j) {
+  if constexpr (T == SFMP_TYPE_FP32) return __uint_as_float(w[j]);
+  const uint32_t bits = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
+  if constexpr (T == SFMP_TYPE_BF16) return __uint_as_float(bits << 16);
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+}
+
+// exp(d) in fp32, always the same bits for a d
+__device__ __forceinline__ float weight_of(float d) {
+  constexpr float kHigh = 1.44269502f, kLow = 1.92596303e-8f;  // log2 e
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(d, kHigh, d * kLow));
+}
+
+// The largest threshold that at least k of the keys of a workgroup's groups reach (each wavefront holds all of them, 4 to a lane); found bit by
+// bit, no further than to one that exactly k reach.  `reach`: how many do.  0 if fewer than k keys are above 0.
+template <typename Key>
+__device__ __forceinline__ Key threshold_of(const Key (&key)[4], int k, int* reach) {
+  Key at = 0;
+  *reach = kGroups;
+  for (int bit = (int)sizeof(Key) * 8 - 1; bit >= 0; --bit) {
+    const Key next = at | (Key)1 << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) n += __popcll(__ballot(key[i] >= next));
+    if (n < k) continue;
+    at = next;
+    *reach = n;
+    if (n == k) break;
+  }
+  return at;
+}
+
+// Ranks of `count` different numbers in LDS, falling; f(rank, number) for those below `wanted`, by all threads.  `ranks` holds `count` counters.
+template <int THREADS, typename F>
+__device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, int wanted, uint32_t* ranks, F f) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  for (int i = threadIdx.x; i < count; i += THREADS) ranks[i] = 0;
+  __syncthreads();
+  for (int base = 0; base < count; base += 64) {
+    const uint64_t mine = base + lane < count ? list[base + lane] : ~0ull;
+    uint32_t above = 0;
+    for (int j = wave; j < count; j += THREADS / 64) above += list[j] > mine;
+    if (base + lane < count && above) atomicAdd(&ranks[base + lane], above);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < count; i += THREADS)
+    if ((int)ranks[i] < wanted) f((int)ranks[i], list[i]);
+}
+
+__device__ __forceinline__ double sum_of_wave(double x) {
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) x += __shfl_xor(x, s);
+  return x;
+}
+
+// LDS of a piece, before its list of numbers and their ranks
+struct PieceLds {
+  double sums[kThreads / 64];
+  uint64_t carried[kMostChoices];
+  uint32_t maxima[kThreads], firsts[kThreads];
+  int32_t count, unused[3];
+};
+// Numbers that a piece lists: those of `choices` pairs of threads and, where equal maxima reach the bound too, of 32 more.
+constexpr int kMorePairs = 32;
+__host__ __device__ constexpr int piece_numbers(int choices, int per_thread) { return (choices + kMorePairs) * 2 * (per_thread + 1); }
+
+// The largest logits and the sum of exponentials of a piece of a row: chunks of R runs of 16 bytes per thread, in registers.
+//
+// Which logits are among the `choices` largest: of the maxima of 256 pairs of threads the choices-th largest is a bound that no fewer logits reach, and
+// only those of the pairs whose maximum reaches it can (where many do that are equal, the lowest numbers), a few more than are wanted; these
+// are ranked in LDS.  Chunks behind the first take the list along.
+template <int T, int R>
+__global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
+  constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
+  extern __shared__ __align__(16) uint8_t lds[];
+  PieceLds& shared = *reinterpret_cast<PieceLds*>(lds);
+  uint32_t(&maxima)[kThreads] = shared.maxima;
+  uint32_t(&firsts)[kThreads] = shared.firsts;
+  uint64_t(&carried)[kMostChoices] = shared.carried;
+  int32_t& count = shared.count;
+  const int pairs = a.choices + kMorePairs;
+  uint64_t* const list = reinterpret_cast<uint64_t*>(lds + sizeof(PieceLds));  // (a thread's logits, and what it holds of the list)
+  uint32_t* const ranks = reinterpret_cast<uint32_t*>(list + piece_numbers(a.choices, R * RUN));
+  const int row = blockIdx.x / a.pieces, piece = blockIdx.x - row * a.pieces, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if ((a.ended && a.ended[row]) || !(a.scores[row] > -INFINITY)) return;  // (no logit of it counts)
+  const uint8_t* const start = (const uint8_t*)a.logits + (int64_t)row * a.stride * SIZE;
+  const int runs = (a.vocab + RUN - 1) / RUN;
+  // (which thread has which logits must not depend on the row's alignment: rows of equal logits have equal sums)
+  typedef u32x4 __attribute__((aligned(2))) Run;
+  if (tid < kMostChoices) carried[tid] = 0;
+  float top = -INFINITY;
+  double sum = 0.0;
+  __syncthreads();
+  for (int chunk = 0; chunk < a.chunks_each; ++chunk) {
+    const int first_run = (piece * a.chunks_each + chunk) * (kThreads * R);
+    if (first_run >= runs) break;
+    u32x4 w[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int i = (first_run + r * kThreads + tid) * RUN;
+      constexpr uint32_t kNone = T == SFMP_TYPE_FP32 ? 0xFF800000u : T == SFMP_TYPE_BF16 ? 0xFF80FF80u : 0xFC00FC00u;  // -infinity
+      w[r] = u32x4{kNone, kNone, kNone, kNone};
+      if (i + RUN <= a.vocab) {
+        w[r] = *reinterpret_cast<const Run*>(start + (int64_t)i * SIZE);
+      } else if (i < a.vocab) {  // the row's end
+#pragma unroll
+        for (int j = 0; j < RUN; ++j)
+          if (i + j < a.vocab) {
+            if constexpr (SIZE == 4)
+              w[r][j] = ((const uint32_t*)start)[i + j];
+            else
+              w[r][j / 2] = j & 1 ? (w[r][j / 2] & 0xFFFFu) | (uint32_t)((const uint16_t*)start)[i + j] << 16
+                                  : (w[r][j / 2] & 0xFFFF0000u) | ((const uint16_t*)start)[i + j];
+          }
+      }
+    }
+    const uint64_t held = tid < a.choices ? carried[tid] : 0;
+    float most = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < RUN; ++j) most = fmaxf(most, logit_at<T>(w[r], j));  // (passes NaN by)
+    most = in_range(most);
+    uint32_t my_key = most > -INFINITY ? key_of(most) : 0;
+    my_key = max(my_key, (uint32_t)(held >> 32));
+    maxima[tid] = max(my_key, (uint32_t)__shfl_xor((int)my_key, 1));
+    if (tid == 0) count = 0;
+    __syncthreads();
+    uint32_t key[4], largest = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      key[i] = maxima[2 * (lane + 64 * i)];
+      largest = max(largest, key[i]);
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, s));
+    if (largest == 0) {  // (no logit so far)
+      __syncthreads();
+      continue;
+    }
+    const float base = logit_of_key(largest);  // of this chunk and those before
+    if (base != top) {
+      sum = top == -INFINITY ? 0.0 : sum * exp((double)top - (double)base);
+      top = base;
+    }
+    int reach;
+    const uint32_t bound = threshold_of(key, a.choices, &reach);
+    uint32_t bound_number = 0;  // of ~number, where the key is the bound's
+    if (bound && reach > pairs) {
+      uint32_t lowest = ~0u;
+#pragma unroll
+      for (int r = R - 1; r >= 0; --r)
+#pragma unroll
+        for (int j = RUN - 1; j >= 0; --j) {
+          const float x = in_range(logit_at<T>(w[r], j));
+          if (x > -INFINITY && key_of(x) == bound) lowest = (first_run + r * kThreads + tid) * RUN + j;
+        }
+      if ((uint32_t)(held >> 32) == bound) lowest = min(lowest, ~(uint32_t)held);
+      firsts[tid] = ~min(lowest, (uint32_t)__shfl_xor((int)lowest, 1));
+      __syncthreads();
+      int more = 0, there;
+      uint32_t number[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        more += __popcll(__ballot(key[i] > bound));
+        number[i] = key[i] == bound ? firsts[2 * (lane + 64 * i)] : 0;
+      }
+      bound_number = threshold_of(number, a.choices - more, &there);
+    }
+    auto wanted = [&](uint32_t k, uint32_t not_number) { return k && (k > bound || (k == bound && not_number >= bound_number)); };
+    // the sum, in fp32 for a run and in fp64 from there on
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      float part = 0.0f;
+#pragma unroll
+      for (int j = 0; j < RUN; ++j) part += weight_of(logit_at<T>(w[r], j) - base);
+      if (!(part <= 2.0f * RUN)) {  // a NaN or an infinity among them
+        part = 0.0f;
+#pragma unroll
+        for (int j = 0; j < RUN; ++j) part += weight_of(in_range(logit_at<T>(w[r], j)) - base);
+      }
+      sum += (double)part;
+    }
+    if (my_key >= bound) {
+      int mine = wanted((uint32_t)(held >> 32), (uint32_t)held);
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int j = 0; j < RUN; ++j) {
+          const float x = in_range(logit_at<T>(w[r], j));
+          mine += x > -INFINITY && wanted(key_of(x), ~(uint32_t)((first_run + r * kThreads + tid) * RUN + j));
+        }
+      if (mine) {
+        int at = atomicAdd(&count, mine);
+        if (wanted((uint32_t)(held >> 32), (uint32_t)held)) list[at++] = held;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int j = 0; j < RUN; ++j) {
+            const float x = in_range(logit_at<T>(w[r], j));
+            const uint32_t not_number = ~(uint32_t)((first_run + r * kThreads + tid) * RUN + j);
+            if (x > -INFINITY && wanted(key_of(x), not_number)) list[at++] = (uint64_t)key_of(x) << 32 | not_number;
+          }
+      }
+    }
+    __syncthreads();
+    if (tid < kMostChoices) carried[tid] = 0;  // (read above, before two barriers)
+    rank_numbers<kThreads>(list, count, a.choices, ranks, [&](int rank, uint64_t x) { carried[rank] = x; });
+    __syncthreads();
+  }
+  sum = sum_of_wave(sum);
+  if (lane == 0) shared.sums[wave] = sum;
+  __syncthreads();
+  if (wave == 0) {
+    // the listed terms again
+    double more = 0.0;
+    if (lane < a.choices) {
+      const uint64_t x = carried[lane];
+      if (x) {
+        const float l = logit_of_key((uint32_t)(x >> 32));
+        more = exp((double)l - (double)top) - (double)weight_of(l - top);
+      }
+      a.listed[((int64_t)row * a.pieces + piece) * a.choices + lane] = x;
+    }
+    more = sum_of_wave(more);
+    if (lane == 0) {
+      double all = more;
+      for (int i = 0; i < kThreads / 64; ++i) all += shared.sums[i];
+      Piece p;
+      p.sum = all, p.top = top, p.unused = 0;
+      a.piece[(int64_t)row * a.pieces + piece] = p;
+    }
+  }
+}
+
+// LDS of a request, before its entries
+struct BestLds {
+  uint64_t maxima[kGroups], orders[kGroups];
+  double tops[kMostBeams], scores[kMostBeams], weights[kMostBeams];
+  int32_t states[kMostBeams];  // 0: of no more use, 1: goes on, 2: ended
+  int32_t best[kMostChoices];
+  int32_t count, unused[3];
+};
+
+// Entries that reach the bound, at most.
+__host__ __device__ inline int most_found(int choices, int all, int threads) { return choices * (threads / kGroups) * ((all + threads - 1) / threads); }
+
+// The best continuations of a request among the listed ones: of the maxima of 256 groups of threads the choices-th largest is a bound, as above.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
+  constexpr int GROUP = THREADS / kGroups;  // threads
+  extern __shared__ __align__(16) uint8_t lds[];
+  BestLds& shared = *reinterpret_cast<BestLds*>(lds);
+  auto& maxima = shared.maxima;
+  auto& orders = shared.orders;
+  auto &tops = shared.tops, &scores = shared.scores, &weights = shared.weights;
+  auto& states = shared.states;
+  auto& best = shared.best;
+  int32_t& count = shared.count;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, request = blockIdx.x;
+  const int lists = a.beams * a.pieces, all = lists * a.choices;
+  const int most = most_found(a.choices, all, THREADS);
+  uint64_t* const value_keys = reinterpret_cast<uint64_t*>(lds + sizeof(BestLds));
+  uint32_t* const order_keys = reinterpret_cast<uint32_t*>(value_keys + most);
+  uint32_t* const numbers = order_keys + most;
+  // of every beam: score less the logarithm of the sum of exponentials, of which the largest logit is left aside
+  for (int b = wave; b < a.beams; b += THREADS / 64) {
+    const int64_t row = (int64_t)request * a.beams + b;
+    const float score = a.scores[row];
+    const bool ended = a.ended && a.ended[row];
+    double sum = 0.0;
+    float top = -INFINITY;
+    if (!ended && score > -INFINITY) {
+      for (int i = lane; i < a.pieces; i += 64) top = fmaxf(top, a.piece[row * a.pieces + i].top);
+#pragma unroll
+      for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
+      for (int i = lane; i < a.pieces; i += 64) {
+        const Piece p = a.piece[row * a.pieces + i];
+        if (p.top > -INFINITY) sum += p.sum * exp((double)p.top - (double)top);
+      }
+      sum = sum_of_wave(sum);
+    }
+    if (lane == 0) {
+      tops[b] = top;
+      scores[b] = ended ? (double)score : (double)score - log(sum);
+      weights[b] = a.weights ? (double)a.weights[row] : 1.0;
+      states[b] = !(score > -INFINITY) ? 0 : ended ? 2 : top > -INFINITY ? 1 : 0;
+    }
+  }
+  if (tid == 0) count = 0;
+  __syncthreads();
+  // The i-th entry: of list i % lists its (i / lists)-th, so that the first ones of all lists fall to different threads
+  auto entry = [&](int i, double* value, uint64_t* key, uint32_t* order) {
+    const int rank = i / lists, which = i - rank * lists, b = which / a.pieces;
+    *key = 0;
+    if (states[b] == 0) return;
+    uint32_t token;
+    if (states[b] == 2) {
+      if (rank || which - b * a.pieces) return;
+      token = a.end_token;
+      *value = scores[b];
+    } else {
+      const uint64_t x = a.listed[((int64_t)request * lists + which) * a.choices + rank];
+      if (!x) return;
+      token = ~(uint32_t)x;
+      *value = scores[b] + ((double)logit_of_key((uint32_t)(x >> 32)) - tops[b]);
+    }
+    *key = key_of(*value * weights[b]);
+    *order = ~((uint32_t)b << 24 | token);  // (larger for those that come first)
+  };
+  uint64_t my_key = 0;
+  uint32_t my_order = 0;
+  for (int i = tid; i < all; i += THREADS) {
+    double value;
+    uint64_t k;
+    uint32_t o = 0;
+    entry(i, &value, &k, &o);
+    if (k > my_key || (k == my_key && o > my_order)) my_key = k, my_order = o;
+  }
+#pragma unroll
+  for (int s = 1; s < GROUP; s *= 2) {
+    const uint64_t k = __shfl_xor(my_key, s);
+    const uint32_t o = (uint32_t)__shfl_xor((int)my_order, s);
+    if (k > my_key || (k == my_key && o > my_order)) my_key = k, my_order = o;
+  }
+  if (tid % GROUP == 0) maxima[tid / GROUP] = my_key, orders[tid / GROUP] = my_order;
+  __syncthreads();
+  uint64_t key[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) key[i] = maxima[lane + 64 * i];
+  int reach;
+  const uint64_t bound = threshold_of(key, a.choices, &reach);
+  uint32_t bound_order = 0;
+  if (bound && reach > a.choices) {  // equal ones: those that come first
+    int more = 0, there;
+    uint32_t order[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      more += __popcll(__ballot(key[i] > bound));
+      order[i] = key[i] == bound ? (uint32_t)orders[lane + 64 * i] : 0;
+    }
+    bound_order = threshold_of(order, a.choices - more, &there);
+  }
+  if (my_key > bound || (my_key == bound && my_order >= bound_order)) {
+    for (int i = tid; i < all; i += THREADS) {
+      double value;
+      uint64_t k;
+      uint32_t o;
+      entry(i, &value, &k, &o);
+      if (k && (k > bound || (k == bound && o >= bound_order))) {
+        const int at = atomicAdd(&count, 1);
+        value_keys[at] = k, order_keys[at] = o, numbers[at] = i;
+      }
+    }
+  }
+  __syncthreads();
+  const int found = count;
+  for (int i = tid; i < found; i += THREADS) {
+    const uint64_t k = value_keys[i];
+    const uint32_t o = order_keys[i];
+    int above = 0;
+    for (int j = 0; j < found; ++j) above += value_keys[j] > k || (value_keys[j] == k && order_keys[j] > o);
+    if (above < a.choices) best[above] = (int)numbers[i];
+  }
+  __syncthreads();
+  if (tid < a.choices) {
+    const int64_t to = (int64_t)request * a.choices + tid;
+    double value = -INFINITY;
+    uint64_t k;
+    uint32_t order = ~0u;
+    if (tid < found) entry(best[tid], &value, &k, &order);
+    order = ~order;
+    a.next_scores[to] = (float)value;
+    a.parents[to] = tid < found ? (int)(request * a.beams + (order >> 24)) : -1;
+    a.tokens[to] = tid < found ? (int)(order & 0xFFFFFF) : -1;
+  }
+}
+
+// How a call runs.
+struct BeamForm {
+  int pieces, chunks_each;   // of a row
+  int runs;                  // of 16 bytes per thread and chunk: 1 or 4
+  int best_threads;
+};
+BeamForm choose_form(int size, int rows, int beams, int vocab, int choices) {
+  BeamForm f;
+  const int64_t small = (vocab + kThreads * 16 / size - 1) / (kThreads * 16 / size), large = (small + 3) / 4;
+  f.runs = (int64_t)rows * large < 256 ? 1 : 4;
+  const int64_t chunks = f.runs == 1 ? small : large;
+  int64_t pieces = rows < 2048 ? 2048 / rows : 1;
+  const int64_t most = kMostListed / (beams * choices);
+  if (pieces > most) pieces = most;
+  if (pieces > chunks) pieces = chunks;
+  f.chunks_each = (int)((chunks + pieces - 1) / pieces);
+  f.pieces = (int)((chunks + f.chunks_each - 1) / f.chunks_each);
+  f.best_threads = (int64_t)beams * f.pieces * choices > 2048 ? 1024 : 256;
+  return f;
+}
+int64_t bytes_of(int64_t pieces, int choices) { return pieces * ((int64_t)sizeof(Piece) + 8 * choices); }
+
+int check_sizes(int32_t requests, int32_t beams, int32_t vocab, int32_t choices) {
+  return requests < 0 || beams < 1 || beams > kMostBeams || (int64_t)requests * beams > 65535 || vocab < 1 || vocab > 1 << 24 || choices < 1 ||
+                 choices > kMostChoices
+             ? SFMP_ERR_SHAPE
+             : SFMP_OK;
+}
+
+template <int T, int R>
+int launch_pieces(const BeamArgs& a, hipStream_t stream) {
+  constexpr int RUN = T == SFMP_TYPE_FP32 ? 4 : 8;
+  const int lds = (int)sizeof(PieceLds) + piece_numbers(a.choices, R * RUN) * 12;
+  if (int e = allow_full_lds((const void*)beam_pieces_kernel<T, R>, "beam_pieces_kernel")) return e;
+  beam_pieces_kernel<T, R><<<a.requests * a.beams * a.pieces, kThreads, lds, stream>>>(a);
+  return SFMP_OK;
+}
+template <int T>
+int launch_rows(const BeamArgs& a, const BeamForm& f, hipStream_t stream) {
+  return f.runs == 1 ? launch_pieces<T, 1>(a, stream) : launch_pieces<T, 4>(a, stream);
+}
+template <int THREADS>
+int launch_best(const BeamArgs& a, hipStream_t stream) {
+  const int lds = (int)sizeof(BestLds) + most_found(a.choices, a.beams * a.pieces * a.choices, THREADS) * 16;
+  if (int e = allow_full_lds((const void*)beam_best_kernel<THREADS>, "beam_best_kernel")) return e;
+  beam_best_kernel<THREADS><<<a.requests, THREADS, lds, stream>>>(a);
+  return SFMP_OK;
+}
+
+bool aligned_to(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+}  // namespace
+}  // namespace sfmp
+
+using namespace sfmp;
+
+extern "C" int sfmp_beam_select_workspace(int32_t requests, int32_t beams, int32_t vocab, int32_t choices, int64_t* bytes) {
+  if (!bytes) return SFMP_ERR_NULL;
+  if (int e = check_sizes(requests, beams, vocab, choices)) return e;
+  // (of all types; pieces of a row fall as rows are added)
+  const int64_t rows = (int64_t)requests * beams, chunks = (vocab + kThreads * 4 - 1) / (kThreads * 4);
+  const int64_t few = rows * chunks, many = rows > 2048 ? rows : 2048;
+  *bytes = round_up_256(bytes_of(few < many ? few : many, choices) + 1);
+  return SFMP_OK;
+}
+
+extern "C" int sfmp_beam_select(const void* logits_dev, int32_t dtype, int32_t requests, int32_t beams, int32_t vocab, int64_t stride,
+                                const float* scores_dev, const float* weights_dev, const int32_t* ended_dev, int32_t end_token, int32_t choices,
+                                float* next_scores_dev, int32_t* parents_dev, int32_t* tokens_dev, void* workspace_dev, int64_t workspace_bytes,
+                                void* hip_stream) {
+  if (dtype != SFMP_TYPE_FP16 && dtype != SFMP_TYPE_BF16 && dtype != SFMP_TYPE_FP32) return SFMP_ERR_LAYOUT;
+  if (int e = check_sizes(requests, beams, vocab, choices)) return e;
+  if (stride < vocab || stride > INT64_MAX / 8 / 65536 || (ended_dev && (end_token < 0 || end_token >= vocab))) return SFMP_ERR_SHAPE;
+  if (requests == 0) return SFMP_OK;
+  if (!logits_dev || !scores_dev || !next_scores_dev || !parents_dev || !tokens_dev) return SFMP_ERR_NULL;
+  const int size = dtype == SFMP_TYPE_FP32 ? 4 : 2;
+  if (!aligned_to(logits_dev, size) || !aligned_to(scores_dev, 4) || !aligned_to(weights_dev, 4) || !aligned_to(ended_dev, 4) ||
+      !aligned_to(next_scores_dev, 4) || !aligned_to(parents_dev, 4) || !aligned_to(tokens_dev, 4))
+    return SFMP_ERR_ALIGN;
+  const int rows = requests * beams;
+  const BeamForm f = choose_form(size, rows, beams, vocab, choices);
+  const int64_t pieces = (int64_t)rows * f.pieces;
+  if (!workspace_dev || !aligned_to(workspace_dev, 256) || workspace_bytes < bytes_of(pieces, choices)) return SFMP_ERR_WORKSPACE;
+  BeamArgs a{};
+  a.logits = logits_dev, a.stride = stride;
+  a.requests = requests, a.beams = beams, a.vocab = vocab, a.choices = choices, a.pieces = f.pieces, a.chunks_each = f.chunks_each;
+  a.scores = scores_dev, a.weights = weights_dev, a.ended = ended_dev, a.end_token = end_token;
+  a.next_scores = next_scores_dev, a.parents = parents_dev, a.tokens = tokens_dev;
+  a.piece = (Piece*)workspace_dev;
+  a.listed = (uint64_t*)(a.piece + pieces);
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const int e = dtype == SFMP_TYPE_FP32   ? launch_rows<SFMP_TYPE_FP32>(a, f, stream)
+                : dtype == SFMP_TYPE_BF16 ? launch_rows<SFMP_TYPE_BF16>(a, f, stream)
+                                          : launch_rows<SFMP_TYPE_FP16>(a, f, stream);
+  if (e) return e;
+  if (const int e2 = f.best_threads == 1024 ? launch_best<1024>(a, stream) : launch_best<256>(a, stream)) return e2;
+  const hipError_t error = hipGetLastError();
+  if (error == hipSuccess) return SFMP_OK;
+  note_hip_error("beam_pieces_kernel", hipGetErrorString(error));
+  return SFMP_ERR_HIP;
+}

@@ -1,4 +1,4 @@
-// Pages of the 8-bit cache: reserving (with copy on write), forking, freeing, compacting.
+// Pages of the 8-bit cache: reserving (with copy on write), forking, freeing, compacting, reordering.
 #include "sfmp_kv.h"
 
 using namespace sfmp;
@@ -249,6 +249,61 @@ __global__ __launch_bounds__(256) void free_kernel(sfmp_kv_tables_t t, int32_t p
   if (threadIdx.x == 0) t.lengths_dev[slot] = kept;
 }
 
+// Sequences that become what their parents were.  Places of the page table do not depend on each other: a workgroup takes `columns` of them for all
+// sequences, through LDS, so that rows can be exchanged in place.  Holders change where a place gets another page; sums of whole numbers,
+// the same in every order.  Lengths are read by all workgroups: they change here only where there is one, else in a launch of their own.
+__global__ __launch_bounds__(kThreads) void reorder_kernel(sfmp_kv_tables_t t, int32_t pages, const int32_t* slots, const int32_t* parents, int32_t n,
+                                                           int32_t columns, int32_t last) {
+  extern __shared__ int32_t lds[];
+  int32_t *const slot_of = lds, *const held_of = slot_of + kThreads, *const parent_of = held_of + kThreads;
+  int32_t *const some = parent_of + kThreads, *const ids = some + 1;  // (whether a sequence has a page here); [n][columns]
+  const int i = threadIdx.x, first = blockIdx.x * columns;
+  int length = 0, parent = -1;
+  if (i == 0) *some = 0;
+  __syncthreads();
+  if (i < n) {
+    int slot = slots[i];
+    parent = parents[i];
+    if ((uint32_t)slot >= (uint32_t)t.sequences) slot = -1;
+    if ((uint32_t)parent >= (uint32_t)n) parent = -1;
+    length = slot < 0 ? 0 : min(max(t.lengths_dev[slot], 0), t.table_pages * kPage);
+    slot_of[i] = slot, held_of[i] = (length + kPage - 1) / kPage, parent_of[i] = parent;
+  }
+  if ((length + kPage - 1) / kPage > first) *some = 1;
+  __syncthreads();
+  const int width = min(columns, t.table_pages - first);
+  if (*some) {
+    for (int x = i; x < n * columns; x += kThreads) {
+      const int y = x / columns, c = x - y * columns;
+      if (c < width && first + c < held_of[y]) ids[x] = t.page_table_dev[(int64_t)slot_of[y] * t.table_pages + first + c];
+    }
+    __syncthreads();
+    for (int x = i; x < n * columns; x += kThreads) {
+      const int y = x / columns, c = x - y * columns, from = parent_of[y];
+      if (c >= width || slot_of[y] < 0 || from == y) continue;
+      const bool had = first + c < held_of[y], gets = from >= 0 && first + c < held_of[from];
+      const int old = had ? ids[x] : -1, now = gets ? ids[from * columns + c] : -1;
+      if (gets && !(had && old == now)) t.page_table_dev[(int64_t)slot_of[y] * t.table_pages + first + c] = now;
+      if (old == now) continue;
+      if ((uint32_t)old < (uint32_t)pages) atomicSub(&t.refs_dev[old], 1);
+      if ((uint32_t)now < (uint32_t)pages) atomicAdd(&t.refs_dev[now], 1);
+    }
+  }
+  if (!last) return;
+  __syncthreads();
+  held_of[i] = length;
+  __syncthreads();
+  if (i < n && slot_of[i] >= 0) t.lengths_dev[slot_of[i]] = parent >= 0 ? held_of[parent] : 0;
+}
+__global__ __launch_bounds__(kThreads) void reorder_lengths_kernel(sfmp_kv_tables_t t, const int32_t* slots, const int32_t* parents, int32_t n) {
+  __shared__ int32_t length_of[kThreads];
+  const int i = threadIdx.x, slot = i < n ? slots[i] : -1, parent = i < n ? parents[i] : -1;
+  const bool there = (uint32_t)slot < (uint32_t)t.sequences;
+  length_of[i] = there ? min(max(t.lengths_dev[slot], 0), t.table_pages * kPage) : 0;
+  __syncthreads();
+  if (there) t.lengths_dev[slot] = (uint32_t)parent < (uint32_t)n ? length_of[parent] : 0;
+}
+
 int check_pages_call(const sfmp_kv_layout_t* L, const sfmp_kv_tables_t* t) {
   if (int e = check_kv_layout(L)) return e;
   return check_kv_tables(t, true);
@@ -329,4 +384,22 @@ extern "C" int sfmp_kv_compact(const sfmp_kv_layout_t* layout, void* codes_dev, 
   compact_kernel<<<1, kThreads, 0, (hipStream_t)hip_stream>>>(*tables, layout->pages, status_dev, ws);
   if (int e = kv_launched("compact_kernel")) return e;
   return launch_move(layout, codes_dev, scales_dev, tables, ws, (layout->pages + 1) / 2, true, hip_stream);
+}
+
+extern "C" int sfmp_kv_reorder(const sfmp_kv_layout_t* layout, const sfmp_kv_tables_t* tables, const int32_t* slots_dev,
+                               const int32_t* parents_dev, int32_t n, void* hip_stream) {
+  if (int e = check_pages_call(layout, tables)) return e;
+  if (n < 0 || n > SFMP_KV_MAX_BATCH) return SFMP_ERR_SHAPE;
+  if (n == 0) return SFMP_OK;
+  if (!slots_dev || !parents_dev) return SFMP_ERR_NULL;
+  if (!kv_aligned(slots_dev, 4) || !kv_aligned(parents_dev, 4)) return SFMP_ERR_ALIGN;
+  const hipStream_t stream = (hipStream_t)hip_stream;
+  const bool one = (int64_t)n * tables->table_pages <= 16384;
+  const int columns = one ? tables->table_pages : 32;
+  if (int e = allow_full_lds((const void*)reorder_kernel, "reorder_kernel")) return e;
+  reorder_kernel<<<(tables->table_pages + columns - 1) / columns, kThreads,
+                   (3 * kThreads + 1 + n * columns) * 4, stream>>>(*tables, layout->pages, slots_dev, parents_dev, n,
+                                                                                                      columns, one);
+  if (!one) reorder_lengths_kernel<<<1, kThreads, 0, stream>>>(*tables, slots_dev, parents_dev, n);
+  return kv_launched("reorder_kernel");
 }

@@ -235,6 +235,8 @@ PyObject* gemm_batched(PyObject*, PyObject* const* a, Py_ssize_t n) {
 struct KvApi {
   decltype(&sfmp_kv_append) append = nullptr;
   decltype(&sfmp_kv_gather) gather = nullptr;
+  decltype(&sfmp_kv_reorder) reorder = nullptr;
+  decltype(&sfmp_beam_select) beam_select = nullptr;
   decltype(&sfmp_kv_attention_sinks) attention_sinks = nullptr;
   decltype(&sfmp_kv_share) share = nullptr;
   decltype(&sfmp_kv_attention_shared) attention_shared = nullptr;
@@ -573,8 +575,9 @@ PyObject* kv_reserve(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// kv_fork(cache, tables, parents, children, stream); kv_free(cache, tables, slots, keep, stream)
-template <bool FORK>
+// kv_fork(cache, tables, parents, children, stream); kv_free(cache, tables, slots, keep, stream); kv_reorder(cache, tables, slots, parents, stream)
+enum { kFork, kFree, kReorder };
+template <int CALL>
 PyObject* kv_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (wrong_count(n, 5)) return nullptr;
   Held held;
@@ -588,7 +591,7 @@ PyObject* kv_tables(PyObject*, PyObject* const* a, Py_ssize_t n) {
   SFMP_READ(checked(a[3], at::kInt, {m}, &y));
   SFMP_READ(stream_handle(a[4], &stream));
   return call([&] {
-    return (FORK ? kv.fork : kv.free_pages)(&c.layout, &c.tables, (const int32_t*)x, (const int32_t*)y, m, stream);
+    return (CALL == kFork ? kv.fork : CALL == kFree ? kv.free_pages : kv.reorder)(&c.layout, &c.tables, (const int32_t*)x, (const int32_t*)y, m, stream);
   });
 }
 
@@ -609,28 +612,34 @@ PyObject* kv_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// [rows, vocab] whose rows may lie apart
+Read logits_of(PyObject* o, const void** logits, int32_t* type, int32_t* rows, int32_t* vocab, int64_t* stride) {
+  if (!THPVariable_CheckExact(o)) return kOther;
+  try {
+    const at::Tensor& t = THPVariable_Unpack(o);
+    const at::ScalarType s = t.scalar_type();
+    if (!t.is_cuda() || t.dim() != 2 || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX || (t.size(1) > 1 && t.stride(1) != 1) ||
+        (s != at::kHalf && s != at::kBFloat16 && s != at::kFloat))
+      return kOther;
+    *type = s == at::kHalf ? SFMP_TYPE_FP16 : s == at::kBFloat16 ? SFMP_TYPE_BF16 : SFMP_TYPE_FP32;
+    *rows = (int32_t)t.size(0);
+    *vocab = (int32_t)t.size(1);
+    *stride = *rows > 1 ? t.stride(0) : *vocab;
+    *logits = t.numel() ? t.data_ptr() : nullptr;
+    return kTaken;
+  } catch (const std::exception&) {
+    return kOther;
+  }
+}
+
 // sample(logits, temperature, top_k, top_p, min_p, uniform, tokens, logprobs, workspace, stream)
 PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (wrong_count(n, 10)) return nullptr;
-  if (!THPVariable_CheckExact(a[0])) Py_RETURN_NONE;
   int32_t type, rows, vocab;
   int64_t stride, bytes = 0;
   const void *logits, *p[7] = {}, *workspace = nullptr;
   void* stream = nullptr;
-  try {
-    const at::Tensor& t = THPVariable_Unpack(a[0]);
-    const at::ScalarType s = t.scalar_type();
-    if (!t.is_cuda() || t.dim() != 2 || t.size(0) > INT32_MAX || t.size(1) > INT32_MAX || (t.size(1) > 1 && t.stride(1) != 1) ||
-        (s != at::kHalf && s != at::kBFloat16 && s != at::kFloat))
-      Py_RETURN_NONE;
-    type = s == at::kHalf ? SFMP_TYPE_FP16 : s == at::kBFloat16 ? SFMP_TYPE_BF16 : SFMP_TYPE_FP32;
-    rows = (int32_t)t.size(0);
-    vocab = (int32_t)t.size(1);
-    stride = rows > 1 ? t.stride(0) : vocab;
-    logits = t.numel() ? t.data_ptr() : nullptr;
-  } catch (const std::exception&) {
-    Py_RETURN_NONE;
-  }
+  SFMP_READ(logits_of(a[0], &logits, &type, &rows, &vocab, &stride));
   for (int i = 0; i < 7; ++i) SFMP_READ(checked(a[1 + i], i == 1 || i == 5 ? at::kInt : at::kFloat, {rows}, &p[i]));
   SFMP_READ(workspace_of(a[8], &workspace, &bytes));
   SFMP_READ(stream_handle(a[9], &stream));
@@ -640,11 +649,44 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// bind_kv(SfmpKvLayout, addresses of the eleven C functions); after bind()
+// beam_select(logits, beams, scores, weights, ended, end_token, next_scores, parents, tokens, workspace, stream)
+PyObject* beam_select(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (wrong_count(n, 11)) return nullptr;
+  int32_t type, rows, vocab, beams, end_token, choices;
+  int64_t stride, bytes = 0;
+  const void *logits, *scores, *weights, *ended, *next_scores, *parents, *tokens, *workspace = nullptr;
+  void* stream = nullptr;
+  SFMP_READ(logits_of(a[0], &logits, &type, &rows, &vocab, &stride));
+  SFMP_READ(int_of(a[1], &beams));
+  if (beams < 1 || rows % beams) Py_RETURN_NONE;
+  SFMP_READ(checked(a[2], at::kFloat, {rows}, &scores));
+  SFMP_READ(checked(a[3], at::kFloat, {rows}, &weights));
+  SFMP_READ(checked(a[4], at::kInt, {rows}, &ended));
+  SFMP_READ(int_of(a[5], &end_token));
+  if (!THPVariable_CheckExact(a[6])) Py_RETURN_NONE;
+  try {
+    const at::Tensor& t = THPVariable_Unpack(a[6]);
+    if (t.dim() != 2 || t.size(1) > INT32_MAX) Py_RETURN_NONE;
+    choices = (int32_t)t.size(1);
+  } catch (const std::exception&) {
+    Py_RETURN_NONE;
+  }
+  SFMP_READ(checked(a[6], at::kFloat, {rows / beams, choices}, &next_scores));
+  SFMP_READ(checked(a[7], at::kInt, {rows / beams, choices}, &parents));
+  SFMP_READ(checked(a[8], at::kInt, {rows / beams, choices}, &tokens));
+  SFMP_READ(workspace_of(a[9], &workspace, &bytes));
+  SFMP_READ(stream_handle(a[10], &stream));
+  return call([&] {
+    return kv.beam_select(logits, type, rows / beams, beams, vocab, stride, (const float*)scores, (const float*)weights, (const int32_t*)ended,
+                          end_token, choices, (float*)next_scores, (int32_t*)parents, (int32_t*)tokens, (void*)workspace, bytes, stream);
+  });
+}
+
+// bind_kv(SfmpKvLayout, addresses of the thirteen C functions); after bind()
 PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (wrong_count(n, 12)) return nullptr;
-  void* f[11];
-  for (int i = 0; i < 11; ++i) {
+  if (wrong_count(n, 14)) return nullptr;
+  void* f[13];
+  for (int i = 0; i < 13; ++i) {
     f[i] = PyLong_AsVoidPtr(a[1 + i]);
     if (!f[i]) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null function");
@@ -664,6 +706,8 @@ PyObject* bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
   kv.attention_sinks = (decltype(kv.attention_sinks))f[8];
   kv.share = (decltype(kv.share))f[9];
   kv.attention_shared = (decltype(kv.attention_shared))f[10];
+  kv.reorder = (decltype(kv.reorder))f[11];
+  kv.beam_select = (decltype(kv.beam_select))f[12];
   Py_RETURN_NONE;
 }
 
@@ -707,8 +751,10 @@ PyMethodDef methods[] = {
     {"kv_share", (PyCFunction)(void (*)(void))kv_share, METH_FASTCALL, nullptr},
     {"kv_attention_shared", (PyCFunction)(void (*)(void))kv_attention_shared, METH_FASTCALL, nullptr},
     {"kv_reserve", (PyCFunction)(void (*)(void))kv_reserve, METH_FASTCALL, nullptr},
-    {"kv_fork", (PyCFunction)(void (*)(void))kv_tables<true>, METH_FASTCALL, nullptr},
-    {"kv_free", (PyCFunction)(void (*)(void))kv_tables<false>, METH_FASTCALL, nullptr},
+    {"kv_fork", (PyCFunction)(void (*)(void))kv_tables<kFork>, METH_FASTCALL, nullptr},
+    {"kv_free", (PyCFunction)(void (*)(void))kv_tables<kFree>, METH_FASTCALL, nullptr},
+    {"kv_reorder", (PyCFunction)(void (*)(void))kv_tables<kReorder>, METH_FASTCALL, nullptr},
+    {"beam_select", (PyCFunction)(void (*)(void))beam_select, METH_FASTCALL, nullptr},
     {"kv_compact", (PyCFunction)(void (*)(void))kv_compact, METH_FASTCALL, nullptr},
     {"sample", (PyCFunction)(void (*)(void))sample, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -322,6 +322,16 @@ def sfmp_kv_fork(cache: DeviceKvCache, tables: DeviceKvTables, parents, children
                                        _tensor(children, "children", "int32", n), n, _stream_ptr(stream)))
 
 
+def sfmp_kv_reorder(cache: DeviceKvCache, tables: DeviceKvTables, slots, parents, stream=None) -> None:
+    """Sequence slots[i] becomes what sequence slots[parents[i]] was, in the same pages (a parent outside of the call: it becomes empty)."""
+    rc = _launcher().kv_reorder(cache, tables, slots, parents, stream)
+    if rc is not None:
+        return _check(rc)
+    t, n = _tables(cache.layout, tables), _length(slots, "slots")
+    _check(load_library().sfmp_kv_reorder(C.byref(cache.layout), C.byref(t), _tensor(slots, "slots", "int32", n),
+                                          _tensor(parents, "parents", "int32", n), n, _stream_ptr(stream)))
+
+
 def sfmp_kv_free(cache: DeviceKvCache, tables: DeviceKvTables, slots, keep=None, stream=None) -> None:
     """Sequence slots[i] keeps its first keep[i] tokens (None: none)."""
     rc = _launcher().kv_free(cache, tables, slots, keep, stream)
@@ -369,3 +379,36 @@ def sfmp_sample(logits, temperature, top_k, top_p, min_p, uniform, tokens, logpr
                                       _tensor(top_p, "top_p", "float32", n), _tensor(min_p, "min_p", "float32", n),
                                       _tensor(uniform, "uniform", "float32", n), _tensor(tokens, "tokens", "int32", n),
                                       _tensor(logprobs, "logprobs", "float32", n), at, size, _stream_ptr(stream)))
+
+
+def sfmp_beam_select_workspace(requests: int, beams: int, vocab: int, choices: int) -> int:
+    """Bytes that are enough for these sizes and for smaller ones."""
+    n = C.c_int64(0)
+    _check(load_library().sfmp_beam_select_workspace(_int(requests, "requests"), _int(beams, "beams"), _int(vocab, "vocab"), _int(choices, "choices"),
+                                                     C.byref(n)))
+    return int(n.value)
+
+
+def sfmp_beam_select(logits, beams: int, scores, weights, ended, end_token: int, next_scores, parents, tokens, workspace, stream=None) -> None:
+    """logits fp16, bf16 or fp32 [requests * beams, vocab] (rows may lie apart), scores fp32, weights fp32 or None, ended int32 or None, each
+    [requests * beams]; next_scores fp32, parents and tokens int32 [requests, choices]: the best continuations of every request."""
+    rc = _launcher().beam_select(logits, beams, scores, weights, ended, end_token, next_scores, parents, tokens, workspace, stream)
+    if rc is not None:
+        return _check(rc)
+    import torch
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise ValueError("logits has to be a tensor on the GPU")
+    if logits.dtype not in _types() or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits has to be fp16, bf16 or fp32 [requests * beams, vocab] with contiguous rows")
+    rows, vocab, beams = _int(logits.shape[0], "rows"), _int(logits.shape[1], "vocab"), _int(beams, "beams")
+    if beams < 1 or rows % beams:
+        raise ValueError(f"logits has to hold {beams} rows for each request, got {rows}")
+    at, size = _workspace(workspace)
+    if not isinstance(next_scores, torch.Tensor) or next_scores.dim() != 2:
+        raise ValueError("next_scores has to be of shape [requests, choices]")
+    out = (rows // beams, _int(next_scores.shape[1], "choices"))
+    _check(load_library().sfmp_beam_select(
+        logits.data_ptr() or None, _types()[logits.dtype], out[0], beams, vocab, logits.stride(0) if rows > 1 else vocab,
+        _tensor(scores, "scores", "float32", rows), _tensor(weights, "weights", "float32", rows), _tensor(ended, "ended", "int32", rows),
+        _int(end_token, "end_token"), out[1], _tensor(next_scores, "next_scores", "float32", *out), _tensor(parents, "parents", "int32", *out),
+        _tensor(tokens, "tokens", "int32", *out), at, size, _stream_ptr(stream)))
