@@ -14,7 +14,9 @@ namespace {
 
 constexpr int32_t kPlanMagic = 0x5348504C;
 constexpr int kMostOwnRows = 64;     // rows of an entry and key head
-constexpr int kPlanThreads = 1024;
+constexpr int kPlanThreads = 1024, kShareThreads = 256;
+constexpr int kSlotsHeld = 1024;     // entries of a group whose slots are held in LDS
+constexpr int kMostSlices = 64;      // workgroups that compare the tables of a group
 constexpr int kPlanHeadBytes = 256;
 constexpr int kMostParts = 2048;     // of shared pages, and of own ones
 
@@ -37,7 +39,8 @@ struct GroupPlan {
   int32_t first, last;       // smallest and largest position
   int32_t each, tiles;       // places of the pages that the rows see, tiles of rows
   int32_t before, unit0;     // steps and units of the groups before
-  int32_t unused[6];
+  int32_t whole;             // full pages of the shortest sequence
+  int32_t unused[5];
 };
 // A sequence behind them.
 struct EntryPlan {
@@ -75,6 +78,8 @@ struct SharedArgs {
   PlanKey key;
   const int32_t* group_start;
   int32_t* prefix;           // or null
+  int32_t* differs;          // [groups][slices] the first place that a workgroup found to differ
+  int32_t slices;
   int32_t tile_rows, workgroups, group_least, own_least;
   int64_t group_units, own_units;
   float group_cost;
@@ -118,167 +123,192 @@ __device__ __forceinline__ PageRange<SINKS> own_pages(const AttentionArgs& a, co
   return pages_from<SINKS>(pages_of_entry<SINKS>(a, e), common);
 }
 
-// What the sequences of a group share, a workgroup per group; the last one takes the entries that belong to none.  Bound by chains of loads (group,
-// slot, length, table) and, for many sequences, by reading their rows of the page table.
-template <bool SINKS>
-__global__ __launch_bounds__(kPlanThreads) void share_groups_kernel(AttentionArgs a, SharedArgs p) {
-  __shared__ int whole, seen, first, last, end_row, differs;
+// Least and largest values over the threads of a workgroup.
+struct Extent {
+  int whole, seen, first, last, end_row;
+};
+
+// What there is of a group, and where its sequences' rows of the page table differ first: gridDim.y workgroups per group take every gridDim.y-th run
+// of 64 places.  The last ones take the entries that belong to no group.  Bound by chains of loads (group, slot, length, table).
+__global__ __launch_bounds__(kShareThreads) void share_groups_kernel(AttentionArgs a, SharedArgs p) {
+  __shared__ Extent all;
+  __shared__ int differs;
+  __shared__ int32_t slots[kSlotsHeld];
   const int g = blockIdx.x, tid = threadIdx.x, batch = a.v.batch, groups = p.key.groups;
-  const bool none = g == groups;
+  const bool none = g == groups, writes = blockIdx.y == 0;
   auto start_of = [&](int i) { return min(max(p.group_start[i], 0), batch); };
   // (none: the entries before the first group and behind the last)
   const int from = none ? 0 : start_of(g), to = none ? start_of(0) : max(start_of(g + 1), from);
   const int from2 = none ? start_of(groups) : to, to2 = none ? batch : to;
-  if (tid == 0) whole = seen = kMaxTablePages, first = INT32_MAX, last = INT32_MIN, end_row = 0, differs = INT32_MAX;
+  if (tid == 0) all = Extent{kMaxTablePages, kMaxTablePages, INT32_MAX, INT32_MIN, 0}, differs = INT32_MAX;
   __syncthreads();
-  const int row0 = from < to ? kv_entry(a.v, from).row0 : 0, slot0 = from < to ? kv_entry(a.v, from).slot : -1;
   for (int side = 0; side < 2; ++side) {
-    const int end = side ? to2 : to;
-    for (int b = (side ? max(from2, to) : from) + tid; b < end; b += kPlanThreads) {
+    const int begin = side ? max(from2, to) : from, end = side ? to2 : to;
+    for (int b = begin + tid; b < end; b += kShareThreads) {
       const KvEntry e = kv_entry(a.v, b);
-      atomicMin(&whole, e.length / kPage);
+      if (b - begin < kSlotsHeld) slots[b - begin] = e.slot;
+      atomicMin(&all.whole, e.length / kPage);
+      if (!writes) continue;
       if (e.n > 0) {
-        atomicMin(&seen, max(e.length - e.n + 1, 0) / kPage);
-        atomicMin(&first, e.length - e.n);
-        atomicMax(&last, e.length - 1);
-        atomicMax(&end_row, e.row0 + e.n);
-        for (int i = 0; p.entries && i < e.n; ++i) p.row_entry[e.row0 + i] = b, p.row_at[e.row0 + i] = e.length - e.n + i;
+        atomicMin(&all.seen, max(e.length - e.n + 1, 0) / kPage);
+        atomicMin(&all.first, e.length - e.n);
+        atomicMax(&all.last, e.length - 1);
+        atomicMax(&all.end_row, e.row0 + e.n);
       }
       if (!p.entries) continue;
+      for (int i = 0; i < e.n; ++i) p.row_entry[e.row0 + i] = b, p.row_at[e.row0 + i] = e.length - e.n + i;
       p.entries[b].entry = e;
       p.entries[b].group = none ? -1 : g;
-      if (none) p.entries[b].common = 0;
     }
   }
   __syncthreads();
   if (none) return;
-  // The first place in which two of the sequences differ: 256 places at a time, four sequences side by side
-  const int most = from < to ? min(whole, a.v.table_pages) : 0;
-  for (int base = 0; base < most; base += kPlanThreads / 4) {
-    const int place = base + tid % (kPlanThreads / 4);
-    if (place < most) {
-      const int32_t id = a.v.table[(int64_t)slot0 * a.v.table_pages + place];
-      bool other = false;
+  const int most = from < to ? min(all.whole, a.v.table_pages) : 0;
+  // (a sequence outside of the table has no page: then `most` is 0)
+  auto slot_of = [&](int b) { return b - from < kSlotsHeld ? slots[b - from] : a.v.slots ? a.v.slots[b] : b; };
+  int place = blockIdx.y * 64 + tid % 64;
+  for (; place < most; place += gridDim.y * 64) {
+    const int32_t id = a.v.table[(int64_t)slot_of(from) * a.v.table_pages + place];
+    bool other = false;
 #pragma unroll 8
-      for (int b = from + 1 + tid / (kPlanThreads / 4); b < to; b += 4) {
-        const int slot = a.v.slots ? a.v.slots[b] : b;  // (inside the table: a sequence outside has no page, and `most` is 0)
-        other |= a.v.table[(int64_t)slot * a.v.table_pages + place] != id;
-      }
-      if (other) atomicMin(&differs, place);
+    for (int b = from + 1 + tid / 64; b < to; b += kShareThreads / 64) other |= a.v.table[(int64_t)slot_of(b) * a.v.table_pages + place] != id;
+    if (other) {  // (the first of this thread's)
+      atomicMin(&differs, place);
+      break;
     }
-    __syncthreads();
-    if (differs != INT32_MAX) break;
   }
-  const int found = min(most, differs);
-  if (p.prefix && tid == 0) p.prefix[g] = found * kPage;
-  if (!p.entries) return;
-  const int common = to - from < 2 ? 0 : min(min(found, seen), a.max_pages);
-  for (int b = from + tid; b < to; b += kPlanThreads) p.entries[b].common = common;
-  if (tid == 0) {
-    GroupPlan plan{};
-    plan.slot = slot0, plan.common = common, plan.row0 = row0;
-    plan.n = (int)min((int64_t)max(end_row - row0, 0), (int64_t)(to - from) * a.v.max_rows);
-    plan.first = first, plan.last = last;
+  __syncthreads();
+  if (tid) return;
+  p.differs[g * p.slices + blockIdx.y] = differs;
+  if (!writes) return;
+  GroupPlan plan{};
+  plan.row0 = plan.n = 0;
+  if (from < to) {
+    const KvEntry e = kv_entry(a.v, from);
+    plan.slot = e.slot, plan.row0 = e.row0;
+    plan.n = (int)min((int64_t)max(all.end_row - e.row0, 0), (int64_t)(to - from) * a.v.max_rows);
+  }
+  plan.first = all.first, plan.last = all.last;
+  plan.whole = most, plan.common = to - from < 2 ? 0 : min(all.seen, a.max_pages);  // (as far as the tables agree)
+  p.groups[g] = plan;
+}
+
+// Sums over the threads before this one, and over all of them, of two numbers.
+struct Sums {
+  int64_t steps, units;
+};
+__device__ __forceinline__ Sums scan_before(Sums x, Sums* sums, Sums* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  Sums up = x;
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    const int64_t y = __shfl_up(up.steps, s), z = __shfl_up(up.units, s);
+    if (lane >= s) up.steps += y, up.units += z;
+  }
+  __syncthreads();
+  if (lane == 63) sums[wave] = up;
+  __syncthreads();
+  Sums ahead = *all;
+#pragma unroll
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
+    const Sums y = sums[w];
+    if (w < wave) ahead.steps += y.steps, ahead.units += y.units;
+    all->steps += y.steps, all->units += y.units;
+  }
+  return Sums{ahead.steps + up.steps - x.steps, ahead.units + up.units - x.units};
+}
+
+// The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part (in LDS as far as they fit).
+template <bool SINKS>
+__global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
+  __shared__ Sums sums[kPlanThreads / 64];
+  __shared__ int32_t group_before[kPlanThreads], own_before[kPlanThreads];
+  const int tid = threadIdx.x, lane = tid & 63, heads = a.v.heads, groups = p.key.groups;
+  // Where the tables of a group differ first: a wavefront per group, or a thread, where there are few numbers of each
+  const bool alone = p.slices <= 4;
+  for (int g = alone ? tid : tid >> 6; g < groups; g += alone ? kPlanThreads : kPlanThreads / 64) {
+    int differs = INT32_MAX;
+    for (int y = alone ? 0 : lane; y < p.slices; y += alone ? 1 : 64) differs = min(differs, p.differs[g * p.slices + y]);
+    if (!alone)
+#pragma unroll
+      for (int s = 1; s < 64; s *= 2) differs = min(differs, __shfl_xor(differs, s));
+    if (!alone && lane) continue;
+    GroupPlan plan = p.groups[g];
+    const int found = min(plan.whole, differs);
+    if (p.prefix) p.prefix[g] = found * kPage;
+    if (!p.entries) continue;
+    plan.common = min(plan.common, found);
     const PageRange<SINKS> pages = pages_of_group<SINKS>(a, plan);
     plan.each = pages.end - pages.begin;
     plan.tiles = plan.each ? (int)(((int64_t)plan.n * a.group + p.tile_rows - 1) / p.tile_rows) : 0;
     p.groups[g] = plan;
   }
-}
-
-// Sums over the threads before this one, and over all of them.
-__device__ __forceinline__ int64_t scan_before(int64_t x, int64_t* sums, int64_t* all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t up = x;
-#pragma unroll
-  for (int s = 1; s < 64; s *= 2) {
-    const int64_t y = __shfl_up(up, s);
-    if (lane >= s) up += y;
-  }
+  if (!p.entries) return;
   __syncthreads();
-  if (lane == 63) sums[wave] = up;
-  __syncthreads();
-  int64_t ahead = 0;
-  *all = 0;
-  for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w < wave) ahead += sums[w];
-    *all += sums[w];
-  }
-  return ahead + up - x;
-}
-
-// The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part.
-template <bool SINKS>
-__global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
-  __shared__ int64_t sums[kPlanThreads / 64];
-  const int tid = threadIdx.x, heads = a.v.heads;
-  int64_t group_steps = 0, group_units = 0, own_steps = 0, own_units = 0, all;
-  for (int base = 0; base < p.key.groups; base += kPlanThreads) {
+  Sums group_all{}, own_all{};
+  for (int base = 0; base < groups; base += kPlanThreads) {
     const int g = base + tid;
-    const int64_t units = g < p.key.groups ? (int64_t)p.groups[g].tiles * heads : 0, steps = units ? units * p.groups[g].each : 0;
-    const int64_t s = scan_before(steps, sums, &all) + group_steps;
-    group_steps += all;
-    const int64_t u = scan_before(units, sums, &all) + group_units;
-    group_units += all;
-    if (g < p.key.groups) p.groups[g].before = (int)s, p.groups[g].unit0 = (int)u;
+    Sums x{};
+    if (g < groups) x.units = (int64_t)p.groups[g].tiles * heads, x.steps = x.units * p.groups[g].each;
+    const Sums before = scan_before(x, sums, &group_all);
+    if (g < groups) p.groups[g].before = (int)before.steps, p.groups[g].unit0 = (int)before.units;
+    if (base == 0) group_before[tid] = (int)before.steps;
   }
   for (int base = 0; base < a.v.batch; base += kPlanThreads) {
     const int b = base + tid;
-    int64_t units = 0, steps = 0;
+    Sums x{};
     if (b < a.v.batch) {
       const KvEntry e = p.entries[b].entry;
-      const PageRange<SINKS> pages = own_pages<SINKS>(a, e, p.entries[b].common);
+      const int g = p.entries[b].group, common = g < 0 ? 0 : p.groups[g].common;
+      const PageRange<SINKS> pages = own_pages<SINKS>(a, e, common);
       const int each = pages.end - pages.begin, tiles = each > 0 ? tiles_of_entry(a, e, 16) : 0;
-      units = (int64_t)tiles * heads;
-      steps = units * each;
-      p.entries[b].each = each, p.entries[b].tiles = tiles;
+      x.units = (int64_t)tiles * heads, x.steps = x.units * each;
+      p.entries[b].common = common, p.entries[b].each = each, p.entries[b].tiles = tiles;
     }
-    const int64_t s = scan_before(steps, sums, &all) + own_steps;
-    own_steps += all;
-    const int64_t u = scan_before(units, sums, &all) + own_units;
-    own_units += all;
-    if (b < a.v.batch) p.entries[b].before = (int)s, p.entries[b].unit0 = (int)u;
+    const Sums before = scan_before(x, sums, &own_all);
+    if (b < a.v.batch) p.entries[b].before = (int)before.steps, p.entries[b].unit0 = (int)before.units;
+    if (base == 0) own_before[tid] = (int)before.steps;
   }
+  const int64_t group_steps = group_all.steps, own_steps = own_all.steps;
   // Workgroups for shared pages and for own ones, in the proportion of their times
-  const bool usable = group_units <= p.group_units && own_units <= p.own_units && group_steps <= INT32_MAX && own_steps <= INT32_MAX;
+  const bool usable = group_all.units <= p.group_units && own_all.units <= p.own_units && group_steps <= INT32_MAX && own_steps <= INT32_MAX;
   const bool wide = p.tile_rows == kPromptRows;
   const float group_time = (float)group_steps * p.group_cost, own_time = (float)own_steps;
-  int64_t group_workgroups = 0;
+  int group_workgroups = 0;
   if (group_steps) {
-    group_workgroups = own_steps ? (int64_t)((float)p.workgroups * group_time / (group_time + own_time) + 0.5f) : p.workgroups;
-    group_workgroups = min(max(group_workgroups, (int64_t)1), (int64_t)p.workgroups - (own_steps > 0));
+    group_workgroups = own_steps ? (int)((float)p.workgroups * group_time / (group_time + own_time) + 0.5f) : p.workgroups;
+    group_workgroups = min(max(group_workgroups, 1), p.workgroups - (own_steps > 0));
   }
-  const int64_t group_parts = max(wide ? group_workgroups : 4 * group_workgroups, (int64_t)1), own_parts = max(4 * (p.workgroups - group_workgroups), (int64_t)1);
+  const int group_parts = max(wide ? group_workgroups : 4 * group_workgroups, 1), own_parts = max(4 * (p.workgroups - group_workgroups), 1);
   const int of_group = (int)max((group_steps + group_parts - 1) / group_parts, (int64_t)p.group_least);
   const int of_own = (int)max((own_steps + own_parts - 1) / own_parts, (int64_t)p.own_least);
-  __syncthreads();
   if (tid < 16) reinterpret_cast<int32_t*>(&p.head->key)[tid] = reinterpret_cast<const int32_t*>(&p.key)[tid];
   if (tid == 0) {
     p.head->usable = usable;
-    p.head->group_workgroups = (int)group_workgroups;
+    p.head->group_workgroups = group_workgroups;
     p.head->of_group_part = of_group, p.head->of_own_part = of_own;
     p.head->group_steps = usable ? (int)group_steps : 0, p.head->own_steps = usable ? (int)own_steps : 0;
   }
+  __syncthreads();
   if (!usable) return;
-  for (int64_t part = tid; part < group_parts && part * of_group < group_steps; part += kPlanThreads) {
-    const int at = (int)part * of_group;
-    int lo = 0, hi = p.key.groups;  // the last group that starts at or before the step
+  // The last of n groups or entries that starts at or before a step
+  auto holder = [&](int at, int n, const int32_t* held, auto before_of) {
+    int lo = 0, hi = n;
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
-      (p.groups[mid].before <= at ? lo : hi) = mid;
+      ((mid < kPlanThreads ? held[mid] : before_of(mid)) <= at ? lo : hi) = mid;
     }
-    const int each = max(p.groups[lo].each, 1), inside = at - p.groups[lo].before;
-    p.group_starts[part] = PartStart{lo, inside / each, inside % each, 0};
+    return lo;
+  };
+  for (int part = tid; part < group_parts && (int64_t)part * of_group < group_steps; part += kPlanThreads) {
+    const int at = part * of_group, g = holder(at, groups, group_before, [&](int i) { return p.groups[i].before; });
+    const int each = max(p.groups[g].each, 1), inside = at - (g < kPlanThreads ? group_before[g] : p.groups[g].before);
+    p.group_starts[part] = PartStart{g, inside / each, inside % each, 0};
   }
-  for (int64_t part = tid; part < own_parts && part * of_own < own_steps; part += kPlanThreads) {
-    const int at = (int)part * of_own;
-    int lo = 0, hi = a.v.batch;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      (p.entries[mid].before <= at ? lo : hi) = mid;
-    }
-    const int each = max(p.entries[lo].each, 1), inside = at - p.entries[lo].before;
-    p.own_starts[part] = PartStart{lo, inside / each, inside % each, 0};
+  for (int part = tid; part < own_parts && (int64_t)part * of_own < own_steps; part += kPlanThreads) {
+    const int at = part * of_own, b = holder(at, a.v.batch, own_before, [&](int i) { return p.entries[i].before; });
+    const int each = max(p.entries[b].each, 1), inside = at - (b < kPlanThreads ? own_before[b] : p.entries[b].before);
+    p.own_starts[part] = PartStart{b, inside / each, inside % each, 0};
   }
 }
 
@@ -396,16 +426,15 @@ __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_ke
   }
 }
 
-// Adds up the partial results of a row and head, a wavefront each: of the parts of its group's unit, then of its own one's.
+// Adds up the partial results of a row and head, a wavefront each: of the parts of its group's unit, then of its own one's.  Bound by its chain of
+// loads (row, entry, group, m and l, o): partial results are asked for 8 at a time.
 template <int D>
 __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, SharedArgs p) {
-  if (!plan_fits(p) || !p.head->usable) return;
-  const int lane = threadIdx.x & 63;
-  const int64_t at = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (at >= (int64_t)a.v.rows * a.q_heads) return;
-  const int row = (int)(at / a.q_heads), q_head = (int)(at - (int64_t)row * a.q_heads), head = q_head / a.group, h = q_head - head * a.group;
-  const int b = p.row_entry[row];
-  if ((uint32_t)b >= (uint32_t)a.v.batch) return;
+  const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= a.v.rows * a.q_heads) return;
+  const int row = at / a.q_heads, q_head = at - row * a.q_heads, head = q_head / a.group, h = q_head - head * a.group;
+  const int b = p.row_entry[row];  // (a place of the plan, whatever it holds)
+  if (!plan_fits(p) || !p.head->usable || (uint32_t)b >= (uint32_t)a.v.batch) return;
   const EntryPlan plan = p.entries[b];
   if (row < plan.entry.row0 || row >= plan.entry.row0 + plan.entry.n) return;  // (a row of no entry)
   // parts [0, group_parts) and [group_parts, parts)
@@ -436,7 +465,9 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
   for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
   const float base = m == -INFINITY ? 0.0f : m;
   constexpr int EACH = D / 64;
-  float o[EACH] = {}, l = 0.0f;
+  typedef float Dims __attribute__((ext_vector_type(EACH)));
+  Dims o = 0.0f;
+  float l = 0.0f;
   for (int i0 = 0; i0 < parts; i0 += 64) {
     float f = 0.0f, li = 0.0f;
     if (i0 + lane < parts) {
@@ -448,19 +479,36 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
     for (int s = 1; s < 64; s *= 2) li += __shfl_xor(li, s);
     l += li;
     const int count = min(parts - i0, 64);
-    for (int i = 0; i < count; ++i) {
-      const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i));
-      const float* const x = (i0 + i < group_parts ? p.group_o + (group_at + (int64_t)(i0 + i) * p.tile_rows) * D
-                                                   : p.own_o + (own_at + (int64_t)(i0 + i - group_parts) * 16) * D) + lane * EACH;
+    auto add = [&](int i, auto width) {
+      Dims x[width];
 #pragma unroll
-      for (int j = 0; j < EACH; ++j) o[j] = __builtin_fmaf(x[j], fi, o[j]);
-    }
+      for (int u = 0; u < width; ++u) {
+        const int part = i0 + i + u;
+        const float* const row_o =
+            part < group_parts ? p.group_o + (group_at + (int64_t)part * p.tile_rows) * D : p.own_o + (own_at + (int64_t)(part - group_parts) * 16) * D;
+        x[u] = reinterpret_cast<const Dims*>(row_o)[lane];
+      }
+#pragma unroll
+      for (int u = 0; u < width; ++u) {
+        const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i + u));
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) o[j] = __builtin_fmaf(x[u][j], fi, o[j]);
+      }
+    };
+    int i = 0;
+    for (; i + 8 <= count; i += 8) add(i, std::integral_constant<int, 8>{});
+    if (i + 4 <= count) add(i, std::integral_constant<int, 4>{}), i += 4;
+    if (i + 2 <= count) add(i, std::integral_constant<int, 2>{}), i += 2;
+    if (i < count) add(i, std::integral_constant<int, 1>{});
   }
   const bool empty = m == -INFINITY && l == 0.0f;  // (not where every score is a NaN)
   const float inverse = empty ? 0.0f : 1.0f / l;
   uint16_t* const dst = a.O + (int64_t)row * a.o_stride + (int64_t)q_head * D + lane * EACH;
+  typedef uint16_t Bits __attribute__((ext_vector_type(EACH)));
+  Bits bits;
 #pragma unroll
-  for (int j = 0; j < EACH; ++j) dst[j] = bits_of(o[j] * inverse, a.bf16);
+  for (int j = 0; j < EACH; ++j) bits[j] = bits_of(o[j] * inverse, a.bf16);
+  *reinterpret_cast<Bits*>(dst) = bits;
   if (a.lse && lane == 0) a.lse[at] = empty ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
@@ -483,21 +531,23 @@ SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int
   return f;
 }
 
+// Workgroups that compare the tables of a group: some thousand of all groups.
+int slices_of(int groups, int table_pages) {
+  const int want = (table_pages + 63) / 64, some = 1024 / (groups + 1);
+  const int most = some < kMostSlices ? some : kMostSlices;
+  return want < most ? want : most > 1 ? most : 1;
+}
+
 // Bytes of plan and workspace that a call needs.
-int64_t plan_bytes(const SharedForm& f, int batch, int rows, int groups) {
-  if (!f.shared) return kPlanHeadBytes;
-  return kPlanHeadBytes + (int64_t)groups * sizeof(GroupPlan) + (int64_t)batch * sizeof(EntryPlan) + 2 * kMostParts * sizeof(PartStart) +
-         round_up_256((int64_t)rows * 4) * 2;
+int64_t plan_bytes(bool shared, int batch, int rows, int groups) {
+  int64_t bytes = kPlanHeadBytes + (int64_t)groups * sizeof(GroupPlan) + round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4);
+  if (shared) bytes += (int64_t)batch * sizeof(EntryPlan) + 2 * kMostParts * sizeof(PartStart) + round_up_256((int64_t)rows * 4) * 2;
+  return bytes;
 }
 int64_t shared_workspace(const SharedForm& f, int dim) {
   return ((f.group_parts + f.group_units) * f.tile_rows + (f.own_parts + f.own_units) * 16) * (dim + 2) * 4;
 }
 // ... and those that every call of no more entries, rows and groups can do with: the rows of partial results are the most with large tiles.
-int64_t plan_bytes_up_to(int batch, int rows, int groups) {
-  SharedForm f{};
-  f.shared = batch > 1 && groups > 0;
-  return plan_bytes(f, batch, rows, groups);
-}
 int64_t shared_workspace_up_to(int dim, int heads, int group, int batch, int groups, int max_rows) {
   if (batch < 2 || groups < 1 || max_rows < 1 || group > kMostOwnRows) return 0;
   const int64_t own_rows = (int64_t)max_rows * group < kMostOwnRows ? max_rows * group : kMostOwnRows;
@@ -515,8 +565,10 @@ SharedArgs shared_args(const SharedForm& f, const sfmp_kv_layout_t* layout, cons
   uint8_t* at = (uint8_t*)plan;
   auto take = [&](int64_t bytes) { uint8_t* const x = at; at += bytes; return x; };
   p.head = (PlanHead*)take(kPlanHeadBytes);
+  p.groups = (GroupPlan*)take((int64_t)groups * sizeof(GroupPlan));
+  p.differs = (int32_t*)take(round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4));
+  p.slices = slices_of(groups, tables->table_pages);
   if (f.shared) {
-    p.groups = (GroupPlan*)take((int64_t)groups * sizeof(GroupPlan));
     p.entries = (EntryPlan*)take((int64_t)batch->batch * sizeof(EntryPlan));
     p.group_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
     p.own_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
@@ -538,7 +590,7 @@ int launch_shared(const AttentionArgs& a, const SharedArgs& p, hipStream_t strea
   if (lds)
     if (int e = allow_full_lds((const void*)attend_shared_kernel<D, FMT, NTP, SINKS>, "attend_shared_kernel")) return e;
   attend_shared_kernel<D, FMT, NTP, SINKS><<<p.workgroups, 256, lds, stream>>>(a, p);
-  const int64_t joins = ((int64_t)a.v.rows * a.q_heads + 3) / 4;
+  const int64_t joins = ((int64_t)a.v.rows * a.q_heads + 3) / 4;  // (rows * q_heads < 2^31: choose_shared)
   join_shared_kernel<D><<<(uint32_t)joins, 256, 0, stream>>>(a, p);
   return kv_launched("attend_shared_kernel");
 }
@@ -585,7 +637,7 @@ extern "C" int sfmp_kv_share_plan(const sfmp_kv_layout_t* layout, int32_t batch,
                                   int32_t max_tokens, int64_t* bytes) {
   if (!bytes) return SFMP_ERR_NULL;
   if (int e = check_group_sizes(layout, batch, rows, groups, q_heads, max_rows, max_tokens)) return e;
-  *bytes = round_up_256(plan_bytes_up_to(batch, rows, groups));
+  *bytes = round_up_256(plan_bytes(batch > 1 && groups > 0, batch, rows, groups));
   return SFMP_OK;
 }
 
@@ -609,7 +661,7 @@ extern "C" int sfmp_kv_share(const sfmp_kv_layout_t* layout, const sfmp_kv_table
   if (!kv_aligned(prefix_dev, 4)) return SFMP_ERR_ALIGN;
   const SharedForm f = choose_shared(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch->batch, batch->rows, groups, batch->max_rows,
                                      max_tokens);
-  if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
+  if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f.shared, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
   if (groups == 0 || (!f.shared && !prefix_dev)) return SFMP_OK;
   a.group = q_heads / layout->kv_heads;
   a.window = window >= tables->table_pages * kPage ? 0 : window;
@@ -619,8 +671,8 @@ extern "C" int sfmp_kv_share(const sfmp_kv_layout_t* layout, const sfmp_kv_table
   p.prefix = prefix_dev;
   const hipStream_t stream = (hipStream_t)hip_stream;
   const bool sinks_seen = a.window && a.sinks;
-  (sinks_seen ? share_groups_kernel<true> : share_groups_kernel<false>)<<<groups + 1, kPlanThreads, 0, stream>>>(a, p);
-  if (f.shared) (sinks_seen ? share_parts_kernel<true> : share_parts_kernel<false>)<<<1, kPlanThreads, 0, stream>>>(a, p);
+  share_groups_kernel<<<dim3(groups + 1, p.slices), kShareThreads, 0, stream>>>(a, p);
+  (sinks_seen ? share_parts_kernel<true> : share_parts_kernel<false>)<<<1, kPlanThreads, 0, stream>>>(a, p);
   return kv_launched("share_groups_kernel");
 }
 
@@ -634,7 +686,7 @@ extern "C" int sfmp_kv_attention_shared(const sfmp_kv_layout_t* layout, int32_t 
   if (int e = check_shared(layout, batch, group_start_dev, groups, q_heads, max_tokens, window, sinks)) return e;
   const SharedForm f = choose_shared(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch->batch, batch->rows, groups, batch->max_rows,
                                      max_tokens);
-  if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
+  if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f.shared, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
   if (!f.shared)
     return sfmp_kv_attention_sinks(layout, layer, codes_dev, scales_dev, tables, batch, Q_dev, q_heads, dtype, q_stride, max_tokens, window, sinks, scale,
                                    O_dev, o_stride, lse_dev, workspace_dev, workspace_bytes, hip_stream);

@@ -19,7 +19,7 @@ namespace {
 constexpr int kThreads = 512;        // of a piece
 constexpr int kGroups = kThreads / 2;
 constexpr int kMostBeams = 32, kMostChoices = 64;
-constexpr int kMostListed = 16384;   // entries of the lists of a request
+constexpr int kMostListed = 8192;    // entries of the lists of a request
 
 struct Piece {
   double sum;    // of exp(l - top)
@@ -72,13 +72,13 @@ __device__ __forceinline__ float weight_of(float d) {
   return __builtin_amdgcn_exp2f(__builtin_fmaf(d, kHigh, d * kLow));
 }
 
-// The largest threshold that at least k of the keys of a workgroup's groups reach (each wavefront holds all of them, 4 to a lane); found bit by
-// bit, no further than to one that exactly k reach.  `reach`: how many do.  0 if fewer than k keys are above 0.
+// A threshold that at least k and no more than `most` of a workgroup's 256 keys reach (4 to a lane of a wavefront), found bit by bit; where
+// that many are equal, their value, which more reach.  `reach`: how many do.  0 if fewer than k keys are above 0.
 template <typename Key>
-__device__ __forceinline__ Key threshold_of(const Key (&key)[4], int k, int* reach) {
+__device__ __forceinline__ Key threshold_of(const Key (&key)[4], int k, int most, int* reach) {
   Key at = 0;
   *reach = kGroups;
-  for (int bit = (int)sizeof(Key) * 8 - 1; bit >= 0; --bit) {
+  for (int bit = (int)sizeof(Key) * 8 - 1; bit >= 0 && *reach > most; --bit) {
     const Key next = at | (Key)1 << bit;
     int n = 0;
 #pragma unroll
@@ -86,7 +86,6 @@ __device__ __forceinline__ Key threshold_of(const Key (&key)[4], int k, int* rea
     if (n < k) continue;
     at = next;
     *reach = n;
-    if (n == k) break;
   }
   return at;
 }
@@ -114,48 +113,46 @@ __device__ __forceinline__ double sum_of_wave(double x) {
   return x;
 }
 
-// LDS of a piece, before its list of numbers and their ranks
+// LDS of a piece, before the runs of the threads that are looked at, the list of numbers and their ranks
 struct PieceLds {
   double sums[kThreads / 64];
   uint64_t carried[kMostChoices];
-  uint32_t maxima[kThreads], firsts[kThreads];
-  int32_t count, unused[3];
+  uint32_t maxima[kGroups];
+  uint32_t bound, bound_not;    // numbers that are listed: those with larger keys, and of equal ones those with ~number >= bound_not
+  uint32_t largest;
+  int32_t threads, count, unused[3];
 };
-// Numbers that a piece lists: those of `choices` pairs of threads and, where equal maxima reach the bound too, of 32 more.
+// Pairs of threads that are looked at: those that `choices` need and, where others reach the bound too, some more.
 constexpr int kMorePairs = 32;
-__host__ __device__ constexpr int piece_numbers(int choices, int per_thread) { return (choices + kMorePairs) * 2 * (per_thread + 1); }
+__host__ __device__ constexpr int most_threads(int choices) { return 2 * (choices + kMorePairs); }
+// Bytes of LDS: with each thread R runs and its number, and its logits and what it holds of the list as numbers.
+__host__ __device__ constexpr int piece_lds(int choices, int R, int run) {
+  return (int)sizeof(PieceLds) + most_threads(choices) * (R * 16 + 4) + (most_threads(choices) * R * run + kMostChoices) * 12;
+}
 
 // The largest logits and the sum of exponentials of a piece of a row: chunks of R runs of 16 bytes per thread, in registers.
 //
-// Which logits are among the `choices` largest: of the maxima of 256 pairs of threads the choices-th largest is a bound that no fewer logits reach, and
-// only those of the pairs whose maximum reaches it can (where many do that are equal, the lowest numbers), a few more than are wanted; these
-// are ranked in LDS.  Chunks behind the first take the list along.
+// Which logits are among the `choices` largest: a bound that between choices and choices + 32 of the maxima of 256 pairs of threads reach is one
+// that no fewer logits reach, and only the logits of those threads can (where more maxima than that are equal, those of the lowest numbers).  The
+// threads leave their runs in LDS, where all threads look through them; what reaches the bound, a few more than are wanted, is ranked.  Chunks
+// behind the first take the list along.
 template <int T, int R>
 __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
   constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
   extern __shared__ __align__(16) uint8_t lds[];
   PieceLds& shared = *reinterpret_cast<PieceLds*>(lds);
-  uint32_t(&maxima)[kThreads] = shared.maxima;
-  uint32_t(&firsts)[kThreads] = shared.firsts;
-  uint64_t(&carried)[kMostChoices] = shared.carried;
-  int32_t& count = shared.count;
-  const int pairs = a.choices + kMorePairs;
-  uint64_t* const list = reinterpret_cast<uint64_t*>(lds + sizeof(PieceLds));  // (a thread's logits, and what it holds of the list)
-  uint32_t* const ranks = reinterpret_cast<uint32_t*>(list + piece_numbers(a.choices, R * RUN));
+  const int threads_most = most_threads(a.choices);
+  u32x4* const runs_of = reinterpret_cast<u32x4*>(lds + sizeof(PieceLds));           // [threads_most][R]
+  uint64_t* const list = reinterpret_cast<uint64_t*>(runs_of + threads_most * R);    // [threads_most * R * RUN + kMostChoices]
+  uint32_t* const ranks = reinterpret_cast<uint32_t*>(list + threads_most * R * RUN + kMostChoices);
+  uint32_t* const owner = ranks + threads_most * R * RUN + kMostChoices;             // [threads_most]
   const int row = blockIdx.x / a.pieces, piece = blockIdx.x - row * a.pieces, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if ((a.ended && a.ended[row]) || !(a.scores[row] > -INFINITY)) return;  // (no logit of it counts)
   const uint8_t* const start = (const uint8_t*)a.logits + (int64_t)row * a.stride * SIZE;
   const int runs = (a.vocab + RUN - 1) / RUN;
   // (which thread has which logits must not depend on the row's alignment: rows of equal logits have equal sums)
   typedef u32x4 __attribute__((aligned(2))) Run;
-  if (tid < kMostChoices) carried[tid] = 0;
-  float top = -INFINITY;
-  double sum = 0.0;
-  __syncthreads();
-  for (int chunk = 0; chunk < a.chunks_each; ++chunk) {
-    const int first_run = (piece * a.chunks_each + chunk) * (kThreads * R);
-    if (first_run >= runs) break;
-    u32x4 w[R];
+  u32x4 w[R];
+  auto load = [&](int first_run) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int i = (first_run + r * kThreads + tid) * RUN;
@@ -175,7 +172,18 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
           }
       }
     }
-    const uint64_t held = tid < a.choices ? carried[tid] : 0;
+  };
+  load(piece * a.chunks_each * (kThreads * R));  // (while the row's state is on its way)
+  if ((a.ended && a.ended[row]) || !(a.scores[row] > -INFINITY)) return;  // (no logit of it counts)
+  if (tid < kMostChoices) shared.carried[tid] = 0;
+  float top = -INFINITY;
+  double sum = 0.0;
+  __syncthreads();
+  for (int chunk = 0; chunk < a.chunks_each; ++chunk) {
+    const int first_run = (piece * a.chunks_each + chunk) * (kThreads * R);
+    if (first_run >= runs) break;
+    if (chunk) load(first_run);
+    const uint64_t held = tid < a.choices ? shared.carried[tid] : 0;
     float most = -INFINITY;
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -184,30 +192,36 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
     most = in_range(most);
     uint32_t my_key = most > -INFINITY ? key_of(most) : 0;
     my_key = max(my_key, (uint32_t)(held >> 32));
-    maxima[tid] = max(my_key, (uint32_t)__shfl_xor((int)my_key, 1));
-    if (tid == 0) count = 0;
+    my_key = max(my_key, (uint32_t)__shfl_xor((int)my_key, 1));  // (of the pair)
+    if ((tid & 1) == 0) shared.maxima[tid / 2] = my_key;
     __syncthreads();
-    uint32_t key[4], largest = 0;
+    // the bound: one wavefront's work
+    uint32_t key[4];
+    int reach = 0;
+    if (wave == 0) {
+      uint32_t largest = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      key[i] = maxima[2 * (lane + 64 * i)];
-      largest = max(largest, key[i]);
+      for (int i = 0; i < 4; ++i) {
+        key[i] = shared.maxima[lane + 64 * i];
+        largest = max(largest, key[i]);
+      }
+#pragma unroll
+      for (int s = 1; s < 64; s *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, s));
+      const uint32_t bound = threshold_of(key, a.choices, a.choices + kMorePairs, &reach);
+      if (lane == 0) {
+        shared.bound = bound, shared.bound_not = 0, shared.largest = largest;
+        // (more equal maxima than there is room for: marked)
+        shared.count = 0, shared.threads = bound && reach > a.choices + kMorePairs ? -1 : 0;
+      }
     }
-#pragma unroll
-    for (int s = 1; s < 64; s *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, s));
+    __syncthreads();
+    const uint32_t bound = shared.bound, largest = shared.largest;
+    const bool crowded = shared.threads < 0;
     if (largest == 0) {  // (no logit so far)
       __syncthreads();
       continue;
     }
-    const float base = logit_of_key(largest);  // of this chunk and those before
-    if (base != top) {
-      sum = top == -INFINITY ? 0.0 : sum * exp((double)top - (double)base);
-      top = base;
-    }
-    int reach;
-    const uint32_t bound = threshold_of(key, a.choices, &reach);
-    uint32_t bound_number = 0;  // of ~number, where the key is the bound's
-    if (bound && reach > pairs) {
+    if (crowded) {
       uint32_t lowest = ~0u;
 #pragma unroll
       for (int r = R - 1; r >= 0; --r)
@@ -217,19 +231,39 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
           if (x > -INFINITY && key_of(x) == bound) lowest = (first_run + r * kThreads + tid) * RUN + j;
         }
       if ((uint32_t)(held >> 32) == bound) lowest = min(lowest, ~(uint32_t)held);
-      firsts[tid] = ~min(lowest, (uint32_t)__shfl_xor((int)lowest, 1));
+      lowest = min(lowest, (uint32_t)__shfl_xor((int)lowest, 1));
+      if ((tid & 1) == 0) shared.maxima[tid / 2] = ~lowest;  // (the first wavefront holds the maxima)
       __syncthreads();
-      int more = 0, there;
-      uint32_t number[4];
+      if (wave == 0) {
+        int more = 0;
+        uint32_t number[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        more += __popcll(__ballot(key[i] > bound));
-        number[i] = key[i] == bound ? firsts[2 * (lane + 64 * i)] : 0;
+        for (int i = 0; i < 4; ++i) {
+          more += __popcll(__ballot(key[i] > bound));
+          number[i] = key[i] == bound ? shared.maxima[lane + 64 * i] : 0;
+        }
+        const uint32_t bound_not = threshold_of(number, a.choices - more, a.choices - more, &reach);
+        if (lane == 0) shared.bound_not = bound_not, shared.threads = 0;
       }
-      bound_number = threshold_of(number, a.choices - more, &there);
+      __syncthreads();
     }
-    auto wanted = [&](uint32_t k, uint32_t not_number) { return k && (k > bound || (k == bound && not_number >= bound_number)); };
-    // the sum, in fp32 for a run and in fp64 from there on
+    const uint32_t bound_not = shared.bound_not;
+    auto wanted = [&](uint32_t k, uint32_t not_number) { return k && (k > bound || (k == bound && not_number >= bound_not)); };
+    bool looked_at = my_key > bound || (my_key == bound && !crowded);
+    if (crowded && my_key == bound) looked_at = shared.maxima[tid / 2] >= bound_not;
+    if (looked_at && my_key) {
+      const int at = atomicAdd(&shared.threads, 1);
+      owner[at] = tid;
+#pragma unroll
+      for (int r = 0; r < R; ++r) runs_of[at * R + r] = w[r];
+    }
+    if (wanted((uint32_t)(held >> 32), (uint32_t)held)) list[atomicAdd(&shared.count, 1)] = held;
+    // the sum, relative to the largest logit so far; in fp32 for a run and in fp64 from there on
+    const float base = logit_of_key(largest);
+    if (base != top) {
+      sum = top == -INFINITY ? 0.0 : sum * exp((double)top - (double)base);
+      top = base;
+    }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float part = 0.0f;
@@ -242,31 +276,22 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
       }
       sum += (double)part;
     }
-    if (my_key >= bound) {
-      int mine = wanted((uint32_t)(held >> 32), (uint32_t)held);
-#pragma unroll
-      for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int j = 0; j < RUN; ++j) {
-          const float x = in_range(logit_at<T>(w[r], j));
-          mine += x > -INFINITY && wanted(key_of(x), ~(uint32_t)((first_run + r * kThreads + tid) * RUN + j));
-        }
-      if (mine) {
-        int at = atomicAdd(&count, mine);
-        if (wanted((uint32_t)(held >> 32), (uint32_t)held)) list[at++] = held;
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-          for (int j = 0; j < RUN; ++j) {
-            const float x = in_range(logit_at<T>(w[r], j));
-            const uint32_t not_number = ~(uint32_t)((first_run + r * kThreads + tid) * RUN + j);
-            if (x > -INFINITY && wanted(key_of(x), not_number)) list[at++] = (uint64_t)key_of(x) << 32 | not_number;
-          }
-      }
+    __syncthreads();
+    const int numbers = shared.threads * (R * RUN);
+    for (int i = tid; i < numbers; i += kThreads) {
+      const int at = i / (R * RUN), r = i / RUN % R, j = i % RUN;
+      uint32_t bits;
+      if constexpr (SIZE == 4)
+        bits = reinterpret_cast<const uint32_t*>(runs_of)[i];
+      else
+        bits = (uint32_t)reinterpret_cast<const uint16_t*>(runs_of)[i] << (j & 1 ? 16 : 0);
+      const float x = in_range(logit_at<T>(u32x4{bits, bits, bits, bits}, j));
+      const uint32_t not_number = ~(uint32_t)((first_run + r * kThreads + (int)owner[at]) * RUN + j);
+      if (x > -INFINITY && wanted(key_of(x), not_number)) list[atomicAdd(&shared.count, 1)] = (uint64_t)key_of(x) << 32 | not_number;
     }
     __syncthreads();
-    if (tid < kMostChoices) carried[tid] = 0;  // (read above, before two barriers)
-    rank_numbers<kThreads>(list, count, a.choices, ranks, [&](int rank, uint64_t x) { carried[rank] = x; });
+    if (tid < kMostChoices) shared.carried[tid] = 0;
+    rank_numbers<kThreads>(list, shared.count, a.choices, ranks, [&](int rank, uint64_t x) { shared.carried[rank] = x; });
     __syncthreads();
   }
   sum = sum_of_wave(sum);
@@ -276,7 +301,7 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
     // the listed terms again
     double more = 0.0;
     if (lane < a.choices) {
-      const uint64_t x = carried[lane];
+      const uint64_t x = shared.carried[lane];
       if (x) {
         const float l = logit_of_key((uint32_t)(x >> 32));
         more = exp((double)l - (double)top) - (double)weight_of(l - top);
@@ -296,87 +321,90 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
 
 // LDS of a request, before its entries
 struct BestLds {
-  uint64_t maxima[kGroups], orders[kGroups];
+  uint64_t maxima[kGroups];
+  uint32_t orders[kGroups];
   double tops[kMostBeams], scores[kMostBeams], weights[kMostBeams];
   int32_t states[kMostBeams];  // 0: of no more use, 1: goes on, 2: ended
   int32_t best[kMostChoices];
-  int32_t count, unused[3];
+  uint64_t bound;
+  uint32_t bound_order;
+  int32_t count;
 };
 
-// Entries that reach the bound, at most.
-__host__ __device__ inline int most_found(int choices, int all, int threads) { return choices * (threads / kGroups) * ((all + threads - 1) / threads); }
+// Groups of threads whose entries may reach the bound, and these entries, at most.
+constexpr int kMoreGroups = 16;
+__host__ __device__ constexpr int most_found(int choices, int threads, int each) { return (choices + kMoreGroups) * (threads / kGroups) * each; }
 
-// The best continuations of a request among the listed ones: of the maxima of 256 groups of threads the choices-th largest is a bound, as above.
-template <int THREADS>
+// The best continuations of a request among the listed ones, EACH of them in the registers of a thread: a bound that between choices and choices + 16
+// of the maxima of 256 groups of threads reach (of more equal ones the first ones), as above.
+template <int THREADS, int EACH>
 __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
   constexpr int GROUP = THREADS / kGroups;  // threads
   extern __shared__ __align__(16) uint8_t lds[];
   BestLds& shared = *reinterpret_cast<BestLds*>(lds);
-  auto& maxima = shared.maxima;
-  auto& orders = shared.orders;
-  auto &tops = shared.tops, &scores = shared.scores, &weights = shared.weights;
-  auto& states = shared.states;
-  auto& best = shared.best;
-  int32_t& count = shared.count;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, request = blockIdx.x;
-  const int lists = a.beams * a.pieces, all = lists * a.choices;
-  const int most = most_found(a.choices, all, THREADS);
-  uint64_t* const value_keys = reinterpret_cast<uint64_t*>(lds + sizeof(BestLds));
-  uint32_t* const order_keys = reinterpret_cast<uint32_t*>(value_keys + most);
-  uint32_t* const numbers = order_keys + most;
+  const int lists = a.beams * a.pieces, all = lists * a.choices, most = most_found(a.choices, THREADS, EACH);
+  uint64_t* const keys = reinterpret_cast<uint64_t*>(lds + sizeof(BestLds));
+  double* const values = reinterpret_cast<double*>(keys + most);
+  uint32_t* const order_keys = reinterpret_cast<uint32_t*>(values + most);
+  // The i-th entry: of list i % lists its (i / lists)-th, so that the first ones of all lists fall to different threads
+  uint64_t listed[EACH];
+  int list_of[EACH];
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    const int i = tid + x * THREADS, rank = i / lists;
+    list_of[x] = i - rank * lists;
+    listed[x] = i < all ? a.listed[((int64_t)request * lists + list_of[x]) * a.choices + rank] : 0;
+    if (rank) list_of[x] |= 1 << 30;
+  }
   // of every beam: score less the logarithm of the sum of exponentials, of which the largest logit is left aside
   for (int b = wave; b < a.beams; b += THREADS / 64) {
     const int64_t row = (int64_t)request * a.beams + b;
     const float score = a.scores[row];
-    const bool ended = a.ended && a.ended[row];
+    const int ended = a.ended ? a.ended[row] : 0;
+    const float weight = a.weights ? a.weights[row] : 1.0f;
     double sum = 0.0;
     float top = -INFINITY;
     if (!ended && score > -INFINITY) {
-      for (int i = lane; i < a.pieces; i += 64) top = fmaxf(top, a.piece[row * a.pieces + i].top);
-#pragma unroll
-      for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s));
       for (int i = lane; i < a.pieces; i += 64) {
         const Piece p = a.piece[row * a.pieces + i];
+        if (p.top > top) sum *= exp((double)top - (double)p.top), top = p.top;
         if (p.top > -INFINITY) sum += p.sum * exp((double)p.top - (double)top);
       }
+      float most_top = top;
+#pragma unroll
+      for (int s = 1; s < 64; s *= 2) most_top = fmaxf(most_top, __shfl_xor(most_top, s));
+      sum = top > -INFINITY ? sum * exp((double)top - (double)most_top) : 0.0;
       sum = sum_of_wave(sum);
+      top = most_top;
     }
     if (lane == 0) {
-      tops[b] = top;
-      scores[b] = ended ? (double)score : (double)score - log(sum);
-      weights[b] = a.weights ? (double)a.weights[row] : 1.0;
-      states[b] = !(score > -INFINITY) ? 0 : ended ? 2 : top > -INFINITY ? 1 : 0;
+      shared.tops[b] = top;
+      shared.scores[b] = ended ? (double)score : (double)score - log(sum);
+      shared.weights[b] = weight;
+      shared.states[b] = !(score > -INFINITY) ? 0 : ended ? 2 : top > -INFINITY ? 1 : 0;
     }
   }
-  if (tid == 0) count = 0;
+  if (tid == 0) shared.count = 0;
   __syncthreads();
-  // The i-th entry: of list i % lists its (i / lists)-th, so that the first ones of all lists fall to different threads
-  auto entry = [&](int i, double* value, uint64_t* key, uint32_t* order) {
-    const int rank = i / lists, which = i - rank * lists, b = which / a.pieces;
-    *key = 0;
-    if (states[b] == 0) return;
-    uint32_t token;
-    if (states[b] == 2) {
-      if (rank || which - b * a.pieces) return;
-      token = a.end_token;
-      *value = scores[b];
-    } else {
-      const uint64_t x = a.listed[((int64_t)request * lists + which) * a.choices + rank];
-      if (!x) return;
-      token = ~(uint32_t)x;
-      *value = scores[b] + ((double)logit_of_key((uint32_t)(x >> 32)) - tops[b]);
+  uint64_t key[EACH], my_key = 0;
+  uint32_t order[EACH], my_order = 0;  // (larger for those that come first)
+  double value[EACH];
+#pragma unroll
+  for (int x = 0; x < EACH; ++x) {
+    key[x] = 0, order[x] = 0, value[x] = 0.0;
+    if (tid + x * THREADS < all) {
+      const int which = list_of[x] & ~(1 << 30), b = which / a.pieces, state = shared.states[b];
+      const bool first = list_of[x] == b * a.pieces;
+      if (state == 2 ? first : state == 1 && listed[x]) {
+        const uint32_t token = state == 2 ? (uint32_t)a.end_token : ~(uint32_t)listed[x];
+        value[x] = shared.scores[b];
+        if (state == 1) value[x] += (double)logit_of_key((uint32_t)(listed[x] >> 32)) - shared.tops[b];
+        key[x] = key_of(value[x] * shared.weights[b]);
+        order[x] = ~((uint32_t)b << 24 | token);
+      }
     }
-    *key = key_of(*value * weights[b]);
-    *order = ~((uint32_t)b << 24 | token);  // (larger for those that come first)
-  };
-  uint64_t my_key = 0;
-  uint32_t my_order = 0;
-  for (int i = tid; i < all; i += THREADS) {
-    double value;
-    uint64_t k;
-    uint32_t o = 0;
-    entry(i, &value, &k, &o);
-    if (k > my_key || (k == my_key && o > my_order)) my_key = k, my_order = o;
+    if (key[x] > my_key || (key[x] == my_key && order[x] > my_order)) my_key = key[x], my_order = order[x];
   }
 #pragma unroll
   for (int s = 1; s < GROUP; s *= 2) {
@@ -384,56 +412,54 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
     const uint32_t o = (uint32_t)__shfl_xor((int)my_order, s);
     if (k > my_key || (k == my_key && o > my_order)) my_key = k, my_order = o;
   }
-  if (tid % GROUP == 0) maxima[tid / GROUP] = my_key, orders[tid / GROUP] = my_order;
+  if (tid % GROUP == 0) shared.maxima[tid / GROUP] = my_key, shared.orders[tid / GROUP] = my_order;
   __syncthreads();
-  uint64_t key[4];
+  if (wave == 0) {
+    uint64_t k[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) key[i] = maxima[lane + 64 * i];
-  int reach;
-  const uint64_t bound = threshold_of(key, a.choices, &reach);
-  uint32_t bound_order = 0;
-  if (bound && reach > a.choices) {  // equal ones: those that come first
-    int more = 0, there;
-    uint32_t order[4];
+    for (int i = 0; i < 4; ++i) k[i] = shared.maxima[lane + 64 * i];
+    int reach;
+    const uint64_t bound = threshold_of(k, a.choices, a.choices + kMoreGroups, &reach);
+    uint32_t bound_order = 0;
+    if (bound && reach > a.choices + kMoreGroups) {  // equal ones: those that come first
+      int more = 0;
+      uint32_t o[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      more += __popcll(__ballot(key[i] > bound));
-      order[i] = key[i] == bound ? (uint32_t)orders[lane + 64 * i] : 0;
-    }
-    bound_order = threshold_of(order, a.choices - more, &there);
-  }
-  if (my_key > bound || (my_key == bound && my_order >= bound_order)) {
-    for (int i = tid; i < all; i += THREADS) {
-      double value;
-      uint64_t k;
-      uint32_t o;
-      entry(i, &value, &k, &o);
-      if (k && (k > bound || (k == bound && o >= bound_order))) {
-        const int at = atomicAdd(&count, 1);
-        value_keys[at] = k, order_keys[at] = o, numbers[at] = i;
+      for (int i = 0; i < 4; ++i) {
+        more += __popcll(__ballot(k[i] > bound));
+        o[i] = k[i] == bound ? shared.orders[lane + 64 * i] : 0;
       }
+      bound_order = threshold_of(o, a.choices - more, a.choices - more, &reach);
     }
+    if (lane == 0) shared.bound = bound, shared.bound_order = bound_order;
   }
   __syncthreads();
-  const int found = count;
+  const uint64_t bound = shared.bound;
+  const uint32_t bound_order = shared.bound_order;
+#pragma unroll
+  for (int x = 0; x < EACH; ++x)
+    if (key[x] && (key[x] > bound || (key[x] == bound && order[x] >= bound_order))) {
+      const int at = atomicAdd(&shared.count, 1);
+      keys[at] = key[x], order_keys[at] = order[x], values[at] = value[x];
+    }
+  __syncthreads();
+  const int found = shared.count;
   for (int i = tid; i < found; i += THREADS) {
-    const uint64_t k = value_keys[i];
+    const uint64_t k = keys[i];
     const uint32_t o = order_keys[i];
     int above = 0;
-    for (int j = 0; j < found; ++j) above += value_keys[j] > k || (value_keys[j] == k && order_keys[j] > o);
-    if (above < a.choices) best[above] = (int)numbers[i];
+    for (int j = 0; j < found; ++j) above += keys[j] > k || (keys[j] == k && order_keys[j] > o);
+    if (above < a.choices) shared.best[above] = i;
   }
   __syncthreads();
   if (tid < a.choices) {
     const int64_t to = (int64_t)request * a.choices + tid;
-    double value = -INFINITY;
-    uint64_t k;
-    uint32_t order = ~0u;
-    if (tid < found) entry(best[tid], &value, &k, &order);
-    order = ~order;
-    a.next_scores[to] = (float)value;
-    a.parents[to] = tid < found ? (int)(request * a.beams + (order >> 24)) : -1;
-    a.tokens[to] = tid < found ? (int)(order & 0xFFFFFF) : -1;
+    const bool there = tid < found;
+    const int at = there ? shared.best[tid] : 0;
+    const uint32_t o = there ? ~order_keys[at] : 0;
+    a.next_scores[to] = there ? (float)values[at] : -INFINITY;
+    a.parents[to] = there ? (int)(request * a.beams + (o >> 24)) : -1;
+    a.tokens[to] = there ? (int)(o & 0xFFFFFF) : -1;
   }
 }
 
@@ -441,7 +467,6 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
 struct BeamForm {
   int pieces, chunks_each;   // of a row
   int runs;                  // of 16 bytes per thread and chunk: 1 or 4
-  int best_threads;
 };
 BeamForm choose_form(int size, int rows, int beams, int vocab, int choices) {
   BeamForm f;
@@ -454,7 +479,6 @@ BeamForm choose_form(int size, int rows, int beams, int vocab, int choices) {
   if (pieces > chunks) pieces = chunks;
   f.chunks_each = (int)((chunks + pieces - 1) / pieces);
   f.pieces = (int)((chunks + f.chunks_each - 1) / f.chunks_each);
-  f.best_threads = (int64_t)beams * f.pieces * choices > 2048 ? 1024 : 256;
   return f;
 }
 int64_t bytes_of(int64_t pieces, int choices) { return pieces * ((int64_t)sizeof(Piece) + 8 * choices); }
@@ -469,7 +493,7 @@ int check_sizes(int32_t requests, int32_t beams, int32_t vocab, int32_t choices)
 template <int T, int R>
 int launch_pieces(const BeamArgs& a, hipStream_t stream) {
   constexpr int RUN = T == SFMP_TYPE_FP32 ? 4 : 8;
-  const int lds = (int)sizeof(PieceLds) + piece_numbers(a.choices, R * RUN) * 12;
+  const int lds = piece_lds(a.choices, R, RUN);
   if (int e = allow_full_lds((const void*)beam_pieces_kernel<T, R>, "beam_pieces_kernel")) return e;
   beam_pieces_kernel<T, R><<<a.requests * a.beams * a.pieces, kThreads, lds, stream>>>(a);
   return SFMP_OK;
@@ -478,12 +502,20 @@ template <int T>
 int launch_rows(const BeamArgs& a, const BeamForm& f, hipStream_t stream) {
   return f.runs == 1 ? launch_pieces<T, 1>(a, stream) : launch_pieces<T, 4>(a, stream);
 }
-template <int THREADS>
+template <int THREADS, int EACH>
 int launch_best(const BeamArgs& a, hipStream_t stream) {
-  const int lds = (int)sizeof(BestLds) + most_found(a.choices, a.beams * a.pieces * a.choices, THREADS) * 16;
-  if (int e = allow_full_lds((const void*)beam_best_kernel<THREADS>, "beam_best_kernel")) return e;
-  beam_best_kernel<THREADS><<<a.requests, THREADS, lds, stream>>>(a);
+  const int lds = (int)sizeof(BestLds) + most_found(a.choices, THREADS, EACH) * 20;
+  static_assert(THREADS * EACH <= kMostListed && sizeof(BestLds) + most_found(kMostChoices, THREADS, EACH) * 20 <= 160 * 1024, "LDS of a compute unit");
+  if (int e = allow_full_lds((const void*)beam_best_kernel<THREADS, EACH>, "beam_best_kernel")) return e;
+  beam_best_kernel<THREADS, EACH><<<a.requests, THREADS, lds, stream>>>(a);
   return SFMP_OK;
+}
+int launch_best_of(const BeamArgs& a, hipStream_t stream) {
+  const int all = a.beams * a.pieces * a.choices;
+  if (all <= 256) return launch_best<256, 1>(a, stream);
+  if (all <= 1024) return launch_best<256, 4>(a, stream);
+  if (all <= 4096) return launch_best<1024, 4>(a, stream);
+  return launch_best<1024, 8>(a, stream);
 }
 
 bool aligned_to(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
@@ -532,7 +564,7 @@ extern "C" int sfmp_beam_select(const void* logits_dev, int32_t dtype, int32_t r
                 : dtype == SFMP_TYPE_BF16 ? launch_rows<SFMP_TYPE_BF16>(a, f, stream)
                                           : launch_rows<SFMP_TYPE_FP16>(a, f, stream);
   if (e) return e;
-  if (const int e2 = f.best_threads == 1024 ? launch_best<1024>(a, stream) : launch_best<256>(a, stream)) return e2;
+  if (const int e2 = launch_best_of(a, stream)) return e2;
   const hipError_t error = hipGetLastError();
   if (error == hipSuccess) return SFMP_OK;
   note_hip_error("beam_pieces_kernel", hipGetErrorString(error));

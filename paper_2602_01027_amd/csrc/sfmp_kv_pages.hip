@@ -249,15 +249,15 @@ __global__ __launch_bounds__(256) void free_kernel(sfmp_kv_tables_t t, int32_t p
   if (threadIdx.x == 0) t.lengths_dev[slot] = kept;
 }
 
-// Sequences that become what their parents were.  Places of the page table do not depend on each other: a workgroup takes `columns` of them for all
+// Sequences that become what their parents were.  Places of the page table do not depend on each other: a workgroup takes 2^bits of them for all
 // sequences, through LDS, so that rows can be exchanged in place.  Holders change where a place gets another page; sums of whole numbers,
-// the same in every order.  Lengths are read by all workgroups: they change here only where there is one, else in a launch of their own.
+// the same in every order.  Lengths are read by all workgroups: they change here only where there is one (`last`), else in a launch of their own.
 __global__ __launch_bounds__(kThreads) void reorder_kernel(sfmp_kv_tables_t t, int32_t pages, const int32_t* slots, const int32_t* parents, int32_t n,
-                                                           int32_t columns, int32_t last) {
+                                                           int32_t bits, int32_t last) {
   extern __shared__ int32_t lds[];
   int32_t *const slot_of = lds, *const held_of = slot_of + kThreads, *const parent_of = held_of + kThreads;
-  int32_t *const some = parent_of + kThreads, *const ids = some + 1;  // (whether a sequence has a page here); [n][columns]
-  const int i = threadIdx.x, first = blockIdx.x * columns;
+  int32_t *const some = parent_of + kThreads, *const ids = some + 1;  // (whether a sequence has a page here); [n][2^bits]
+  const int i = threadIdx.x, first = blockIdx.x << bits, all = n << bits;
   int length = 0, parent = -1;
   if (i == 0) *some = 0;
   __syncthreads();
@@ -271,19 +271,21 @@ __global__ __launch_bounds__(kThreads) void reorder_kernel(sfmp_kv_tables_t t, i
   }
   if ((length + kPage - 1) / kPage > first) *some = 1;
   __syncthreads();
-  const int width = min(columns, t.table_pages - first);
   if (*some) {
-    for (int x = i; x < n * columns; x += kThreads) {
-      const int y = x / columns, c = x - y * columns;
-      if (c < width && first + c < held_of[y]) ids[x] = t.page_table_dev[(int64_t)slot_of[y] * t.table_pages + first + c];
+    auto place_of = [&](int x) { return first + (x & ((1 << bits) - 1)); };
+#pragma unroll 4
+    for (int x = i; x < all; x += kThreads) {
+      const int y = x >> bits, place = place_of(x);
+      if (place < held_of[y]) ids[x] = t.page_table_dev[(int64_t)slot_of[y] * t.table_pages + place];
     }
     __syncthreads();
-    for (int x = i; x < n * columns; x += kThreads) {
-      const int y = x / columns, c = x - y * columns, from = parent_of[y];
-      if (c >= width || slot_of[y] < 0 || from == y) continue;
-      const bool had = first + c < held_of[y], gets = from >= 0 && first + c < held_of[from];
-      const int old = had ? ids[x] : -1, now = gets ? ids[from * columns + c] : -1;
-      if (gets && !(had && old == now)) t.page_table_dev[(int64_t)slot_of[y] * t.table_pages + first + c] = now;
+#pragma unroll 4
+    for (int x = i; x < all; x += kThreads) {
+      const int y = x >> bits, place = place_of(x), from = parent_of[y];
+      if (slot_of[y] < 0 || from == y) continue;
+      const bool had = place < held_of[y], gets = from >= 0 && place < held_of[from];
+      const int old = had ? ids[x] : -1, now = gets ? ids[(from << bits) + place - first] : -1;
+      if (gets && !(had && old == now)) t.page_table_dev[(int64_t)slot_of[y] * t.table_pages + place] = now;
       if (old == now) continue;
       if ((uint32_t)old < (uint32_t)pages) atomicSub(&t.refs_dev[old], 1);
       if ((uint32_t)now < (uint32_t)pages) atomicAdd(&t.refs_dev[now], 1);
@@ -394,12 +396,14 @@ extern "C" int sfmp_kv_reorder(const sfmp_kv_layout_t* layout, const sfmp_kv_tab
   if (!slots_dev || !parents_dev) return SFMP_ERR_NULL;
   if (!kv_aligned(slots_dev, 4) || !kv_aligned(parents_dev, 4)) return SFMP_ERR_ALIGN;
   const hipStream_t stream = (hipStream_t)hip_stream;
-  const bool one = (int64_t)n * tables->table_pages <= 16384;
-  const int columns = one ? tables->table_pages : 32;
+  int bits = 0;
+  while (1 << bits < tables->table_pages) ++bits;
+  // (one workgroup and no second launch, or 8 places to a workgroup)
+  const bool one = (int64_t)n << bits <= 8192;
+  if (!one) bits = 3;
   if (int e = allow_full_lds((const void*)reorder_kernel, "reorder_kernel")) return e;
-  reorder_kernel<<<(tables->table_pages + columns - 1) / columns, kThreads,
-                   (3 * kThreads + 1 + n * columns) * 4, stream>>>(*tables, layout->pages, slots_dev, parents_dev, n,
-                                                                                                      columns, one);
+  reorder_kernel<<<((tables->table_pages - 1) >> bits) + 1, kThreads, (3 * kThreads + 1 + (n << bits)) * 4, stream>>>(*tables, layout->pages, slots_dev,
+                                                                                                                     parents_dev, n, bits, one);
   if (!one) reorder_lengths_kernel<<<1, kThreads, 0, stream>>>(*tables, slots_dev, parents_dev, n);
   return kv_launched("reorder_kernel");
 }
