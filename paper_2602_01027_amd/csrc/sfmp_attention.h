@@ -1158,6 +1158,7 @@ struct AttentionForm {
   bool prompt;     // tiles of kPromptRows rows: then
   int tiles, units;
   int least;       // pages of a wavefront (of a prompt's workgroup)
+  double time;     // us, as estimated; not of prompts
 };
 
 // With more rows of an entry and key/value head than these, attend_prompt_kernel (48 rows, 8 heads of 128 dims, us: one sequence of 512
@@ -1226,10 +1227,11 @@ AttentionForm choose_form(int dim, int heads, int group, int batch, int all_rows
   // (10, 5.0) us with 128 dims, int8.  The first form waits for its longest unit, the second reads what there is: the host knows
   // the longest sequence alone, and counts half of it for each.
   const double cut = (double)((units * pages + 256 * f.waves - 1) / (256 * f.waves)) * (batch > 1 ? 0.5 : 1.0);
-  const double start = parts_start(f.waves), of_parts = start + (dim == 64 ? 2.9 : 5.0) * cut;
+  const double start = parts_start(f.waves), of_parts = start + (dim == 64 ? 2.9 : 5.0) * cut, of_units = time_of_units(dim, f.waves, units, pages);
   f.may_cut = batch <= kMostPlanned && tiles <= kMostCutTiles && time_of_units(dim, f.waves, units, all_pages) > start;
   f.cut_bytes = cut_bytes_of(dim, f.nt);
-  if (f.may_cut && of_parts < time_of_units(dim, f.waves, units, pages)) f.workgroups = 256;
+  if (f.may_cut && of_parts < of_units) f.workgroups = 256;
+  f.time = f.workgroups ? of_parts : of_units;
   return f;
 }
 

@@ -15,6 +15,7 @@ namespace {
 constexpr int32_t kPlanMagic = 0x5348504C;
 constexpr int kMostOwnRows = 64;     // rows of an entry and key head
 constexpr int kPlanThreads = 1024, kShareThreads = 256;
+constexpr int kJoinAhead = 8;        // partial results that are asked for at a time
 constexpr int kSlotsHeld = 1024;     // entries of a group whose slots are held in LDS
 constexpr int kMostSlices = 64;      // workgroups that compare the tables of a group
 constexpr int kPlanHeadBytes = 256;
@@ -142,51 +143,76 @@ __global__ __launch_bounds__(kShareThreads) void share_groups_kernel(AttentionAr
   const int from2 = none ? start_of(groups) : to, to2 = none ? batch : to;
   if (tid == 0) all = Extent{kMaxTablePages, kMaxTablePages, INT32_MAX, INT32_MIN, 0}, differs = INT32_MAX;
   __syncthreads();
+  Extent mine{kMaxTablePages, kMaxTablePages, INT32_MAX, INT32_MIN, 0};
   for (int side = 0; side < 2; ++side) {
     const int begin = side ? max(from2, to) : from, end = side ? to2 : to;
     for (int b = begin + tid; b < end; b += kShareThreads) {
       const KvEntry e = kv_entry(a.v, b);
       if (b - begin < kSlotsHeld) slots[b - begin] = e.slot;
-      atomicMin(&all.whole, e.length / kPage);
-      if (!writes) continue;
+      mine.whole = min(mine.whole, e.length / kPage);
       if (e.n > 0) {
-        atomicMin(&all.seen, max(e.length - e.n + 1, 0) / kPage);
-        atomicMin(&all.first, e.length - e.n);
-        atomicMax(&all.last, e.length - 1);
-        atomicMax(&all.end_row, e.row0 + e.n);
+        mine.seen = min(mine.seen, max(e.length - e.n + 1, 0) / kPage);
+        mine.first = min(mine.first, e.length - e.n), mine.last = max(mine.last, e.length - 1);
+        mine.end_row = max(mine.end_row, e.row0 + e.n);
       }
-      if (!p.entries) continue;
+      if (!writes || !p.entries) continue;
       for (int i = 0; i < e.n; ++i) p.row_entry[e.row0 + i] = b, p.row_at[e.row0 + i] = e.length - e.n + i;
       p.entries[b].entry = e;
       p.entries[b].group = none ? -1 : g;
     }
   }
-  __syncthreads();
   if (none) return;
+  // (over the wavefront first: atomics of all lanes at one address take a turn for each)
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) {
+    mine.whole = min(mine.whole, __shfl_xor(mine.whole, s)), mine.seen = min(mine.seen, __shfl_xor(mine.seen, s));
+    mine.first = min(mine.first, __shfl_xor(mine.first, s)), mine.last = max(mine.last, __shfl_xor(mine.last, s));
+    mine.end_row = max(mine.end_row, __shfl_xor(mine.end_row, s));
+  }
+  if (tid % 64 == 0) {
+    atomicMin(&all.whole, mine.whole), atomicMin(&all.seen, mine.seen), atomicMin(&all.first, mine.first);
+    atomicMax(&all.last, mine.last), atomicMax(&all.end_row, mine.end_row);
+  }
+  __syncthreads();
+  const int32_t first_row = from < to ? kv_entry(a.v, from).row0 : 0;  // (asked for before the tables)
   const int most = from < to ? min(all.whole, a.v.table_pages) : 0;
   // (a sequence outside of the table has no page: then `most` is 0)
-  auto slot_of = [&](int b) { return b - from < kSlotsHeld ? slots[b - from] : a.v.slots ? a.v.slots[b] : b; };
-  int place = blockIdx.y * 64 + tid % 64;
-  for (; place < most; place += gridDim.y * 64) {
-    const int32_t id = a.v.table[(int64_t)slot_of(from) * a.v.table_pages + place];
+  auto id_of = [&](int slot, int place) { return a.v.table[(int64_t)slot * a.v.table_pages + place]; };
+  constexpr int kRows = kShareThreads / 64, kAhead = 8;
+  const int row = tid / 64, rows = to - from, near = min(rows, kSlotsHeld);
+  int found = INT32_MAX;
+  for (int place = blockIdx.y * 64 + tid % 64; place < most; place += gridDim.y * 64) {
+    const int32_t id = id_of(slots[0], place);
     bool other = false;
-#pragma unroll 8
-    for (int b = from + 1 + tid / 64; b < to; b += kShareThreads / 64) other |= a.v.table[(int64_t)slot_of(b) * a.v.table_pages + place] != id;
+    for (int b = row; b < near; b += kRows * kAhead) {
+      int32_t x[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) x[u] = id_of(slots[min(b + u * kRows, near - 1)], place);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) other |= x[u] != id;
+    }
+    for (int b = near + row; b < rows; b += kRows) other |= id_of(a.v.slots ? a.v.slots[from + b] : from + b, place) != id;
     if (other) {  // (the first of this thread's)
-      atomicMin(&differs, place);
+      found = place;
       break;
     }
   }
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) found = min(found, __shfl_xor(found, s));
+  if (tid % 64 == 0 && found != INT32_MAX) atomicMin(&differs, found);
   __syncthreads();
   if (tid) return;
+  if (!p.entries && gridDim.y == 1) {  // (all that is asked for)
+    p.prefix[g] = min(most, differs) * kPage;
+    return;
+  }
   p.differs[g * p.slices + blockIdx.y] = differs;
   if (!writes) return;
   GroupPlan plan{};
   plan.row0 = plan.n = 0;
   if (from < to) {
-    const KvEntry e = kv_entry(a.v, from);
-    plan.slot = e.slot, plan.row0 = e.row0;
-    plan.n = (int)min((int64_t)max(all.end_row - e.row0, 0), (int64_t)(to - from) * a.v.max_rows);
+    plan.slot = slots[0], plan.row0 = first_row;
+    plan.n = (int)min((int64_t)max(all.end_row - first_row, 0), (int64_t)(to - from) * a.v.max_rows);
   }
   plan.first = all.first, plan.last = all.last;
   plan.whole = most, plan.common = to - from < 2 ? 0 : min(all.seen, a.max_pages);  // (as far as the tables agree)
@@ -218,22 +244,28 @@ __device__ __forceinline__ Sums scan_before(Sums x, Sums* sums, Sums* all) {
   return Sums{ahead.steps + up.steps - x.steps, ahead.units + up.units - x.units};
 }
 
-// The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part (in LDS as far as they fit).
+// The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part.  What it finds of the first
+// 1024 groups and entries it holds in LDS: it is bound by its chain of loads.
 template <bool SINKS>
 __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
   __shared__ Sums sums[kPlanThreads / 64];
-  __shared__ int32_t group_before[kPlanThreads], own_before[kPlanThreads];
+  __shared__ int32_t group_before[kPlanThreads], group_each[kPlanThreads], group_common[kPlanThreads];
+  __shared__ int32_t own_before[kPlanThreads], own_each[kPlanThreads];
   const int tid = threadIdx.x, lane = tid & 63, heads = a.v.heads, groups = p.key.groups;
+  // (of the first entries: asked for before the groups)
+  KvEntry near_entry{-1, 0, 0, 0};
+  int near_group = -1;
+  if (p.entries && tid < a.v.batch) near_entry = p.entries[tid].entry, near_group = p.entries[tid].group;
   // Where the tables of a group differ first: a wavefront per group, or a thread, where there are few numbers of each
   const bool alone = p.slices <= 4;
   for (int g = alone ? tid : tid >> 6; g < groups; g += alone ? kPlanThreads : kPlanThreads / 64) {
+    GroupPlan plan = p.groups[g];
     int differs = INT32_MAX;
     for (int y = alone ? 0 : lane; y < p.slices; y += alone ? 1 : 64) differs = min(differs, p.differs[g * p.slices + y]);
     if (!alone)
 #pragma unroll
       for (int s = 1; s < 64; s *= 2) differs = min(differs, __shfl_xor(differs, s));
     if (!alone && lane) continue;
-    GroupPlan plan = p.groups[g];
     const int found = min(plan.whole, differs);
     if (p.prefix) p.prefix[g] = found * kPage;
     if (!p.entries) continue;
@@ -241,7 +273,8 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     const PageRange<SINKS> pages = pages_of_group<SINKS>(a, plan);
     plan.each = pages.end - pages.begin;
     plan.tiles = plan.each ? (int)(((int64_t)plan.n * a.group + p.tile_rows - 1) / p.tile_rows) : 0;
-    p.groups[g] = plan;
+    p.groups[g].common = plan.common, p.groups[g].each = plan.each, p.groups[g].tiles = plan.tiles;
+    if (g < kPlanThreads) group_common[g] = plan.common, group_each[g] = plan.each, group_before[g] = plan.tiles;  // (tiles, for now)
   }
   if (!p.entries) return;
   __syncthreads();
@@ -249,7 +282,7 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
   for (int base = 0; base < groups; base += kPlanThreads) {
     const int g = base + tid;
     Sums x{};
-    if (g < groups) x.units = (int64_t)p.groups[g].tiles * heads, x.steps = x.units * p.groups[g].each;
+    if (g < groups) x.units = (int64_t)(base ? p.groups[g].tiles : group_before[g]) * heads, x.steps = x.units * (base ? p.groups[g].each : group_each[g]);
     const Sums before = scan_before(x, sums, &group_all);
     if (g < groups) p.groups[g].before = (int)before.steps, p.groups[g].unit0 = (int)before.units;
     if (base == 0) group_before[tid] = (int)before.steps;
@@ -258,12 +291,13 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     const int b = base + tid;
     Sums x{};
     if (b < a.v.batch) {
-      const KvEntry e = p.entries[b].entry;
-      const int g = p.entries[b].group, common = g < 0 ? 0 : p.groups[g].common;
+      const KvEntry e = base ? p.entries[b].entry : near_entry;
+      const int g = base ? p.entries[b].group : near_group, common = g < 0 ? 0 : g < kPlanThreads ? group_common[g] : p.groups[g].common;
       const PageRange<SINKS> pages = own_pages<SINKS>(a, e, common);
       const int each = pages.end - pages.begin, tiles = each > 0 ? tiles_of_entry(a, e, 16) : 0;
       x.units = (int64_t)tiles * heads, x.steps = x.units * each;
       p.entries[b].common = common, p.entries[b].each = each, p.entries[b].tiles = tiles;
+      if (base == 0) own_each[tid] = each;
     }
     const Sums before = scan_before(x, sums, &own_all);
     if (b < a.v.batch) p.entries[b].before = (int)before.steps, p.entries[b].unit0 = (int)before.units;
@@ -302,12 +336,12 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
   };
   for (int part = tid; part < group_parts && (int64_t)part * of_group < group_steps; part += kPlanThreads) {
     const int at = part * of_group, g = holder(at, groups, group_before, [&](int i) { return p.groups[i].before; });
-    const int each = max(p.groups[g].each, 1), inside = at - (g < kPlanThreads ? group_before[g] : p.groups[g].before);
+    const int each = max(g < kPlanThreads ? group_each[g] : p.groups[g].each, 1), inside = at - (g < kPlanThreads ? group_before[g] : p.groups[g].before);
     p.group_starts[part] = PartStart{g, inside / each, inside % each, 0};
   }
   for (int part = tid; part < own_parts && (int64_t)part * of_own < own_steps; part += kPlanThreads) {
     const int at = part * of_own, b = holder(at, a.v.batch, own_before, [&](int i) { return p.entries[i].before; });
-    const int each = max(p.entries[b].each, 1), inside = at - (b < kPlanThreads ? own_before[b] : p.entries[b].before);
+    const int each = max(b < kPlanThreads ? own_each[b] : p.entries[b].each, 1), inside = at - (b < kPlanThreads ? own_before[b] : p.entries[b].before);
     p.own_starts[part] = PartStart{b, inside / each, inside % each, 0};
   }
 }
@@ -459,13 +493,24 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
   auto ml_of = [&](int i) {
     return i < group_parts ? p.group_ml + 2 * (group_at + (int64_t)i * p.tile_rows) : p.own_ml + 2 * (own_at + (int64_t)(i - group_parts) * 16);
   };
+  constexpr int EACH = D / 64;
+  typedef float Dims __attribute__((ext_vector_type(EACH)));
+  Dims x[kJoinAhead];
+  auto ask = [&](int from, Dims(&x)[kJoinAhead]) {
+#pragma unroll
+    for (int u = 0; u < kJoinAhead; ++u) {
+      const int part = min(from + u, parts - 1);
+      const float* const row_o =
+          part < group_parts ? p.group_o + (group_at + (int64_t)part * p.tile_rows) * D : p.own_o + (own_at + (int64_t)(part - group_parts) * 16) * D;
+      x[u] = reinterpret_cast<const Dims*>(row_o)[lane];
+    }
+  };
+  if (parts) ask(0, x);  // (while m and l are on their way)
   float m = -INFINITY;
   for (int i = lane; i < parts; i += 64) m = fmaxf(m, ml_of(i)[0]);
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
   const float base = m == -INFINITY ? 0.0f : m;
-  constexpr int EACH = D / 64;
-  typedef float Dims __attribute__((ext_vector_type(EACH)));
   Dims o = 0.0f;
   float l = 0.0f;
   for (int i0 = 0; i0 < parts; i0 += 64) {
@@ -479,27 +524,16 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
     for (int s = 1; s < 64; s *= 2) li += __shfl_xor(li, s);
     l += li;
     const int count = min(parts - i0, 64);
-    auto add = [&](int i, auto width) {
-      Dims x[width];
+    for (int i = 0; i < count; i += kJoinAhead) {
+      if (i0 + i) ask(i0 + i, x);
 #pragma unroll
-      for (int u = 0; u < width; ++u) {
-        const int part = i0 + i + u;
-        const float* const row_o =
-            part < group_parts ? p.group_o + (group_at + (int64_t)part * p.tile_rows) * D : p.own_o + (own_at + (int64_t)(part - group_parts) * 16) * D;
-        x[u] = reinterpret_cast<const Dims*>(row_o)[lane];
+      for (int u = 0; u < kJoinAhead; ++u) {
+        const bool there = i + u < count;  // (the same in all lanes; what is asked for beyond is not used)
+        const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), (i + u) & 63));
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) o[j] = there ? __builtin_fmaf(x[u][j], fi, o[j]) : o[j];
       }
-#pragma unroll
-      for (int u = 0; u < width; ++u) {
-        const float fi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i + u));
-#pragma unroll
-        for (int j = 0; j < EACH; ++j) o[j] = __builtin_fmaf(x[u][j], fi, o[j]);
-      }
-    };
-    int i = 0;
-    for (; i + 8 <= count; i += 8) add(i, std::integral_constant<int, 8>{});
-    if (i + 4 <= count) add(i, std::integral_constant<int, 4>{}), i += 4;
-    if (i + 2 <= count) add(i, std::integral_constant<int, 2>{}), i += 2;
-    if (i < count) add(i, std::integral_constant<int, 1>{});
+    }
   }
   const bool empty = m == -INFINITY && l == 0.0f;  // (not where every score is a NaN)
   const float inverse = empty ? 0.0f : 1.0f / l;
@@ -514,10 +548,13 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
 
 // ---- launches ------------------------------------------------------------------------------------------------------
 
-SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int groups, int max_rows, int max_tokens) {
+constexpr double kLeastTime = 13.0;  // us of a call without sharing, below which there is nothing to gain
+
+SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int groups, int max_rows, int max_tokens, int window, int sinks) {
   SharedForm f{};
   const int64_t own_rows = (int64_t)max_rows * group, mean = groups ? ((int64_t)rows * group + groups - 1) / groups : 0;
-  f.shared = groups > 0 && groups < batch && max_rows > 0 && own_rows <= kMostOwnRows && (int64_t)rows * heads * group <= INT32_MAX;
+  f.shared = groups > 0 && groups < batch && max_rows > 0 && own_rows <= kMostOwnRows && (int64_t)rows * heads * group <= INT32_MAX &&
+             choose_form(dim, heads, group, batch, rows, max_rows, max_tokens, window, window ? sinks : 0).time > kLeastTime;
   if (!f.shared) return f;
   f.tile_rows = dim == 256 ? (mean <= 16 ? 16 : kPromptRows) : mean <= 32 ? 32 : kPromptRows;
   f.workgroups = dim == 256 || (dim == 128 && f.tile_rows == 32) ? 256 : 512;
@@ -527,7 +564,7 @@ SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int
   f.own_least = 1;
   f.group_units = ((int64_t)batch * own_rows / f.tile_rows + groups) * heads;
   f.own_units = (int64_t)batch * ((own_rows + 15) / 16) * heads;
-  f.group_cost = f.tile_rows == kPromptRows ? 2.2f : 1.0f;
+  f.group_cost = f.tile_rows == kPromptRows ? 3.0f : 1.0f;
   return f;
 }
 
@@ -567,7 +604,7 @@ SharedArgs shared_args(const SharedForm& f, const sfmp_kv_layout_t* layout, cons
   p.head = (PlanHead*)take(kPlanHeadBytes);
   p.groups = (GroupPlan*)take((int64_t)groups * sizeof(GroupPlan));
   p.differs = (int32_t*)take(round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4));
-  p.slices = slices_of(groups, tables->table_pages);
+  p.slices = f.shared ? slices_of(groups, tables->table_pages) : 1;
   if (f.shared) {
     p.entries = (EntryPlan*)take((int64_t)batch->batch * sizeof(EntryPlan));
     p.group_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
@@ -660,7 +697,7 @@ extern "C" int sfmp_kv_share(const sfmp_kv_layout_t* layout, const sfmp_kv_table
   if (int e = check_shared(layout, batch, group_start_dev, groups, q_heads, max_tokens, window, sinks)) return e;
   if (!kv_aligned(prefix_dev, 4)) return SFMP_ERR_ALIGN;
   const SharedForm f = choose_shared(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch->batch, batch->rows, groups, batch->max_rows,
-                                     max_tokens);
+                                     max_tokens, window, sinks);
   if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f.shared, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
   if (groups == 0 || (!f.shared && !prefix_dev)) return SFMP_OK;
   a.group = q_heads / layout->kv_heads;
@@ -672,7 +709,7 @@ extern "C" int sfmp_kv_share(const sfmp_kv_layout_t* layout, const sfmp_kv_table
   const hipStream_t stream = (hipStream_t)hip_stream;
   const bool sinks_seen = a.window && a.sinks;
   share_groups_kernel<<<dim3(groups + 1, p.slices), kShareThreads, 0, stream>>>(a, p);
-  (sinks_seen ? share_parts_kernel<true> : share_parts_kernel<false>)<<<1, kPlanThreads, 0, stream>>>(a, p);
+  if (f.shared) (sinks_seen ? share_parts_kernel<true> : share_parts_kernel<false>)<<<1, kPlanThreads, 0, stream>>>(a, p);
   return kv_launched("share_groups_kernel");
 }
 
@@ -685,7 +722,7 @@ extern "C" int sfmp_kv_attention_shared(const sfmp_kv_layout_t* layout, int32_t 
   if (int e = make_kv_view(layout, layer, codes_dev, scales_dev, tables, batch, &a.v)) return e;
   if (int e = check_shared(layout, batch, group_start_dev, groups, q_heads, max_tokens, window, sinks)) return e;
   const SharedForm f = choose_shared(layout->head_dim, layout->kv_heads, q_heads / layout->kv_heads, batch->batch, batch->rows, groups, batch->max_rows,
-                                     max_tokens);
+                                     max_tokens, window, sinks);
   if (!plan_dev || !kv_aligned(plan_dev, 256) || plan_bytes_given < plan_bytes(f.shared, batch->batch, batch->rows, groups)) return SFMP_ERR_WORKSPACE;
   if (!f.shared)
     return sfmp_kv_attention_sinks(layout, layer, codes_dev, scales_dev, tables, batch, Q_dev, q_heads, dtype, q_stride, max_tokens, window, sinks, scale,

@@ -38,6 +38,7 @@ struct BeamArgs {
   float* next_scores;
   int32_t* parents;
   int32_t* tokens;
+  uint32_t of_lists, of_pieces;   // x / (beams * pieces) and x / pieces as (x * of_...) >> 32, for x < 2^13
   Piece* piece;      // [rows][pieces]
   uint64_t* listed;  // [rows][pieces][choices], falling; 0: none
 };
@@ -72,6 +73,24 @@ __device__ __forceinline__ float weight_of(float d) {
   return __builtin_amdgcn_exp2f(__builtin_fmaf(d, kHigh, d * kLow));
 }
 
+// exp(d) for d <= 0 in fp64: 2^n times the series of r = d - n ln 2, |r| <= ln 2 / 2, whose first term left out is below 2^-47 (the library's
+// function, with every argument's special cases, takes twice the registers).  UNROLL 1 inside of loops, out of which the compiler brings a
+// register pair for every coefficient otherwise.
+constexpr int kTerms = 11;
+__constant__ double kInverseFactorials[kTerms] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0,
+                                                  1.0 / 120.0,      1.0 / 24.0,      1.0 / 6.0,      0.5,           1.0};
+template <int UNROLL = kTerms>
+__device__ __forceinline__ double exp_of(double d) {
+  d = fmax(d, -800.0);  // (0 there)
+  const double n = rint(d * 1.4426950408889634);
+  const double r = fma(n, -0.6931471805599453, d);
+  double p = 0.0;
+#pragma unroll UNROLL
+  for (int i = 0; i < kTerms; ++i) p = fma(p, r, kInverseFactorials[i]);
+  p = fma(p, r, 1.0);
+  return ldexp(p, (int)n);
+}
+
 // A threshold that at least k and no more than `most` of a workgroup's 256 keys reach (4 to a lane of a wavefront), found bit by bit; where
 // that many are equal, their value, which more reach.  `reach`: how many do.  0 if fewer than k keys are above 0.
 template <typename Key>
@@ -90,10 +109,21 @@ __device__ __forceinline__ Key threshold_of(const Key (&key)[4], int k, int most
   return at;
 }
 
-// Ranks of `count` different numbers in LDS, falling; f(rank, number) for those below `wanted`, by all threads.  `ranks` holds `count` counters.
+// Ranks of `count` different numbers in LDS, falling; f(rank, number) for those below `wanted`.  Up to 64 are ranked by the first wavefront, a
+// number per lane, more by all threads (`ranks`: a counter for each).
 template <int THREADS, typename F>
 __device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, int wanted, uint32_t* ranks, F f) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (count <= 64) {
+    if (wave) return;
+    const uint64_t mine = lane < count ? list[lane] : 0;
+    const int low = (int)(uint32_t)mine, high = (int)(uint32_t)(mine >> 32);
+    int rank = 0;
+    for (int j = 0; j < count; ++j)
+      rank += ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, j)) > mine;
+    if (lane < count && rank < wanted) f(rank, mine);
+    return;
+  }
   for (int i = threadIdx.x; i < count; i += THREADS) ranks[i] = 0;
   __syncthreads();
   for (int base = 0; base < count; base += 64) {
@@ -116,6 +146,7 @@ __device__ __forceinline__ double sum_of_wave(double x) {
 // LDS of a piece, before the runs of the threads that are looked at, the list of numbers and their ranks
 struct PieceLds {
   double sums[kThreads / 64];
+  double scale, unused_scale;
   uint64_t carried[kMostChoices];
   uint32_t maxima[kGroups];
   uint32_t bound, bound_not;    // numbers that are listed: those with larger keys, and of equal ones those with ~number >= bound_not
@@ -130,6 +161,14 @@ __host__ __device__ constexpr int piece_lds(int choices, int R, int run) {
   return (int)sizeof(PieceLds) + most_threads(choices) * (R * 16 + 4) + (most_threads(choices) * R * run + kMostChoices) * 12;
 }
 
+// What was made of w is made again from here on: its logits as fp32 take twice its registers, and what is kept of them keeps other workgroups out
+// (118 registers and 2 workgroups of a compute unit against XX).
+template <int R>
+__device__ __forceinline__ void forget(u32x4 (&w)[R]) {
+#pragma unroll
+  for (int r = 0; r < R; ++r) asm volatile("" : "+v"(w[r]));
+}
+
 // The largest logits and the sum of exponentials of a piece of a row: chunks of R runs of 16 bytes per thread, in registers.
 //
 // Which logits are among the `choices` largest: a bound that between choices and choices + 32 of the maxima of 256 pairs of threads reach is one
@@ -137,7 +176,7 @@ __host__ __device__ constexpr int piece_lds(int choices, int R, int run) {
 // threads leave their runs in LDS, where all threads look through them; what reaches the bound, a few more than are wanted, is ranked.  Chunks
 // behind the first take the list along.
 template <int T, int R>
-__global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
+__global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
   constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
   extern __shared__ __align__(16) uint8_t lds[];
   PieceLds& shared = *reinterpret_cast<PieceLds*>(lds);
@@ -160,16 +199,20 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
       w[r] = u32x4{kNone, kNone, kNone, kNone};
       if (i + RUN <= a.vocab) {
         w[r] = *reinterpret_cast<const Run*>(start + (int64_t)i * SIZE);
-      } else if (i < a.vocab) {  // the row's end
-#pragma unroll
-        for (int j = 0; j < RUN; ++j)
-          if (i + j < a.vocab) {
-            if constexpr (SIZE == 4)
-              w[r][j] = ((const uint32_t*)start)[i + j];
-            else
-              w[r][j / 2] = j & 1 ? (w[r][j / 2] & 0xFFFFu) | (uint32_t)((const uint16_t*)start)[i + j] << 16
-                                  : (w[r][j / 2] & 0xFFFF0000u) | ((const uint16_t*)start)[i + j];
-          }
+      } else if (i < a.vocab) {  // the row's end: its last 16 bytes, moved down, or element by element where it has no 16
+        typedef unsigned __int128 Bits;
+        const Bits none = (Bits)(((uint64_t)kNone << 32) | kNone) << 64 | (((uint64_t)kNone << 32) | kNone);
+        Bits bits = none;
+        if (a.vocab >= RUN) {
+          const int over = (i + RUN - a.vocab) * SIZE * 8;
+          const u32x4 x = *reinterpret_cast<const Run*>(start + (int64_t)(a.vocab - RUN) * SIZE);
+          bits = __builtin_bit_cast(Bits, x) >> over | none << (128 - over);
+        } else {
+#pragma unroll 1
+          for (int j = a.vocab - 1; j >= 0; --j)
+            bits = bits << (SIZE * 8) | (SIZE == 4 ? ((const uint32_t*)start)[j] : (uint32_t)((const uint16_t*)start)[j]);
+        }
+        w[r] = __builtin_bit_cast(u32x4, bits);
       }
     }
   };
@@ -194,6 +237,7 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
     my_key = max(my_key, (uint32_t)(held >> 32));
     my_key = max(my_key, (uint32_t)__shfl_xor((int)my_key, 1));  // (of the pair)
     if ((tid & 1) == 0) shared.maxima[tid / 2] = my_key;
+    forget(w);
     __syncthreads();
     // the bound: one wavefront's work
     uint32_t key[4];
@@ -210,6 +254,7 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
       const uint32_t bound = threshold_of(key, a.choices, a.choices + kMorePairs, &reach);
       if (lane == 0) {
         shared.bound = bound, shared.bound_not = 0, shared.largest = largest;
+        if (top > -INFINITY) shared.scale = exp_of<1>((double)top - (double)logit_of_key(largest));  // (of sums so far)
         // (more equal maxima than there is room for: marked)
         shared.count = 0, shared.threads = bound && reach > a.choices + kMorePairs ? -1 : 0;
       }
@@ -258,12 +303,11 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
       for (int r = 0; r < R; ++r) runs_of[at * R + r] = w[r];
     }
     if (wanted((uint32_t)(held >> 32), (uint32_t)held)) list[atomicAdd(&shared.count, 1)] = held;
+    forget(w);
     // the sum, relative to the largest logit so far; in fp32 for a run and in fp64 from there on
     const float base = logit_of_key(largest);
-    if (base != top) {
-      sum = top == -INFINITY ? 0.0 : sum * exp((double)top - (double)base);
-      top = base;
-    }
+    if (top > -INFINITY) sum *= shared.scale;
+    top = base;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float part = 0.0f;
@@ -289,8 +333,8 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
       const uint32_t not_number = ~(uint32_t)((first_run + r * kThreads + (int)owner[at]) * RUN + j);
       if (x > -INFINITY && wanted(key_of(x), not_number)) list[atomicAdd(&shared.count, 1)] = (uint64_t)key_of(x) << 32 | not_number;
     }
+    if (tid < kMostChoices) shared.carried[tid] = 0;  // (read at the chunk's start)
     __syncthreads();
-    if (tid < kMostChoices) shared.carried[tid] = 0;
     rank_numbers<kThreads>(list, shared.count, a.choices, ranks, [&](int rank, uint64_t x) { shared.carried[rank] = x; });
     __syncthreads();
   }
@@ -304,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void beam_pieces_kernel(BeamArgs a) {
       const uint64_t x = shared.carried[lane];
       if (x) {
         const float l = logit_of_key((uint32_t)(x >> 32));
-        more = exp((double)l - (double)top) - (double)weight_of(l - top);
+        more = exp_of((double)l - (double)top) - (double)weight_of(l - top);
       }
       a.listed[((int64_t)row * a.pieces + piece) * a.choices + lane] = x;
     }
@@ -352,7 +396,7 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
   int list_of[EACH];
 #pragma unroll
   for (int x = 0; x < EACH; ++x) {
-    const int i = tid + x * THREADS, rank = i / lists;
+    const int i = tid + x * THREADS, rank = lists == 1 ? i : (int)__umulhi(i, a.of_lists);
     list_of[x] = i - rank * lists;
     listed[x] = i < all ? a.listed[((int64_t)request * lists + list_of[x]) * a.choices + rank] : 0;
     if (rank) list_of[x] |= 1 << 30;
@@ -360,6 +404,7 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
   // of every beam: score less the logarithm of the sum of exponentials, of which the largest logit is left aside
   for (int b = wave; b < a.beams; b += THREADS / 64) {
     const int64_t row = (int64_t)request * a.beams + b;
+    Piece p = a.piece[row * a.pieces + min(lane, a.pieces - 1)];  // (of a row that does not go on, whatever lies there)
     const float score = a.scores[row];
     const int ended = a.ended ? a.ended[row] : 0;
     const float weight = a.weights ? a.weights[row] : 1.0f;
@@ -367,14 +412,14 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
     float top = -INFINITY;
     if (!ended && score > -INFINITY) {
       for (int i = lane; i < a.pieces; i += 64) {
-        const Piece p = a.piece[row * a.pieces + i];
-        if (p.top > top) sum *= exp((double)top - (double)p.top), top = p.top;
-        if (p.top > -INFINITY) sum += p.sum * exp((double)p.top - (double)top);
+        if (i >= 64) p = a.piece[row * a.pieces + i];
+        if (p.top > top) sum *= exp_of((double)top - (double)p.top), top = p.top;
+        if (p.top > -INFINITY) sum += p.sum * exp_of((double)p.top - (double)top);
       }
       float most_top = top;
 #pragma unroll
       for (int s = 1; s < 64; s *= 2) most_top = fmaxf(most_top, __shfl_xor(most_top, s));
-      sum = top > -INFINITY ? sum * exp((double)top - (double)most_top) : 0.0;
+      sum = top > -INFINITY ? sum * exp_of((double)top - (double)most_top) : 0.0;
       sum = sum_of_wave(sum);
       top = most_top;
     }
@@ -394,7 +439,7 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
   for (int x = 0; x < EACH; ++x) {
     key[x] = 0, order[x] = 0, value[x] = 0.0;
     if (tid + x * THREADS < all) {
-      const int which = list_of[x] & ~(1 << 30), b = which / a.pieces, state = shared.states[b];
+      const int which = list_of[x] & ~(1 << 30), b = a.pieces == 1 ? which : (int)__umulhi(which, a.of_pieces), state = shared.states[b];
       const bool first = list_of[x] == b * a.pieces;
       if (state == 2 ? first : state == 1 && listed[x]) {
         const uint32_t token = state == 2 ? (uint32_t)a.end_token : ~(uint32_t)listed[x];
@@ -444,12 +489,27 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
     }
   __syncthreads();
   const int found = shared.count;
-  for (int i = tid; i < found; i += THREADS) {
-    const uint64_t k = keys[i];
-    const uint32_t o = order_keys[i];
-    int above = 0;
-    for (int j = 0; j < found; ++j) above += keys[j] > k || (keys[j] == k && order_keys[j] > o);
-    if (above < a.choices) shared.best[above] = i;
+  if (found <= 64) {
+    if (wave == 0) {
+      const uint64_t k = lane < found ? keys[lane] : 0;
+      const uint32_t o = lane < found ? order_keys[lane] : 0;
+      int rank = 0;
+      for (int j = 0; j < found; ++j) {
+        const uint64_t kj = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(k >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)k, j);
+        const uint32_t oj = (uint32_t)__builtin_amdgcn_readlane((int)o, j);
+        rank += kj > k || (kj == k && oj > o);
+      }
+      if (lane < found && rank < a.choices) shared.best[rank] = lane;
+    }
+  } else {
+    for (int i = tid; i < found; i += THREADS) {
+      const uint64_t k = keys[i];
+      const uint32_t o = order_keys[i];
+      int above = 0;
+#pragma unroll 4
+      for (int j = 0; j < found; ++j) above += keys[j] > k || (keys[j] == k && order_keys[j] > o);
+      if (above < a.choices) shared.best[above] = i;
+    }
   }
   __syncthreads();
   if (tid < a.choices) {
@@ -557,6 +617,7 @@ extern "C" int sfmp_beam_select(const void* logits_dev, int32_t dtype, int32_t r
   a.requests = requests, a.beams = beams, a.vocab = vocab, a.choices = choices, a.pieces = f.pieces, a.chunks_each = f.chunks_each;
   a.scores = scores_dev, a.weights = weights_dev, a.ended = ended_dev, a.end_token = end_token;
   a.next_scores = next_scores_dev, a.parents = parents_dev, a.tokens = tokens_dev;
+  a.of_lists = (uint32_t)((1ull << 32) / (beams * f.pieces) + 1), a.of_pieces = (uint32_t)((1ull << 32) / f.pieces + 1);
   a.piece = (Piece*)workspace_dev;
   a.listed = (uint64_t*)(a.piece + pieces);
   const hipStream_t stream = (hipStream_t)hip_stream;
