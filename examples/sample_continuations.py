@@ -1,11 +1,12 @@
 """Several continuations of one prompt, sampled from a small decoder whose projections are mixed-precision SFMP matrices
 (random ones: there is no checkpoint here) and whose keys and values live in the 8-bit paged cache.
 
-    python examples/sample_continuations.py [--steps 64] [--continuations 8] [--eager]
+    python examples/sample_continuations.py [--steps 64] [--continuations 8] [--eager] [--share] [--window 0] [--sinks 0]
 
 The prompt's tokens are reserved, appended and attended to once; the continuations are forked off it and share its pages.
 A decoding step reserves one token for each (a shared, partly filled page is copied then), runs the layers, and chooses the next
-tokens.  Nothing in a step asks the host, so it is captured once as a graph and replayed.  At the end half of the continuations
+tokens.  With --share the attention of a step reads the pages that the continuations share once for all of them, as planned once for all layers; with
+--window every token sees the last of the tokens before it alone, and the first ones (--sinks).  Nothing in a step asks the host, so it is captured once as a graph and replayed.  At the end half of the continuations
 are given back and the pool is compacted."""
 import argparse
 import math
@@ -60,9 +61,11 @@ def norm(x):
 
 
 class Decoder:
-    def __init__(self, shape: Shape, pages: int, sequences: int, table_pages: int, seed: int = 0, device="cuda:0", format="int8"):
+    def __init__(self, shape: Shape, pages: int, sequences: int, table_pages: int, seed: int = 0, device="cuda:0", format="int8",
+                 window: int = 0, sinks: int = 0):
         s = self.shape = shape
         self.device = device
+        self.window, self.sinks = window, sinks
         width = (s.q_heads + 2 * s.kv_heads) * s.head_dim
         seeds = iter(range(1000 * seed, 1000 * seed + 1000))
         make = lambda K, N: Matrix(K, N, next(seeds), device)  # noqa: E731
@@ -84,19 +87,33 @@ class Decoder:
         a, b = x.float().chunk(2, -1)
         return torch.cat((a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()), -1).half()
 
-    def run(self, tokens, positions, slots, row_start, max_rows, max_tokens):
+    def attention(self, slots, row_start, rows, max_rows, max_tokens, groups):
+        """What attends to the cache, (layer, queries, output), in a step; groups: the first sequence of every group that shares its pages, and their
+        end, or None."""
+        s, scale, masks = self.shape, 1.0 / math.sqrt(self.shape.head_dim), dict(window=self.window, sinks=self.sinks)
+        new = lambda size: torch.empty(size, dtype=torch.uint8, device=self.device)  # noqa: E731
+        sizes = (s.q_heads, max_rows, max_tokens)
+        if groups is None:
+            workspace = new(S.sfmp_kv_attention_workspace(self.layout, slots.shape[0], rows, *sizes))
+            return lambda i, q, out: S.sfmp_kv_attention_sinks(self.cache, i, self.tables, slots, row_start, q, out, max_rows, max_tokens, scale,
+                                                               workspace, **masks)
+        sizes = (self.layout, slots.shape[0], rows, groups.shape[0] - 1, *sizes)
+        plan, workspace = new(S.sfmp_kv_share_plan(*sizes)), new(S.sfmp_kv_attention_shared_workspace(*sizes))
+        S.sfmp_kv_share(self.cache, self.tables, slots, row_start, groups, rows, s.q_heads, max_rows, max_tokens, plan, **masks)
+        return lambda i, q, out: S.sfmp_kv_attention_shared(self.cache, i, self.tables, slots, row_start, groups, q, out, max_rows, max_tokens, scale,
+                                                            plan, workspace, **masks)
+
+    def run(self, tokens, positions, slots, row_start, max_rows, max_tokens, groups=None):
         """Hidden states of new tokens, whose places in their sequences have been reserved."""
         s, rows = self.shape, tokens.shape[0]
         x = self.embedding[tokens]
-        size = S.sfmp_kv_attention_workspace(self.layout, slots.shape[0], rows, s.q_heads, max_rows, max_tokens)
-        workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
+        attend = self.attention(slots, row_start, rows, max_rows, max_tokens, groups)
         for i, m in enumerate(self.layers):
             heads = m["qkv"](norm(x)).unflatten(1, (-1, s.head_dim))
             q, k, v = heads.split((s.q_heads, s.kv_heads, s.kv_heads), 1)
             S.sfmp_kv_append(self.cache, i, self.tables, slots, row_start, self.turn(k, positions), v, max_rows)
             attended = torch.empty((rows, s.q_heads, s.head_dim), dtype=torch.float16, device=self.device)
-            S.sfmp_kv_attention(self.cache, i, self.tables, slots, row_start, self.turn(q, positions), attended, max_rows, max_tokens,
-                                1.0 / math.sqrt(s.head_dim), workspace)
+            attend(i, self.turn(q, positions), attended)
             x = x + m["out"](attended.flatten(1))
             gate, up = m["up"](norm(x)).float().chunk(2, -1)
             x = x + m["down"]((torch.nn.functional.silu(gate) * up).half())
@@ -134,9 +151,9 @@ def room(status):
     return "the page table is too short" if int(status) < 0 else f"{int(status)} pages are missing"
 
 
-def sample_continuations(decoder, prompt, n, steps, sampling, seed=0, graph=True):
+def sample_continuations(decoder, prompt, n, steps, sampling, seed=0, graph=True, share=False):
     """tokens int32 and their log-probabilities [steps, n].  Sequence 0 of the decoder and 1 .. n have to be empty; the
-    continuations are left in 1 .. n."""
+    continuations are left in 1 .. n.  share: their attention reads the pages that they share once."""
     device, vocab = decoder.device, decoder.shape.vocab
     numbers = lambda a, b: torch.arange(a, b, dtype=torch.int32, device=device)  # noqa: E731
     slots = numbers(1, n + 1)
@@ -146,6 +163,7 @@ def sample_continuations(decoder, prompt, n, steps, sampling, seed=0, graph=True
     workspace = torch.empty(S.sfmp_sample_workspace(n, vocab), dtype=torch.uint8, device=device)
     failed = torch.zeros(1, dtype=torch.int32, device=device)
     max_tokens = prompt.shape[0] + steps
+    groups = torch.tensor([0, n], dtype=torch.int32, device=device) if share else None
 
     def choose(logits):
         S.sfmp_sample(logits, *filters, u, tokens, logprobs, workspace)
@@ -154,7 +172,7 @@ def sample_continuations(decoder, prompt, n, steps, sampling, seed=0, graph=True
         decoder.reserve(slots)
         failed.copy_(torch.where(failed == 0, decoder.status, failed))
         positions = decoder.tables.lengths[1:n + 1] - 1
-        choose(decoder.logits(decoder.run(tokens, positions, slots, None, 1, max_tokens)))
+        choose(decoder.logits(decoder.run(tokens, positions, slots, None, 1, max_tokens, groups)))
 
     first = decoder.prefill(0, prompt)
     if int(decoder.status):  # (a prompt without room: nothing was reserved, and nothing may be appended for good)
@@ -196,15 +214,20 @@ def main():
     a.add_argument("--steps", type=int, default=64)
     a.add_argument("--layers", type=int, default=2)
     a.add_argument("--eager", action="store_true", help="launch every step instead of replaying a graph")
+    a.add_argument("--share", action="store_true", help="read shared pages once for all continuations")
+    a.add_argument("--window", type=int, default=0, help="tokens that a token sees (0: all before it)")
+    a.add_argument("--sinks", type=int, default=0, help="first tokens that it sees too")
     a = a.parse_args()
     shape = Shape(layers=a.layers)
     each = (a.prompt + a.steps) // 64 + 2
-    decoder = Decoder(shape, pages=each * (a.continuations + 1), sequences=a.continuations + 1, table_pages=each)
+    decoder = Decoder(shape, pages=each * (a.continuations + 1), sequences=a.continuations + 1, table_pages=each,
+                      window=a.window, sinks=a.sinks)
     prompt = torch.randint(0, shape.vocab, (a.prompt,), generator=torch.Generator().manual_seed(1)).to(decoder.device)
     for turn in range(2):  # (the first turn loads the kernels)
         torch.cuda.synchronize()
         start = time.perf_counter()
-        tokens, logprobs = sample_continuations(decoder, prompt, a.continuations, a.steps, Sampling(), seed=turn, graph=not a.eager)
+        tokens, logprobs = sample_continuations(decoder, prompt, a.continuations, a.steps, Sampling(), seed=turn, graph=not a.eager,
+                                                share=a.share)
         torch.cuda.synchronize()
         took = time.perf_counter() - start
         live = give_back(decoder, list(range(1, a.continuations + 1, 2)))
