@@ -15,6 +15,7 @@ namespace {
 constexpr int32_t kPlanMagic = 0x5348504C;
 constexpr int kMostOwnRows = 64;     // rows of an entry and key head
 constexpr int kPlanThreads = 1024, kShareThreads = 256;
+constexpr int kMostJoinedByAll = 512;  // rows and heads whose partial results four wavefronts add up
 constexpr int kJoinAhead = 8;        // partial results that are asked for at a time
 constexpr int kSlotsHeld = 1024;     // entries of a group whose slots are held in LDS
 constexpr int kMostSlices = 64;      // workgroups that compare the tables of a group
@@ -63,7 +64,8 @@ struct SharedForm {
   int tile_rows;             // of a unit of shared pages: 16, 32 (a wavefront's) or kPromptRows (a workgroup's)
   int workgroups;
   int group_parts, own_parts;        // at most
-  int group_least, own_least;        // steps of a part
+  float group_least;                 // steps of a part, times the root of a unit's pages
+  int own_least;                     // steps of a part
   int64_t group_units, own_units;    // at most
   float group_cost;                  // time of a step of shared pages, in that of an own one of a wavefront
 };
@@ -81,7 +83,8 @@ struct SharedArgs {
   int32_t* prefix;           // or null
   int32_t* differs;          // [groups][slices] the first place that a workgroup found to differ
   int32_t slices;
-  int32_t tile_rows, workgroups, group_least, own_least;
+  int32_t tile_rows, workgroups, own_least;
+  float group_least;
   int64_t group_units, own_units;
   float group_cost;
   // partial results: o [slot][rows][dim], m and l [slot][rows][2].  The slot of a unit in a part is the sum of their numbers: from one
@@ -249,6 +252,7 @@ __device__ __forceinline__ Sums scan_before(Sums x, Sums* sums, Sums* all) {
 template <bool SINKS>
 __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
   __shared__ Sums sums[kPlanThreads / 64];
+  __shared__ int longest_of_all;
   __shared__ int32_t group_before[kPlanThreads], group_each[kPlanThreads], group_common[kPlanThreads];
   __shared__ int32_t own_before[kPlanThreads], own_each[kPlanThreads];
   const int tid = threadIdx.x, lane = tid & 63, heads = a.v.heads, groups = p.key.groups;
@@ -277,12 +281,15 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     if (g < kPlanThreads) group_common[g] = plan.common, group_each[g] = plan.each, group_before[g] = plan.tiles;  // (tiles, for now)
   }
   if (!p.entries) return;
+  if (tid == 0) longest_of_all = 1;
   __syncthreads();
   Sums group_all{}, own_all{};
+  int longest = 1;
   for (int base = 0; base < groups; base += kPlanThreads) {
     const int g = base + tid;
     Sums x{};
     if (g < groups) x.units = (int64_t)(base ? p.groups[g].tiles : group_before[g]) * heads, x.steps = x.units * (base ? p.groups[g].each : group_each[g]);
+    if (x.units) longest = max(longest, (int)(x.steps / x.units));
     const Sums before = scan_before(x, sums, &group_all);
     if (g < groups) p.groups[g].before = (int)before.steps, p.groups[g].unit0 = (int)before.units;
     if (base == 0) group_before[tid] = (int)before.steps;
@@ -303,6 +310,11 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     if (b < a.v.batch) p.entries[b].before = (int)before.steps, p.entries[b].unit0 = (int)before.units;
     if (base == 0) own_before[tid] = (int)before.steps;
   }
+#pragma unroll
+  for (int s = 1; s < 64; s *= 2) longest = max(longest, __shfl_xor(longest, s));
+  if (lane == 0) atomicMax(&longest_of_all, longest);
+  __syncthreads();
+  longest = longest_of_all;
   const int64_t group_steps = group_all.steps, own_steps = own_all.steps;
   // Workgroups for shared pages and for own ones, in the proportion of their times
   const bool usable = group_all.units <= p.group_units && own_all.units <= p.own_units && group_steps <= INT32_MAX && own_steps <= INT32_MAX;
@@ -314,7 +326,9 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     group_workgroups = min(max(group_workgroups, 1), p.workgroups - (own_steps > 0));
   }
   const int group_parts = max(wide ? group_workgroups : 4 * group_workgroups, 1), own_parts = max(4 * (p.workgroups - group_workgroups), 1);
-  const int of_group = (int)max((group_steps + group_parts - 1) / group_parts, (int64_t)p.group_least);
+  // (a unit of n pages in parts of n / x: x steps after one another, and what joins n / x partial results; the least together near sqrt(n) / 10)
+  const int least = max((int)ceilf(sqrtf((float)longest) * p.group_least), 1);
+  const int of_group = (int)max((group_steps + group_parts - 1) / group_parts, (int64_t)least);
   const int of_own = (int)max((own_steps + own_parts - 1) / own_parts, (int64_t)p.own_least);
   if (tid < 16) reinterpret_cast<int32_t*>(&p.head->key)[tid] = reinterpret_cast<const int32_t*>(&p.key)[tid];
   if (tid == 0) {
@@ -460,11 +474,13 @@ __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_ke
   }
 }
 
-// Adds up the partial results of a row and head, a wavefront each: of the parts of its group's unit, then of its own one's.  Bound by its chain of
-// loads (row, entry, group, m and l, o): partial results are asked for 8 at a time.
-template <int D>
+// Adds up the partial results of a row and head: of the parts of its group's unit, then of its own one's.  J wavefronts share them (4 where there are few rows
+// and heads, 1 for many).  Bound by its chain of loads (row, entry, group, m and l, o): partial results are asked for 8 at a time.
+template <int D, int J>
 __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, SharedArgs p) {
-  const int lane = threadIdx.x & 63, at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int EACH = D / 64;
+  typedef float Dims __attribute__((ext_vector_type(EACH)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = J == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
   if (at >= a.v.rows * a.q_heads) return;
   const int row = at / a.q_heads, q_head = at - row * a.q_heads, head = q_head / a.group, h = q_head - head * a.group;
   const int b = p.row_entry[row];  // (a place of the plan, whatever it holds)
@@ -489,43 +505,43 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
     own_parts = (from + plan.each - 1) / p.head->of_own_part - w0 + 1;
     own_at = ((int64_t)w0 + plan.unit0 + unit) * 16 + i - tile * 16;
   }
-  const int parts = group_parts + own_parts;
+  const int all = group_parts + own_parts, share = (all + J - 1) / J, first = J == 1 ? 0 : min(wave * share, all);
+  const int parts = J == 1 ? all : min(share, all - first);  // (of this wavefront: from `first` on)
   auto ml_of = [&](int i) {
+    i += first;
     return i < group_parts ? p.group_ml + 2 * (group_at + (int64_t)i * p.tile_rows) : p.own_ml + 2 * (own_at + (int64_t)(i - group_parts) * 16);
   };
-  constexpr int EACH = D / 64;
-  typedef float Dims __attribute__((ext_vector_type(EACH)));
   Dims x[kJoinAhead];
-  auto ask = [&](int from, Dims(&x)[kJoinAhead]) {
+  auto ask = [&](int from) {
 #pragma unroll
     for (int u = 0; u < kJoinAhead; ++u) {
-      const int part = min(from + u, parts - 1);
+      const int part = first + min(from + u, parts - 1);
       const float* const row_o =
           part < group_parts ? p.group_o + (group_at + (int64_t)part * p.tile_rows) * D : p.own_o + (own_at + (int64_t)(part - group_parts) * 16) * D;
       x[u] = reinterpret_cast<const Dims*>(row_o)[lane];
     }
   };
-  if (parts) ask(0, x);  // (while m and l are on their way)
+  if (parts > 0) ask(0);  // (while m and l are on their way)
   float m = -INFINITY;
   for (int i = lane; i < parts; i += 64) m = fmaxf(m, ml_of(i)[0]);
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) m = fmaxf(m, __shfl_xor(m, s));
-  const float base = m == -INFINITY ? 0.0f : m;
+  float base = m == -INFINITY ? 0.0f : m;
   Dims o = 0.0f;
   float l = 0.0f;
   for (int i0 = 0; i0 < parts; i0 += 64) {
     float f = 0.0f, li = 0.0f;
     if (i0 + lane < parts) {
-      const float* const x = ml_of(i0 + lane);
-      f = __builtin_amdgcn_exp2f(x[0] - base);
-      li = x[1] * f;
+      const float* const ml = ml_of(i0 + lane);
+      f = __builtin_amdgcn_exp2f(ml[0] - base);
+      li = ml[1] * f;
     }
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) li += __shfl_xor(li, s);
     l += li;
     const int count = min(parts - i0, 64);
     for (int i = 0; i < count; i += kJoinAhead) {
-      if (i0 + i) ask(i0 + i, x);
+      if (i0 + i) ask(i0 + i);
 #pragma unroll
       for (int u = 0; u < kJoinAhead; ++u) {
         const bool there = i + u < count;  // (the same in all lanes; what is asked for beyond is not used)
@@ -533,6 +549,26 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
 #pragma unroll
         for (int j = 0; j < EACH; ++j) o[j] = there ? __builtin_fmaf(x[u][j], fi, o[j]) : o[j];
       }
+    }
+  }
+  if constexpr (J > 1) {
+    __shared__ Dims wave_o[J][64];
+    __shared__ float wave_m[J], wave_l[J];
+    wave_o[wave][lane] = o;
+    if (lane == 0) wave_m[wave] = m, wave_l[wave] = l;
+    __syncthreads();
+    if (wave) return;
+    m = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < J; ++w) m = fmaxf(m, wave_m[w]);
+    base = m == -INFINITY ? 0.0f : m;
+    o = 0.0f, l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < J; ++w) {
+      const float f = __builtin_amdgcn_exp2f(wave_m[w] - base);
+      l += wave_l[w] * f;
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) o[j] = __builtin_fmaf(wave_o[w][lane][j], f, o[j]);
     }
   }
   const bool empty = m == -INFINITY && l == 0.0f;  // (not where every score is a NaN)
@@ -548,22 +584,26 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
 
 // ---- launches ------------------------------------------------------------------------------------------------------
 
-constexpr double kLeastTime = 13.0;  // us of a call without sharing, below which there is nothing to gain
+// Time (us) that sharing takes at least: plan aside, two launches, a page of the group's rows and one of each sequence's own.
+double least_time(int dim, int tile_rows, int64_t own_units) {
+  const double start = tile_rows == kPromptRows ? (dim == 64 ? 13.0 : dim == 128 ? 16.0 : 27.0) : dim == 256 ? 13.5 : 11.5;
+  return start + 0.012 * (double)own_units;
+}
 
 SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int groups, int max_rows, int max_tokens, int window, int sinks) {
   SharedForm f{};
   const int64_t own_rows = (int64_t)max_rows * group, mean = groups ? ((int64_t)rows * group + groups - 1) / groups : 0;
-  f.shared = groups > 0 && groups < batch && max_rows > 0 && own_rows <= kMostOwnRows && (int64_t)rows * heads * group <= INT32_MAX &&
-             choose_form(dim, heads, group, batch, rows, max_rows, max_tokens, window, window ? sinks : 0).time > kLeastTime;
+  if (groups < 1 || groups >= batch || max_rows < 1 || own_rows > kMostOwnRows || (int64_t)rows * heads * group > INT32_MAX) return f;
+  f.own_units = (int64_t)batch * ((own_rows + 15) / 16) * heads;
+  f.tile_rows = dim == 256 ? (mean <= 64 ? 16 : kPromptRows) : mean <= 32 ? 32 : kPromptRows;
+  f.shared = choose_form(dim, heads, group, batch, rows, max_rows, max_tokens, window, window ? sinks : 0).time > least_time(dim, f.tile_rows, f.own_units);
   if (!f.shared) return f;
-  f.tile_rows = dim == 256 ? (mean <= 16 ? 16 : kPromptRows) : mean <= 32 ? 32 : kPromptRows;
   f.workgroups = dim == 256 || (dim == 128 && f.tile_rows == 32) ? 256 : 512;
   f.group_parts = f.tile_rows == kPromptRows ? f.workgroups : 4 * f.workgroups;
   f.own_parts = 4 * f.workgroups;
-  f.group_least = f.tile_rows == kPromptRows ? 4 : 1;
+  f.group_least = 0.1f;
   f.own_least = 1;
   f.group_units = ((int64_t)batch * own_rows / f.tile_rows + groups) * heads;
-  f.own_units = (int64_t)batch * ((own_rows + 15) / 16) * heads;
   f.group_cost = f.tile_rows == kPromptRows ? 3.0f : 1.0f;
   return f;
 }
@@ -577,9 +617,9 @@ int slices_of(int groups, int table_pages) {
 
 // Bytes of plan and workspace that a call needs.
 int64_t plan_bytes(bool shared, int batch, int rows, int groups) {
-  int64_t bytes = kPlanHeadBytes + (int64_t)groups * sizeof(GroupPlan) + round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4);
-  if (shared) bytes += (int64_t)batch * sizeof(EntryPlan) + 2 * kMostParts * sizeof(PartStart) + round_up_256((int64_t)rows * 4) * 2;
-  return bytes;
+  if (!shared) return kPlanHeadBytes;  // (not used)
+  return kPlanHeadBytes + (int64_t)groups * sizeof(GroupPlan) + round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4) +
+         (int64_t)batch * sizeof(EntryPlan) + 2 * kMostParts * sizeof(PartStart) + round_up_256((int64_t)rows * 4) * 2;
 }
 int64_t shared_workspace(const SharedForm& f, int dim) {
   return ((f.group_parts + f.group_units) * f.tile_rows + (f.own_parts + f.own_units) * 16) * (dim + 2) * 4;
@@ -601,11 +641,12 @@ SharedArgs shared_args(const SharedForm& f, const sfmp_kv_layout_t* layout, cons
   SharedArgs p{};
   uint8_t* at = (uint8_t*)plan;
   auto take = [&](int64_t bytes) { uint8_t* const x = at; at += bytes; return x; };
-  p.head = (PlanHead*)take(kPlanHeadBytes);
-  p.groups = (GroupPlan*)take((int64_t)groups * sizeof(GroupPlan));
-  p.differs = (int32_t*)take(round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4));
-  p.slices = f.shared ? slices_of(groups, tables->table_pages) : 1;
+  p.slices = 1;
   if (f.shared) {
+    p.head = (PlanHead*)take(kPlanHeadBytes);
+    p.groups = (GroupPlan*)take((int64_t)groups * sizeof(GroupPlan));
+    p.differs = (int32_t*)take(round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4));
+    p.slices = slices_of(groups, tables->table_pages);
     p.entries = (EntryPlan*)take((int64_t)batch->batch * sizeof(EntryPlan));
     p.group_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
     p.own_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
@@ -627,8 +668,11 @@ int launch_shared(const AttentionArgs& a, const SharedArgs& p, hipStream_t strea
   if (lds)
     if (int e = allow_full_lds((const void*)attend_shared_kernel<D, FMT, NTP, SINKS>, "attend_shared_kernel")) return e;
   attend_shared_kernel<D, FMT, NTP, SINKS><<<p.workgroups, 256, lds, stream>>>(a, p);
-  const int64_t joins = ((int64_t)a.v.rows * a.q_heads + 3) / 4;  // (rows * q_heads < 2^31: choose_shared)
-  join_shared_kernel<D><<<(uint32_t)joins, 256, 0, stream>>>(a, p);
+  const int64_t joins = (int64_t)a.v.rows * a.q_heads;  // (below 2^31: choose_shared)
+  if (joins <= kMostJoinedByAll)
+    join_shared_kernel<D, 4><<<(uint32_t)joins, 256, 0, stream>>>(a, p);
+  else
+    join_shared_kernel<D, 1><<<(uint32_t)((joins + 3) / 4), 256, 0, stream>>>(a, p);
   return kv_launched("attend_shared_kernel");
 }
 

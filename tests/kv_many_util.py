@@ -53,9 +53,12 @@ def compare(pool, tables, order, start, q, got, lse, fmt, dtype, scale, window, 
 
 
 class Groups:
-    """Sequences that share the first pages of their group.  `groups`: (tokens of the prompt, [(rows, tokens behind the prompt)])."""
+    """Sequences that share the first pages of their group.  `groups`: (tokens of the prompt, [(rows, tokens behind the prompt)]).
+    max_tokens: what the call is told of its longest sequence: by it the library decides whether a plan is worth its while (LONG: it is)."""
 
-    def __init__(self, groups, fmt, dim, heads, group, dtype, seed, apart=8, change=None, spare=2, max_tokens=None, slots=True):
+    LONG = 60000
+
+    def __init__(self, groups, fmt, dim, heads, group, dtype, seed, apart=8, change=None, spare=2, max_tokens=LONG, slots=True):
         torch, S = modules()
         rng = np.random.default_rng(5000 + seed)
         self.torch, self.S, self.fmt, self.dtype, self.apart = torch, S, fmt, dtype, apart
@@ -116,6 +119,18 @@ class Groups:
         self.torch.cuda.synchronize()
         assert self.apart == 0 or self.torch.isnan(self.out[:, self.q_heads * self.dim:]).all()
         compare(self.pool, self.tables, self.order, self.start, self.q, self.got, self.lse, self.fmt, self.dtype, self.scale, window, sinks, layer)
+
+    def planned(self, window=0, sinks=0):
+        """Whether the call with these numbers uses a plan (else it needs none of more than its head)."""
+        whole, self.plan = self.plan, self.plan[:256].clone()
+        try:
+            self.attend(window, sinks)
+            return False
+        except self.S.SfmpError as e:
+            assert e.code == -5
+            return True
+        finally:
+            self.plan = whole
 
     def common_tokens(self):
         """What the sequences of each group share, from the tables."""

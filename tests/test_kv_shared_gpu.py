@@ -16,8 +16,10 @@ ONE = [(900, [(1, 1 + 11 * i) for i in range(23)])]
 SMALL = [(128 + 64 * i, [(1, 3), (1, 40)]) for i in range(9)]
 
 
-def _run(groups, fmt, dim, heads, group, dtype, window=0, sinks=0, seed=0, **more):
+def _run(groups, fmt, dim, heads, group, dtype, window=0, sinks=0, seed=0, planned=True, **more):
     g = Groups(groups, fmt, dim, heads, group, dtype, seed, **more)
+    if planned is not None:
+        assert g.planned(window, sinks) == planned
     g.share(window, sinks)
     g.attend(window, sinks)
     g.check(window, sinks)
@@ -38,18 +40,34 @@ def test_against_the_oracle(fmt, groups, dim, heads, group, dtype):
 @pytest.mark.parametrize("groups", [TOKENS, DRAFTS, ONE])
 @pytest.mark.parametrize("dim,group", [(64, 2), (128, 4), (256, 3)])
 def test_with_a_window_and_first_tokens(fmt, window, sinks, groups, dim, group):
-    _run(groups, fmt, dim, 2, group, "float16", window, sinks, seed=dim + window)
+    # (a short window leaves too little to read for a plan)
+    _run(groups, fmt, dim, 2, group, "float16", window, sinks, seed=dim + window, planned=None)
+
+
+@pytest.mark.parametrize("window,sinks", [(2100, 0), (2100, 3), (1950, 65), (30, 5000), (1100, 1000), (1600, 700)])
+@pytest.mark.parametrize("rows,dim,group,fmt", [(1, 64, 4, "int8"), (1, 128, 8, "fp8"), (3, 128, 4, "int8"), (1, 256, 4, "fp8"), (2, 128, 16, "fp8")])
+def test_planned_with_a_window_and_first_tokens(rows, dim, group, fmt, window, sinks):
+    groups = [(2000, [(rows, rows + 11 * i) for i in range(20)]), (1400, [(rows, 5 + 70 * i) for i in range(12)]), (2200, [(rows, 80)])]
+    _run(groups, fmt, dim, 8, group, "float16", window, sinks, seed=dim + window, planned=True)
+
+
+@pytest.mark.parametrize("groups", [TOKENS, DRAFTS, ONE])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_short_calls_run_without_a_plan(groups, window, sinks):
+    _run(groups, "int8", 64, 2, 2, "float16", window, sinks, max_tokens=None, planned=False)  # (8 us by themselves)
+    g = Groups(groups, "int8", 128, 2, 40, "float16", 1)  # (neither do rows that fill large tiles by themselves)
+    assert g.planned(window, sinks) == (40 * max(g.counts) <= 64 and not window)
 
 
 @pytest.mark.parametrize("rows,each", [(1, 40), (2, 20), (5, 3)])
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_tall_groups(rows, each, dim):
-    _run([(2000, [(rows, rows + 3 * i) for i in range(each)])], "int8", dim, 2, 12 if rows < 5 else 8, "bfloat16", seed=rows)
+    _run([(2000, [(rows, rows + 3 * i) for i in range(each)])], "int8", dim, 2, 12 if rows < 5 else 8, "bfloat16", seed=rows, planned=True)
 
 
 def test_sequences_without_slots_and_with_room_in_max_tokens():
     _run(TOKENS, "int8", 128, 2, 4, "float16", slots=False, max_tokens=70000, apart=0)
-    _run(DRAFTS, "fp8", 64, 2, 2, "bfloat16", slots=False, max_tokens=9000, apart=0)
+    _run(DRAFTS, "fp8", 64, 2, 2, "bfloat16", slots=False, max_tokens=19000, apart=0)
 
 
 def test_many_sequences():
