@@ -112,8 +112,8 @@ __device__ __forceinline__ Key threshold_of(const Key (&key)[4], int k, int most
 // Ranks of `count` different numbers in LDS, falling; f(rank, number) for those below `wanted`.  Up to 64 are ranked by the first wavefront, a
 // number per lane, more by all threads (`ranks`: a counter for each).
 template <int THREADS, typename F>
-__device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, int wanted, uint32_t* ranks, F f) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+__device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, int wanted, uint32_t* ranks, int tid, F f) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if (count <= 64) {
     if (wave) return;
     const uint64_t mine = lane < count ? list[lane] : 0;
@@ -124,7 +124,7 @@ __device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, in
     if (lane < count && rank < wanted) f(rank, mine);
     return;
   }
-  for (int i = threadIdx.x; i < count; i += THREADS) ranks[i] = 0;
+  for (int i = tid; i < count; i += THREADS) ranks[i] = 0;
   __syncthreads();
   for (int base = 0; base < count; base += 64) {
     const uint64_t mine = base + lane < count ? list[base + lane] : ~0ull;
@@ -133,7 +133,7 @@ __device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, in
     if (base + lane < count && above) atomicAdd(&ranks[base + lane], above);
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < count; i += THREADS)
+  for (int i = tid; i < count; i += THREADS)
     if ((int)ranks[i] < wanted) f((int)ranks[i], list[i]);
 }
 
@@ -148,17 +148,46 @@ struct PieceLds {
   double sums[kThreads / 64];
   double scale, unused_scale;
   uint64_t carried[kMostChoices];
-  uint32_t maxima[kGroups];
+  uint32_t maxima[kGroups], firsts[kGroups];
   uint32_t bound, bound_not;    // numbers that are listed: those with larger keys, and of equal ones those with ~number >= bound_not
   uint32_t largest;
   int32_t threads, count, unused[3];
 };
 // Pairs of threads that are looked at: those that `choices` need and, where others reach the bound too, some more.
-constexpr int kMorePairs = 32;
+constexpr int kMorePairs = 16;
 __host__ __device__ constexpr int most_threads(int choices) { return 2 * (choices + kMorePairs); }
 // Bytes of LDS: with each thread R runs and its number, and its logits and what it holds of the list as numbers.
 __host__ __device__ constexpr int piece_lds(int choices, int R, int run) {
   return (int)sizeof(PieceLds) + most_threads(choices) * (R * 16 + 4) + (most_threads(choices) * R * run + kMostChoices) * 12;
+}
+
+// The largest logit of a thread (NaN are passed by).
+template <int T, int R>
+__device__ __forceinline__ float most_of(const u32x4 (&w)[R]) {
+  if constexpr (T == SFMP_TYPE_FP16) {  // two at a time
+    half2_ most = {(_Float16)-INFINITY, (_Float16)-INFINITY};
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t pair = w[r][j];  // (the cast of an element of a vector takes the first one)
+        most = __builtin_elementwise_max(most, __builtin_bit_cast(half2_, pair));
+      }
+    return fmaxf((float)most[0], (float)most[1]);
+  }
+  float most = -INFINITY, high = -INFINITY;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (T == SFMP_TYPE_BF16) {
+        most = fmaxf(most, __uint_as_float(w[r][j] << 16));
+        high = fmaxf(high, __uint_as_float(w[r][j] & 0xFFFF0000u));
+      } else {
+        most = fmaxf(most, __uint_as_float(w[r][j]));
+      }
+    }
+  return fmaxf(most, high);
 }
 
 // What was made of w is made again from here on: its logits as fp32 take twice its registers, and what is kept of them keeps other workgroups out
@@ -176,7 +205,7 @@ __device__ __forceinline__ void forget(u32x4 (&w)[R]) {
 // threads leave their runs in LDS, where all threads look through them; what reaches the bound, a few more than are wanted, is ranked.  Chunks
 // behind the first take the list along.
 template <int T, int R>
-__global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
+__global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
   constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
   extern __shared__ __align__(16) uint8_t lds[];
   PieceLds& shared = *reinterpret_cast<PieceLds*>(lds);
@@ -226,13 +255,11 @@ __global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
     const int first_run = (piece * a.chunks_each + chunk) * (kThreads * R);
     if (first_run >= runs) break;
     if (chunk) load(first_run);
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));  // (or the compiler keeps what it makes of it, in registers, over all chunks)
+    const int lane = tid & 63;
     const uint64_t held = tid < a.choices ? shared.carried[tid] : 0;
-    float most = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-      for (int j = 0; j < RUN; ++j) most = fmaxf(most, logit_at<T>(w[r], j));  // (passes NaN by)
-    most = in_range(most);
+    const float most = in_range(most_of<T>(w));
     uint32_t my_key = most > -INFINITY ? key_of(most) : 0;
     my_key = max(my_key, (uint32_t)(held >> 32));
     my_key = max(my_key, (uint32_t)__shfl_xor((int)my_key, 1));  // (of the pair)
@@ -240,10 +267,9 @@ __global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
     forget(w);
     __syncthreads();
     // the bound: one wavefront's work
-    uint32_t key[4];
-    int reach = 0;
     if (wave == 0) {
-      uint32_t largest = 0;
+      uint32_t key[4], largest = 0;
+      int reach;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         key[i] = shared.maxima[lane + 64 * i];
@@ -269,23 +295,26 @@ __global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
     if (crowded) {
       uint32_t lowest = ~0u;
 #pragma unroll
-      for (int r = R - 1; r >= 0; --r)
+      for (int r = R - 1; r >= 0; --r) {
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int j = RUN - 1; j >= 0; --j) {
           const float x = in_range(logit_at<T>(w[r], j));
           if (x > -INFINITY && key_of(x) == bound) lowest = (first_run + r * kThreads + tid) * RUN + j;
         }
+      }
       if ((uint32_t)(held >> 32) == bound) lowest = min(lowest, ~(uint32_t)held);
       lowest = min(lowest, (uint32_t)__shfl_xor((int)lowest, 1));
-      if ((tid & 1) == 0) shared.maxima[tid / 2] = ~lowest;  // (the first wavefront holds the maxima)
+      if ((tid & 1) == 0) shared.firsts[tid / 2] = ~lowest;
       __syncthreads();
       if (wave == 0) {
-        int more = 0;
+        int more = 0, reach;
         uint32_t number[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          more += __popcll(__ballot(key[i] > bound));
-          number[i] = key[i] == bound ? shared.maxima[lane + 64 * i] : 0;
+          const uint32_t key = shared.maxima[lane + 64 * i];
+          more += __popcll(__ballot(key > bound));
+          number[i] = key == bound ? shared.firsts[lane + 64 * i] : 0;
         }
         const uint32_t bound_not = threshold_of(number, a.choices - more, a.choices - more, &reach);
         if (lane == 0) shared.bound_not = bound_not, shared.threads = 0;
@@ -295,7 +324,7 @@ __global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
     const uint32_t bound_not = shared.bound_not;
     auto wanted = [&](uint32_t k, uint32_t not_number) { return k && (k > bound || (k == bound && not_number >= bound_not)); };
     bool looked_at = my_key > bound || (my_key == bound && !crowded);
-    if (crowded && my_key == bound) looked_at = shared.maxima[tid / 2] >= bound_not;
+    if (crowded && my_key == bound) looked_at = shared.firsts[tid / 2] >= bound_not;
     if (looked_at && my_key) {
       const int at = atomicAdd(&shared.threads, 1);
       owner[at] = tid;
@@ -319,6 +348,7 @@ __global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
         for (int j = 0; j < RUN; ++j) part += weight_of(in_range(logit_at<T>(w[r], j)) - base);
       }
       sum += (double)part;
+      __builtin_amdgcn_sched_barrier(0);  // (a run after the other: registers)
     }
     __syncthreads();
     const int numbers = shared.threads * (R * RUN);
@@ -335,7 +365,7 @@ __global__ __launch_bounds__(kThreads, 6) void beam_pieces_kernel(BeamArgs a) {
     }
     if (tid < kMostChoices) shared.carried[tid] = 0;  // (read at the chunk's start)
     __syncthreads();
-    rank_numbers<kThreads>(list, shared.count, a.choices, ranks, [&](int rank, uint64_t x) { shared.carried[rank] = x; });
+    rank_numbers<kThreads>(list, shared.count, a.choices, ranks, tid, [&](int rank, uint64_t x) { shared.carried[rank] = x; });
     __syncthreads();
   }
   sum = sum_of_wave(sum);
