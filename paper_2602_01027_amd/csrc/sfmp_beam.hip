@@ -67,11 +67,23 @@ __device__ __forceinline__ float logit_at(const u32x4& w, int j) {
   return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
 }
 
-// exp(d) in fp32, always the same bits for a d
-__device__ __forceinline__ float weight_of(float d) {
-  constexpr float kHigh = 1.44269502f, kLow = 1.92596303e-8f;  // log2 e
-  return __builtin_amdgcn_exp2f(__builtin_fmaf(d, kHigh, d * kLow));
-}
+// Terms of a sum in fp32, exp(l - base) but for a factor that all of them share, by one operation before the exponential: 2^(l k + c) with
+// k = log2 e and c = -base k, each rounded to fp32.  l k is exact inside, so that the exponent is (l - base) k, off by its own rounding, and
+// base k + c, some 2^-24 of base, which `factor` makes good.  Past kMostBase, where that is no small number: exp(l - base) from the difference.
+constexpr float kLog2e = 1.44269502f, kMostBase = 4096.0f;
+struct Terms {
+  float base, c;
+  __device__ __forceinline__ explicit Terms(float b) : base(b), c(-b * kLog2e) {}
+  __device__ __forceinline__ bool far() const { return !(fabsf(base) < kMostBase); }
+  __device__ __forceinline__ float operator()(float l) const { return __builtin_amdgcn_exp2f(__builtin_fmaf(l, kLog2e, c)); }
+  __device__ __forceinline__ float of_any(float l) const {
+    return __builtin_amdgcn_exp2f(far() ? (l - base) * kLog2e : __builtin_fmaf(l, kLog2e, c));
+  }
+  __device__ __forceinline__ double factor() const {
+    const double x = far() ? 0.0 : -0.6931471805599453 * fma((double)base, (double)kLog2e, (double)c);  // (below 2^-11)
+    return 1.0 + x * (1.0 + x * (0.5 + x * (1.0 / 6.0)));
+  }
+};
 
 // exp(d) for d <= 0 in fp64: 2^n times the series of r = d - n ln 2, |r| <= ln 2 / 2, whose first term left out is below 2^-47 (the library's
 // function, with every argument's special cases, takes twice the registers).  UNROLL 1 inside of loops, out of which the compiler brings a
@@ -175,19 +187,23 @@ __device__ __forceinline__ float most_of(const u32x4 (&w)[R]) {
       }
     return fmaxf((float)most[0], (float)most[1]);
   }
-  float most = -INFINITY, high = -INFINITY;
+  // As whole numbers, positive floats are in their order: two at an operation, and none to quiet a NaN
+  int32_t most = INT32_MIN;
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if constexpr (T == SFMP_TYPE_BF16) {
-        most = fmaxf(most, __uint_as_float(w[r][j] << 16));
-        high = fmaxf(high, __uint_as_float(w[r][j] & 0xFFFF0000u));
-      } else {
-        most = fmaxf(most, __uint_as_float(w[r][j]));
-      }
+      if constexpr (T == SFMP_TYPE_BF16) most = max(most, (int32_t)(w[r][j] << 16));
+      most = max(most, (int32_t)w[r][j]);  // (bf16: the lower half is more digits of the upper one, taken off below)
     }
-  return fmaxf(most, high);
+  if constexpr (T == SFMP_TYPE_BF16) most &= 0xFFFF0000;
+  if (most >= 0 && most <= 0x7F800000) return __uint_as_float((uint32_t)most);
+  float x = -INFINITY;  // none is positive, or there is a NaN
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int j = 0; j < (T == SFMP_TYPE_FP32 ? 4 : 8); ++j) x = fmaxf(x, logit_at<T>(w[r], j));
+  return x;
 }
 
 // What was made of w is made again from here on: its logits as fp32 take twice its registers, and what is kept of them keeps other workgroups out
@@ -261,9 +277,8 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
     const uint64_t held = tid < a.choices ? shared.carried[tid] : 0;
     const float most = in_range(most_of<T>(w));
     uint32_t my_key = most > -INFINITY ? key_of(most) : 0;
-    my_key = max(my_key, (uint32_t)(held >> 32));
-    my_key = max(my_key, (uint32_t)__shfl_xor((int)my_key, 1));  // (of the pair)
-    if ((tid & 1) == 0) shared.maxima[tid / 2] = my_key;
+    const uint32_t pair_key = max(max(my_key, (uint32_t)(held >> 32)), (uint32_t)__shfl_xor((int)max(my_key, (uint32_t)(held >> 32)), 1));
+    if ((tid & 1) == 0) shared.maxima[tid / 2] = pair_key;
     forget(w);
     __syncthreads();
     // the bound: one wavefront's work
@@ -280,7 +295,10 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
       const uint32_t bound = threshold_of(key, a.choices, a.choices + kMorePairs, &reach);
       if (lane == 0) {
         shared.bound = bound, shared.bound_not = 0, shared.largest = largest;
-        if (top > -INFINITY) shared.scale = exp_of<1>((double)top - (double)logit_of_key(largest));  // (of sums so far)
+        if (top > -INFINITY) {  // (of sums so far)
+          const float base = logit_of_key(largest);
+          shared.scale = exp_of<1>((double)top - (double)base) * Terms(top).factor() / Terms(base).factor();
+        }
         // (more equal maxima than there is room for: marked)
         shared.count = 0, shared.threads = bound && reach > a.choices + kMorePairs ? -1 : 0;
       }
@@ -323,9 +341,10 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
     }
     const uint32_t bound_not = shared.bound_not;
     auto wanted = [&](uint32_t k, uint32_t not_number) { return k && (k > bound || (k == bound && not_number >= bound_not)); };
-    bool looked_at = my_key > bound || (my_key == bound && !crowded);
-    if (crowded && my_key == bound) looked_at = shared.firsts[tid / 2] >= bound_not;
-    if (looked_at && my_key) {
+    // (in a crowd a thread of a pair whose maximum is the bound waits for its turn)
+    bool looked_at = my_key && my_key >= bound;
+    if (crowded && shared.maxima[tid / 2] == bound) looked_at &= shared.firsts[tid / 2] >= bound_not;
+    if (looked_at) {
       const int at = atomicAdd(&shared.threads, 1);
       owner[at] = tid;
 #pragma unroll
@@ -334,18 +353,18 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
     if (wanted((uint32_t)(held >> 32), (uint32_t)held)) list[atomicAdd(&shared.count, 1)] = held;
     forget(w);
     // the sum, relative to the largest logit so far; in fp32 for a run and in fp64 from there on
-    const float base = logit_of_key(largest);
     if (top > -INFINITY) sum *= shared.scale;
-    top = base;
+    top = logit_of_key(largest);
+    const Terms terms(top);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       float part = 0.0f;
 #pragma unroll
-      for (int j = 0; j < RUN; ++j) part += weight_of(logit_at<T>(w[r], j) - base);
-      if (!(part <= 2.0f * RUN)) {  // a NaN or an infinity among them
+      for (int j = 0; j < RUN; ++j) part += terms(logit_at<T>(w[r], j));
+      if (!(part <= 2.0f * RUN) || terms.far()) {  // a NaN or an infinity among them, or large numbers
         part = 0.0f;
 #pragma unroll
-        for (int j = 0; j < RUN; ++j) part += weight_of(in_range(logit_at<T>(w[r], j)) - base);
+        for (int j = 0; j < RUN; ++j) part += terms.of_any(in_range(logit_at<T>(w[r], j)));
       }
       sum += (double)part;
       __builtin_amdgcn_sched_barrier(0);  // (a run after the other: registers)
@@ -372,22 +391,23 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
   if (lane == 0) shared.sums[wave] = sum;
   __syncthreads();
   if (wave == 0) {
+    const Terms terms(top);
     // the listed terms again
     double more = 0.0;
     if (lane < a.choices) {
       const uint64_t x = shared.carried[lane];
       if (x) {
         const float l = logit_of_key((uint32_t)(x >> 32));
-        more = exp_of((double)l - (double)top) - (double)weight_of(l - top);
+        more = exp_of((double)l - (double)top) - (double)terms.of_any(l) * terms.factor();
       }
       a.listed[((int64_t)row * a.pieces + piece) * a.choices + lane] = x;
     }
     more = sum_of_wave(more);
     if (lane == 0) {
-      double all = more;
+      double all = 0.0;
       for (int i = 0; i < kThreads / 64; ++i) all += shared.sums[i];
       Piece p;
-      p.sum = all, p.top = top, p.unused = 0;
+      p.sum = top > -INFINITY ? all * terms.factor() + more : 0.0, p.top = top, p.unused = 0;
       a.piece[(int64_t)row * a.pieces + piece] = p;
     }
   }
