@@ -103,20 +103,50 @@ __device__ __forceinline__ double exp_of(double d) {
   return ldexp(p, (int)n);
 }
 
-// A threshold that at least k and no more than `most` of a workgroup's 256 keys reach (4 to a lane of a wavefront), found bit by bit; where
-// that many are equal, their value, which more reach.  `reach`: how many do.  0 if fewer than k keys are above 0.
+// Maximum over a wavefront, in all lanes; without the LDS.
+__device__ __forceinline__ uint32_t max_of_wave(uint32_t x) {
+  auto step = [&](auto ctrl, auto rows) {
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, ctrl(), rows(), 0xF, false));
+  };
+  using std::integral_constant;
+  constexpr integral_constant<int, 0xF> kAllRows{};
+  step(integral_constant<int, 0x111>{}, kAllRows), step(integral_constant<int, 0x112>{}, kAllRows);  // from 1, 2, 4, 8 lanes before, in rows of 16
+  step(integral_constant<int, 0x114>{}, kAllRows), step(integral_constant<int, 0x118>{}, kAllRows);
+  step(integral_constant<int, 0x142>{}, integral_constant<int, 0xA>{});  // from the last lane of the row before
+  step(integral_constant<int, 0x143>{}, integral_constant<int, 0xC>{});  // ... of the first two rows
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ __forceinline__ uint64_t max_of_wave(uint64_t x) {
+  const uint32_t high = max_of_wave((uint32_t)(x >> 32));
+  return (uint64_t)high << 32 | max_of_wave((uint32_t)(x >> 32) == high ? (uint32_t)x : 0u);
+}
+
+// A threshold that at least k and no more than `most` of a workgroup's 256 keys reach (4 to a lane of a wavefront); where that many are equal,
+// their value, which more reach.  `reach`: how many do.  0 if fewer than k keys are above 0.  From the largest key, less and less of whose bits
+// from `bit` on, to the first that k keys reach, then bit by bit up again: the keys that matter agree with the largest in most of their bits.
 template <typename Key>
-__device__ __forceinline__ Key threshold_of(const Key (&key)[4], int k, int most, int* reach) {
-  Key at = 0;
-  *reach = kGroups;
-  for (int bit = (int)sizeof(Key) * 8 - 1; bit >= 0 && *reach > most; --bit) {
-    const Key next = at | (Key)1 << bit;
+__device__ __forceinline__ Key threshold_of(const Key (&key)[4], Key largest, int bit, int k, int most, int* reach) {
+  auto count = [&](Key at) {
     int n = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) n += __popcll(__ballot(key[i] >= next));
+    for (int i = 0; i < 4; ++i) n += __popcll(__ballot(key[i] >= at));
+    return n;
+  };
+  constexpr int BITS = (int)sizeof(Key) * 8;
+  Key at = 0;
+  *reach = kGroups;
+  for (; bit < BITS; ++bit) {
+    const Key next = largest >> bit << bit;
+    const int n = next ? count(next) : 0;
     if (n < k) continue;
-    at = next;
-    *reach = n;
+    at = next, *reach = n;
+    break;
+  }
+  for (bit = min(bit, BITS) - 1; bit >= 0 && *reach > most; --bit) {
+    const Key next = at | (Key)1 << bit;
+    const int n = count(next);
+    if (n < k) continue;
+    at = next, *reach = n;
   }
   return at;
 }
@@ -290,9 +320,8 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
         key[i] = shared.maxima[lane + 64 * i];
         largest = max(largest, key[i]);
       }
-#pragma unroll
-      for (int s = 1; s < 64; s *= 2) largest = max(largest, (uint32_t)__shfl_xor((int)largest, s));
-      const uint32_t bound = threshold_of(key, a.choices, a.choices + kMorePairs, &reach);
+      largest = max_of_wave(largest);
+      const uint32_t bound = threshold_of(key, largest, 20, a.choices, a.choices + kMorePairs, &reach);
       if (lane == 0) {
         shared.bound = bound, shared.bound_not = 0, shared.largest = largest;
         if (top > -INFINITY) {  // (of sums so far)
@@ -304,8 +333,9 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
       }
     }
     __syncthreads();
-    const uint32_t bound = shared.bound, largest = shared.largest;
-    const bool crowded = shared.threads < 0;
+    auto same = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };  // (in all lanes)
+    const uint32_t bound = same(shared.bound), largest = same(shared.largest);
+    const bool crowded = (int32_t)same((uint32_t)shared.threads) < 0;
     if (largest == 0) {  // (no logit so far)
       __syncthreads();
       continue;
@@ -334,12 +364,12 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
           more += __popcll(__ballot(key > bound));
           number[i] = key == bound ? shared.firsts[lane + 64 * i] : 0;
         }
-        const uint32_t bound_not = threshold_of(number, a.choices - more, a.choices - more, &reach);
+        const uint32_t bound_not = threshold_of(number, ~0u, 0, a.choices - more, a.choices - more, &reach);
         if (lane == 0) shared.bound_not = bound_not, shared.threads = 0;
       }
       __syncthreads();
     }
-    const uint32_t bound_not = shared.bound_not;
+    const uint32_t bound_not = same(shared.bound_not);
     auto wanted = [&](uint32_t k, uint32_t not_number) { return k && (k > bound || (k == bound && not_number >= bound_not)); };
     // (in a crowd a thread of a pair whose maximum is the bound waits for its turn)
     bool looked_at = my_key && my_key >= bound;
@@ -514,7 +544,8 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) k[i] = shared.maxima[lane + 64 * i];
     int reach;
-    const uint64_t bound = threshold_of(k, a.choices, a.choices + kMoreGroups, &reach);
+    const uint64_t largest = max_of_wave(max(max(k[0], k[1]), max(k[2], k[3])));
+    const uint64_t bound = threshold_of(k, largest, 47, a.choices, a.choices + kMoreGroups, &reach);
     uint32_t bound_order = 0;
     if (bound && reach > a.choices + kMoreGroups) {  // equal ones: those that come first
       int more = 0;
@@ -524,7 +555,7 @@ __global__ __launch_bounds__(THREADS) void beam_best_kernel(BeamArgs a) {
         more += __popcll(__ballot(k[i] > bound));
         o[i] = k[i] == bound ? shared.orders[lane + 64 * i] : 0;
       }
-      bound_order = threshold_of(o, a.choices - more, a.choices - more, &reach);
+      bound_order = threshold_of(o, ~0u, 0, a.choices - more, a.choices - more, &reach);
     }
     if (lane == 0) shared.bound = bound, shared.bound_order = bound_order;
   }
