@@ -133,7 +133,8 @@ struct Extent {
 };
 
 // What there is of a group, and where its sequences' rows of the page table differ first: gridDim.y workgroups per group take every gridDim.y-th run
-// of 64 places.  The last ones take the entries that belong to no group.  Bound by chains of loads (group, slot, length, table).
+// of 64 places.  The last ones take the entries that belong to no group.  Bound by chains of loads (group, slot, length, table): 3.8 us for 4
+// sequences, 5.4 us for 64 over 33000 tokens (26 us with a workgroup per group).
 __global__ __launch_bounds__(kShareThreads) void share_groups_kernel(AttentionArgs a, SharedArgs p) {
   __shared__ Extent all;
   __shared__ int differs;
@@ -248,7 +249,7 @@ __device__ __forceinline__ Sums scan_before(Sums x, Sums* sums, Sums* all) {
 }
 
 // The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part.  What it finds of the first
-// 1024 groups and entries it holds in LDS: it is bound by its chain of loads.
+// 1024 groups and entries it holds in LDS: it is bound by its chain of loads and barriers (8.8 us, whether 8 groups or 1), once for all layers.
 template <bool SINKS>
 __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
   __shared__ Sums sums[kPlanThreads / 64];
@@ -395,6 +396,11 @@ __device__ __forceinline__ void store_partial_rows(float* o, float* ml, int rows
 template <int D, int NTP>
 constexpr int kWavesPerSimd = D == 256 || (D == 128 && NTP == 2) ? 1 : 2;
 
+// The first workgroups take parts of shared pages, the others of own ones, in the proportion of their times.  A unit of shared pages is a tile of the
+// group's rows and a key head: 16 or 32 rows of a wavefront by 16-row products, where a group has few, so that its bytes bound it, or 128 rows of
+// a workgroup by 32-row products with the pages in LDS, as in prompts, where matrix instructions and the softmax
+// between them do.  8 key heads of 128 dims: 64 sequences behind 32768 tokens (256 rows of a key head) 66 us, of which its products at the rate of a large
+// one are 31; 8 groups of 8 sequences behind 1000 to 7000 tokens (32 rows of a key head) 27.5 us for 89 MB, 3.2 TB/s.
 template <int D, int FMT, int NTP, bool SINKS>
 __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_kernel(AttentionArgs a, SharedArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -590,6 +596,8 @@ double least_time(int dim, int tile_rows, int64_t own_units) {
   return start + 0.012 * (double)own_units;
 }
 
+// Rows of a unit of shared pages: 32 of a wavefront while a key head has no more (16 with 256 dims, up to 64), else 128 of a workgroup.  A step
+// of the latter takes 2.2 to 3 times an own one of a wavefront (64 sequences behind 32768 tokens: 73 us with 3, 79 with 4.5, 100 with 7).
 SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int groups, int max_rows, int max_tokens, int window, int sinks) {
   SharedForm f{};
   const int64_t own_rows = (int64_t)max_rows * group, mean = groups ? ((int64_t)rows * group + groups - 1) / groups : 0;

@@ -1,4 +1,4 @@
-// Equal parts of a row of pages (sfmp_attention.hip), also for a host program (tests/parts_driver.cpp).
+// Equal parts of a row of pages (sfmp_attention.h), also for a host program (tests/parts_driver.cpp).
 #pragma once
 
 #include <stdint.h>
