@@ -20,7 +20,7 @@ constexpr int kJoinAhead = 8;        // partial results that are asked for at a 
 constexpr int kSlotsHeld = 1024;     // entries of a group whose slots are held in LDS
 constexpr int kMostSlices = 64;      // workgroups that compare the tables of a group
 constexpr int kPlanHeadBytes = 256;
-constexpr int kMostParts = 2048;     // of shared pages, and of own ones
+constexpr int kMostParts = 2048;     // of shared pages, and of own ones: wavefronts of a launch
 
 // Numbers that a plan and the calls that use it have to agree in.
 struct PlanKey {
@@ -31,7 +31,6 @@ struct PlanHead {
   int32_t usable;            // 0: more units than the workspace holds (group starts that do not ascend)
   int32_t group_workgroups;  // those that work on shared pages: the first ones
   int32_t of_group_part, of_own_part;   // steps of a part
-  int32_t group_steps, own_steps;
 };
 // Rows of a group over the pages that its sequences share.
 struct GroupPlan {
@@ -52,11 +51,25 @@ struct EntryPlan {
   int32_t each, tiles, before, unit0;
   int32_t unused[6];
 };
-// Where a part starts: group or entry, its unit (head * tiles + tile), place of the page.
+// Where a part starts: group or entry, its unit (head * tiles + tile), place of the page; its steps (0: none), and of the group or entry what the
+// part needs, so that it does not have to wait for that as well.
 struct PartStart {
-  int32_t of, unit, first, unused;
+  int32_t of, unit, first, left;
+  int32_t common, each, tiles, unit0;
+  int32_t slot, length, row0, n;   // (length: of an entry)
+  int32_t from, to;                // (smallest and largest position: of a group)
+  int32_t unused[2];
 };
-static_assert(sizeof(PlanKey) == 64 && sizeof(PlanHead) <= kPlanHeadBytes && sizeof(GroupPlan) == 64 && sizeof(EntryPlan) == 64 && sizeof(PartStart) == 16, "");
+// What joins the results of a row, for the same reason: of its group and of its own pages the steps and units before, places of the pages
+// (0: none), tiles, and its first row of products.
+struct RowPlan {
+  int32_t there;                   // 0: a row of no entry
+  int32_t group_row, group_before, group_unit0;
+  int32_t group_each, group_tiles, own_each, own_tiles;
+  int32_t own_row, own_before, own_unit0, unused;
+};
+static_assert(sizeof(PlanKey) == 64 && sizeof(PlanHead) <= kPlanHeadBytes && sizeof(GroupPlan) == 64 && sizeof(EntryPlan) == 64 && sizeof(PartStart) == 64 &&
+                  sizeof(RowPlan) == 48, "");
 
 // How a call runs.
 struct SharedForm {
@@ -74,10 +87,10 @@ struct SharedArgs {
   PlanHead* head;
   GroupPlan* groups;
   EntryPlan* entries;
-  int32_t* row_entry;        // [rows] its batch entry
+  RowPlan* row_plans;        // [rows]
   int32_t* row_at;           // [rows] its position
-  PartStart* group_starts;
-  PartStart* own_starts;
+  PartStart* group_starts;   // by workgroup, or by wavefront where a wavefront takes a part
+  PartStart* own_starts;     // by wavefront
   PlanKey key;
   const int32_t* group_start;
   int32_t* prefix;           // or null
@@ -147,6 +160,8 @@ __global__ __launch_bounds__(kShareThreads) void share_groups_kernel(AttentionAr
   const int from2 = none ? start_of(groups) : to, to2 = none ? batch : to;
   if (tid == 0) all = Extent{kMaxTablePages, kMaxTablePages, INT32_MAX, INT32_MIN, 0}, differs = INT32_MAX;
   __syncthreads();
+  if (p.entries)
+    for (int i = (g * gridDim.y + blockIdx.y) * kShareThreads + tid; i < a.v.rows; i += gridDim.x * gridDim.y * kShareThreads) p.row_plans[i].there = 0;
   Extent mine{kMaxTablePages, kMaxTablePages, INT32_MAX, INT32_MIN, 0};
   for (int side = 0; side < 2; ++side) {
     const int begin = side ? max(from2, to) : from, end = side ? to2 : to;
@@ -160,7 +175,7 @@ __global__ __launch_bounds__(kShareThreads) void share_groups_kernel(AttentionAr
         mine.end_row = max(mine.end_row, e.row0 + e.n);
       }
       if (!writes || !p.entries) continue;
-      for (int i = 0; i < e.n; ++i) p.row_entry[e.row0 + i] = b, p.row_at[e.row0 + i] = e.length - e.n + i;
+      for (int i = 0; i < e.n; ++i) p.row_at[e.row0 + i] = e.length - e.n + i;
       p.entries[b].entry = e;
       p.entries[b].group = none ? -1 : g;
     }
@@ -223,29 +238,34 @@ __global__ __launch_bounds__(kShareThreads) void share_groups_kernel(AttentionAr
   p.groups[g] = plan;
 }
 
-// Sums over the threads before this one, and over all of them, of two numbers.
+// Sums over the threads before this one, and over all of them (added to `all`).
 struct Sums {
-  int64_t steps, units;
+  int64_t group_steps, group_units, own_steps, own_units;
+  __device__ __forceinline__ Sums& operator+=(const Sums& x) {
+    group_steps += x.group_steps, group_units += x.group_units, own_steps += x.own_steps, own_units += x.own_units;
+    return *this;
+  }
 };
-__device__ __forceinline__ Sums scan_before(Sums x, Sums* sums, Sums* all) {
+__device__ __forceinline__ Sums scan_before(const Sums& x, Sums* sums, Sums* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   Sums up = x;
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) {
-    const int64_t y = __shfl_up(up.steps, s), z = __shfl_up(up.units, s);
-    if (lane >= s) up.steps += y, up.units += z;
+    const Sums y{__shfl_up(up.group_steps, s), __shfl_up(up.group_units, s), __shfl_up(up.own_steps, s), __shfl_up(up.own_units, s)};
+    if (lane >= s) up += y;
   }
   __syncthreads();
   if (lane == 63) sums[wave] = up;
   __syncthreads();
-  Sums ahead = *all;
-#pragma unroll
+  Sums before = *all;
+#pragma unroll 4  // (registers)
   for (int w = 0; w < kPlanThreads / 64; ++w) {
     const Sums y = sums[w];
-    if (w < wave) ahead.steps += y.steps, ahead.units += y.units;
-    all->steps += y.steps, all->units += y.units;
+    if (w < wave) before += y;
+    *all += y;
   }
-  return Sums{ahead.steps + up.steps - x.steps, ahead.units + up.units - x.units};
+  before += up;
+  return Sums{before.group_steps - x.group_steps, before.group_units - x.group_units, before.own_steps - x.own_steps, before.own_units - x.own_units};
 }
 
 // The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part.  What it finds of the first
@@ -255,6 +275,7 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
   __shared__ Sums sums[kPlanThreads / 64];
   __shared__ int longest_of_all;
   __shared__ int32_t group_before[kPlanThreads], group_each[kPlanThreads], group_common[kPlanThreads];
+  __shared__ int32_t group_tiles[kPlanThreads], group_unit0[kPlanThreads], group_row0[kPlanThreads], group_n[kPlanThreads];
   __shared__ int32_t own_before[kPlanThreads], own_each[kPlanThreads];
   const int tid = threadIdx.x, lane = tid & 63, heads = a.v.heads, groups = p.key.groups;
   // (of the first entries: asked for before the groups)
@@ -277,48 +298,77 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     plan.common = min(plan.common, found);
     const PageRange<SINKS> pages = pages_of_group<SINKS>(a, plan);
     plan.each = pages.end - pages.begin;
-    plan.tiles = plan.each ? (int)(((int64_t)plan.n * a.group + p.tile_rows - 1) / p.tile_rows) : 0;
+    plan.tiles = plan.each ? (plan.n * a.group + p.tile_rows - 1) >> __builtin_ctz(p.tile_rows) : 0;  // (below 2^31: choose_shared)
     p.groups[g].common = plan.common, p.groups[g].each = plan.each, p.groups[g].tiles = plan.tiles;
-    if (g < kPlanThreads) group_common[g] = plan.common, group_each[g] = plan.each, group_before[g] = plan.tiles;  // (tiles, for now)
+    if (g < kPlanThreads) group_common[g] = plan.common, group_each[g] = plan.each, group_tiles[g] = plan.tiles, group_row0[g] = plan.row0, group_n[g] = plan.n;
   }
   if (!p.entries) return;
   if (tid == 0) longest_of_all = 1;
   __syncthreads();
-  Sums group_all{}, own_all{};
-  int longest = 1;
-  for (int base = 0; base < groups; base += kPlanThreads) {
-    const int g = base + tid;
+  Sums all{};
+  int longest = 1, near_each = 0, near_tiles = 0, near_before = 0, near_unit0 = 0;
+  for (int base = 0; base < max(groups, a.v.batch); base += kPlanThreads) {
+    const int i = base + tid;
     Sums x{};
-    if (g < groups) x.units = (int64_t)(base ? p.groups[g].tiles : group_before[g]) * heads, x.steps = x.units * (base ? p.groups[g].each : group_each[g]);
-    if (x.units) longest = max(longest, (int)(x.steps / x.units));
-    const Sums before = scan_before(x, sums, &group_all);
-    if (g < groups) p.groups[g].before = (int)before.steps, p.groups[g].unit0 = (int)before.units;
-    if (base == 0) group_before[tid] = (int)before.steps;
-  }
-  for (int base = 0; base < a.v.batch; base += kPlanThreads) {
-    const int b = base + tid;
-    Sums x{};
-    if (b < a.v.batch) {
-      const KvEntry e = base ? p.entries[b].entry : near_entry;
-      const int g = base ? p.entries[b].group : near_group, common = g < 0 ? 0 : g < kPlanThreads ? group_common[g] : p.groups[g].common;
+    if (i < groups) {
+      const int each = base ? p.groups[i].each : group_each[i];
+      x.group_units = (int64_t)(base ? p.groups[i].tiles : group_tiles[i]) * heads, x.group_steps = x.group_units * each;
+      if (x.group_units) longest = max(longest, each);
+    }
+    if (i < a.v.batch) {
+      KvEntry e = near_entry;
+      int g = near_group;
+      if (base) e = p.entries[i].entry, g = p.entries[i].group;
+      const int common = g < 0 ? 0 : g < kPlanThreads ? group_common[g] : p.groups[g].common;
       const PageRange<SINKS> pages = own_pages<SINKS>(a, e, common);
       const int each = pages.end - pages.begin, tiles = each > 0 ? tiles_of_entry(a, e, 16) : 0;
-      x.units = (int64_t)tiles * heads, x.steps = x.units * each;
-      p.entries[b].common = common, p.entries[b].each = each, p.entries[b].tiles = tiles;
-      if (base == 0) own_each[tid] = each;
+      x.own_units = (int64_t)tiles * heads, x.own_steps = x.own_units * each;
+      p.entries[i].common = common, p.entries[i].each = each, p.entries[i].tiles = tiles;
+      if (base == 0) own_each[tid] = near_each = each, near_tiles = tiles;
     }
-    const Sums before = scan_before(x, sums, &own_all);
-    if (b < a.v.batch) p.entries[b].before = (int)before.steps, p.entries[b].unit0 = (int)before.units;
-    if (base == 0) own_before[tid] = (int)before.steps;
+    const Sums before = scan_before(x, sums, &all);
+    if (i < groups) p.groups[i].before = (int)before.group_steps, p.groups[i].unit0 = (int)before.group_units;
+    if (i < a.v.batch) p.entries[i].before = (int)before.own_steps, p.entries[i].unit0 = (int)before.own_units;
+    if (base) continue;
+    group_before[tid] = (int)before.group_steps, group_unit0[tid] = (int)before.group_units;
+    own_before[tid] = near_before = (int)before.own_steps, near_unit0 = (int)before.own_units;
   }
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) longest = max(longest, __shfl_xor(longest, s));
   if (lane == 0) atomicMax(&longest_of_all, longest);
   __syncthreads();
   longest = longest_of_all;
-  const int64_t group_steps = group_all.steps, own_steps = own_all.steps;
+  for (int b = tid; b < a.v.batch; b += kPlanThreads) {
+    KvEntry e = near_entry;
+    int g = near_group;
+    RowPlan r{};
+    r.there = 1, r.own_each = near_each, r.own_tiles = near_tiles, r.own_before = near_before, r.own_unit0 = near_unit0;
+    if (b >= kPlanThreads) {
+      const EntryPlan own = p.entries[b];
+      e = own.entry, g = own.group;
+      r.own_each = own.each, r.own_tiles = own.tiles, r.own_before = own.before, r.own_unit0 = own.unit0;
+    }
+    int first_row = 0, rows = 0;
+    if (g >= kPlanThreads) {
+      const GroupPlan plan = p.groups[g];
+      first_row = plan.row0, rows = plan.n;
+      r.group_before = plan.before, r.group_unit0 = plan.unit0, r.group_each = plan.each, r.group_tiles = plan.tiles;
+    } else if (g >= 0) {
+      first_row = group_row0[g], rows = group_n[g];
+      r.group_before = group_before[g], r.group_unit0 = group_unit0[g], r.group_each = group_each[g], r.group_tiles = group_tiles[g];
+    }
+    const int each_of_group = r.group_each;
+    for (int i = 0; i < e.n; ++i) {
+      const int row = e.row0 + i - first_row;
+      r.group_each = row >= 0 && row < rows ? each_of_group : 0;
+      r.group_row = row * a.group, r.own_row = i * a.group;
+      p.row_plans[e.row0 + i] = r;
+    }
+  }
+  const int64_t most_steps = INT32_MAX;
+  const bool usable = all.group_units <= p.group_units && all.own_units <= p.own_units && all.group_steps <= most_steps && all.own_steps <= most_steps;
+  const uint32_t group_steps = usable ? (uint32_t)all.group_steps : 0, own_steps = usable ? (uint32_t)all.own_steps : 0;
   // Workgroups for shared pages and for own ones, in the proportion of their times
-  const bool usable = group_all.units <= p.group_units && own_all.units <= p.own_units && group_steps <= INT32_MAX && own_steps <= INT32_MAX;
   const bool wide = p.tile_rows == kPromptRows;
   const float group_time = (float)group_steps * p.group_cost, own_time = (float)own_steps;
   int group_workgroups = 0;
@@ -329,17 +379,15 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
   const int group_parts = max(wide ? group_workgroups : 4 * group_workgroups, 1), own_parts = max(4 * (p.workgroups - group_workgroups), 1);
   // (a unit of n pages in parts of n / x: x steps after one another, and what joins n / x partial results; the least together near sqrt(n) / 10)
   const int least = max((int)ceilf(sqrtf((float)longest) * p.group_least), 1);
-  const int of_group = (int)max((group_steps + group_parts - 1) / group_parts, (int64_t)least);
-  const int of_own = (int)max((own_steps + own_parts - 1) / own_parts, (int64_t)p.own_least);
+  const int of_group = max((int)((group_steps + group_parts - 1) / group_parts), least);
+  const int of_own = max((int)((own_steps + own_parts - 1) / own_parts), p.own_least);
   if (tid < 16) reinterpret_cast<int32_t*>(&p.head->key)[tid] = reinterpret_cast<const int32_t*>(&p.key)[tid];
   if (tid == 0) {
     p.head->usable = usable;
     p.head->group_workgroups = group_workgroups;
     p.head->of_group_part = of_group, p.head->of_own_part = of_own;
-    p.head->group_steps = usable ? (int)group_steps : 0, p.head->own_steps = usable ? (int)own_steps : 0;
   }
   __syncthreads();
-  if (!usable) return;
   // The last of n groups or entries that starts at or before a step
   auto holder = [&](int at, int n, const int32_t* held, auto before_of) {
     int lo = 0, hi = n;
@@ -349,15 +397,31 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     }
     return lo;
   };
-  for (int part = tid; part < group_parts && (int64_t)part * of_group < group_steps; part += kPlanThreads) {
+  for (int part = tid; part < (wide ? group_workgroups : 4 * group_workgroups); part += kPlanThreads) {
+    if ((int64_t)part * of_group >= group_steps) {
+      p.group_starts[part].left = 0;
+      continue;
+    }
     const int at = part * of_group, g = holder(at, groups, group_before, [&](int i) { return p.groups[i].before; });
-    const int each = max(g < kPlanThreads ? group_each[g] : p.groups[g].each, 1), inside = at - (g < kPlanThreads ? group_before[g] : p.groups[g].before);
-    p.group_starts[part] = PartStart{g, inside / each, inside % each, 0};
+    const GroupPlan plan = p.groups[g];
+    const int each = max(plan.each, 1), inside = at - plan.before;
+    p.group_starts[part] = PartStart{g,         inside / each, inside % each, min(of_group, (int)group_steps - at),
+                                     plan.common, plan.each,   plan.tiles,    plan.unit0,
+                                     plan.slot,   0,           plan.row0,     plan.n,
+                                     plan.first,  plan.last};
   }
-  for (int part = tid; part < own_parts && (int64_t)part * of_own < own_steps; part += kPlanThreads) {
+  for (int part = tid; part < 4 * (p.workgroups - group_workgroups); part += kPlanThreads) {
+    PartStart& start = p.own_starts[4 * group_workgroups + part];
+    if ((int64_t)part * of_own >= own_steps) {
+      start.left = 0;
+      continue;
+    }
     const int at = part * of_own, b = holder(at, a.v.batch, own_before, [&](int i) { return p.entries[i].before; });
-    const int each = max(b < kPlanThreads ? own_each[b] : p.entries[b].each, 1), inside = at - (b < kPlanThreads ? own_before[b] : p.entries[b].before);
-    p.own_starts[part] = PartStart{b, inside / each, inside % each, 0};
+    const EntryPlan plan = p.entries[b];
+    const int each = max(plan.each, 1), inside = at - plan.before;
+    start = PartStart{b,               inside / each,     inside % each,   min(of_own, (int)own_steps - at),
+                      plan.common,     plan.each,         plan.tiles,      plan.unit0,
+                      plan.entry.slot, plan.entry.length, plan.entry.row0, plan.entry.n};
   }
 }
 
@@ -406,19 +470,22 @@ __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_ke
   extern __shared__ __align__(16) uint8_t lds[];
   if (!plan_fits(p)) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group_workgroups = p.head->group_workgroups;
+  const int group_workgroups = p.head->group_workgroups, by_wave = blockIdx.x * 4 + wave, of_group = NTP ? by_wave : blockIdx.x;
+  // (both kinds at once: a part waits for one load, not for two)
+  const PartStart group_start = p.group_starts[of_group], own_start = p.own_starts[by_wave];
+  asm volatile("" ::"s"(group_workgroups), "s"(group_start.left), "s"(own_start.left));
   if ((int)blockIdx.x < group_workgroups) {
-    const int part = NTP ? blockIdx.x * 4 + wave : blockIdx.x;
-    const int64_t begin = (int64_t)part * p.head->of_group_part;
-    int left = (int)min((int64_t)p.head->of_group_part, (int64_t)p.head->group_steps - begin);
-    if (left <= 0) return;
-    const PartStart start = p.group_starts[part];
-    int g = start.of, unit = start.unit, first = start.first;
+    const int part = of_group;
+    const PartStart& start = group_start;
+    int left = start.left, g = start.of, unit = start.unit, first = start.first;
+    GroupPlan plan{};
+    plan.slot = start.slot, plan.common = start.common, plan.row0 = start.row0, plan.n = start.n, plan.first = start.from, plan.last = start.to;
+    plan.each = start.each, plan.tiles = start.tiles, plan.unit0 = start.unit0;
     while (left > 0) {
-      if (g >= p.key.groups) break;
-      const GroupPlan plan = p.groups[g];
       if (unit >= plan.tiles * a.v.heads) {  // the next group
-        ++g, unit = 0;
+        if (++g >= p.key.groups) break;
+        plan = p.groups[g];
+        unit = 0;
         continue;
       }
       const GroupRows e{plan.slot, plan.common * kPage, plan.row0, plan.n, plan.first, plan.last, p.row_at};
@@ -452,17 +519,17 @@ __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_ke
     }
     return;
   }
-  const int part = ((int)blockIdx.x - group_workgroups) * 4 + wave;
-  const int64_t begin = (int64_t)part * p.head->of_own_part;
-  int left = (int)min((int64_t)p.head->of_own_part, (int64_t)p.head->own_steps - begin);
-  if (left <= 0) return;
-  const PartStart start = p.own_starts[part];
-  int b = start.of, unit = start.unit, first = start.first;
+  const int part = by_wave - 4 * group_workgroups;
+  const PartStart& start = own_start;
+  int left = start.left, b = start.of, unit = start.unit, first = start.first;
+  EntryPlan plan{};
+  plan.entry = KvEntry{start.slot, start.length, start.row0, start.n};
+  plan.common = start.common, plan.each = start.each, plan.tiles = start.tiles, plan.unit0 = start.unit0;
   while (left > 0) {
-    if (b >= a.v.batch) break;
-    const EntryPlan plan = p.entries[b];
     if (unit >= plan.tiles * a.v.heads) {
-      ++b, unit = 0;
+      if (++b >= a.v.batch) break;
+      plan = p.entries[b];
+      unit = 0;
       continue;
     }
     const KvEntry e = plan.entry;
@@ -489,27 +556,23 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), at = J == 4 ? blockIdx.x : blockIdx.x * 4 + wave;
   if (at >= a.v.rows * a.q_heads) return;
   const int row = at / a.q_heads, q_head = at - row * a.q_heads, head = q_head / a.group, h = q_head - head * a.group;
-  const int b = p.row_entry[row];  // (a place of the plan, whatever it holds)
-  if (!plan_fits(p) || !p.head->usable || (uint32_t)b >= (uint32_t)a.v.batch) return;
-  const EntryPlan plan = p.entries[b];
-  if (row < plan.entry.row0 || row >= plan.entry.row0 + plan.entry.n) return;  // (a row of no entry)
+  const RowPlan plan = p.row_plans[row];  // (a place of the plan, whatever it holds)
+  const int of_group_part = p.head->of_group_part, of_own_part = p.head->of_own_part, usable = p.head->usable;
+  if (!plan_fits(p) || !usable || !plan.there) return;
   // parts [0, group_parts) and [group_parts, parts)
   int group_parts = 0, own_parts = 0;
   int64_t group_at = 0, own_at = 0;  // rows of the first partial results; those of the next parts lie a slot further each
-  if (plan.group >= 0 && plan.common > 0) {
-    const GroupPlan g = p.groups[plan.group];
-    const int i = (row - g.row0) * a.group + h, tile = i / p.tile_rows, unit = head * g.tiles + tile;
-    if (g.each > 0 && row >= g.row0 && row - g.row0 < g.n) {
-      const int from = g.before + unit * g.each, w0 = from / p.head->of_group_part;
-      group_parts = (from + g.each - 1) / p.head->of_group_part - w0 + 1;
-      group_at = ((int64_t)w0 + g.unit0 + unit) * p.tile_rows + i - tile * p.tile_rows;
-    }
+  if (plan.group_each > 0) {
+    const int i = plan.group_row + h, tile = i >> __builtin_ctz(p.tile_rows), unit = head * plan.group_tiles + tile;
+    const int from = plan.group_before + unit * plan.group_each, w0 = from / of_group_part;
+    group_parts = (from + plan.group_each - 1) / of_group_part - w0 + 1;
+    group_at = ((int64_t)w0 + plan.group_unit0 + unit) * p.tile_rows + i - tile * p.tile_rows;
   }
-  if (plan.each > 0) {
-    const int i = (row - plan.entry.row0) * a.group + h, tile = i / 16, unit = head * plan.tiles + tile;
-    const int from = plan.before + unit * plan.each, w0 = from / p.head->of_own_part;
-    own_parts = (from + plan.each - 1) / p.head->of_own_part - w0 + 1;
-    own_at = ((int64_t)w0 + plan.unit0 + unit) * 16 + i - tile * 16;
+  if (plan.own_each > 0) {
+    const int i = plan.own_row + h, tile = i / 16, unit = head * plan.own_tiles + tile;
+    const int from = plan.own_before + unit * plan.own_each, w0 = from / of_own_part;
+    own_parts = (from + plan.own_each - 1) / of_own_part - w0 + 1;
+    own_at = ((int64_t)w0 + plan.own_unit0 + unit) * 16 + i - tile * 16;
   }
   const int all = group_parts + own_parts, share = (all + J - 1) / J, first = J == 1 ? 0 : min(wave * share, all);
   const int parts = J == 1 ? all : min(share, all - first);  // (of this wavefront: from `first` on)
@@ -603,7 +666,7 @@ SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int
   const int64_t own_rows = (int64_t)max_rows * group, mean = groups ? ((int64_t)rows * group + groups - 1) / groups : 0;
   if (groups < 1 || groups >= batch || max_rows < 1 || own_rows > kMostOwnRows || (int64_t)rows * heads * group > INT32_MAX) return f;
   f.own_units = (int64_t)batch * ((own_rows + 15) / 16) * heads;
-  f.tile_rows = dim == 256 ? (mean <= 64 ? 16 : kPromptRows) : mean <= 32 ? 32 : kPromptRows;
+  f.tile_rows = dim == 256 ? (mean <= 64 ? 16 : kPromptRows) : mean <= 64 ? 32 : kPromptRows;
   f.shared = choose_form(dim, heads, group, batch, rows, max_rows, max_tokens, window, window ? sinks : 0).time > least_time(dim, f.tile_rows, f.own_units);
   if (!f.shared) return f;
   f.workgroups = dim == 256 || (dim == 128 && f.tile_rows == 32) ? 256 : 512;
@@ -627,7 +690,7 @@ int slices_of(int groups, int table_pages) {
 int64_t plan_bytes(bool shared, int batch, int rows, int groups) {
   if (!shared) return kPlanHeadBytes;  // (not used)
   return kPlanHeadBytes + (int64_t)groups * sizeof(GroupPlan) + round_up_256((groups > 1024 ? groups : 1024) * (int64_t)4) +
-         (int64_t)batch * sizeof(EntryPlan) + 2 * kMostParts * sizeof(PartStart) + round_up_256((int64_t)rows * 4) * 2;
+         (int64_t)batch * sizeof(EntryPlan) + 2 * kMostParts * sizeof(PartStart) + round_up_256(rows * (int64_t)sizeof(RowPlan)) + round_up_256((int64_t)rows * 4);
 }
 int64_t shared_workspace(const SharedForm& f, int dim) {
   return ((f.group_parts + f.group_units) * f.tile_rows + (f.own_parts + f.own_units) * 16) * (dim + 2) * 4;
@@ -658,7 +721,7 @@ SharedArgs shared_args(const SharedForm& f, const sfmp_kv_layout_t* layout, cons
     p.entries = (EntryPlan*)take((int64_t)batch->batch * sizeof(EntryPlan));
     p.group_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
     p.own_starts = (PartStart*)take(kMostParts * sizeof(PartStart));
-    p.row_entry = (int32_t*)take(round_up_256((int64_t)batch->rows * 4));
+    p.row_plans = (RowPlan*)take(round_up_256(batch->rows * (int64_t)sizeof(RowPlan)));
     p.row_at = (int32_t*)take(round_up_256((int64_t)batch->rows * 4));
   }
   p.key = PlanKey{kPlanMagic, batch->batch, batch->rows, groups, layout->kv_heads, q_heads, layout->head_dim, batch->max_rows, max_tokens, window, sinks,
