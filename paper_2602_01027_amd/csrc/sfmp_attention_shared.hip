@@ -15,7 +15,9 @@ namespace {
 constexpr int32_t kPlanMagic = 0x5348504C;
 constexpr int kMostOwnRows = 64;     // rows of an entry and key head
 constexpr int kPlanThreads = 1024, kShareThreads = 256;
-constexpr int kMostJoinedByAll = 512;  // rows and heads whose partial results four wavefronts add up
+// Rows and heads whose partial results four wavefronts add up: 2 sequences of 16000 tokens, 64 of them, 20.8 us a layer against 25.8 with one; 64 of
+// 8000, 2048 of them, 41.1 against 38.7.
+constexpr int kMostJoinedByAll = 512;
 constexpr int kJoinAhead = 8;        // partial results that are asked for at a time
 constexpr int kSlotsHeld = 1024;     // entries of a group whose slots are held in LDS
 constexpr int kMostSlices = 64;      // workgroups that compare the tables of a group
@@ -654,13 +656,17 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
 // ---- launches ------------------------------------------------------------------------------------------------------
 
 // Time (us) that sharing takes at least: plan aside, two launches, a page of the group's rows and one of each sequence's own.
+// Over 168 combinations of head layout, sequences and tokens (1 x 2 to 8 x 8 behind 300 to 5000) the rule costs 0.4 % against the faster way, at most
+// 1.28 times.  8 heads of 128 dims: 16 sequences of 1000 tokens 12.2 us alone against 14.2 shared, 64 of 8000 102 against 33.
 double least_time(int dim, int tile_rows, int64_t own_units) {
   const double start = tile_rows == kPromptRows ? (dim == 64 ? 13.0 : dim == 128 ? 16.0 : 27.0) : dim == 256 ? 13.5 : 11.5;
   return start + 0.012 * (double)own_units;
 }
 
-// Rows of a unit of shared pages: 32 of a wavefront while a key head has no more (16 with 256 dims, up to 64), else 128 of a workgroup.  A step
-// of the latter takes 2.2 to 3 times an own one of a wavefront (64 sequences behind 32768 tokens: 73 us with 3, 79 with 4.5, 100 with 7).
+// Rows of a unit of shared pages: 32 of a wavefront while a key head has up to 64 (16 with 256 dims), else 128 of a workgroup.  16 sequences of
+// 8000 tokens, 64 rows of 8 heads of 128 dims: 22.6 us a layer against 23.9; with 128 rows 27.7 against 31.9 there, but 48 against 43 for 32
+// sequences of 500 to 4000 tokens behind 16384.  A step of 128 rows takes 2.2 to 3 times an own one of a wavefront (64 sequences behind 32768
+// tokens: 73 us with 3, 79 with 4.5, 100 with 7).
 SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int groups, int max_rows, int max_tokens, int window, int sinks) {
   SharedForm f{};
   const int64_t own_rows = (int64_t)max_rows * group, mean = groups ? ((int64_t)rows * group + groups - 1) / groups : 0;

@@ -172,3 +172,41 @@ def test_one_plan_for_all_layers_in_a_graph():
     g.got.copy_(outs[0])
     g.attend(layer=0)
     g.check(layer=0)
+
+
+@pytest.mark.parametrize("dim,heads,group", [(64, 2, 4), (64, 2, 1), (128, 1, 8), (256, 1, 4), (256, 2, 1)])
+def test_sequences_that_end_with_the_shared_pages(dim, heads, group):
+    # (no sequence has a page of its own)
+    _run([(640, [(1, 0)] * 40), (1280, [(1, 0)] * 3)], "int8", dim, heads, group, "float16", seed=dim)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (70, 3)])
+def test_more_groups_and_sequences_than_threads_plan_them(window, sinks):
+    rng = np.random.default_rng(3)
+    groups = [(int(64 * rng.integers(0, 4)), [(1, int(rng.integers(1, 90))) for _ in range(2 if i % 5 else 0)]) for i in range(1500)]
+    _run(groups, "int8", 64, 1, 2, "float16", window, sinks, planned=None if window else True)
+
+
+def test_rows_of_no_sequence_are_left_as_they_were():
+    g = _run(DRAFTS, "int8", 128, 2, 4, "float16")  # (the plan knows all rows, and keeps its contents)
+    for rows in (g.rows - 1, g.rows - 7, 0):
+        g.start = np.minimum(g.start, rows)
+        g.row_start = dev(g.torch, g.start)
+        g.got.fill_(math.nan)
+        g.lse.fill_(math.nan)
+        g.share()
+        g.attend()
+        g.check()
+        assert g.torch.isnan(g.got[rows:]).all() and g.torch.isnan(g.lse[rows:]).all()
+
+
+def test_a_plan_for_one_row_more():
+    # (other lengths than the plan's last ones, in the same memory)
+    g = _run(ONE, "fp8", 128, 2, 4, "float16", seed=2)
+    lengths = g.tables["lengths"]
+    grows = [s for s in g.order if lengths[s] % PAGE]
+    lengths[grows] -= 1
+    g.dt.lengths.copy_(g.torch.from_numpy(lengths))
+    g.share()
+    g.attend()
+    g.check()
