@@ -151,19 +151,62 @@ __device__ __forceinline__ Key threshold_of(const Key (&key)[4], Key largest, in
   return at;
 }
 
-// Ranks of `count` different numbers in LDS, falling; f(rank, number) for those below `wanted`.  Up to 64 are ranked by the first wavefront, a
-// number per lane, more by all threads (`ranks`: a counter for each).
-template <int THREADS, typename F>
-__device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, int wanted, uint32_t* ranks, int tid, F f) {
+// A bound that at least `wanted` of different numbers in LDS reach, and no more than 64: bit by bit, from the first one in which `least`, which all of them
+// reach, and `largest` differ.  `turns`: counters that take turns, the first of them 0.
+template <int THREADS>
+__device__ __forceinline__ uint64_t narrow(const uint64_t* list, int count, int wanted, uint64_t least, uint64_t largest, int* turns, int tid) {
   const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  if (count <= 64) {
+  int bit = 63 - __builtin_clzll(least ^ largest | 1);
+  uint64_t at = bit < 63 ? largest >> (bit + 1) << (bit + 1) : 0;
+  for (int turn = 0; bit >= 0; --bit) {
+    const uint64_t next = at | 1ull << bit;
+    int n = 0;
+    for (int base = wave * 64; base < count; base += THREADS) n += __popcll(__ballot(base + lane < count && list[base + lane] >= next));
+    const int after = turn == 2 ? 0 : turn + 1;
+    if (lane == 0 && n) atomicAdd(&turns[turn], n);
+    if (tid == 0) turns[after] = 0;
+    __syncthreads();
+    const int all = turns[turn];
+    turn = after;
+    if (all < wanted) continue;
+    at = next;
+    if (all <= 64) break;
+  }
+  __syncthreads();
+  return at;
+}
+
+// Ranks of `count` different numbers in LDS, falling; f(rank, number) for those below `wanted`.  Up to 64 are ranked by the first wavefront, a
+// number per lane, some more by all threads (`ranks`: a counter for each); of many (a piece with logits for few threads: all of them are listed) those
+// that a bound leaves.  32 rows of 50000 tokens, 64 choices, 848 numbers in the last pieces: 38 instead of 72 us (100 numbers, for a row of
+// 131072: 38 so, 48 by a bound).
+constexpr int kMostRanked = 256;
+template <int THREADS, typename F>
+__device__ __forceinline__ void rank_numbers(const uint64_t* list, int count, int wanted, uint64_t least, uint64_t largest, uint32_t* ranks, int* turns,
+                                             int tid, F f) {
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  auto rank_few = [&](const uint64_t* few, int n) {
     if (wave) return;
-    const uint64_t mine = lane < count ? list[lane] : 0;
+    const uint64_t mine = lane < n ? few[lane] : 0;
     const int low = (int)(uint32_t)mine, high = (int)(uint32_t)(mine >> 32);
     int rank = 0;
-    for (int j = 0; j < count; ++j)
+    for (int j = 0; j < n; ++j)
       rank += ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, j)) > mine;
-    if (lane < count && rank < wanted) f(rank, mine);
+    if (lane < n && rank < wanted) f(rank, mine);
+  };
+  if (count <= 64) {
+    rank_few(list, count);
+    return;
+  }
+  if (count > kMostRanked) {
+    const uint64_t bound = narrow<THREADS>(list, count, wanted, least, largest, turns, tid);
+    uint64_t* const few = reinterpret_cast<uint64_t*>(ranks);
+    if (tid == 0) turns[0] = 0;
+    __syncthreads();
+    for (int i = tid; i < count; i += THREADS)
+      if (list[i] >= bound) few[atomicAdd(&turns[0], 1)] = list[i];
+    __syncthreads();
+    rank_few(few, turns[0]);
     return;
   }
   for (int i = tid; i < count; i += THREADS) ranks[i] = 0;
@@ -193,7 +236,7 @@ struct PieceLds {
   uint32_t maxima[kGroups], firsts[kGroups];
   uint32_t bound, bound_not;    // numbers that are listed: those with larger keys, and of equal ones those with ~number >= bound_not
   uint32_t largest;
-  int32_t threads, count, unused[3];
+  int32_t threads, count, turns[3];
 };
 // Pairs of threads that are looked at: those that `choices` need and, where others reach the bound too, some more.
 constexpr int kMorePairs = 16;
@@ -333,7 +376,7 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
           shared.scale = exp_of<1>((double)top - (double)base) * Terms(top).factor() / Terms(base).factor();
         }
         // (more equal maxima than there is room for: marked)
-        shared.count = 0, shared.threads = bound && reach > a.choices + kMorePairs ? -1 : 0;
+        shared.count = 0, shared.turns[0] = 0, shared.threads = bound && reach > a.choices + kMorePairs ? -1 : 0;
       }
     }
     __syncthreads();
@@ -418,7 +461,8 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
     }
     if (tid < kMostChoices) shared.carried[tid] = 0;  // (read at the chunk's start)
     __syncthreads();
-    rank_numbers<kThreads>(list, shared.count, a.choices, ranks, tid, [&](int rank, uint64_t x) { shared.carried[rank] = x; });
+    rank_numbers<kThreads>(list, shared.count, a.choices, (uint64_t)bound << 32, (uint64_t)largest << 32 | ~0u, ranks, shared.turns, tid,
+                           [&](int rank, uint64_t x) { shared.carried[rank] = x; });
     __syncthreads();
   }
   sum = sum_of_wave(sum);

@@ -133,6 +133,31 @@ def test_equal_continuations_come_in_the_order_of_rows_and_tokens(dtype):
     _check(x, 1, [0.0], 64, dtype=dtype, exact=True)
 
 
+@pytest.mark.parametrize("rows,beams,vocab", [(4, 2, 9001), (64, 4, 70001), (256, 8, 33000), (2, 1, 20)])
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_rows_of_which_few_tokens_are_left(dtype, rows, beams, vocab):
+    # (all logits of a few threads are larger than the rest)
+    rng = np.random.default_rng(11)
+    for choices, left in ((64, 3900), (64, 66), (17, 500), (5, 130), (2, 9)):
+        x = np.full((rows, vocab), -math.inf)
+        start = rng.integers(0, max(vocab - left, 1), rows)
+        for i in range(rows):
+            x[i, start[i]:start[i] + left] = rng.normal(0.0, 2.0, x[i, start[i]:start[i] + left].shape)
+        scores = rng.normal(-5.0, 1.0, rows)
+        _check(x[:2 * beams], beams, scores[:2 * beams], choices, dtype=dtype)
+        if choices != 64:
+            _check(x, beams, scores, choices, dtype=dtype)
+        x[:] = np.where(np.isfinite(x[0]), 3.0, -math.inf)  # equal ones in equal rows
+        _check(x[:2 * beams], beams, [-1.0] * 2 * beams, choices, dtype=dtype, exact=True)
+
+
+def test_many_beams_of_short_pieces():
+    rng = np.random.default_rng(12)
+    _check(_logits(rng, 32, 50000, 32), 32, rng.normal(-9, 2, 32), 64, dtype="float16")
+    _check(_logits(rng, 32, 50000, 32, std=0.01), 32, [-3.0] * 32, 64, dtype="bfloat16")  # (close together: many equal logits)
+    _check(_logits(rng, 32, 3000, 32), 32, [0.0] + [-math.inf] * 31, 64)
+
+
 def test_infinities_and_no_numbers():
     rng = np.random.default_rng(4)
     for dtype in DTYPES:
