@@ -79,7 +79,7 @@ struct SharedForm {
   int tile_rows;             // of a unit of shared pages: 16, 32 (a wavefront's) or kPromptRows (a workgroup's)
   int workgroups;
   int group_parts, own_parts;        // at most
-  float group_least;                 // steps of a part, times the root of a unit's pages
+  float least_of_steps, least_of_unit;   // steps of a part at least: the root of these times all steps and the longest unit's pages
   int own_least;                     // steps of a part
   int64_t group_units, own_units;    // at most
   float group_cost;                  // time of a step of shared pages, in that of an own one of a wavefront
@@ -99,7 +99,7 @@ struct SharedArgs {
   int32_t* differs;          // [groups][slices] the first place that a workgroup found to differ
   int32_t slices;
   int32_t tile_rows, workgroups, own_least;
-  float group_least;
+  float least_of_steps, least_of_unit;
   int64_t group_units, own_units;
   float group_cost;
   // partial results: o [slot][rows][dim], m and l [slot][rows][2].  The slot of a unit in a part is the sum of their numbers: from one
@@ -379,8 +379,9 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     group_workgroups = min(max(group_workgroups, 1), p.workgroups - (own_steps > 0));
   }
   const int group_parts = max(wide ? group_workgroups : 4 * group_workgroups, 1), own_parts = max(4 * (p.workgroups - group_workgroups), 1);
-  // (a unit of n pages in parts of n / x: x steps after one another, and what joins n / x partial results; the least together near sqrt(n) / 10)
-  const int least = max((int)ceilf(sqrtf((float)longest) * p.group_least), 1);
+  // (parts of x steps: x steps after one another, what all parts leave to be written and read, and the longest unit's parts to be added up one after the
+  // other; the least together at the root)
+  const int least = max((int)(sqrtf((float)group_steps * p.least_of_steps + (float)longest * p.least_of_unit)), 1);
   const int of_group = max((int)((group_steps + group_parts - 1) / group_parts), least);
   const int of_own = max((int)((own_steps + own_parts - 1) / own_parts), p.own_least);
   if (tid < 16) reinterpret_cast<int32_t*>(&p.head->key)[tid] = reinterpret_cast<const int32_t*>(&p.key)[tid];
@@ -678,7 +679,11 @@ SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int
   f.workgroups = dim == 256 || (dim == 128 && f.tile_rows == 32) ? 256 : 512;
   f.group_parts = f.tile_rows == kPromptRows ? f.workgroups : 4 * f.workgroups;
   f.own_parts = 4 * f.workgroups;
-  f.group_least = 0.1f;
+  // (us: a part leaves 8 bytes of a row and dimension at 4 TB/s, takes 0.09 to be added up by one wavefront, and for a step 1.5, 4
+  // or 1.7; over 168 combinations 1.1 % less than the root of the longest unit's pages alone, 64 sequences behind 8192 tokens 34 against 38)
+  const float step = f.tile_rows == kPromptRows ? (dim == 256 ? 4.0f : 1.5f) : 1.7f, rows_left = (float)(mean < f.tile_rows ? mean : f.tile_rows);
+  f.least_of_steps = rows_left * (float)dim * 8.0f / 4e6f / step;
+  f.least_of_unit = 0.09f / step / ((int64_t)rows * heads * group <= kMostJoinedByAll ? 4.0f : 1.0f);
   f.own_least = 1;
   f.group_units = ((int64_t)batch * own_rows / f.tile_rows + groups) * heads;
   f.group_cost = f.tile_rows == kPromptRows ? 3.0f : 1.0f;
@@ -733,7 +738,7 @@ SharedArgs shared_args(const SharedForm& f, const sfmp_kv_layout_t* layout, cons
   p.key = PlanKey{kPlanMagic, batch->batch, batch->rows, groups, layout->kv_heads, q_heads, layout->head_dim, batch->max_rows, max_tokens, window, sinks,
                   layout->pages, tables->sequences, tables->table_pages, batch->slots_dev != nullptr, batch->row_start_dev != nullptr};
   p.group_start = group_start;
-  p.tile_rows = f.tile_rows, p.workgroups = f.workgroups, p.group_least = f.group_least, p.own_least = f.own_least;
+  p.tile_rows = f.tile_rows, p.workgroups = f.workgroups, p.least_of_steps = f.least_of_steps, p.least_of_unit = f.least_of_unit, p.own_least = f.own_least;
   p.group_units = f.group_units, p.own_units = f.own_units, p.group_cost = f.group_cost;
   return p;
 }

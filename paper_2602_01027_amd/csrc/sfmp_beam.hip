@@ -294,9 +294,9 @@ __device__ __forceinline__ void forget(u32x4 (&w)[R]) {
 // threads leave their runs in LDS, where all threads look through them; what reaches the bound, a few more than are wanted, is ranked.  Chunks
 // behind the first take the list along.
 //
-// Bound by the barriers of a chunk, of which one wavefront's search for the bound is the longest, and by the loads that wait behind them: 60 % of the
-// wavefronts' time is waiting, so that as many of them as fit share a compute unit (32, at 64 registers).  32 x 8 rows of 131072 bf16 logits, 16
-// choices: 23 us, 2.9 TB/s.  The next chunk's loads in flight over this one's barriers cost a workgroup per compute unit and 2 us.
+// Bound by vector instructions (they issue for 57 % of the cycles) and by the barriers of a chunk, of which one wavefront's search for the bound is the
+// longest, with loads that wait behind them: as many wavefronts as fit share a compute unit (32, at 64 registers).  32 x 8 rows of 131072 bf16
+// logits, 16 choices: 23 us, 2.9 TB/s.  The next chunk's loads in flight over this one's barriers cost a workgroup per compute unit and 2 us.
 template <int T, int R>
 __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
   constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
