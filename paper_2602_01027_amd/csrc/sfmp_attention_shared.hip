@@ -22,6 +22,7 @@ constexpr int kJoinAhead = 8;        // partial results that are asked for at a 
 constexpr int kSlotsHeld = 1024;     // entries of a group whose slots are held in LDS
 constexpr int kMostSlices = 64;      // workgroups that compare the tables of a group
 constexpr int kPlanHeadBytes = 256;
+constexpr int64_t kMostSteps = 1 << 29;  // of each kind: with the room behind units they have to fit 32 bits
 constexpr int kMostParts = 2048;     // of shared pages, and of own ones: wavefronts of a launch
 
 // Numbers that a plan and the calls that use it have to agree in.
@@ -271,15 +272,18 @@ __device__ __forceinline__ Sums scan_before(const Sums& x, Sums* sums, Sums* all
 }
 
 // The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part.  What it finds of the first
-// 1024 groups and entries it holds in LDS: it is bound by its chain of loads and barriers (8.8 us, whether 8 groups or 1), once for all layers.
+// 1024 groups and entries it holds in LDS: it is bound by its chain of loads and barriers (10 us, whether 8 groups or 1), once for all layers.
 template <bool SINKS>
 __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
   __shared__ Sums sums[kPlanThreads / 64];
   __shared__ int longest_of_all;
   __shared__ int32_t group_before[kPlanThreads], group_each[kPlanThreads], group_common[kPlanThreads];
   __shared__ int32_t group_tiles[kPlanThreads], group_unit0[kPlanThreads], group_row0[kPlanThreads], group_n[kPlanThreads];
-  __shared__ int32_t own_before[kPlanThreads], own_each[kPlanThreads];
+  __shared__ int32_t own_before[kPlanThreads], own_each[kPlanThreads], own_common[kPlanThreads], own_tiles[kPlanThreads], own_unit0[kPlanThreads];
+  __shared__ int32_t prefix[kPlanThreads];
   const int tid = threadIdx.x, lane = tid & 63, heads = a.v.heads, groups = p.key.groups;
+  // (what is found is written at the end: a barrier behind a write waits for it.  Not where LDS does not hold it)
+  const bool far = groups > kPlanThreads || a.v.batch > kPlanThreads;
   // (of the first entries: asked for before the groups)
   KvEntry near_entry{-1, 0, 0, 0};
   int near_group = -1;
@@ -295,13 +299,17 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
       for (int s = 1; s < 64; s *= 2) differs = min(differs, __shfl_xor(differs, s));
     if (!alone && lane) continue;
     const int found = min(plan.whole, differs);
-    if (p.prefix) p.prefix[g] = found * kPage;
+    if (far || !p.entries) {
+      if (p.prefix) p.prefix[g] = found * kPage;
+    } else {
+      prefix[g] = found * kPage;
+    }
     if (!p.entries) continue;
     plan.common = min(plan.common, found);
     const PageRange<SINKS> pages = pages_of_group<SINKS>(a, plan);
     plan.each = pages.end - pages.begin;
     plan.tiles = plan.each ? (plan.n * a.group + p.tile_rows - 1) >> __builtin_ctz(p.tile_rows) : 0;  // (below 2^31: choose_shared)
-    p.groups[g].common = plan.common, p.groups[g].each = plan.each, p.groups[g].tiles = plan.tiles;
+    if (far) p.groups[g].common = plan.common, p.groups[g].each = plan.each, p.groups[g].tiles = plan.tiles;
     if (g < kPlanThreads) group_common[g] = plan.common, group_each[g] = plan.each, group_tiles[g] = plan.tiles, group_row0[g] = plan.row0, group_n[g] = plan.n;
   }
   if (!p.entries) return;
@@ -325,21 +333,58 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
       const PageRange<SINKS> pages = own_pages<SINKS>(a, e, common);
       const int each = pages.end - pages.begin, tiles = each > 0 ? tiles_of_entry(a, e, 16) : 0;
       x.own_units = (int64_t)tiles * heads, x.own_steps = x.own_units * each;
-      p.entries[i].common = common, p.entries[i].each = each, p.entries[i].tiles = tiles;
-      if (base == 0) own_each[tid] = near_each = each, near_tiles = tiles;
+      if (far) p.entries[i].common = common, p.entries[i].each = each, p.entries[i].tiles = tiles;
+      if (base == 0) own_each[tid] = near_each = each, own_tiles[tid] = near_tiles = tiles, own_common[tid] = common;
     }
     const Sums before = scan_before(x, sums, &all);
-    if (i < groups) p.groups[i].before = (int)before.group_steps, p.groups[i].unit0 = (int)before.group_units;
-    if (i < a.v.batch) p.entries[i].before = (int)before.own_steps, p.entries[i].unit0 = (int)before.own_units;
+    if (far && i < groups) p.groups[i].before = (int)before.group_steps, p.groups[i].unit0 = (int)before.group_units;
+    if (far && i < a.v.batch) p.entries[i].before = (int)before.own_steps, p.entries[i].unit0 = (int)before.own_units;
     if (base) continue;
     group_before[tid] = (int)before.group_steps, group_unit0[tid] = (int)before.group_units;
-    own_before[tid] = near_before = (int)before.own_steps, near_unit0 = (int)before.own_units;
+    own_before[tid] = near_before = (int)before.own_steps, own_unit0[tid] = near_unit0 = (int)before.own_units;
   }
 #pragma unroll
   for (int s = 1; s < 64; s *= 2) longest = max(longest, __shfl_xor(longest, s));
   if (lane == 0) atomicMax(&longest_of_all, longest);
   __syncthreads();
   longest = longest_of_all;
+  const bool usable = all.group_units <= p.group_units && all.own_units <= p.own_units && all.group_steps <= kMostSteps && all.own_steps <= kMostSteps;
+  const uint32_t group_steps = usable ? (uint32_t)all.group_steps : 0, own_steps = usable ? (uint32_t)all.own_steps : 0;
+  // Workgroups for shared pages and for own ones, in the proportion of their times
+  const bool wide = p.tile_rows == kPromptRows;
+  const float group_time = (float)group_steps * p.group_cost, own_time = (float)own_steps;
+  int group_workgroups = 0;
+  if (group_steps) {
+    group_workgroups = own_steps ? (int)((float)p.workgroups * group_time / (group_time + own_time) + 0.5f) : p.workgroups;
+    group_workgroups = min(max(group_workgroups, 1), p.workgroups - (own_steps > 0));
+  }
+  const int group_parts = max(wide ? group_workgroups : 4 * group_workgroups, 1), own_parts = max(4 * (p.workgroups - group_workgroups), 1);
+  // (parts of x steps: x steps after one another, what all parts leave to be written and read, and the longest unit's parts to be added up one after the
+  // other; the least together at the root)
+  const int least = max((int)(sqrtf((float)group_steps * p.least_of_steps + (float)longest * p.least_of_unit)), 1);
+  // Parts that begin with a unit, each unit cut by itself, where there are parts enough for the units' last ones to be shorter: one that goes on in the next
+  // unit loads rows anew and leaves two results (64 sequences behind 8192 tokens, 39.6 us a layer with parts of 7 of a unit's 128 pages, 33.7 with 8)
+  const bool whole_units = groups <= 64 && all.group_units * 4 <= group_parts;
+  const uint32_t inner_parts = whole_units ? group_parts - (uint32_t)all.group_units : group_parts;
+  const int of_group = max((int)((group_steps + inner_parts - 1) / inner_parts), least);
+  auto row_of_steps = [&](int each) { return whole_units ? (each + of_group - 1) / of_group * of_group : each; };
+  uint32_t group_end = group_steps;
+  if (whole_units) {  // (every wavefront for itself)
+    const uint32_t steps = lane < groups ? (uint32_t)group_tiles[lane] * heads * row_of_steps(group_each[lane]) : 0;
+    uint32_t up = steps;
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) {
+      const uint32_t x = __shfl_up(up, s);
+      if (lane >= s) up += x;
+    }
+    group_end = usable ? (uint32_t)__builtin_amdgcn_readlane((int)up, 63) : 0;
+    if (tid < groups) {
+      group_before[tid] = (int)(up - steps);
+      if (far) p.groups[tid].before = (int)(up - steps);
+    }
+  }
+  __syncthreads();
+  const int of_own = max((int)((own_steps + own_parts - 1) / own_parts), p.own_least);
   for (int b = tid; b < a.v.batch; b += kPlanThreads) {
     KvEntry e = near_entry;
     int g = near_group;
@@ -359,38 +404,20 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
       first_row = group_row0[g], rows = group_n[g];
       r.group_before = group_before[g], r.group_unit0 = group_unit0[g], r.group_each = group_each[g], r.group_tiles = group_tiles[g];
     }
-    const int each_of_group = r.group_each;
+    const int each_of_group = row_of_steps(r.group_each);
     for (int i = 0; i < e.n; ++i) {
       const int row = e.row0 + i - first_row;
-      r.group_each = row >= 0 && row < rows ? each_of_group : 0;
+      r.group_each = row >= 0 && row < rows ? each_of_group : 0;  // (with the room behind its last part)
       r.group_row = row * a.group, r.own_row = i * a.group;
       p.row_plans[e.row0 + i] = r;
     }
   }
-  const int64_t most_steps = INT32_MAX;
-  const bool usable = all.group_units <= p.group_units && all.own_units <= p.own_units && all.group_steps <= most_steps && all.own_steps <= most_steps;
-  const uint32_t group_steps = usable ? (uint32_t)all.group_steps : 0, own_steps = usable ? (uint32_t)all.own_steps : 0;
-  // Workgroups for shared pages and for own ones, in the proportion of their times
-  const bool wide = p.tile_rows == kPromptRows;
-  const float group_time = (float)group_steps * p.group_cost, own_time = (float)own_steps;
-  int group_workgroups = 0;
-  if (group_steps) {
-    group_workgroups = own_steps ? (int)((float)p.workgroups * group_time / (group_time + own_time) + 0.5f) : p.workgroups;
-    group_workgroups = min(max(group_workgroups, 1), p.workgroups - (own_steps > 0));
-  }
-  const int group_parts = max(wide ? group_workgroups : 4 * group_workgroups, 1), own_parts = max(4 * (p.workgroups - group_workgroups), 1);
-  // (parts of x steps: x steps after one another, what all parts leave to be written and read, and the longest unit's parts to be added up one after the
-  // other; the least together at the root)
-  const int least = max((int)(sqrtf((float)group_steps * p.least_of_steps + (float)longest * p.least_of_unit)), 1);
-  const int of_group = max((int)((group_steps + group_parts - 1) / group_parts), least);
-  const int of_own = max((int)((own_steps + own_parts - 1) / own_parts), p.own_least);
   if (tid < 16) reinterpret_cast<int32_t*>(&p.head->key)[tid] = reinterpret_cast<const int32_t*>(&p.key)[tid];
   if (tid == 0) {
     p.head->usable = usable;
     p.head->group_workgroups = group_workgroups;
     p.head->of_group_part = of_group, p.head->of_own_part = of_own;
   }
-  __syncthreads();
   // The last of n groups or entries that starts at or before a step
   auto holder = [&](int at, int n, const int32_t* held, auto before_of) {
     int lo = 0, hi = n;
@@ -401,14 +428,16 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
     return lo;
   };
   for (int part = tid; part < (wide ? group_workgroups : 4 * group_workgroups); part += kPlanThreads) {
-    if ((int64_t)part * of_group >= group_steps) {
+    if ((int64_t)part * of_group >= group_end) {
       p.group_starts[part].left = 0;
       continue;
     }
     const int at = part * of_group, g = holder(at, groups, group_before, [&](int i) { return p.groups[i].before; });
-    const GroupPlan plan = p.groups[g];
-    const int each = max(plan.each, 1), inside = at - plan.before;
-    p.group_starts[part] = PartStart{g,         inside / each, inside % each, min(of_group, (int)group_steps - at),
+    GroupPlan plan = p.groups[g];
+    if (g < kPlanThreads)
+      plan.common = group_common[g], plan.each = group_each[g], plan.tiles = group_tiles[g], plan.before = group_before[g], plan.unit0 = group_unit0[g];
+    const int each = max(row_of_steps(plan.each), 1), inside = at - plan.before, first = inside % each;
+    p.group_starts[part] = PartStart{g,         inside / each, first,         whole_units ? min(of_group, plan.each - first) : min(of_group, (int)group_steps - at),
                                      plan.common, plan.each,   plan.tiles,    plan.unit0,
                                      plan.slot,   0,           plan.row0,     plan.n,
                                      plan.first,  plan.last};
@@ -420,11 +449,24 @@ __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs
       continue;
     }
     const int at = part * of_own, b = holder(at, a.v.batch, own_before, [&](int i) { return p.entries[i].before; });
-    const EntryPlan plan = p.entries[b];
+    EntryPlan plan = p.entries[b];
+    if (b < kPlanThreads)
+      plan.common = own_common[b], plan.each = own_each[b], plan.tiles = own_tiles[b], plan.before = own_before[b], plan.unit0 = own_unit0[b];
     const int each = max(plan.each, 1), inside = at - plan.before;
     start = PartStart{b,               inside / each,     inside % each,   min(of_own, (int)own_steps - at),
                       plan.common,     plan.each,         plan.tiles,      plan.unit0,
                       plan.entry.slot, plan.entry.length, plan.entry.row0, plan.entry.n};
+  }
+  if (far) return;
+  if (tid < groups) {
+    GroupPlan& plan = p.groups[tid];
+    plan.common = group_common[tid], plan.each = group_each[tid], plan.tiles = group_tiles[tid];
+    plan.before = group_before[tid], plan.unit0 = group_unit0[tid];
+    if (p.prefix) p.prefix[tid] = prefix[tid];
+  }
+  if (tid < a.v.batch) {
+    EntryPlan& plan = p.entries[tid];
+    plan.common = own_common[tid], plan.each = near_each, plan.tiles = near_tiles, plan.before = near_before, plan.unit0 = near_unit0;
   }
 }
 
@@ -657,8 +699,8 @@ __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, Share
 // ---- launches ------------------------------------------------------------------------------------------------------
 
 // Time (us) that sharing takes at least: plan aside, two launches, a page of the group's rows and one of each sequence's own.
-// Over 168 combinations of head layout, sequences and tokens (1 x 2 to 8 x 8 behind 300 to 5000) the rule costs 0.4 % against the faster way, at most
-// 1.28 times.  8 heads of 128 dims: 16 sequences of 1000 tokens 12.2 us alone against 14.2 shared, 64 of 8000 102 against 33.
+// Over 168 combinations of head layout, sequences and tokens (1 x 2 to 8 x 8 behind 300 to 5000) the rule costs 0.9 % against the faster way, at most
+// 1.3 times.  8 heads of 128 dims: 16 sequences of 1000 tokens 12.2 us alone against 14.2 shared, 64 of 8000 102 against 33.
 double least_time(int dim, int tile_rows, int64_t own_units) {
   const double start = tile_rows == kPromptRows ? (dim == 64 ? 13.0 : dim == 128 ? 16.0 : 27.0) : dim == 256 ? 13.5 : 11.5;
   return start + 0.012 * (double)own_units;
@@ -687,6 +729,8 @@ SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int
   f.own_least = 1;
   f.group_units = ((int64_t)batch * own_rows / f.tile_rows + groups) * heads;
   f.group_cost = f.tile_rows == kPromptRows ? 3.0f : 1.0f;
+  const int64_t units = f.group_units > f.own_units ? f.group_units : f.own_units;
+  f.shared = units * ((max_tokens + kPage - 1) / kPage) <= kMostSteps;
   return f;
 }
 
