@@ -272,7 +272,7 @@ __device__ __forceinline__ Sums scan_before(const Sums& x, Sums* sums, Sums* all
 }
 
 // The row of steps and its parts: one workgroup, prefix sums over groups and entries, a binary search for each part.  What it finds of the first
-// 1024 groups and entries it holds in LDS: it is bound by its chain of loads and barriers (10 us, whether 8 groups or 1), once for all layers.
+// 1024 groups and entries it holds in LDS: it is bound by its chain of loads and barriers (11 us, whether 8 groups or 1), once for all layers.
 template <bool SINKS>
 __global__ __launch_bounds__(kPlanThreads) void share_parts_kernel(AttentionArgs a, SharedArgs p) {
   __shared__ Sums sums[kPlanThreads / 64];
@@ -508,8 +508,8 @@ constexpr int kWavesPerSimd = D == 256 || (D == 128 && NTP == 2) ? 1 : 2;
 // The first workgroups take parts of shared pages, the others of own ones, in the proportion of their times.  A unit of shared pages is a tile of the
 // group's rows and a key head: 16 or 32 rows of a wavefront by 16-row products, where a group has few, so that its bytes bound it, or 128 rows of
 // a workgroup by 32-row products with the pages in LDS, as in prompts, where matrix instructions and the softmax
-// between them do.  8 key heads of 128 dims: 64 sequences behind 32768 tokens (256 rows of a key head) 66 us, of which its products at the rate of a large
-// one are 31; 8 groups of 8 sequences behind 1000 to 7000 tokens (32 rows of a key head) 27.5 us for 89 MB, 3.2 TB/s.
+// between them do.  8 key heads of 128 dims: 64 sequences behind 32768 tokens (256 rows of a key head) 62 us, of which its products at the rate of a large
+// one are 27; 8 groups of 8 sequences behind 1000 to 7000 tokens (32 rows of a key head) 25.3 us for 89 MB, 3.5 TB/s.
 template <int D, int FMT, int NTP, bool SINKS>
 __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_kernel(AttentionArgs a, SharedArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];
@@ -593,7 +593,8 @@ __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_ke
 }
 
 // Adds up the partial results of a row and head: of the parts of its group's unit, then of its own one's.  J wavefronts share them (4 where there are few rows
-// and heads, 1 for many).  Bound by its chain of loads (row, entry, group, m and l, o): partial results are asked for 8 at a time.
+// and heads, 1 for many).  Bound by its chain of loads (row, m and l, o; partial results are asked for 8 at a time): 5.9 us for 64 rows of 32 heads with some
+// 16 parts each, 8.0 with 32.
 template <int D, int J>
 __global__ __launch_bounds__(256) void join_shared_kernel(AttentionArgs a, SharedArgs p) {
   constexpr int EACH = D / 64;

@@ -210,3 +210,12 @@ def test_a_plan_for_one_row_more():
     g.share()
     g.attend()
     g.check()
+
+
+@pytest.mark.parametrize("differs", [False, True])
+def test_more_sequences_in_a_group_than_are_held(differs):
+    def change(pool, tables, order):
+        if differs:
+            tables["table"][order[1090], 1] = tables["table"][order[1090], 3]
+    g = _run([(192, [(1, 1 + i % 70) for i in range(1100)])], "int8", 64, 1, 1, "float16", change=change)
+    assert g.prefix.tolist() == [64 if differs else 192]
