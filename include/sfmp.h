@@ -528,9 +528,11 @@ int sfmp_sample(const void* logits_dev, int32_t dtype, int32_t rows, int32_t voc
  * NaN logits count as -infinity, +infinity as the largest number of fp32; tokens of -infinity and rows whose score is -infinity or NaN (or that have
  * no logit above -infinity) have no continuation.  Where a request has fewer than `choices`, the rest is -infinity, -1, -1.  (A request that starts
  * from one prompt has the scores 0, -infinity, -infinity, ...)
- * Values are held and compared in 64 bits and rounded once.  Of the sum of exponentials the largest `choices` terms of each piece of the row are made
- * in 64 bits; another one, whose logit lies d below the largest, is off by at most 2^-24 (6 + 4 d) of itself, mostly far less.  Rows of equal
- * logits have equal values, whatever their alignment.  The same call on the same inputs gives the same bits.  Results do not overlap inputs.
+ * Values are held and compared in 64 bits and rounded once.  Of the sum of exponentials the row's largest `choices` terms are made in 64 bits, the
+ * others in 32: one whose logit lies d below the largest enters the sum with an error of at most 2^-24 (10 + 4 d) of itself, mostly far less (with
+ * d above 87 it may be left out).  Continuations of different beams whose values lie closer together than that, in proportion to what these other
+ * terms weigh (up to 2^-20 where all tokens are alike), may change places.  Rows of equal logits have equal values, whatever their alignment.
+ * The same call on the same inputs gives the same bits.  Results do not overlap inputs.
  * SFMP_ERR_SHAPE: requests < 0, beams outside 1 .. 32, requests * beams > 65535, choices outside 1 .. 64, vocab outside 1 .. 2^24, stride < vocab,
  * with ended an end_token outside the vocabulary.  Alignment: logits to their element size.  The workspace is 256-byte aligned, its contents
  * irrelevant on entry; sfmp_beam_select_workspace: bytes that are enough for every call of no more requests, beams, tokens and choices. */

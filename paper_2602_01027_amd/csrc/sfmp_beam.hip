@@ -5,8 +5,10 @@
 // exponentials: the row is read once.  A second launch, a workgroup per request, makes values of what the pieces of all beams have left and picks
 // the best.
 //
-// Continuations of different beams can lie closer together than fp32 tells apart (scores of -50 in steps of 4e-6), so that values are fp64,
-// and of the sum, which fp32 exponentials make to some 2^-24 of each term, the listed terms - the largest ones - are made again in fp64.
+// Continuations of different beams can lie closer together than fp32 tells apart (scores of -50 in steps of 4e-6), so that values are fp64.  Of the
+// sum, which fp32 exponentials make to some 2^-24 of each term, the listed terms - the largest ones, which are most of it where a beam is sure of its
+// next token - are made again in fp64, and so are the additions of the runs that hold them, whose other terms fp32 would round to what stands beside
+// them.  What is left is an error of 2^-24 of the other terms, with some factor: of rows without large terms no more is known than that.
 #include <float.h>
 #include <math.h>
 
@@ -79,26 +81,32 @@ struct Terms {
   __device__ __forceinline__ float of_any(float l) const {
     return __builtin_amdgcn_exp2f(far() ? (l - base) * kLog2e : __builtin_fmaf(l, kLog2e, c));
   }
+  // (its logarithm: below 2^-11)
+  __device__ __forceinline__ double log_factor() const { return far() ? 0.0 : -0.6931471805599453 * fma((double)base, (double)kLog2e, (double)c); }
   __device__ __forceinline__ double factor() const {
-    const double x = far() ? 0.0 : -0.6931471805599453 * fma((double)base, (double)kLog2e, (double)c);  // (below 2^-11)
+    const double x = log_factor();
     return 1.0 + x * (1.0 + x * (0.5 + x * (1.0 / 6.0)));
   }
 };
 
 // exp(d) for d <= 0 in fp64: 2^n times the series of r = d - n ln 2, |r| <= ln 2 / 2, whose first term left out is below 2^-47 (the library's
-// function, with every argument's special cases, takes twice the registers).  UNROLL 1 inside of loops, out of which the compiler brings a
-// register pair for every coefficient otherwise.
+// function, with every argument's special cases, takes twice the registers).  Inside of loops every coefficient is made where it is used (INSIDE), or
+// the compiler brings a register pair for each of them out; loads of them wait for one another.
 constexpr int kTerms = 11;
-__constant__ double kInverseFactorials[kTerms] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0,
-                                                  1.0 / 120.0,      1.0 / 24.0,      1.0 / 6.0,      0.5,           1.0};
-template <int UNROLL = kTerms>
+template <bool INSIDE = false>
 __device__ __forceinline__ double exp_of(double d) {
+  constexpr double kInverseFactorials[kTerms] = {1.0 / 39916800.0, 1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0,
+                                                 1.0 / 120.0,      1.0 / 24.0,      1.0 / 6.0,      0.5,           1.0};
   d = fmax(d, -800.0);  // (0 there)
   const double n = rint(d * 1.4426950408889634);
   const double r = fma(n, -0.6931471805599453, d);
   double p = 0.0;
-#pragma unroll UNROLL
-  for (int i = 0; i < kTerms; ++i) p = fma(p, r, kInverseFactorials[i]);
+#pragma unroll
+  for (int i = 0; i < kTerms; ++i) {
+    double coefficient = kInverseFactorials[i];
+    if constexpr (INSIDE) asm volatile("" : "+s"(coefficient));
+    p = fma(p, r, coefficient);
+  }
   p = fma(p, r, 1.0);
   return ldexp(p, (int)n);
 }
@@ -237,7 +245,9 @@ struct PieceLds {
   uint32_t bound, bound_not;    // numbers that are listed: those with larger keys, and of equal ones those with ~number >= bound_not
   uint32_t largest;
   int32_t threads, count, turns[3];
+  uint8_t place[kThreads];      // of a thread's runs among those of the threads that are looked at
 };
+static_assert(sizeof(PieceLds) % 16 == 0, "runs of 16 bytes lie behind it");
 // Pairs of threads that are looked at: those that `choices` need and, where others reach the bound too, some more.
 constexpr int kMorePairs = 16;
 __host__ __device__ constexpr int most_threads(int choices) { return 2 * (choices + kMorePairs); }
@@ -338,6 +348,38 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
       }
     }
   };
+  // Logit number i of the threads that are looked at.
+  auto left_logit = [&](int i) {
+    uint32_t bits;
+    if constexpr (SIZE == 4)
+      bits = reinterpret_cast<const uint32_t*>(runs_of)[i];
+    else
+      bits = (uint32_t)reinterpret_cast<const uint16_t*>(runs_of)[i] << (i & 1 ? 16 : 0);
+    return in_range(logit_at<T>(u32x4{bits, bits, bits, bits}, i & 1));
+  };
+  // What the sum of a chunk lacks of its runs with listed terms: these in fp64 instead of fp32, relative to what they were added with, and the other
+  // terms as far as fp32 has rounded them to what stands beside them.  RUN threads for each listed term, a term of its run for each; of several
+  // terms of a run those of the first one do it.
+  auto listed_again = [&](int first_run, float top) {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int j = tid % RUN;
+    const uint64_t x = shared.carried[tid / RUN];
+    const int at = (int)~(uint32_t)x - first_run * RUN;
+    if (!x || at < 0) return 0.0;  // (not of this chunk)
+    const uint64_t least = max(shared.carried[a.choices - 1], (uint64_t)1);  // (of a list that is not full: all logits are listed)
+    const int run = at / RUN;
+    const float l = left_logit((shared.place[run % kThreads] * R + run / kThreads) * RUN + j);
+    const Terms terms(top);
+    const float term = terms.of_any(l);
+    const bool again = l > -INFINITY && ((uint64_t)key_of(l) << 32 | ~(uint32_t)((first_run + run) * RUN + j)) >= least;
+    const uint32_t all_again = (uint32_t)(__ballot(again) >> (tid & 63 & -RUN)) & ((1u << RUN) - 1);
+    float part = 0.0f;  // (the same additions as before)
+#pragma unroll
+    for (int u = 0; u < RUN; ++u) part += __shfl(term, u, RUN);
+    if (__builtin_ctz(all_again | 1u << RUN) != at % RUN) return 0.0;
+    return (again ? exp_of<true>((double)l - (double)top - terms.log_factor()) : (double)term) - (j ? 0.0 : (double)part);
+  };
   load(piece * a.chunks_each * (kThreads * R));  // (while the row's state is on its way)
   if ((a.ended && a.ended[row]) || !(a.scores[row] > -INFINITY)) return;  // (no logit of it counts)
   if (tid < kMostChoices) shared.carried[tid] = 0;
@@ -373,7 +415,7 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
         shared.bound = bound, shared.bound_not = 0, shared.largest = largest;
         if (top > -INFINITY) {  // (of sums so far)
           const float base = logit_of_key(largest);
-          shared.scale = exp_of<1>((double)top - (double)base) * Terms(top).factor() / Terms(base).factor();
+          shared.scale = exp_of<true>((double)top - (double)base) * Terms(top).factor() / Terms(base).factor();
         }
         // (more equal maxima than there is room for: marked)
         shared.count = 0, shared.turns[0] = 0, shared.threads = bound && reach > a.choices + kMorePairs ? -1 : 0;
@@ -423,7 +465,7 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
     if (crowded && shared.maxima[tid / 2] == bound) looked_at &= shared.firsts[tid / 2] >= bound_not;
     if (looked_at) {
       const int at = atomicAdd(&shared.threads, 1);
-      owner[at] = tid;
+      owner[at] = tid, shared.place[tid] = (uint8_t)at;
 #pragma unroll
       for (int r = 0; r < R; ++r) runs_of[at * R + r] = w[r];
     }
@@ -450,42 +492,29 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
     const int numbers = shared.threads * (R * RUN);
     for (int i = tid; i < numbers; i += kThreads) {
       const int at = i / (R * RUN), r = i / RUN % R, j = i % RUN;
-      uint32_t bits;
-      if constexpr (SIZE == 4)
-        bits = reinterpret_cast<const uint32_t*>(runs_of)[i];
-      else
-        bits = (uint32_t)reinterpret_cast<const uint16_t*>(runs_of)[i] << (j & 1 ? 16 : 0);
-      const float x = in_range(logit_at<T>(u32x4{bits, bits, bits, bits}, j));
+      const float x = left_logit(i);
       const uint32_t not_number = ~(uint32_t)((first_run + r * kThreads + (int)owner[at]) * RUN + j);
       if (x > -INFINITY && wanted(key_of(x), not_number)) list[atomicAdd(&shared.count, 1)] = (uint64_t)key_of(x) << 32 | not_number;
     }
-    if (tid < kMostChoices) shared.carried[tid] = 0;  // (read at the chunk's start)
+    uint64_t none = 0;
+    asm volatile("" : "+v"(none));  // (or two registers hold it over all chunks)
+    if (tid < kMostChoices) shared.carried[tid] = none;  // (read at the chunk's start)
     __syncthreads();
     rank_numbers<kThreads>(list, shared.count, a.choices, (uint64_t)bound << 32, (uint64_t)largest << 32 | ~0u, ranks, shared.turns, tid,
                            [&](int rank, uint64_t x) { shared.carried[rank] = x; });
     __syncthreads();
+    if (tid < a.choices * RUN) sum += listed_again(first_run, top);
   }
   sum = sum_of_wave(sum);
   if (lane == 0) shared.sums[wave] = sum;
   __syncthreads();
   if (wave == 0) {
-    const Terms terms(top);
-    // the listed terms again
-    double more = 0.0;
-    if (lane < a.choices) {
-      const uint64_t x = shared.carried[lane];
-      if (x) {
-        const float l = logit_of_key((uint32_t)(x >> 32));
-        more = exp_of((double)l - (double)top) - (double)terms.of_any(l) * terms.factor();
-      }
-      a.listed[((int64_t)row * a.pieces + piece) * a.choices + lane] = x;
-    }
-    more = sum_of_wave(more);
+    if (lane < a.choices) a.listed[((int64_t)row * a.pieces + piece) * a.choices + lane] = shared.carried[lane];
     if (lane == 0) {
       double all = 0.0;
       for (int i = 0; i < kThreads / 64; ++i) all += shared.sums[i];
       Piece p;
-      p.sum = top > -INFINITY ? all * terms.factor() + more : 0.0, p.top = top, p.unused = 0;
+      p.sum = top > -INFINITY ? all * Terms(top).factor() : 0.0, p.top = top, p.unused = 0;
       a.piece[(int64_t)row * a.pieces + piece] = p;
     }
   }
