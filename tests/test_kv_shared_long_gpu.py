@@ -199,3 +199,24 @@ def test_groups_of_very_different_size_and_sequences_of_none():
     g.buffers(5)
     assert g.planned()
     _run(g)
+
+
+@pytest.mark.parametrize("begin", [[5, 9, 7, 12], [3, 20, 1, 18, -5, 17, 7], [2, 2, 2], [30, 4, 50, -1], [9, 8, 7, 6, 5, 4, 3, 2, 1], [0, 24] * 12])
+def test_group_starts_that_do_not_ascend_write_nothing_else(begin):
+    """Entries in several groups have unspecified results; nothing is written behind any buffer, and the entries in front of all groups and behind
+    them have their results, or, where such starts leave more to do than the workspace holds, no entry has."""
+    g = Long([(9000, [(1, 11 * i) for i in range(12)]), (20000, [(1, 5 + i) for i in range(12)])], "int8", 128, 2, 4, "float16", 2)
+    g.starts = dev(g.torch, np.array(begin, dtype=np.int32))
+    g.buffers(len(begin) - 1)
+    assert g.planned()
+    g.share()
+    g.attend()
+    assert g.unharmed()
+    usable = g.head()[0]
+    start = np.clip(begin, 0, 24)
+    held = {b for i in range(len(start) - 1) for b in range(start[i], start[i + 1])}
+    alone = [b for b in range(24) if (b < start[0] or b >= start[-1]) and b not in held]
+    if usable:
+        g.check(entries=alone)
+    else:
+        assert g.torch.isnan(g.got).all() and g.torch.isnan(g.lse).all()
