@@ -441,7 +441,7 @@ int sfmp_kv_attention_sinks(const sfmp_kv_layout_t* layout, int32_t layer, const
  *   max_tokens, window, sinks and pool layout until lengths, tables, slots, row or group starts change.  A plan that was made
  *   with other numbers than the call's is not used: O and lse stay as they were.  One with the numbers of the call but of other contents
  *   gives unspecified results.
- * Where there is nothing to gain (no more sequences than groups, more than 64 rows of a sequence and key head, short contexts) or more to plan than 32 bits
+ * Where there is nothing to gain (nearly as many groups as sequences, more than 64 rows of a sequence and key head, short contexts) or more to plan than 32 bits
  * hold (about 2^29 pages times key heads and tiles of rows), the call runs as
  * sfmp_kv_attention_sinks, and sfmp_kv_share only finds what prefix_dev asks for.
  * Errors as sfmp_kv_attention_sinks; SFMP_ERR_SHAPE for groups < 0 or above 65535, SFMP_ERR_WORKSPACE for a plan that is missing, not aligned or too

@@ -717,7 +717,13 @@ SharedForm choose_shared(int dim, int heads, int group, int batch, int rows, int
   if (groups < 1 || groups >= batch || max_rows < 1 || own_rows > kMostOwnRows || (int64_t)rows * heads * group > INT32_MAX) return f;
   f.own_units = (int64_t)batch * ((own_rows + 15) / 16) * heads;
   f.tile_rows = dim == 256 ? (mean <= 64 ? 16 : kPromptRows) : mean <= 64 ? 32 : kPromptRows;
-  f.shared = choose_form(dim, heads, group, batch, rows, max_rows, max_tokens, window, window ? sinks : 0).time > least_time(dim, f.tile_rows, f.own_units);
+  // (what the host knows of how much is shared: no more than the pages of all but one sequence of each group.  The others are left to be read, which
+  // takes a plan some 1.4 times as long.  2 to 96 sequences of 1000 to 8000 tokens in 1 group to as many as sequences but one, that share all but a page:
+  // 1.4 % over the faster way, at most 1.33 times, and 5.8 % and 1.48 without this term (64 sequences of 3000 tokens in 63 groups 94 us a layer against 73,
+  // 32 of 3000 in 24 36 against 26).  Where groups share nothing, which only the device finds out: 2.0 %, at most 1.27 times)
+  const AttentionForm alone = choose_form(dim, heads, group, batch, rows, max_rows, max_tokens, window, window ? sinks : 0);
+  const double beyond_start = alone.time - parts_start(alone.waves) - 3.0, left = 1.4 * groups / batch * (beyond_start > 0.0 ? beyond_start : 0.0);
+  f.shared = alone.time - left > least_time(dim, f.tile_rows, f.own_units);
   if (!f.shared) return f;
   f.workgroups = dim == 256 || (dim == 128 && f.tile_rows == 32) ? 256 : 512;
   f.group_parts = f.tile_rows == kPromptRows ? f.workgroups : 4 * f.workgroups;
