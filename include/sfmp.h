@@ -432,7 +432,8 @@ int sfmp_kv_attention_sinks(const sfmp_kv_layout_t* layout, int32_t layer, const
  *
  * Group g is the batch entries group_start[g] .. group_start[g+1]-1 (int32 [groups + 1], ascending; entries outside of all groups attend for
  * themselves).  sfmp_kv_share, called once for all layers when the step's tokens have been reserved, finds the pages that the sequences of each
- * group hold in common before they differ, and divides the work; sfmp_kv_attention_shared then computes what sfmp_kv_attention_sinks does
+ * group hold in common before they differ - all of its sequences: one that is empty, shorter than the others or of another prompt (a beam that
+ * sfmp_kv_reorder has left empty) limits what its whole group shares, and is better left outside of it - and divides the work; sfmp_kv_attention_shared then computes what sfmp_kv_attention_sinks does
  * (window 0: sfmp_kv_attention), with the same O, lse, errors and numerics but for the order of its sums.  The same call on the same
  * inputs gives the same bits.
  *   prefix_dev: NULL, or int32 [groups], the tokens of these pages (a multiple of 64; of a group of one sequence all its full pages; 0 for an
