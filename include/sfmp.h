@@ -417,9 +417,11 @@ int sfmp_kv_attention(const sfmp_kv_layout_t* layout, int32_t layer, const void*
                       int64_t o_stride, float* lse_dev, void* workspace_dev, int64_t workspace_bytes, void* hip_stream);
 
 /* Device.  The same with first tokens that stay visible behind the window: a row at position p sees the tokens j <= p with
- * j > p - window or j < sinks (window 0: all tokens j <= p, whatever `sinks`).  The pages that lie between are not read, so that an endless
- * sequence costs what its window and its first pages do.  Positions count from the sequence's first token; keys keep the rotation that they were
- * appended with.  Everything else, errors and workspace (sfmp_kv_attention_workspace) too, as sfmp_kv_attention; SFMP_ERR_SHAPE if sinks < 0. */
+ * j > p - window or j < sinks (window 0: all tokens j <= p, whatever `sinks`).  The pages that lie between are not read, so that
+ * a call takes the time of its window and first pages, however long the sequence is.  They stay held: no call gives back pages from the middle of a
+ * sequence, so that it takes the memory of all its tokens and ends at 64 * table_pages of them; a stream that goes on is started again, its first
+ * and last tokens appended to an empty sequence.  Positions count from the sequence's first token; keys keep the rotation that they were appended
+ * with.  Everything else, errors and workspace (sfmp_kv_attention_workspace) too, as sfmp_kv_attention; SFMP_ERR_SHAPE if sinks < 0. */
 int sfmp_kv_attention_sinks(const sfmp_kv_layout_t* layout, int32_t layer, const void* codes_dev, const float* scales_dev,
                             const sfmp_kv_tables_t* tables, const sfmp_kv_batch_t* batch, const void* Q_dev, int32_t q_heads,
                             int32_t dtype, int64_t q_stride, int32_t max_tokens, int32_t window, int32_t sinks, float scale,
