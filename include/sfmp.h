@@ -88,7 +88,7 @@ extern "C" {
 #define SFMP_KV_PAGE 64        /* tokens of a cache page */
 #define SFMP_KV_INT8 0         /* cache codes: whole numbers -127..127, stored plus 128 */
 #define SFMP_KV_FP8 1          /* ... 8-bit floating point, 4 exponent and 3 mantissa bits, no infinities (OCP E4M3) */
-#define SFMP_KV_MAX_BATCH 1024 /* sequences of one sfmp_kv_reserve call */
+#define SFMP_KV_MAX_BATCH 1024 /* sequences of one sfmp_kv_reserve or sfmp_kv_reorder call */
 
 #define SFMP_TYPE_FP16 0
 #define SFMP_TYPE_BF16 1
@@ -477,7 +477,8 @@ int sfmp_kv_attention_shared(const sfmp_kv_layout_t* layout, int32_t layer, cons
  * child must be empty (length 0) and no sequence may be both a parent and a child.
  * sfmp_kv_reorder: sequence slots[i] becomes what sequence slots[parents[i]] was before the call: it holds the same pages (several may have one
  * parent; a sequence that is nobody's parent is gone, and the pages that it alone held are free).  parents[i] outside 0 .. n-1: it becomes
- * empty.  What a beam search does with its sequences after sfmp_beam_select.  n <= SFMP_KV_MAX_BATCH.
+ * empty.  What a beam search does with its sequences after sfmp_beam_select.  n <= SFMP_KV_MAX_BATCH; more sequences (sfmp_beam_select takes 65535
+ * rows) go in several calls of whole requests, each with its parents less the number of its first row.
  * sfmp_kv_free: sequence slots[i] keeps its first keep[i] tokens (keep NULL: none) and gives back the other pages.
  * sfmp_kv_compact: moves the live pages with numbers >= n_live, n_live being the number of live pages, in ascending order into the free pages
  * below it, in all layers, and renumbers page table and refs: afterwards the pages n_live .. pages-1 are free.
