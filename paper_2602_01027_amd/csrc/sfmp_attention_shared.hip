@@ -508,8 +508,8 @@ constexpr int kWavesPerSimd = D == 256 || (D == 128 && NTP == 2) ? 1 : 2;
 // The first workgroups take parts of shared pages, the others of own ones, in the proportion of their times.  A unit of shared pages is a tile of the
 // group's rows and a key head: 16 or 32 rows of a wavefront by 16-row products, where a group has few, so that its bytes bound it, or 128 rows of
 // a workgroup by 32-row products with the pages in LDS, as in prompts, where matrix instructions and the softmax
-// between them do.  8 key heads of 128 dims: 64 sequences behind 32768 tokens (256 rows of a key head) 62 us, of which its products at the rate of a large
-// one are 27; 8 groups of 8 sequences behind 1000 to 7000 tokens (32 rows of a key head) 25.3 us for 89 MB, 3.5 TB/s.
+// between them do.  8 key heads of 128 dims: 64 sequences behind 32768 tokens (256 rows of a key head) 55 us, of which its products at the rate of a large
+// one are 27; 8 groups of 8 sequences behind 1000 to 7000 tokens (32 rows of a key head) 24.7 us for 89 MB, 3.6 TB/s.
 template <int D, int FMT, int NTP, bool SINKS>
 __global__ __launch_bounds__(256, (kWavesPerSimd<D, NTP>)) void attend_shared_kernel(AttentionArgs a, SharedArgs p) {
   extern __shared__ __align__(16) uint8_t lds[];

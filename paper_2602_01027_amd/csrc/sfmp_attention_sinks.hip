@@ -2,8 +2,9 @@
 //
 // The kernels are those of sfmp_attention.h, over a list of pages that holds those of the first tokens and then those of the window: what lies
 // between is neither read nor counted where the work is divided.  The mask has one more comparison per score, in pages at the edge of the window or of
-// the first tokens only.  8 key heads of 128 dims and groups of 4: a token behind 20000, window 1024, 11 us; 48 sequences, window 2048, 29 us for
-// 124 MB, 4.3 TB/s, and 5 us to join; a chunk of 2048 rows, window 1000, 66 us, 28 of them the products of what is seen at the rate of a large one.
+// the first tokens only.  8 key heads of 128 dims and groups of 4: a token behind 20000, window 1024, 11 us; 48 sequences, window 2048, 28 us for
+// 124 MB, 4.4 TB/s, and 5 us to join; a chunk of 2048 rows, window 1000, 66 us, 28 of them the products of what is seen at the rate of a large one (75 us
+// in the first 15 ms of a card that was idle).
 #include "sfmp_attention.h"
 
 using namespace sfmp;

@@ -304,9 +304,9 @@ __device__ __forceinline__ void forget(u32x4 (&w)[R]) {
 // threads leave their runs in LDS, where all threads look through them; what reaches the bound, a few more than are wanted, is ranked.  Chunks
 // behind the first take the list along.
 //
-// Bound by vector instructions (they issue for 57 % of the cycles) and by the barriers of a chunk, of which one wavefront's search for the bound is the
+// Bound by vector instructions (they issue for 58 % of the cycles) and by the barriers of a chunk, of which one wavefront's search for the bound is the
 // longest, with loads that wait behind them: as many wavefronts as fit share a compute unit (32, at 64 registers).  32 x 8 rows of 131072 bf16
-// logits, 16 choices: 23 us, 2.9 TB/s.  The next chunk's loads in flight over this one's barriers cost a workgroup per compute unit and 2 us.
+// logits, 16 choices: 22 us, 3.0 TB/s.  The next chunk's loads in flight over this one's barriers cost a workgroup per compute unit and 2 us.
 template <int T, int R>
 __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
   constexpr int SIZE = T == SFMP_TYPE_FP32 ? 4 : 2, RUN = 16 / SIZE;
@@ -359,7 +359,7 @@ __global__ __launch_bounds__(kThreads, 8) void beam_pieces_kernel(BeamArgs a) {
   };
   // What the sum of a chunk lacks of its runs with listed terms: these in fp64 instead of fp32, relative to what they were added with, and the other
   // terms as far as fp32 has rounded them to what stands beside them.  RUN threads for each listed term, a term of its run for each; of several
-  // terms of a run those of the first one do it.
+  // terms of a run those of the first one do it.  (32 x 8 rows of 131072, 16 choices: 31.6 us instead of 31.3; 34.0 with a thread for each term.)
   auto listed_again = [&](int first_run, float top) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));

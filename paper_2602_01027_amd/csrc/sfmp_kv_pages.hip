@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256) void free_kernel(sfmp_kv_tables_t t, int32_t p
 // Sequences that become what their parents were.  Places of the page table do not depend on each other: a workgroup takes 2^bits of them for all
 // sequences, through LDS, so that rows can be exchanged in place.  Holders change where a place gets another page; sums of whole numbers,
 // the same in every order.  Lengths are read by all workgroups: they change here only where there is one (`last`), else in a launch of their own.
-// Bound by its chain of loads (slot, length, place, holder): 4 sequences of 1024 tokens 2.4 us, 512 of 200 to 8190 6.7 and 1.3 us.
+// Bound by its chain of loads (slot, length, place, holder): 4 sequences of 1024 tokens 2.3 us, 512 of 200 to 8190 6.6 and 1.4 us.
 __global__ __launch_bounds__(kThreads) void reorder_kernel(sfmp_kv_tables_t t, int32_t pages, const int32_t* slots, const int32_t* parents, int32_t n,
                                                            int32_t bits, int32_t last) {
   extern __shared__ int32_t lds[];
